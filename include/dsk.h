@@ -18,6 +18,15 @@
  *                           which each sequence has its own region with room to grow.
  *   dsk_dense_decode_attn   full attention over the whole cache: the full-KV baseline the method
  *                           is compared with (Sec. 5, GPU Inference analysis).
+ * Four calls make a step of several new tokens per sequence, drafted as a tree (or prompts), on the
+ * same cache; they come before dsk_append_tokens_batch and the calls above:
+ *   dsk_step_plan           where the new tokens go: packed starts, slot map (cache rows), positions,
+ *                           ancestor masks, from the sequences' lengths.
+ *   dsk_qk_norm_rope        per-head norm and position rotation of their queries and keys in one pass,
+ *                           keys and values into the cache rows of the slot map.
+ *   dsk_tree_decode_attn    attention of every drafted node over the cached prefix (all of it, or the
+ *                           slots of a selection) and its own ancestors.
+ *   dsk_accept_draft        the accepted path of every tree, its K/V rows moved behind the sequences.
  *
  * Conventions that hold for every call
  *   - Pointers marked [dev] are device (HBM) addresses, [host] are host addresses.
@@ -493,6 +502,172 @@ typedef struct dsk_reuse_args {
   size_t workspace_bytes;
 } dsk_reuse_args;
 
+/* ------------------------------------------------------------------------------------------
+ * dsk_step_plan -- the tables of a step with several new tokens per sequence, built on the device
+ * from the sequences' lengths.  Sequence s owns the rows from seq_row0[s] on, seq_len[s] of them are
+ * in use (the regions of dsk_append_tokens_batch), and gets n_new[s] tokens.  New tokens are packed:
+ * token t = cu_new[s] + i is the i-th new one of sequence s, and
+ *   tok_row[t] = seq_row0[s] + seq_len[s] + i     the slot map: its row in K / V
+ *   tok_pos[t] = seq_len[s] + depth(i)            its position
+ * Without `parent` every token follows the one before (prompts, plain decoding): depth(i) = i.  With it
+ * the new tokens are the nodes of a tree (or forest): parent[t] is the place in the sequence (0 .. i-1) of
+ * the node that it follows, -1 if it follows the last cached token; depth counts a node's ancestors.
+ * mask (what dsk_tree_decode_attn takes): bit j of row t is set if node j is an ancestor of the node, or
+ * the node itself.  Entries from cu_new[B] on are padding: tok_seq = tok_row = -1, tok_pos = 0, no mask bit.
+ * One launch; no workspace.  Data-dependent errors through *dev_status, everything else still written:
+ *   DSK_ERR_SHAPE     a negative n_new (taken as 0), or with parent / mask more than max_nodes (cut)
+ *   DSK_ERR_CAPACITY  more than max_tokens tokens (the last are dropped, cu_new ends at max_tokens), or a
+ *                     row outside [0, total_rows) (tok_row = -1: the other calls skip the token)
+ *   DSK_ERR_ORDER     a parent that is not in [-1, i) (taken as -1)
+ * ---------------------------------------------------------------------------------------- */
+#define DSK_TREE_MAX_NODES 256
+
+typedef struct dsk_step_plan_args {
+  uint32_t struct_size;
+  int32_t B;
+  int32_t max_tokens;          /* [host] entries of the token arrays, >= 1 */
+  int32_t total_rows;          /* [host] rows of the token axis of K and V */
+  int32_t max_nodes;           /* [host] bound on n_new, 1..DSK_TREE_MAX_NODES; read with parent or mask only */
+  int32_t mask_words;          /* [host] 32-bit words of a mask row, >= ceil(max_nodes / 32); read with mask only */
+  const int32_t* seq_row0;     /* [dev] [B] */
+  const int32_t* seq_len;      /* [dev] [B] */
+  const int32_t* n_new;        /* [dev] [B] */
+  const int32_t* parent;       /* [dev] optional [max_tokens] */
+  int32_t* cu_new;             /* [dev] out [B+1] */
+  int32_t* tok_seq;            /* [dev] out [max_tokens] sequence of the token */
+  int32_t* tok_pos;            /* [dev] out [max_tokens] */
+  int32_t* tok_row;            /* [dev] out [max_tokens] */
+  uint32_t* mask;              /* [dev] optional out [max_tokens, mask_words] */
+  int32_t* dev_status;         /* [dev] optional */
+} dsk_step_plan_args;
+
+/* ------------------------------------------------------------------------------------------
+ * dsk_qk_norm_rope -- queries and keys of new tokens made ready for the cache in one pass: for every
+ * token t and head,
+ *   y = x / sqrt(mean_d x_d^2 + eps) * weight_d          (no weight: y = x)
+ *   the first rot_dim channels of y rotated by the angles tok_pos[t] * inv_freq[i], i < rot_dim / 2:
+ *   (a, b) -> (a cos - b sin, a sin + b cos) with the pair (a, b) = channels (i, i + rot_dim / 2), or
+ *   (2i, 2i + 1) with DSK_ROPE_INTERLEAVED
+ * in fp32, angles reduced in fp64, rounded to bf16 once.  Queries go to q_out, keys to row tok_row[t] of K, values as they
+ * are to the same row of V.  A token whose tok_row is outside [0, total_rows) is skipped: nothing of it
+ * is written, q_out included.  The rows of tokens that are not skipped must be distinct.  q_out may be q itself
+ * if q is packed.  Inputs are strided views, e.g. of one fused projection's output.
+ * ---------------------------------------------------------------------------------------- */
+#define DSK_ROPE_INTERLEAVED 1u
+
+typedef struct dsk_norm_rope_args {
+  uint32_t struct_size;
+  int32_t n_tokens;            /* [host] >= 0 */
+  int32_t Hq, Hkv, D;
+  const void* q;               /* [dev] bf16 [n_tokens, Hq, D], or NULL: no queries in this call */
+  const void* k;               /* [dev] bf16 [n_tokens, Hkv, D], or NULL */
+  const void* v;               /* [dev] bf16 [n_tokens, Hkv, D], or NULL: V is not written */
+  int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head; /* multiples of 8 */
+  const float* q_weight;       /* [dev] optional [D]: norm of the queries */
+  const float* k_weight;       /* [dev] optional [D] */
+  float eps;                   /* > 0 with a weight */
+  const int32_t* tok_pos;      /* [dev] [n_tokens]; read if rot_dim > 0 */
+  const int32_t* tok_row;      /* [dev] optional [n_tokens]; NULL: row t */
+  const float* inv_freq;       /* [dev] [rot_dim / 2], 16-byte aligned; read if rot_dim > 0 */
+  int32_t rot_dim;             /* multiple of 16, 0..D */
+  uint32_t flags;              /* DSK_ROPE_* bits */
+  void* q_out;                 /* [dev] out bf16 [n_tokens, Hq, D] */
+  void* K;                     /* [dev] out bf16, as in dsk_compress_args */
+  void* V;                     /* [dev] out bf16 */
+  int64_t kc_stride_tok, kc_stride_head, vc_stride_tok, vc_stride_head; /* of K and V */
+  int32_t total_rows;          /* [host] rows of K and V; bounds tok_row also where K is NULL */
+} dsk_norm_rope_args;
+
+/* ------------------------------------------------------------------------------------------
+ * dsk_tree_decode_attn -- attention of the nodes of drafted trees, all nodes of a sequence in one pass
+ * over its K/V.  Node i of sequence s (row cu_new[s] + i of q) attends to
+ *   the prefix   rows seq_row0[s] .. + seq_len[s] - 1 of K / V, or with sel_start the tokens of the
+ *                slots selected for its KV head (as dsk_select_topk writes them with
+ *                DSK_SELECT_SHARED_BY_KV_GROUP, spans as in dsk_sparse_decode_attn)
+ *   the nodes j  whose bit is set in its mask row (no mask: j <= i)
+ *   out = sum p_t V_t / sum p_t,  p_t = exp(q.K_t * scale);  lse = log sum p_t
+ * K and V of node j lie in row seq_row0[s] + seq_len[s] + j of the cache, or, with Kd / Vd, in row
+ * cu_new[s] + j of these.  A node that sees nothing gets out = 0 and lse = -inf.  K or V rows that no bit
+ * lets a node see may hold anything, NaN included.  Mask bits of nodes that do not exist are ignored.
+ * `out` asks for fp32 accuracy; where only out_bf16 is asked for, the softmax weights are rounded to bf16
+ * for the products with V (lse is fp32 in both).  Sums are in fp32, split over the keys with a merge in a fixed
+ * order; how they are split, and with it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen (k and b with
+ * a selection) and which outputs are asked for.
+ * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths or spans outside the
+ * arrays are cut, never followed: a prefix to max_seqlen and total_rows, nodes to max_nodes.
+ * ---------------------------------------------------------------------------------------- */
+typedef struct dsk_tree_attn_args {
+  uint32_t struct_size;
+  int32_t B, Hq, Hkv, D;
+  int32_t n_tokens;            /* [host] rows of q, out and mask (and of Kd / Vd); bounds cu_new[B] */
+  int32_t max_nodes;           /* [host] bound on the nodes of a sequence, 1..DSK_TREE_MAX_NODES */
+  int32_t max_seqlen;          /* [host] bound on seq_len, >= 0 */
+  int32_t total_rows;          /* [host] rows per head of K / V */
+  const void* q;               /* [dev] bf16 [n_tokens, Hq, D] */
+  const void* K;               /* [dev] bf16, strides as in dsk_compress_args */
+  const void* V;               /* [dev] */
+  int64_t k_stride_tok, k_stride_head, v_stride_tok, v_stride_head;
+  const void* Kd;              /* [dev] optional bf16: K of the nodes; both or neither */
+  const void* Vd;              /* [dev] */
+  int64_t kd_stride_tok, kd_stride_head, vd_stride_tok, vd_stride_head;
+  const int32_t* seq_row0;     /* [dev] [B] */
+  const int32_t* seq_len;      /* [dev] [B] */
+  const int32_t* cu_new;       /* [dev] [B+1] */
+  const uint32_t* mask;        /* [dev] optional [n_tokens, mask_words] */
+  int32_t mask_words;          /* >= ceil(max_nodes / 32); read with mask only */
+  int32_t k, b;                /* slots per (sequence, KV head) and upper bound of sel_len; read with sel_start only */
+  const int32_t* sel_start;    /* [dev] optional [B, Hkv, k]; all three or none */
+  const int32_t* sel_len;      /* [dev] [B, Hkv, k] */
+  const int32_t* sel_count;    /* [dev] [B, Hkv] */
+  float scale;                 /* 0 -> D^-1/2 */
+  uint32_t flags;              /* must be 0 */
+  float* out;                  /* [dev] f32 [n_tokens, Hq, D]; one of out and out_bf16 may be NULL */
+  void* out_bf16;              /* [dev] bf16 [n_tokens, Hq, D] */
+  float* lse;                  /* [dev] f32 [n_tokens, Hq], natural log; may be NULL */
+  void* workspace;             /* [dev] 256-byte aligned, dsk_tree_attn_workspace_bytes() */
+  size_t workspace_bytes;
+} dsk_tree_attn_args;
+
+/* ------------------------------------------------------------------------------------------
+ * dsk_accept_draft -- which drafted nodes stay.  target_ids[t] is the token that the model chose after node
+ * t (argmax or a sample of its logits).  Node 0 of a sequence is its last token, already chosen; from
+ * there the walk goes to the lowest node j whose parent is the current node and whose draft_ids equals the
+ * current node's target_ids, as long as there is one.  The path's nodes (n_accepted of them, max_path
+ * at most) are the sequence's next tokens: the K/V rows of all layers go to rows seq_row0[s] + seq_len[s]
+ * + 0, 1, .. of the cache, from where dsk_tree_decode_attn reads them (behind the sequence, in place, or Kd / Vd), their ids to
+ * the same rows of token_ids.  len_new = seq_len + n_accepted is what dsk_append_tokens_batch takes next, next_id
+ * the target's choice after the last accepted node (-1 without nodes).  seq_len is not changed.
+ * One launch; no workspace.  Data-dependent errors through *dev_status: DSK_ERR_CAPACITY if a path ends at
+ * max_path or total_rows although a further node fits, DSK_ERR_SHAPE if cu_new does not fit n_tokens or max_nodes (cut).
+ * ---------------------------------------------------------------------------------------- */
+typedef struct dsk_accept_args {
+  uint32_t struct_size;
+  int32_t B, Hkv, D;
+  int32_t n_layers;            /* [host] >= 1 */
+  int32_t total_rows;          /* [host] rows of the token axis of K, V, token_ids */
+  int32_t n_tokens;            /* [host] entries of parent, draft_ids, target_ids; rows of Kd / Vd */
+  int32_t max_nodes;           /* [host] bound on the nodes of a sequence, 1..DSK_TREE_MAX_NODES */
+  int32_t max_path;            /* [host] entries of a path, 1..max_nodes */
+  const int32_t* seq_row0;     /* [dev] [B] */
+  const int32_t* seq_len;      /* [dev] [B] */
+  const int32_t* cu_new;       /* [dev] [B+1] */
+  const int32_t* parent;       /* [dev] [n_tokens] as in dsk_step_plan_args */
+  const int32_t* draft_ids;    /* [dev] [n_tokens] */
+  const int32_t* target_ids;   /* [dev] [n_tokens] */
+  void* K;                     /* [dev] in/out bf16: K[l*k_stride_layer + h*k_stride_head + t*k_stride_tok + d]; */
+  void* V;                     /* [dev]   both NULL: the walk alone */
+  int64_t k_stride_tok, k_stride_head, k_stride_layer, v_stride_tok, v_stride_head, v_stride_layer; /* multiples of 8 */
+  const void* Kd;              /* [dev] optional: the nodes' own buffers; both or neither */
+  const void* Vd;              /* [dev] */
+  int64_t kd_stride_tok, kd_stride_head, kd_stride_layer, vd_stride_tok, vd_stride_head, vd_stride_layer;
+  int32_t* path;               /* [dev] out [B, max_path] accepted nodes, -1 padding */
+  int32_t* n_accepted;         /* [dev] out [B] */
+  int32_t* len_new;            /* [dev] out [B]; not seq_len itself */
+  int32_t* next_id;            /* [dev] out [B] */
+  int32_t* token_ids;          /* [dev] optional in/out [total_rows] */
+  int32_t* dev_status;         /* [dev] optional */
+} dsk_accept_args;
+
 /* Library / ABI version (DSK_ABI_VERSION of the build). */
 uint32_t dsk_version(void);
 
@@ -514,6 +689,7 @@ size_t dsk_dense_attn_workspace_bytes(const dsk_dense_attn_args* args);
 size_t dsk_append_workspace_bytes(const dsk_append_args* args);
 size_t dsk_append_batch_workspace_bytes(const dsk_append_batch_args* args);
 size_t dsk_reuse_workspace_bytes(const dsk_reuse_args* args);
+size_t dsk_tree_attn_workspace_bytes(const dsk_tree_attn_args* args);
 
 /* Where dsk_sparse_decode_attn leaves its split-K partials in args->workspace (what a caller
  * that sets DSK_ATTN_PARTIALS_ONLY reads).  Chunk c of (sequence s, head h) covers the selected
@@ -565,6 +741,10 @@ dsk_status dsk_sparse_decode_attn_static(const dsk_attn_args* args, void* stream
 dsk_status dsk_append_tokens(const dsk_append_args* args, void* stream);
 dsk_status dsk_append_tokens_batch(const dsk_append_batch_args* args, void* stream);
 dsk_status dsk_reuse_update(const dsk_reuse_args* args, void* stream);
+dsk_status dsk_step_plan(const dsk_step_plan_args* args, void* stream);
+dsk_status dsk_qk_norm_rope(const dsk_norm_rope_args* args, void* stream);
+dsk_status dsk_tree_decode_attn(const dsk_tree_attn_args* args, void* stream);
+dsk_status dsk_accept_draft(const dsk_accept_args* args, void* stream);
 
 #ifdef __cplusplus
 }

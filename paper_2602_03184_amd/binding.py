@@ -38,6 +38,8 @@ DSK_SELECT_SHARED_BY_KV_GROUP = 1
 DSK_REUSE_PLAN_ONLY = 1
 DSK_REUSE_MAX_K = 2048
 DSK_SUMMARY_MINMAX, DSK_SUMMARY_MEAN = 0, 1
+DSK_TREE_MAX_NODES = 256
+DSK_ROPE_INTERLEAVED = 1
 
 _p = C.c_void_p
 
@@ -178,6 +180,73 @@ class dsk_reuse_args(C.Structure):
     ]
 
 
+class dsk_step_plan_args(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("B", C.c_int32), ("max_tokens", C.c_int32), ("total_rows", C.c_int32), ("max_nodes", C.c_int32),
+        ("mask_words", C.c_int32),
+        ("seq_row0", _p), ("seq_len", _p), ("n_new", _p), ("parent", _p),
+        ("cu_new", _p), ("tok_seq", _p), ("tok_pos", _p), ("tok_row", _p), ("mask", _p),
+        ("dev_status", _p),
+    ]
+
+
+class dsk_norm_rope_args(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("n_tokens", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+        ("q", _p), ("k", _p), ("v", _p),
+        ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
+        ("k_stride_tok", C.c_int64), ("k_stride_head", C.c_int64),
+        ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64),
+        ("q_weight", _p), ("k_weight", _p), ("eps", C.c_float),
+        ("tok_pos", _p), ("tok_row", _p), ("inv_freq", _p),
+        ("rot_dim", C.c_int32), ("flags", C.c_uint32),
+        ("q_out", _p), ("K", _p), ("V", _p),
+        ("kc_stride_tok", C.c_int64), ("kc_stride_head", C.c_int64),
+        ("vc_stride_tok", C.c_int64), ("vc_stride_head", C.c_int64),
+        ("total_rows", C.c_int32),
+    ]
+
+
+class dsk_tree_attn_args(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+        ("n_tokens", C.c_int32), ("max_nodes", C.c_int32), ("max_seqlen", C.c_int32), ("total_rows", C.c_int32),
+        ("q", _p), ("K", _p), ("V", _p),
+        ("k_stride_tok", C.c_int64), ("k_stride_head", C.c_int64),
+        ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64),
+        ("Kd", _p), ("Vd", _p),
+        ("kd_stride_tok", C.c_int64), ("kd_stride_head", C.c_int64),
+        ("vd_stride_tok", C.c_int64), ("vd_stride_head", C.c_int64),
+        ("seq_row0", _p), ("seq_len", _p), ("cu_new", _p), ("mask", _p), ("mask_words", C.c_int32),
+        ("k", C.c_int32), ("b", C.c_int32),
+        ("sel_start", _p), ("sel_len", _p), ("sel_count", _p),
+        ("scale", C.c_float), ("flags", C.c_uint32),
+        ("out", _p), ("out_bf16", _p), ("lse", _p),
+        ("workspace", _p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class dsk_accept_args(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("B", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("n_layers", C.c_int32),
+        ("total_rows", C.c_int32), ("n_tokens", C.c_int32), ("max_nodes", C.c_int32), ("max_path", C.c_int32),
+        ("seq_row0", _p), ("seq_len", _p), ("cu_new", _p),
+        ("parent", _p), ("draft_ids", _p), ("target_ids", _p),
+        ("K", _p), ("V", _p),
+        ("k_stride_tok", C.c_int64), ("k_stride_head", C.c_int64), ("k_stride_layer", C.c_int64),
+        ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64), ("v_stride_layer", C.c_int64),
+        ("Kd", _p), ("Vd", _p),
+        ("kd_stride_tok", C.c_int64), ("kd_stride_head", C.c_int64), ("kd_stride_layer", C.c_int64),
+        ("vd_stride_tok", C.c_int64), ("vd_stride_head", C.c_int64), ("vd_stride_layer", C.c_int64),
+        ("path", _p), ("n_accepted", _p), ("len_new", _p), ("next_id", _p), ("token_ids", _p),
+        ("dev_status", _p),
+    ]
+
+
 class dsk_attn_partials(C.Structure):
     _fields_ = [
         ("ml_offset", C.c_size_t), ("acc_offset", C.c_size_t),
@@ -193,7 +262,8 @@ _lib.dsk_block_capacity.restype = C.c_int64
 _lib.dsk_block_capacity.argtypes = [C.c_int32, C.c_int32, C.c_int32]
 for _name, _cls in (("compress", dsk_compress_args), ("select", dsk_select_args), ("attn", dsk_attn_args),
                     ("dense_attn", dsk_dense_attn_args), ("append", dsk_append_args),
-                    ("append_batch", dsk_append_batch_args), ("reuse", dsk_reuse_args)):
+                    ("append_batch", dsk_append_batch_args), ("reuse", dsk_reuse_args),
+                    ("tree_attn", dsk_tree_attn_args)):
     _f = getattr(_lib, "dsk_%s_workspace_bytes" % _name)
     _f.restype = C.c_size_t
     _f.argtypes = [C.POINTER(_cls)]
@@ -215,6 +285,14 @@ _lib.dsk_sparse_decode_attn.restype = C.c_int32
 _lib.dsk_sparse_decode_attn.argtypes = [C.POINTER(dsk_attn_args), _p]
 _lib.dsk_sparse_decode_attn_static.restype = C.c_int32
 _lib.dsk_sparse_decode_attn_static.argtypes = [C.POINTER(dsk_attn_args), _p]
+_lib.dsk_step_plan.restype = C.c_int32
+_lib.dsk_step_plan.argtypes = [C.POINTER(dsk_step_plan_args), _p]
+_lib.dsk_qk_norm_rope.restype = C.c_int32
+_lib.dsk_qk_norm_rope.argtypes = [C.POINTER(dsk_norm_rope_args), _p]
+_lib.dsk_tree_decode_attn.restype = C.c_int32
+_lib.dsk_tree_decode_attn.argtypes = [C.POINTER(dsk_tree_attn_args), _p]
+_lib.dsk_accept_draft.restype = C.c_int32
+_lib.dsk_accept_draft.argtypes = [C.POINTER(dsk_accept_args), _p]
 DSK_STATIC_SCRATCH_BYTES = 2112 * 1024
 
 
@@ -335,6 +413,38 @@ def dsk_sparse_decode_attn_static(args: dsk_attn_args, stream=None, check: bool 
     st = int(_lib.dsk_sparse_decode_attn_static(C.byref(args), _stream_handle(stream)))
     if check and st != DSK_OK:
         raise DskError(st, "dsk_sparse_decode_attn_static")
+    return st
+
+
+def dsk_step_plan(args: dsk_step_plan_args, stream=None, check: bool = True) -> int:
+    st = int(_lib.dsk_step_plan(C.byref(args), _stream_handle(stream)))
+    if check and st != DSK_OK:
+        raise DskError(st, "dsk_step_plan")
+    return st
+
+
+def dsk_qk_norm_rope(args: dsk_norm_rope_args, stream=None, check: bool = True) -> int:
+    st = int(_lib.dsk_qk_norm_rope(C.byref(args), _stream_handle(stream)))
+    if check and st != DSK_OK:
+        raise DskError(st, "dsk_qk_norm_rope")
+    return st
+
+
+def dsk_tree_attn_workspace_bytes(args: dsk_tree_attn_args) -> int:
+    return int(_lib.dsk_tree_attn_workspace_bytes(C.byref(args)))
+
+
+def dsk_tree_decode_attn(args: dsk_tree_attn_args, stream=None, check: bool = True) -> int:
+    st = int(_lib.dsk_tree_decode_attn(C.byref(args), _stream_handle(stream)))
+    if check and st != DSK_OK:
+        raise DskError(st, "dsk_tree_decode_attn")
+    return st
+
+
+def dsk_accept_draft(args: dsk_accept_args, stream=None, check: bool = True) -> int:
+    st = int(_lib.dsk_accept_draft(C.byref(args), _stream_handle(stream)))
+    if check and st != DSK_OK:
+        raise DskError(st, "dsk_accept_draft")
     return st
 
 
@@ -909,3 +1019,256 @@ def make_reuser(sel: Selection, K: Optional[torch.Tensor], V: Optional[torch.Ten
                   load_pos=load_pos, load_slot=load_slot, load_start=load_start, load_len=load_len,
                   load_count=load_count, reuse_count=reuse_count, Kres=Kres, Vres=Vres, args=a,
                   keep=(sel, K, V, stale_from, ws))
+
+
+# ---- a step of several new tokens per sequence -------------------------------------------------
+def _i32_on(t: Optional[torch.Tensor], n: int) -> None:
+    """An int32 device array of at least n entries (or none)."""
+    assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= n)
+
+
+@dataclass
+class StepPlan:
+    """Tables of a step's new tokens (dsk_step_plan); refilled by every step() from the arrays that it was made with."""
+    cu_new: torch.Tensor              # int32 [B+1]
+    tok_seq: torch.Tensor             # int32 [max_tokens]; -1 padding
+    tok_pos: torch.Tensor
+    tok_row: torch.Tensor             # the slot map; -1 padding
+    mask: Optional[torch.Tensor]      # int32 (32 bits each) [max_tokens, words]
+    dev_status: torch.Tensor
+    args: dsk_step_plan_args
+    keep: tuple
+
+    def step(self, stream=None, check: bool = True) -> int:
+        return dsk_step_plan(self.args, stream, check=check)
+
+
+def make_step_plan(*, seq_row0: torch.Tensor, seq_len: torch.Tensor, n_new: torch.Tensor, max_tokens: int,
+                   total_rows: int, parent: Optional[torch.Tensor] = None, max_nodes: int = 0,
+                   want_mask: Optional[bool] = None) -> StepPlan:
+    """seq_row0 / seq_len / n_new: int32 [B] on the device (those of a RegionBatch, say); parent: int32
+    [max_tokens], the trees.  Masks are made with `parent` unless want_mask says otherwise."""
+    dev = seq_len.device
+    B = seq_len.numel()
+    for t in (seq_row0, seq_len, n_new):
+        _i32_on(t, B)
+    _i32_on(parent, max_tokens)
+    i32 = dict(dtype=torch.int32, device=dev)
+    want_mask = parent is not None if want_mask is None else want_mask
+    words = (max_nodes + 31) // 32 if want_mask else 0
+    a = dsk_step_plan_args()
+    a.struct_size = C.sizeof(dsk_step_plan_args)
+    a.B, a.max_tokens, a.total_rows, a.max_nodes, a.mask_words = B, max_tokens, total_rows, max_nodes, words
+    a.seq_row0, a.seq_len, a.n_new, a.parent = _ptr(seq_row0), _ptr(seq_len), _ptr(n_new), _ptr(parent)
+    cu_new = torch.zeros(B + 1, **i32)
+    tok_seq, tok_pos, tok_row = (torch.empty(max(max_tokens, 1), **i32) for _ in range(3))
+    mask = torch.empty(max(max_tokens, 1), max(words, 1), **i32) if want_mask else None
+    dev_status = torch.zeros(1, **i32)
+    a.cu_new, a.tok_seq, a.tok_pos, a.tok_row = _ptr(cu_new), _ptr(tok_seq), _ptr(tok_pos), _ptr(tok_row)
+    a.mask, a.dev_status = _ptr(mask), _ptr(dev_status)
+    return StepPlan(cu_new=cu_new, tok_seq=tok_seq, tok_pos=tok_pos, tok_row=tok_row, mask=mask, dev_status=dev_status,
+                    args=a, keep=(seq_row0, seq_len, n_new, parent))
+
+
+def _token_strides(X: torch.Tensor, n: int):
+    """X: bf16 [tokens, heads, D] view with unit channel stride."""
+    assert X.dim() == 3 and X.dtype == torch.bfloat16 and X.shape[0] == n and X.shape[2] == DSK_HEAD_DIM
+    if X.numel() == 0:
+        return DSK_HEAD_DIM, DSK_HEAD_DIM
+    assert X.stride(2) == 1
+    return X.stride(0), X.stride(1)
+
+
+@dataclass
+class NormRope:
+    """Argument struct of dsk_qk_norm_rope bound to its inputs and the cache."""
+    q_out: Optional[torch.Tensor]     # bf16 [tokens, Hq, D]
+    args: dsk_norm_rope_args
+    keep: tuple
+
+    def step(self, stream=None, check: bool = True) -> int:
+        return dsk_qk_norm_rope(self.args, stream, check=check)
+
+
+def make_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optional[torch.Tensor],
+                   K: Optional[torch.Tensor], V: Optional[torch.Tensor], *, pos: Optional[torch.Tensor] = None,
+                   row: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                   k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                   inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
+                   q_out: Optional[torch.Tensor] = None, total_rows: Optional[int] = None) -> NormRope:
+    """q [tokens, Hq, D], k / v [tokens, Hkv, D]: bf16 views, e.g. of one projection's output; K / V: bf16 cache
+    [Hkv, rows, D]; pos / row: int32 [tokens] (tok_pos and tok_row of a StepPlan); weights: fp32 [D]; inv_freq: fp32
+    [rot_dim / 2], none = no rotation.  total_rows bounds `row`; it defaults to the rows of K (of V, else the tokens)."""
+    x = q if q is not None else k
+    n, dev = x.shape[0], x.device
+    a = dsk_norm_rope_args()
+    a.struct_size = C.sizeof(dsk_norm_rope_args)
+    a.n_tokens, a.D = n, DSK_HEAD_DIM
+    if q is not None:
+        a.Hq = q.shape[1]
+        a.q_stride_tok, a.q_stride_head = _token_strides(q, n)
+        if q_out is None:
+            q_out = torch.empty(n, a.Hq, DSK_HEAD_DIM, dtype=torch.bfloat16, device=dev)
+        assert q_out.shape == q.shape and q_out.dtype == torch.bfloat16 and q_out.is_contiguous()
+        a.q, a.q_out = _ptr(q), _ptr(q_out)
+    rows = n
+    if v is not None:
+        a.Hkv, rows = v.shape[1], V.shape[1]
+        a.v_stride_tok, a.v_stride_head = _token_strides(v, n)
+        a.vc_stride_tok, a.vc_stride_head = _kv_strides(V)
+        assert V.shape[0] == a.Hkv
+        a.v, a.V = _ptr(v), _ptr(V)
+    if k is not None:
+        assert v is None or k.shape == v.shape
+        a.Hkv = k.shape[1]
+        rows = K.shape[1] if v is None else min(rows, K.shape[1])
+        a.k_stride_tok, a.k_stride_head = _token_strides(k, n)
+        a.kc_stride_tok, a.kc_stride_head = _kv_strides(K)
+        assert K.shape[0] == a.Hkv
+        a.k, a.K = _ptr(k), _ptr(K)
+    a.total_rows = rows if total_rows is None else total_rows
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == DSK_HEAD_DIM)
+    a.q_weight, a.k_weight, a.eps = _ptr(q_weight), _ptr(k_weight), eps
+    if inv_freq is not None:
+        assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
+        assert pos is not None
+        a.rot_dim = 2 * inv_freq.numel()
+    _i32_on(pos, n)
+    _i32_on(row, n)
+    a.tok_pos, a.tok_row, a.inv_freq = _ptr(pos), _ptr(row), _ptr(inv_freq)
+    a.flags = DSK_ROPE_INTERLEAVED if interleaved else 0
+    return NormRope(q_out=q_out, args=a, keep=(q, k, v, K, V, pos, row, q_weight, k_weight, inv_freq))
+
+
+@dataclass
+class TreeAttnOut:
+    out: Optional[torch.Tensor]       # f32 [tokens, Hq, D]
+    lse: torch.Tensor                 # f32 [tokens, Hq]
+    args: dsk_tree_attn_args
+    keep: tuple
+    out_bf16: Optional[torch.Tensor] = None
+
+
+def make_tree_attn_args(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *, seq_row0: torch.Tensor,
+                        seq_len: torch.Tensor, cu_new: torch.Tensor, mask: Optional[torch.Tensor], max_nodes: int,
+                        max_seqlen: int, Kd: Optional[torch.Tensor] = None, Vd: Optional[torch.Tensor] = None,
+                        sel_start: Optional[torch.Tensor] = None, sel_len: Optional[torch.Tensor] = None,
+                        sel_count: Optional[torch.Tensor] = None, b: int = 0, scale: float = 0.0,
+                        want_f32: bool = True, want_bf16: bool = False) -> TreeAttnOut:
+    """q: bf16 [tokens, Hq, D], the nodes of all sequences one after the other (cu_new, mask: of a StepPlan; no mask:
+    every node sees those before it).  Kd / Vd: bf16 [Hkv, tokens, D], none = the nodes' rows lie behind the sequences
+    in K / V.  sel_*: a selection per KV head (select_topk with shared=True), none = the whole prefix."""
+    dev = q.device
+    n, Hq, D = q.shape
+    B = seq_len.numel()
+    assert D == DSK_HEAD_DIM and q.dtype == torch.bfloat16 and q.is_contiguous()
+    _i32_on(seq_row0, B)
+    _i32_on(seq_len, B)
+    _i32_on(cu_new, B + 1)
+    a = dsk_tree_attn_args()
+    a.struct_size = C.sizeof(dsk_tree_attn_args)
+    a.B, a.Hq, a.Hkv, a.D = B, Hq, K.shape[0], D
+    a.n_tokens, a.max_nodes, a.max_seqlen, a.total_rows = n, max_nodes, max_seqlen, K.shape[1]
+    assert V.shape[:2] == K.shape[:2]
+    a.q, a.K, a.V = _ptr(q), _ptr(K), _ptr(V)
+    a.k_stride_tok, a.k_stride_head = _kv_strides(K)
+    a.v_stride_tok, a.v_stride_head = _kv_strides(V)
+    if Kd is not None:
+        assert Kd.shape == Vd.shape == (K.shape[0], n, D)
+        a.Kd, a.Vd = _ptr(Kd), _ptr(Vd)
+        a.kd_stride_tok, a.kd_stride_head = _kv_strides(Kd)
+        a.vd_stride_tok, a.vd_stride_head = _kv_strides(Vd)
+    a.seq_row0, a.seq_len, a.cu_new = _ptr(seq_row0), _ptr(seq_len), _ptr(cu_new)
+    if mask is not None:
+        assert mask.dtype == torch.int32 and mask.is_contiguous() and mask.shape[0] >= n
+        a.mask, a.mask_words = _ptr(mask), mask.shape[1]
+    if sel_start is not None:
+        assert sel_start.shape[:2] == (B, K.shape[0]) and sel_len.shape == sel_start.shape
+        assert sel_count.shape == sel_start.shape[:2]
+        for t in (sel_start, sel_len, sel_count):
+            _i32_on(t, 0)
+        a.k, a.b = sel_start.shape[2], b
+        a.sel_start, a.sel_len, a.sel_count = _ptr(sel_start), _ptr(sel_len), _ptr(sel_count)
+    a.scale, a.flags = scale, 0
+    out = torch.empty(n, Hq, D, dtype=torch.float32, device=dev) if want_f32 else None
+    ob = torch.empty(n, Hq, D, dtype=torch.bfloat16, device=dev) if want_bf16 else None
+    lse = torch.empty(n, Hq, dtype=torch.float32, device=dev)
+    a.out, a.out_bf16, a.lse = _ptr(out), _ptr(ob), _ptr(lse)
+    ws = _ws(dsk_tree_attn_workspace_bytes(a), dev)
+    a.workspace, a.workspace_bytes = _ptr(ws), ws.numel()
+    return TreeAttnOut(out=out, lse=lse, args=a, out_bf16=ob,
+                       keep=(q, K, V, Kd, Vd, seq_row0, seq_len, cu_new, mask, sel_start, sel_len, sel_count, ws))
+
+
+def tree_decode_attn(q, K, V, *, stream=None, check: bool = True, **kw) -> TreeAttnOut:
+    """dsk_tree_decode_attn with outputs and workspace made here; keywords as in make_tree_attn_args."""
+    r = make_tree_attn_args(q, K, V, **kw)
+    dsk_tree_decode_attn(r.args, stream, check=check)
+    return r
+
+
+@dataclass
+class Acceptor:
+    """Argument struct of dsk_accept_draft bound to the cache of all layers.  `len_new` can serve as the len_new of a
+    BatchAppender."""
+    path: torch.Tensor                # int32 [B, max_path] accepted nodes, -1 padding
+    n_accepted: torch.Tensor          # int32 [B]
+    len_new: torch.Tensor
+    next_id: torch.Tensor
+    dev_status: torch.Tensor
+    args: dsk_accept_args
+    keep: tuple
+
+    def step(self, stream=None, check: bool = True) -> int:
+        return dsk_accept_draft(self.args, stream, check=check)
+
+
+def make_acceptor(K: Optional[torch.Tensor], V: Optional[torch.Tensor], *, seq_row0: torch.Tensor,
+                  seq_len: torch.Tensor, cu_new: torch.Tensor, parent: torch.Tensor, draft_ids: torch.Tensor,
+                  target_ids: torch.Tensor, max_nodes: int, max_path: Optional[int] = None,
+                  Kd: Optional[torch.Tensor] = None, Vd: Optional[torch.Tensor] = None,
+                  token_ids: Optional[torch.Tensor] = None, len_new: Optional[torch.Tensor] = None,
+                  total_rows: Optional[int] = None) -> Acceptor:
+    """K / V: bf16 [layers, Hkv, rows, D] (or [Hkv, rows, D]); Kd / Vd: the same with the tokens as rows, none = the
+    nodes' rows lie behind the sequences in K / V; both none: only the walk (total_rows then bounds the rows).
+    len_new: where the new lengths go (a BatchAppender's, say)."""
+    dev = seq_len.device
+    B, n = seq_len.numel(), parent.numel()
+    for t in (seq_row0, seq_len):
+        _i32_on(t, B)
+    _i32_on(cu_new, B + 1)
+    for t in (parent, draft_ids, target_ids):
+        _i32_on(t, n)
+    max_path = max_nodes if max_path is None else max_path
+    i32 = dict(dtype=torch.int32, device=dev)
+    a = dsk_accept_args()
+    a.struct_size = C.sizeof(dsk_accept_args)
+    a.B, a.Hkv, a.D, a.n_layers = B, 1, DSK_HEAD_DIM, 1
+    a.n_tokens, a.max_nodes, a.max_path = n, max_nodes, max_path
+    a.seq_row0, a.seq_len, a.cu_new = _ptr(seq_row0), _ptr(seq_len), _ptr(cu_new)
+    a.parent, a.draft_ids, a.target_ids = _ptr(parent), _ptr(draft_ids), _ptr(target_ids)
+    if K is not None:
+        four = [None if X is None else (X if X.dim() == 4 else X.unsqueeze(0)) for X in (K, V, Kd, Vd)]
+        a.n_layers, a.Hkv, total_rows = four[0].shape[:3]
+        assert four[1].shape == four[0].shape
+        for X, name in zip(four, ("k", "v", "kd", "vd")):
+            if X is not None:
+                assert name in ("k", "v") or X.shape == (a.n_layers, a.Hkv, n, DSK_HEAD_DIM)
+                tok, head = _kv_strides(X[0])
+                setattr(a, name + "_stride_tok", tok)
+                setattr(a, name + "_stride_head", head)
+                setattr(a, name + "_stride_layer", X.stride(0))
+        a.K, a.V, a.Kd, a.Vd = (_ptr(X) for X in four)
+    assert total_rows is not None, "without K / V say how many rows the cache has"
+    a.total_rows = total_rows
+    path = torch.empty(B, max_path, **i32)
+    n_accepted, next_id = torch.empty(B, **i32), torch.empty(B, **i32)
+    len_new = torch.empty(B, **i32) if len_new is None else len_new
+    _i32_on(len_new, B)
+    _i32_on(token_ids, total_rows)
+    dev_status = torch.zeros(1, **i32)
+    a.path, a.n_accepted, a.len_new, a.next_id = _ptr(path), _ptr(n_accepted), _ptr(len_new), _ptr(next_id)
+    a.token_ids, a.dev_status = _ptr(token_ids), _ptr(dev_status)
+    return Acceptor(path=path, n_accepted=n_accepted, len_new=len_new, next_id=next_id, dev_status=dev_status, args=a,
+                    keep=(K, V, Kd, Vd, seq_row0, seq_len, cu_new, parent, draft_ids, target_ids, token_ids))

@@ -279,6 +279,109 @@ static dsk_status validate_reuse(const dsk_reuse_args* a) {
   return DSK_OK;
 }
 
+// a cache that is written: strides of its token and head axes, H heads
+static dsk_status cache_ok(const void* X, int64_t stride_tok, int64_t stride_head, int H) {
+  if (stride_tok < DSK_HEAD_DIM || stride_head < 0 || (H > 1 && stride_head == 0)) return DSK_ERR_SHAPE;
+  return !aligned16(X) || stride_tok % 8 || stride_head % 8 ? DSK_ERR_ALIGN : DSK_OK;
+}
+
+static dsk_status validate_step_plan(const dsk_step_plan_args* a) {
+  if (a == nullptr) return DSK_ERR_NULL;
+  if (a->struct_size != sizeof(dsk_step_plan_args)) return DSK_ERR_VERSION;
+  if (a->B < 1 || a->B > 65535 || a->max_tokens < 1 || a->total_rows < 0) return DSK_ERR_SHAPE;
+  if (a->parent != nullptr || a->mask != nullptr) {
+    if (a->max_nodes < 1 || a->max_nodes > DSK_TREE_MAX_NODES) return DSK_ERR_PARAM;
+    if (a->mask != nullptr && (a->mask_words < (a->max_nodes + 31) / 32 || a->mask_words > DSK_TREE_MAX_NODES / 32))
+      return DSK_ERR_PARAM;
+  }
+  if (!a->seq_row0 || !a->seq_len || !a->n_new || !a->cu_new || !a->tok_seq || !a->tok_pos || !a->tok_row)
+    return DSK_ERR_NULL;
+  return DSK_OK;
+}
+
+static dsk_status validate_norm_rope(const dsk_norm_rope_args* a) {
+  if (a == nullptr) return DSK_ERR_NULL;
+  if (a->struct_size != sizeof(dsk_norm_rope_args)) return DSK_ERR_VERSION;
+  if (a->D != DSK_HEAD_DIM || a->n_tokens < 0 || a->total_rows < 0) return DSK_ERR_SHAPE;
+  if (!a->q && !a->k) return DSK_ERR_NULL;
+  if ((a->q && (a->Hq < 1 || a->Hq > 65535)) || ((a->k || a->v) && (a->Hkv < 1 || a->Hkv > 65535))) return DSK_ERR_SHAPE;
+  if (a->flags & ~DSK_ROPE_INTERLEAVED) return DSK_ERR_PARAM;
+  if (a->rot_dim < 0 || a->rot_dim > DSK_HEAD_DIM || a->rot_dim % 16) return DSK_ERR_PARAM;
+  if ((a->q_weight || a->k_weight) && !(a->eps > 0.0f)) return DSK_ERR_PARAM;
+  if (a->rot_dim > 0 && (!a->tok_pos || !a->inv_freq)) return DSK_ERR_NULL;
+  if ((a->q && !a->q_out) || (a->k && !a->K) || (a->v && !a->V)) return DSK_ERR_NULL;
+  if ((a->q && (a->q_stride_tok < 0 || a->q_stride_head < 0)) || (a->k && (a->k_stride_tok < 0 || a->k_stride_head < 0)) ||
+      (a->v && (a->v_stride_tok < 0 || a->v_stride_head < 0)))
+    return DSK_ERR_SHAPE;
+  if (a->q && (!aligned16(a->q) || !aligned16(a->q_out) || a->q_stride_tok % 8 || a->q_stride_head % 8)) return DSK_ERR_ALIGN;
+  if (a->k && (!aligned16(a->k) || a->k_stride_tok % 8 || a->k_stride_head % 8)) return DSK_ERR_ALIGN;
+  if (a->v && (!aligned16(a->v) || a->v_stride_tok % 8 || a->v_stride_head % 8)) return DSK_ERR_ALIGN;
+  if (!aligned16(a->q_weight) || !aligned16(a->k_weight) || (a->rot_dim > 0 && !aligned16(a->inv_freq))) return DSK_ERR_ALIGN;
+  if (a->k)
+    if (const dsk_status v = cache_ok(a->K, a->kc_stride_tok, a->kc_stride_head, a->Hkv); v != DSK_OK) return v;
+  if (a->v)
+    if (const dsk_status v = cache_ok(a->V, a->vc_stride_tok, a->vc_stride_head, a->Hkv); v != DSK_OK) return v;
+  return DSK_OK;
+}
+
+static dsk_status validate_tree(const dsk_tree_attn_args* a) {
+  if (a == nullptr) return DSK_ERR_NULL;
+  if (a->struct_size != sizeof(dsk_tree_attn_args)) return DSK_ERR_VERSION;
+  if (!geometry_ok(a->B, a->Hq, a->Hkv, a->D)) return DSK_ERR_SHAPE;
+  if (a->n_tokens < 0 || a->max_seqlen < 0 || a->total_rows < 0) return DSK_ERR_SHAPE;
+  if (a->max_nodes < 1 || a->max_nodes > DSK_TREE_MAX_NODES) return DSK_ERR_PARAM;
+  if (!(a->scale >= 0.0f) || a->flags != 0) return DSK_ERR_PARAM;
+  if (a->mask != nullptr && a->mask_words < (a->max_nodes + 31) / 32) return DSK_ERR_PARAM;
+  if (!a->seq_row0 || !a->seq_len || !a->cu_new || (!a->out && !a->out_bf16)) return DSK_ERR_NULL;
+  if (!a->q && a->n_tokens > 0) return DSK_ERR_NULL;
+  if ((!a->K || !a->V) && a->total_rows > 0) return DSK_ERR_NULL;
+  if ((a->Kd == nullptr) != (a->Vd == nullptr)) return DSK_ERR_NULL;
+  if (a->sel_start || a->sel_len || a->sel_count) {
+    if (!a->sel_start || !a->sel_len || !a->sel_count) return DSK_ERR_NULL;
+    if (a->k < 1 || a->b < 1 || a->b > 1024) return DSK_ERR_PARAM;
+  }
+  if (a->k_stride_tok < DSK_HEAD_DIM || a->v_stride_tok < DSK_HEAD_DIM || a->k_stride_head < 0 || a->v_stride_head < 0)
+    return DSK_ERR_SHAPE;
+  if (!aligned16(a->q) || !aligned16(a->K) || !aligned16(a->V) || !aligned16(a->out) || !aligned16(a->out_bf16) ||
+      a->k_stride_tok % 8 || a->k_stride_head % 8 || a->v_stride_tok % 8 || a->v_stride_head % 8)
+    return DSK_ERR_ALIGN;
+  if (a->Kd != nullptr) {
+    if (a->kd_stride_tok < DSK_HEAD_DIM || a->vd_stride_tok < DSK_HEAD_DIM || a->kd_stride_head < 0 || a->vd_stride_head < 0)
+      return DSK_ERR_SHAPE;
+    if (!aligned16(a->Kd) || !aligned16(a->Vd) || a->kd_stride_tok % 8 || a->kd_stride_head % 8 || a->vd_stride_tok % 8 ||
+        a->vd_stride_head % 8)
+      return DSK_ERR_ALIGN;
+  }
+  if (a->workspace == nullptr || a->workspace_bytes < dsk_tree_attn_workspace_bytes(a)) return DSK_ERR_WORKSPACE;
+  if (!aligned256(a->workspace)) return DSK_ERR_ALIGN;
+  return DSK_OK;
+}
+
+static dsk_status validate_accept(const dsk_accept_args* a) {
+  if (a == nullptr) return DSK_ERR_NULL;
+  if (a->struct_size != sizeof(dsk_accept_args)) return DSK_ERR_VERSION;
+  if (a->B < 1 || a->B > 65535 || a->Hkv < 1 || a->Hkv > 65535 || a->D != DSK_HEAD_DIM || a->n_layers < 1 ||
+      a->n_layers > 65535 || a->total_rows < 0 || a->n_tokens < 0)
+    return DSK_ERR_SHAPE;
+  if (a->max_nodes < 1 || a->max_nodes > DSK_TREE_MAX_NODES || a->max_path < 1 || a->max_path > a->max_nodes)
+    return DSK_ERR_PARAM;
+  if (!a->seq_row0 || !a->seq_len || !a->cu_new || !a->path || !a->n_accepted || !a->len_new || !a->next_id)
+    return DSK_ERR_NULL;
+  if ((!a->parent || !a->draft_ids || !a->target_ids) && a->n_tokens > 0) return DSK_ERR_NULL;
+  if ((a->K == nullptr) != (a->V == nullptr) || (a->Kd == nullptr) != (a->Vd == nullptr)) return DSK_ERR_NULL;
+  if (a->len_new == a->seq_len) return DSK_ERR_PARAM;          // read by every workgroup while one of them writes
+  if (a->K == nullptr) return a->Kd == nullptr ? DSK_OK : DSK_ERR_NULL;
+  const struct { const void* X; int64_t tok, head, layer; } x[4] = {
+      {a->K, a->k_stride_tok, a->k_stride_head, a->k_stride_layer}, {a->V, a->v_stride_tok, a->v_stride_head, a->v_stride_layer},
+      {a->Kd, a->kd_stride_tok, a->kd_stride_head, a->kd_stride_layer}, {a->Vd, a->vd_stride_tok, a->vd_stride_head, a->vd_stride_layer}};
+  for (int i = 0; i < (a->Kd != nullptr ? 4 : 2); ++i) {
+    if (x[i].layer < 0 || (i < 2 && a->n_layers > 1 && x[i].layer == 0)) return DSK_ERR_SHAPE;
+    if (const dsk_status v = cache_ok(x[i].X, x[i].tok, x[i].head, i < 2 ? a->Hkv : 1); v != DSK_OK) return v;
+    if (x[i].layer % 8) return DSK_ERR_ALIGN;
+  }
+  return DSK_OK;
+}
+
 // ---- scratch of dsk_sparse_decode_attn_static ------------------------------------------------
 // One array per GPU the library runs on, held until the process ends.  Host code never uses the
 // array's name as an address: the device address is looked up once per device and kept.
@@ -397,6 +500,44 @@ dsk_status dsk_reuse_update(const dsk_reuse_args* a, void* stream) {
   const dsk_status v = validate_reuse(a);
   if (v != DSK_OK) return v;
   if (launch_reuse(*a, static_cast<hipStream_t>(stream)) != hipSuccess) return DSK_ERR_LAUNCH;
+  return DSK_OK;
+}
+
+dsk_status dsk_step_plan(const dsk_step_plan_args* a, void* stream) {
+  const dsk_status v = validate_step_plan(a);
+  if (v != DSK_OK) return v;
+  if (launch_step_plan(*a, static_cast<hipStream_t>(stream)) != hipSuccess) return DSK_ERR_LAUNCH;
+  return DSK_OK;
+}
+
+dsk_status dsk_qk_norm_rope(const dsk_norm_rope_args* a, void* stream) {
+  const dsk_status v = validate_norm_rope(a);
+  if (v != DSK_OK) return v;
+  if (a->n_tokens == 0) return DSK_OK;
+  if (launch_norm_rope(*a, static_cast<hipStream_t>(stream)) != hipSuccess) return DSK_ERR_LAUNCH;
+  return DSK_OK;
+}
+
+size_t dsk_tree_attn_workspace_bytes(const dsk_tree_attn_args* a) {
+  if (a == nullptr || a->struct_size != sizeof(dsk_tree_attn_args)) return 0;
+  if (!geometry_ok(a->B, a->Hq, a->Hkv, a->D) || a->n_tokens < 0 || a->max_seqlen < 0 || a->max_nodes < 1 ||
+      a->max_nodes > DSK_TREE_MAX_NODES || (a->sel_start && (a->k < 1 || a->b < 1 || a->b > 1024)))
+    return 0;
+  return tree_ws_bytes(*a);
+}
+
+dsk_status dsk_tree_decode_attn(const dsk_tree_attn_args* a, void* stream) {
+  const dsk_status v = validate_tree(a);
+  if (v != DSK_OK) return v;
+  if (a->n_tokens == 0) return DSK_OK;
+  if (launch_tree_attn(*a, static_cast<hipStream_t>(stream)) != hipSuccess) return DSK_ERR_LAUNCH;
+  return DSK_OK;
+}
+
+dsk_status dsk_accept_draft(const dsk_accept_args* a, void* stream) {
+  const dsk_status v = validate_accept(a);
+  if (v != DSK_OK) return v;
+  if (launch_accept(*a, static_cast<hipStream_t>(stream)) != hipSuccess) return DSK_ERR_LAUNCH;
   return DSK_OK;
 }
 

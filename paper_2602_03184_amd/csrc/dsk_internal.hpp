@@ -139,4 +139,11 @@ hipError_t launch_append_batch(const dsk_append_batch_args& a, hipStream_t st);
 size_t reuse_ws_bytes(const dsk_reuse_args& a);
 hipError_t launch_reuse(const dsk_reuse_args& a, hipStream_t st);
 
+// ---- a step of several new tokens per sequence -------------------------------------------------
+hipError_t launch_step_plan(const dsk_step_plan_args& a, hipStream_t st);
+hipError_t launch_norm_rope(const dsk_norm_rope_args& a, hipStream_t st);
+hipError_t launch_accept(const dsk_accept_args& a, hipStream_t st);
+size_t tree_ws_bytes(const dsk_tree_attn_args& a);
+hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st);
+
 }  // namespace dsk

@@ -1,0 +1,293 @@
+"""dsk_tree_decode_attn against the definition in 64 bits.
+Bars, with size = sum p |V| / sum p: fp32 logits (128 exact products summed), exponentials and sums are off by some units of 2^-24
+of terms whose largest is about 2^5: 1e-5 of the size covers them.  bf16 outputs: the weights are rounded to bf16 for the products
+with V, half a step 2^-8 of each and so of the size, the result once more, 2^-8 of it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from step_testutil import D, ancestors, i32, pack_mask, random_parents, starts, tree_reference
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = 1e-5, 2.0 ** -8
+
+
+def _dsk():
+    import paper_2602_03184_amd as dsk
+    return dsk
+
+
+class Case:
+    """A batch with a region per sequence, K and V with outlier channels, and its reference."""
+
+    def __init__(self, lens, n_new, Hq, Hkv, *, packed=False, nhd=False, seed=0, masks="tree", spare=3, pad_tokens=0, sharp=1.0):
+        self.rng = np.random.default_rng(seed)
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        self.lens, self.n_new, self.Hq, self.Hkv, self.packed = lens, n_new, Hq, Hkv, packed
+        self.row0 = starts([a + b + spare for a, b in zip(lens, n_new)])
+        self.cu, self.rows = starts(n_new), self.row0[-1]
+        self.N = self.cu[-1] + pad_tokens
+
+        def rows(n):
+            if nhd:
+                X = torch.randn(max(n, 1), Hkv, D + 24, generator=g, device="cuda").bfloat16()[..., :D].transpose(0, 1)
+            else:
+                X = torch.randn(Hkv, max(n, 1), D, generator=g, device="cuda").bfloat16()
+            X[..., 7::31] *= 4.0
+            return X
+        self.K, self.V = rows(self.rows), rows(self.rows)
+        self.Kd, self.Vd = (rows(self.N), rows(self.N)) if packed else (None, None)
+        self.q = (torch.randn(max(self.N, 1), Hq, D, generator=g, device="cuda") * sharp).bfloat16()[: self.N]
+        self.words = (max(max(n_new), 1) + 31) // 32
+        self.seen = []
+        for n in n_new:
+            if masks == "tree":
+                self.seen.append(ancestors(random_parents(self.rng, n))[0])
+            elif masks == "chain":
+                self.seen.append(np.tril(np.ones((n, n), dtype=bool)))
+            else:                                                # any bits at all, some rows empty, also of later nodes
+                m = self.rng.random((n, n)) < self.rng.choice([0.0, 0.1, 0.9], (n, 1))
+                self.seen.append(m)
+        self.masks = masks
+        self.sel = None
+
+    def select(self, k, b, empty=()):
+        """A selection per KV head: any slots of 1..b tokens, in order, the counts of `empty` (sequence, head) 0."""
+        start = np.zeros((len(self.lens), self.Hkv, k), dtype=np.int32)
+        length, count = np.zeros_like(start), np.zeros(start.shape[:2], dtype=np.int32)
+        for s, L in enumerate(self.lens):
+            for h in range(self.Hkv):
+                slots = -(-L // b)
+                n = min(k, slots) if (s, h) not in empty else 0
+                pick = np.sort(self.rng.permutation(slots)[:n])
+                start[s, h, :n] = self.row0[s] + pick * b
+                length[s, h, :n] = np.minimum(self.rng.integers(1, b + 1, n), L - pick * b)
+                count[s, h] = n
+        self.sel, self.b = (start, length, count), b
+        return self
+
+    def kwargs(self, **over):
+        kw = dict(seq_row0=i32(self.row0[:-1]), seq_len=i32(self.lens), cu_new=i32(self.cu), max_nodes=max(max(self.n_new), 1),
+                  max_seqlen=max(self.lens), Kd=self.Kd, Vd=self.Vd, mask=None)
+        if self.masks != "chain":
+            m = pack_mask(self.seen, self.words)
+            kw["mask"] = torch.cat([m, torch.zeros(self.N - len(m), self.words, dtype=torch.int32)]).cuda()
+        if self.sel is not None:
+            kw.update(zip(("sel_start", "sel_len", "sel_count"), (torch.from_numpy(x).cuda() for x in self.sel)), b=self.b)
+        kw.update(over)
+        return kw
+
+    def run(self, **over):
+        r = _dsk().make_tree_attn_args(self.q, self.K, self.V, **self.kwargs(**over))
+        for t in (r.out, r.out_bf16, r.lse):
+            if t is not None:
+                t.fill_(9.0)
+        _dsk().dsk_tree_decode_attn(r.args)
+        torch.cuda.synchronize()
+        return r
+
+    def prefix(self, s, h):
+        if self.sel is None:
+            return torch.arange(self.row0[s], self.row0[s] + self.lens[s], device="cuda")
+        start, length, count = (x[s, h] for x in self.sel)
+        spans = [torch.arange(a, a + n, device="cuda") for a, n in zip(start[:count], length[:count])]
+        return torch.cat(spans) if spans else torch.arange(0, device="cuda")
+
+    def reference(self, scale=None):
+        G = self.Hq // self.Hkv
+        scale = 1.0 / math.sqrt(D) if scale is None else scale
+        out, size = (torch.zeros(self.cu[-1], self.Hq, D, dtype=torch.float64, device="cuda") for _ in range(2))
+        lse = torch.zeros(self.cu[-1], self.Hq, dtype=torch.float64, device="cuda")
+        for s, n in enumerate(self.n_new):
+            t = slice(self.cu[s], self.cu[s + 1])
+            for h in range(self.Hkv):
+                p, hs = self.prefix(s, h), slice(h * G, (h + 1) * G)
+                nodes = slice(self.row0[s] + self.lens[s], self.row0[s] + self.lens[s] + n)
+                Kn, Vn = (self.Kd[h, t], self.Vd[h, t]) if self.packed else (self.K[h, nodes], self.V[h, nodes])
+                out[t, hs], size[t, hs], lse[t, hs] = tree_reference(self.q[t, hs], self.K[h][p], self.V[h][p], Kn, Vn,
+                                                                     self.seen[s], scale)
+        return out, size, lse
+
+    def check(self, scale=None, want=None):
+        out, size, lse = self.reference(scale) if want is None else want
+        n = self.cu[-1]
+        sc = 0.0 if scale is None else scale
+        a = self.run(scale=sc)
+        b = self.run(scale=sc, want_f32=False, want_bf16=True)
+        c = self.run(scale=sc, want_bf16=True)
+        assert bool(((a.out[:n].double() - out).abs() <= F32 * size).all())
+        assert bool(((b.out_bf16[:n].double() - out).abs() <= BF16 * (out.abs() * (1 + BF16) + size) + F32 * size).all())
+        assert torch.equal(c.out[:n], a.out[:n]) and torch.equal(c.out_bf16[:n], a.out[:n].bfloat16())
+        fine = torch.isfinite(lse)
+        for r in (a, b, c):
+            got = r.lse[:n].double()
+            assert torch.equal(got[~fine], lse[~fine])
+            assert bool(((got - lse)[fine].abs() <= 1e-5 * (1 + lse[fine].abs())).all())
+            for t in (r.out, r.out_bf16, r.lse):                 # rows behind the last sequence stay as they were
+                assert t is None or bool((t[n:] == 9.0).all())
+
+
+LENS = [0, 1, 31, 32, 33, 64, 127, 129, 700, 1025]
+
+
+@pytest.mark.parametrize("Hq, Hkv", [(1, 1), (8, 8), (8, 2), (6, 2), (5, 1), (16, 2), (14, 2)])
+@pytest.mark.parametrize("nodes", [1, 2, 7, 16, 33])
+def test_group_widths_tree_sizes_and_ragged_lengths(Hq, Hkv, nodes):
+    n_new = [max(0, nodes - (s % 3)) for s in range(len(LENS))]
+    Case(LENS, n_new, Hq, Hkv, seed=nodes, packed=nodes % 2 == 0, nhd=nodes == 7).check()
+
+
+@pytest.mark.parametrize("nodes", [64, 65, 100, 256])
+@pytest.mark.parametrize("Hq, Hkv", [(4, 4), (8, 2), (8, 1)])
+def test_large_trees(Hq, Hkv, nodes):
+    Case([600, 45, 0], [nodes, nodes // 3, nodes], Hq, Hkv, seed=nodes, packed=nodes == 100).check()
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("lens", [[0, 40, 300], [0, 0, 0]])
+def test_any_mask_and_rows_that_see_nothing(packed, lens):
+    c = Case(lens, [40, 33, 12], 8, 2, masks="any", packed=packed, seed=5)
+    assert any((~m.any(1)).any() for m in c.seen)
+    c.check()
+
+
+@pytest.mark.parametrize("nodes", [1, 5, 40])
+def test_no_mask_means_a_chain(nodes):
+    Case([100, 0, 77], [nodes, nodes, 1], 8, 2, masks="chain", seed=nodes).check()
+
+
+def test_bits_of_nodes_that_do_not_exist_are_ignored():
+    c = Case([50, 20], [10, 3], 4, 2, seed=2)
+    kw = c.kwargs()
+    extra = kw["mask"].clone()
+    extra[:10] |= ~((1 << 10) - 1)
+    extra[10:] |= ~((1 << 3) - 1)
+    a, b = c.run(), c.run(mask=extra)
+    assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+
+
+@pytest.mark.parametrize("b, k", [(1, 40), (8, 5), (16, 40), (32, 17), (64, 3), (1024, 2)])
+@pytest.mark.parametrize("Hq, Hkv, nodes", [(8, 2, 9), (4, 4, 30), (16, 2, 1)])
+def test_selected_slots(Hq, Hkv, nodes, b, k):
+    c = Case([0, 1, 33, 500, 1500], [nodes, nodes, 0, nodes, 1], Hq, Hkv, seed=b + k, packed=nodes == 9)
+    c.select(k, b, empty=((3, 0), (4, Hkv - 1))).check()
+
+
+def test_spans_outside_the_cache_are_skipped():
+    c = Case([200, 100], [5, 5], 4, 2, seed=4).select(6, 16)
+    want = c.reference()
+    start, length, count = c.sel
+    bad = [(x.copy()) for x in c.sel]
+    room = [np.concatenate([x, x], axis=2) for x in bad[:2]]
+    n = start.shape[2]
+    for s in range(2):
+        for h in range(2):
+            c0 = count[s, h]
+            room[0][s, h, c0:c0 + 4] = [-3, c.rows - 2, 5, 2 ** 31 - 1]
+            room[1][s, h, c0:c0 + 4] = [4, 7, -1, 9]
+            bad[2][s, h] = c0 + 4
+    assert bad[2].max() <= 2 * n
+    c.sel = (room[0], room[1], bad[2])
+    c.check(want=want)
+
+
+def test_long_contexts_split_over_many_workgroups():
+    Case([20011, 40000, 3], [12, 3, 12], 8, 2, seed=8).check()
+    Case([33333], [16], 4, 4, seed=9, packed=True, nhd=True).check()
+    Case([9000], [128], 8, 1, seed=10).check()
+    Case([30000], [20], 8, 2, seed=11).select(400, 32).check()
+
+
+def test_scale_and_sharp_logits():
+    c = Case([300, 40], [9, 9], 8, 2, seed=6)
+    c.check(scale=0.3)
+    # queries as large as bf16 activations get: one key takes nearly all the weight.  A logit of some 2^8 is off by 2^-24 of the
+    # sum of its terms' sizes, 2^11 at most here: 2^-13 of the weights
+    c = Case([300, 40], [9, 9], 8, 2, seed=7, sharp=30.0)
+    out, size, lse = c.reference()
+    r = c.run()
+    assert bool(((r.out.double() - out).abs() <= 2.0 ** -12 * size).all())
+    assert bool(((r.lse.double() - lse).abs() <= 1e-5 * lse.abs()).all())
+
+
+def test_logits_near_the_end_of_the_range():
+    """Logits of 1e30: all the weight is on the largest, and nothing overflows."""
+    c = Case([400], [6], 4, 2, seed=12)
+    c.q = (c.q.float() * 1e30).bfloat16()
+    out, size, lse = c.reference()
+    for kw in ({}, dict(want_f32=False, want_bf16=True)):
+        r = c.run(**kw)
+        got = (r.out if r.out is not None else r.out_bf16).double()
+        assert bool(((got - out).abs() <= BF16 * out.abs() + 1e-5 * size).all())
+        assert bool(((r.lse.double() - lse).abs() <= 1e-5 * lse.abs()).all())
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_rows_that_are_masked_may_hold_anything(what, packed):
+    """K and V rows that no bit lets a node see: of other branches, of the room behind the nodes, of other sequences."""
+    c = Case([70, 0, 33], [21, 40, 3], 8, 2, seed=13, packed=packed)
+    want = c.reference()
+    clean = [c.run(), c.run(want_f32=False, want_bf16=True)]
+    for s, n in enumerate(c.n_new):
+        for j in range(n):                                       # one node's rows at a time: the others must not notice
+            if j % 5 != 3:
+                continue
+            blind = ~c.seen[s][:, j]
+            X, at = ((c.Kd, c.Vd), c.cu[s] + j) if packed else ((c.K, c.V), c.row0[s] + c.lens[s] + j)
+            old = [x[:, at].clone() for x in X]
+            for x in X:
+                x[:, at] = what
+            for r0, kw in zip(clean, ({}, dict(want_f32=False, want_bf16=True))):
+                r = c.run(**kw)
+                t = torch.arange(c.cu[s], c.cu[s + 1], device="cuda")[torch.from_numpy(blind).cuda()]
+                a, b = (x.out if x.out is not None else x.out_bf16 for x in (r, r0))
+                assert torch.equal(a[t], b[t]) and torch.equal(r.lse[t], r0.lse[t])
+            for x, o in zip(X, old):
+                x[:, at] = o
+    for s in range(3):                                           # the room behind every sequence
+        for x in (c.K, c.V):
+            x[:, c.row0[s] + c.lens[s] + (0 if packed else c.n_new[s]): c.row0[s + 1]] = what
+    c.check(want=want)
+
+
+def test_malformed_tables_are_cut():
+    c = Case([64, 64], [8, 8], 4, 2, seed=14)
+    base = c.run()
+    r = c.run(cu_new=i32([0, 8, 400]))                           # more nodes than there are rows and max_nodes
+    assert torch.equal(r.out, base.out)
+    r = c.run(cu_new=i32([0, 8, 3]))
+    assert torch.equal(r.out[:8], base.out[:8]) and bool((r.out[8:] == 9.0).all())
+    r = c.run(cu_new=i32([-1, 8, 16]))
+    assert bool((r.out[:8] == 9.0).all()) and torch.equal(r.out[8:], base.out[8:])
+    r = c.run(seq_len=i32([10 ** 9, 64]))                        # cut to max_seqlen = 64
+    assert torch.equal(r.out, base.out)
+    for kw in (dict(seq_row0=i32([-5, c.row0[1]])), dict(seq_len=i32([-5, 64])), dict(seq_row0=i32([2 ** 31 - 1, c.row0[1]]))):
+        r = c.run(**kw)
+        assert torch.equal(r.out[8:], base.out[8:]) and bool(torch.isfinite(r.out).all())
+
+
+def test_bit_identical_from_call_to_call_and_on_another_stream():
+    c = Case([5000, 700], [20, 9], 8, 2, seed=15)
+    a, b = c.run(), c.run()
+    st = torch.cuda.Stream()
+    r = _dsk().make_tree_attn_args(c.q, c.K, c.V, **c.kwargs())
+    torch.cuda.synchronize()
+    _dsk().dsk_tree_decode_attn(r.args, st)
+    st.synchronize()
+    for x in (b, r):
+        assert torch.equal(a.out, x.out) and torch.equal(a.lse, x.lse)
+
+
+def test_one_node_equals_the_decode_attention():
+    """A tree of its root alone is a decode step: dense attention over the prefix and the new row."""
+    dsk = _dsk()
+    c = Case([3000], [1], 32, 8, seed=16, spare=0)
+    den = dsk.dense_decode_attn(c.q, c.K, c.V, i32([0, c.rows]), c.rows)
+    r = c.run()
+    torch.cuda.synchronize()
+    assert float((r.out - den.out).abs().max()) <= 1e-5 and float((r.lse - den.lse).abs().max()) <= 1e-5
