@@ -328,7 +328,7 @@ static dsk_status validate_tree(const dsk_tree_attn_args* a) {
   if (a == nullptr) return DSK_ERR_NULL;
   if (a->struct_size != sizeof(dsk_tree_attn_args)) return DSK_ERR_VERSION;
   if (!geometry_ok(a->B, a->Hq, a->Hkv, a->D)) return DSK_ERR_SHAPE;
-  if (a->n_tokens < 0 || a->max_seqlen < 0 || a->total_rows < 0) return DSK_ERR_SHAPE;
+  if (a->n_tokens < 0 || a->max_seqlen < 0 || a->max_seqlen > kMaxTreePrefix || a->total_rows < 0) return DSK_ERR_SHAPE;
   if (a->max_nodes < 1 || a->max_nodes > DSK_TREE_MAX_NODES) return DSK_ERR_PARAM;
   if (!(a->scale >= 0.0f) || a->flags != 0) return DSK_ERR_PARAM;
   if (a->mask != nullptr && a->mask_words < (a->max_nodes + 31) / 32) return DSK_ERR_PARAM;
@@ -520,8 +520,8 @@ dsk_status dsk_qk_norm_rope(const dsk_norm_rope_args* a, void* stream) {
 
 size_t dsk_tree_attn_workspace_bytes(const dsk_tree_attn_args* a) {
   if (a == nullptr || a->struct_size != sizeof(dsk_tree_attn_args)) return 0;
-  if (!geometry_ok(a->B, a->Hq, a->Hkv, a->D) || a->n_tokens < 0 || a->max_seqlen < 0 || a->max_nodes < 1 ||
-      a->max_nodes > DSK_TREE_MAX_NODES || (a->sel_start && (a->k < 1 || a->b < 1 || a->b > 1024)))
+  if (!geometry_ok(a->B, a->Hq, a->Hkv, a->D) || a->n_tokens < 0 || a->max_seqlen < 0 || a->max_seqlen > kMaxTreePrefix ||
+      a->max_nodes < 1 || a->max_nodes > DSK_TREE_MAX_NODES || (a->sel_start && (a->k < 1 || a->b < 1 || a->b > 1024)))
     return 0;
   return tree_ws_bytes(*a);
 }
