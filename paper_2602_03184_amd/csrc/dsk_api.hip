@@ -340,7 +340,8 @@ static dsk_status validate_tree(const dsk_tree_attn_args* a) {
     if (!a->sel_start || !a->sel_len || !a->sel_count) return DSK_ERR_NULL;
     if (a->k < 1 || a->b < 1 || a->b > 1024) return DSK_ERR_PARAM;
   }
-  if (a->k_stride_tok < DSK_HEAD_DIM || a->v_stride_tok < DSK_HEAD_DIM || a->k_stride_head < 0 || a->v_stride_head < 0)
+  if (a->k_stride_tok < DSK_HEAD_DIM || a->v_stride_tok < DSK_HEAD_DIM || a->k_stride_head < 0 || a->v_stride_head < 0 ||
+      a->k_stride_tok > kMaxTokenStride || a->v_stride_tok > kMaxTokenStride)
     return DSK_ERR_SHAPE;
   if (!aligned16(a->q) || !aligned16(a->K) || !aligned16(a->V) || !aligned16(a->out) || !aligned16(a->out_bf16) ||
       a->k_stride_tok % 8 || a->k_stride_head % 8 || a->v_stride_tok % 8 || a->v_stride_head % 8)

@@ -16,6 +16,8 @@
 #include "dsk_common.hpp"
 #include "dsk_internal.hpp"
 
+#include <type_traits>
+
 namespace dsk {
 
 typedef __bf16 tree_bf16x8 __attribute__((ext_vector_type(8)));
@@ -28,11 +30,34 @@ constexpr int kTreeTile = 32;                   // keys and queries of a matrix 
 constexpr int kTreeRowBytes = 2 * DSK_HEAD_DIM;
 constexpr int kTreeMaxSlots = 256;              // selected slots of a workgroup
 constexpr int kTreeMaxListed = 2048;            // and their tokens
-constexpr int kTreeMaxSplit = 64;               // parts of a sequence: a lane each in the merge
+constexpr int kTreeMaxSplit = 64;               // parts of a sequence
+constexpr int kTreeMixedTiles = 16;             // tiles from the first one with a node on: 256 nodes, and a stage's other tiles
+constexpr int kTreeTileBytes = kTreeTile * kTreeRowBytes;
 
 __device__ __forceinline__ uint32_t tree_pack(float lo, float hi) {   // nearest-even bf16 pair
   const tree_f32x2 f = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, tree_bf16x2));
+}
+
+// 16 bytes at a uniform address and a lane's 32-bit offset, which is one instruction and no arithmetic; left to itself the
+// compiler adds the parts the other way round, with a 64-bit product or sum per lane and load.
+typedef const __attribute__((address_space(1))) char* tree_global;
+template <bool STREAM>
+__device__ __forceinline__ uint4 load16_at(tree_global base, uint32_t off) {
+  asm("" : "+s"(base));
+  typedef const __attribute__((address_space(1))) u32x4_t* at_t;
+  const at_t at = (at_t)(base + off);
+  u32x4_t v;
+  if constexpr (STREAM) v = __builtin_nontemporal_load(at);
+  else v = *at;
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+
+// a bf16 pair with 0 for what is not finite
+__device__ __forceinline__ uint32_t finite_bf16(uint32_t w) {
+  if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
+  if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
+  return w;
 }
 
 // bits x of a node's mask row for nodes 32 w .. 32 w + 31, of those that exist
@@ -65,328 +90,402 @@ struct TreeSplit {
   int slots_per_split;          // with a selection
 };
 
-// TERMS: bf16 terms that a weight is split into for the second product, 1 (bf16 result) or 3 (all 24 bits of it: fp32 result)
-template <int QW, int KW, int NT, int TERMS, bool SEL>
-__global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree_attn_kernel(
-    dsk_tree_attn_args a, int G, int q_tiles, TreeSplit sp, float scale, float2* __restrict__ part_ml,
-    float* __restrict__ part_acc) {
-  constexpr int kThreads = QW * KW * DSK_WAVE;
-  constexpr int kKeys = kTreeTile * KW * NT;             // keys of a stage
-  constexpr int kLoads = kKeys * 16 / kThreads;          // 16-byte chunks of K (and of V) of a thread
-  constexpr int kRowStep = kThreads / 16;
-  __shared__ __align__(16) unsigned char sm_kv[2 * kKeys * kTreeRowBytes];
-  __shared__ float2 sm_ml[KW > 1 ? (KW - 1) * QW * DSK_WAVE : 1];
-  __shared__ uint32_t sm_bad[2][KW * NT];                // rows of V that hold values that are not finite
-  __shared__ int32_t sm_rows[SEL ? kTreeMaxListed : 1];
-  __shared__ int32_t sm_slot[SEL ? 3 : 1][SEL ? kTreeMaxSlots : 1];
-  __shared__ int32_t sm_wave[SEL ? kTreeMaxSlots / DSK_WAVE : 1];
-
-  unsigned char* const sm_k = sm_kv;
-  unsigned char* const sm_v = sm_kv + kKeys * kTreeRowBytes;
-  const int split = blockIdx.x, s = blockIdx.z;
-  const int hk = blockIdx.y / q_tiles, q_tile = blockIdx.y - hk * q_tiles;
-  const int tid = threadIdx.x, lane = tid & (DSK_WAVE - 1), wave = tid / DSK_WAVE;
-  const int qw = wave % QW, kw = wave / QW;
-  const int col = lane & 31, half = lane >> 5;
-
-  int tok0 = a.cu_new[s], n = a.cu_new[s + 1] - tok0;
-  if (tok0 < 0 || n <= 0 || tok0 > a.n_tokens) return;
-  n = n < a.max_nodes ? n : a.max_nodes;
-  n = n < a.n_tokens - tok0 ? n : a.n_tokens - tok0;
-  const int R = n * G, r0 = (q_tile * QW + qw) * kTreeTile;
-  if (q_tile * QW * kTreeTile >= R) return;              // uniform: no row of this pass
-  int64_t row0 = a.seq_row0[s], len = a.seq_len[s];
-  if (row0 < 0 || row0 > a.total_rows || len < 0) row0 = len = 0;
-  len = len < a.max_seqlen ? len : a.max_seqlen;
-  len = len < a.total_rows - row0 ? len : a.total_rows - row0;
-  // nodes that have a K/V row
-  const int n_keys = a.Kd != nullptr || n < a.total_rows - row0 - len ? n : (int)(a.total_rows - row0 - len);
-
-  // Keys of this workgroup: t in [t_begin, t_end), of which those below P are the prefix's and t - P is a node's number.
-  int P, t_begin, t_end, used;
-  if constexpr (SEL) {
-    const int64_t sk = (int64_t)s * a.Hkv + hk;
-    int count = a.sel_count[sk];
-    count = count < 0 ? 0 : (count < a.k ? count : a.k);
-    used = (count + sp.slots_per_split - 1) / sp.slots_per_split;
-    used = used > 0 ? used : 1;                          // the nodes go with the last slots
-    if (split >= used) return;
-    const int first = split * sp.slots_per_split;
-    const int here = count - first < sp.slots_per_split ? count - first : sp.slots_per_split;
-    int start = 0, ln = 0;
-    if (tid < here) {
-      start = a.sel_start[sk * a.k + first + tid];
-      ln = a.sel_len[sk * a.k + first + tid];
-      ln = ln < a.b ? ln : a.b;
-      if (start < 0 || ln <= 0 || start > a.total_rows - ln) ln = 0;
-    }
-    if (tid < kTreeMaxSlots) {
-      const int incl = wave_incl_scan_i(ln, lane);
-      if (lane == DSK_WAVE - 1) sm_wave[wave] = incl;
-      sm_slot[0][tid] = incl - ln;
-      sm_slot[1][tid] = start;
-      sm_slot[2][tid] = ln;
-    }
-    __syncthreads();
-    P = 0;
-#pragma unroll
-    for (int w = 0; w < kTreeMaxSlots / DSK_WAVE; ++w) P += sm_wave[w];
-    for (int i = tid; i < here * a.b; i += kThreads) {
-      const int slot = i / a.b, off = i - slot * a.b;
-      int base = sm_slot[0][slot];
-      for (int w = 0; w < slot / DSK_WAVE; ++w) base += sm_wave[w];
-      if (off < sm_slot[2][slot]) sm_rows[base + off] = sm_slot[1][slot] + off;
-    }
-    __syncthreads();
-    t_begin = 0;
-    t_end = P + (split == used - 1 ? n_keys : 0);
-  } else {
-    P = (int)len;
-    const int64_t T = len + n_keys;
-    used = (int)((T + sp.keys_per_split - 1) / sp.keys_per_split);
-    used = used > 0 ? used : 1;
-    used = used < sp.nsplit ? used : sp.nsplit;          // (never more: the host counts max_seqlen + max_nodes keys)
-    if (split >= used) return;
-    t_begin = split * sp.keys_per_split;
-    t_end = (int)(T - t_begin < sp.keys_per_split ? T : t_begin + sp.keys_per_split);
+// What a sequence has in fact, malformed tables cut to the bounds that the host knows.
+struct TreePlace {
+  int tok0, n;          // its nodes' first token and their number; 0: nothing to do
+  int64_t row0, len;    // prefix
+  int n_keys;           // nodes that have a K/V row
+  __device__ __forceinline__ TreePlace(const dsk_tree_attn_args& a, int s) {
+    tok0 = a.cu_new[s];
+    n = a.cu_new[s + 1] - tok0;
+    if (tok0 < 0 || n <= 0 || tok0 > a.n_tokens) n = 0;
+    n = n < a.max_nodes ? n : a.max_nodes;
+    n = n < a.n_tokens - tok0 ? n : a.n_tokens - tok0;
+    row0 = a.seq_row0[s];
+    len = a.seq_len[s];
+    if (row0 < 0 || row0 > a.total_rows || len < 0) row0 = len = 0;
+    len = len < a.max_seqlen ? len : a.max_seqlen;
+    len = len < a.total_rows - row0 ? len : a.total_rows - row0;
+    n_keys = a.Kd != nullptr || n < a.total_rows - row0 - len ? n : (int)(a.total_rows - row0 - len);
   }
+  // parts of its keys that have any
+  __device__ __forceinline__ int used(const dsk_tree_attn_args& a, const TreeSplit& sp, bool selected, int64_t s_hk) const {
+    int64_t u;
+    if (selected) {
+      int count = a.sel_count[s_hk];
+      count = count < 0 ? 0 : (count < a.k ? count : a.k);
+      u = (count + sp.slots_per_split - 1) / sp.slots_per_split;
+    } else {
+      u = (len + n_keys + sp.keys_per_split - 1) / sp.keys_per_split;
+    }
+    u = u > 0 ? u : 1;                                   // the nodes go with the last slots
+    return (int)(u < sp.nsplit ? u : sp.nsplit);         // (never more: the host counts max_seqlen + max_nodes keys)
+  }
+};
 
-  // ---- queries: a lane's row, 8 channels of every 16 of its half --------------------------------------------
-  const bool busy = r0 < R;                              // rows for this wavefront (uniform over it)
-  const int r = r0 + col;
-  const bool real = r < R;
-  const int node = real ? r / G : 0, g = real ? r - node * G : 0;
-  const int64_t out_row = (int64_t)(tok0 + node) * a.Hq + hk * G + g;
-  tree_bf16x8 qf[8];
-  {
-    const uint16_t* q = static_cast<const uint16_t*>(a.q) + out_row * DSK_HEAD_DIM + half * 8;
+// The keys of a workgroup: t in [t_begin, t_end), of which those below P are the prefix's and t - P is a node's number.  A
+// stage of LOADS * THREADS / 16 keys is fetched to registers and put to LDS, a thread taking a 16-byte chunk of every
+// THREADS / 16-th row.
+template <int THREADS, int LOADS, bool SEL, bool STREAM>
+struct TreeKeys {
+  static constexpr int kRowStep = THREADS / 16;
+  static constexpr int kKeys = LOADS * kRowStep;
+  int P, t_begin, t_end;
+  int t_mixed;                          // first stage that is not the prefix's alone
+  int lrow, lc;
+  int64_t kst, vst, row0;
+  const uint16_t *K, *V, *Kn, *Vn;      // this lane's chunk of the prefix (of the whole cache with SEL) and of the nodes
+  int64_t knst, vnst;
+  tree_global Ku, Vu;                   // the prefix of the head, without the lane's part
+  uint32_t k_off, v_off;                // the lane's part in bytes
+  const int32_t* rows;                  // cache rows of the selected tokens, in LDS
+  struct Regs {
+    uint4 k[LOADS], v[LOADS];
+  };
+
+  __device__ __forceinline__ TreeKeys(const dsk_tree_attn_args& a, const TreeSplit& sp, const TreePlace& at, int s, int hk,
+                                      int split, int used, int32_t* sm_rows) {
+    const int tid = threadIdx.x, lane = tid & (DSK_WAVE - 1), wave = tid / DSK_WAVE;
+    lrow = tid >> 4;
+    lc = tid & 15;
+    kst = a.k_stride_tok;
+    vst = a.v_stride_tok;
+    row0 = SEL ? 0 : at.row0;
+    rows = sm_rows;
+    K = static_cast<const uint16_t*>(a.K) + hk * a.k_stride_head + row0 * kst;
+    V = static_cast<const uint16_t*>(a.V) + hk * a.v_stride_head + row0 * vst;
+    Ku = (tree_global)K;
+    Vu = (tree_global)V;
+    k_off = (uint32_t)(lrow * (int)kst + lc * 8) * 2u;   // 32 rows of 2^24 channels at most
+    v_off = (uint32_t)(lrow * (int)vst + lc * 8) * 2u;
+    K += lc * 8;
+    V += lc * 8;
+    if (a.Kd != nullptr) {
+      knst = a.kd_stride_tok;
+      vnst = a.vd_stride_tok;
+      Kn = static_cast<const uint16_t*>(a.Kd) + hk * a.kd_stride_head + at.tok0 * knst + lc * 8;
+      Vn = static_cast<const uint16_t*>(a.Vd) + hk * a.vd_stride_head + at.tok0 * vnst + lc * 8;
+    } else {
+      knst = kst;
+      vnst = vst;
+      Kn = K + (at.row0 - row0 + at.len) * kst;
+      Vn = V + (at.row0 - row0 + at.len) * vst;
+    }
+    if constexpr (SEL) {
+      __shared__ int32_t sm_slot[3][kTreeMaxSlots];
+      __shared__ int32_t sm_wave[kTreeMaxSlots / DSK_WAVE];
+      const int64_t sk = (int64_t)s * a.Hkv + hk;
+      int count = a.sel_count[sk];
+      count = count < 0 ? 0 : (count < a.k ? count : a.k);
+      const int first = split * sp.slots_per_split;
+      const int here = count - first < sp.slots_per_split ? count - first : sp.slots_per_split;
+      int start = 0, ln = 0;
+      if (tid < here) {
+        start = a.sel_start[sk * a.k + first + tid];
+        ln = a.sel_len[sk * a.k + first + tid];
+        ln = ln < a.b ? ln : a.b;
+        if (start < 0 || ln <= 0 || start > a.total_rows - ln) ln = 0;
+      }
+      if (tid < kTreeMaxSlots) {
+        const int incl = wave_incl_scan_i(ln, lane);
+        if (lane == DSK_WAVE - 1) sm_wave[wave] = incl;
+        sm_slot[0][tid] = incl - ln;
+        sm_slot[1][tid] = start;
+        sm_slot[2][tid] = ln;
+      }
+      __syncthreads();
+      P = 0;
+#pragma unroll
+      for (int w = 0; w < kTreeMaxSlots / DSK_WAVE; ++w) P += sm_wave[w];
+      for (int i = tid; i < here * a.b; i += THREADS) {
+        const int slot = i / a.b, off = i - slot * a.b;
+        int base = sm_slot[0][slot];
+        for (int w = 0; w < slot / DSK_WAVE; ++w) base += sm_wave[w];
+        if (off < sm_slot[2][slot]) sm_rows[base + off] = sm_slot[1][slot] + off;
+      }
+      __syncthreads();
+      t_begin = 0;
+      t_end = P + (split == used - 1 ? at.n_keys : 0);
+    } else {
+      P = (int)at.len;
+      t_begin = split * sp.keys_per_split;
+      t_end = P + at.n_keys - t_begin < sp.keys_per_split ? P + at.n_keys : t_begin + sp.keys_per_split;
+    }
+    t_mixed = P > t_begin ? t_begin + (P - t_begin) / kKeys * kKeys : t_begin;
+  }
+  __device__ __forceinline__ bool plain(int t0) const { return t0 + kKeys <= P; }   // a stage of the prefix alone: nothing is masked
+  __device__ __forceinline__ int nodes() const { return t_end > P ? t_end - P : 0; }
+  __device__ __forceinline__ const uint16_t* k_at(int t) const {
+    return t < P ? K + (int64_t)(SEL ? rows[t] : t) * kst : Kn + (int64_t)(t - P) * knst;
+  }
+  __device__ __forceinline__ const uint16_t* v_at(int t) const {
+    return t < P ? V + (int64_t)(SEL ? rows[t] : t) * vst : Vn + (int64_t)(t - P) * vnst;
+  }
+  // a stage of the prefix alone
+  __device__ __forceinline__ void fetch_plain(Regs& x, int t0) const {
+    if constexpr (SEL) {
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) x.k[u] = load16<false>(K + rows[t0 + lrow + u * kRowStep] * kst);
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) x.v[u] = load16<false>(V + rows[t0 + lrow + u * kRowStep] * vst);
+    } else {
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) x.k[u] = load16_at<STREAM>(Ku + (t0 + u * kRowStep) * kst * 2, k_off);
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) x.v[u] = load16_at<STREAM>(Vu + (t0 + u * kRowStep) * vst * 2, v_off);
+    }
+  }
+  __device__ __forceinline__ void fetch_mixed(Regs& x, int t0) const {
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      const int t = t0 + lrow + u * kRowStep;
+      x.k[u] = x.v[u] = make_uint4(0, 0, 0, 0);
+      if (t < t_end) {
+        x.k[u] = load16<false>(k_at(t));
+        x.v[u] = load16<false>(v_at(t));
+      }
+    }
+  }
+  __device__ __forceinline__ void fetch(Regs& x, int t0) const {
+    if (t0 >= t_end) return;
+    if (plain(t0)) fetch_plain(x, t0);
+    else fetch_mixed(x, t0);
+  }
+  // sm_bad: a word per tile from t_mixed on, zero before; rows of V that hold values that are not finite
+  template <bool MIXED>
+  __device__ __forceinline__ void put(Regs& x, int t0, unsigned char* sm_k, unsigned char* sm_v, uint32_t* sm_bad) const {
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      const int row = lrow + u * kRowStep;
+      uint4 v = x.v[u];
+      if constexpr (MIXED) {
+        // a masked row may hold anything, and 0 * NaN is NaN: such values stay out of the product, and their row is noted
+        v = make_uint4(finite_bf16(v.x), finite_bf16(v.y), finite_bf16(v.z), finite_bf16(v.w));
+        if (v.x != x.v[u].x || v.y != x.v[u].y || v.z != x.v[u].z || v.w != x.v[u].w)
+          atomicOr(&sm_bad[(t0 - t_mixed + row) / kTreeTile], 1u << (row % kTreeTile));
+      }
+      *reinterpret_cast<uint4*>(sm_k + row * kTreeRowBytes + ((lc ^ (row & 15)) << 4)) = x.k[u];
+      *reinterpret_cast<uint4*>(sm_v + row * kTreeRowBytes + ((lc ^ ((row & 3) << 2)) << 4)) = v;
+    }
+  }
+};
+
+// A wavefront's 32 queries: a lane has query lane % 32 and of a tile's 32 keys those at 8 (i / 4) + 4 (lane / 32) + i % 4.
+struct TreeQueries {
+  bool busy, real;      // the wavefront has rows; the lane's row exists
+  int col, half, node;
+  int64_t out_row;
+  TreeMask mask;
+  tree_bf16x8 q[8];     // channels 16 t + 8 half .. + 7
+
+  __device__ __forceinline__ TreeQueries(const dsk_tree_attn_args& a, const TreePlace& at, int G, int hk, int r0, int n_keys) {
+    const int lane = threadIdx.x & (DSK_WAVE - 1);
+    col = lane & 31;
+    half = lane >> 5;
+    busy = r0 < at.n * G;
+    const int r = r0 + col;
+    real = r < at.n * G;
+    node = real ? r / G : 0;
+    out_row = (int64_t)(at.tok0 + node) * a.Hq + hk * G + (real ? r - node * G : 0);
+    const uint16_t* from = static_cast<const uint16_t*>(a.q) + out_row * DSK_HEAD_DIM + half * 8;
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
       uint4 x = make_uint4(0, 0, 0, 0);
-      if (real) x = *reinterpret_cast<const uint4*>(q + t * 16);
-      qf[t] = __builtin_bit_cast(tree_bf16x8, x);
+      if (real) x = *reinterpret_cast<const uint4*>(from + t * 16);
+      q[t] = __builtin_bit_cast(tree_bf16x8, x);
     }
+    mask.row = a.mask != nullptr ? a.mask + (int64_t)(at.tok0 + node) * a.mask_words : nullptr;
+    mask.node = node;
+    mask.n = n_keys;
   }
-  const TreeMask mask = {a.mask != nullptr ? a.mask + (int64_t)(tok0 + node) * a.mask_words : nullptr, node,
-                         t_end > P ? t_end - P : 0};
+  __device__ __forceinline__ uint32_t allowed(int t0, int P) const { return real ? mask.window(t0 - P) : 0u; }
+};
 
-  // ---- tiles ------------------------------------------------------------------------------------------------
-  const int lrow = tid >> 4, lc = tid & 15;
-  const uint16_t* Kh = static_cast<const uint16_t*>(a.K) + hk * a.k_stride_head + lc * 8;
-  const uint16_t* Vh = static_cast<const uint16_t*>(a.V) + hk * a.v_stride_head + lc * 8;
-  uint4 kx[kLoads], vx[kLoads];
-  auto v_row = [&](int t, const uint16_t* prefix, int chunk) -> const uint16_t* {   // V of key t, nullptr: no such key
-    if (t < P) return prefix + (int64_t)(SEL ? sm_rows[t] : row0 + t) * a.v_stride_tok;
-    const int j = t - P;
-    if (t >= t_end) return nullptr;
-    if (a.Kd == nullptr) return prefix + (row0 + len + j) * a.v_stride_tok;
-    return static_cast<const uint16_t*>(a.Vd) + hk * a.vd_stride_head + (int64_t)(tok0 + j) * a.vd_stride_tok + chunk * 8;
-  };
-  auto k_row = [&](int t) -> const uint16_t* {
-    if (t < P) return Kh + (int64_t)(SEL ? sm_rows[t] : row0 + t) * a.k_stride_tok;
-    const int j = t - P;
-    if (t >= t_end) return nullptr;
-    if (a.Kd == nullptr) return Kh + (row0 + len + j) * a.k_stride_tok;
-    return static_cast<const uint16_t*>(a.Kd) + hk * a.kd_stride_head + (int64_t)(tok0 + j) * a.kd_stride_tok + lc * 8;
-  };
-  auto fetch = [&](int t0) {
-    if (t0 + kKeys <= P) {
+// Fragments of a tile of 32 keys.
+struct TreeKFrag {
+  tree_bf16x8 k[8];
+  template <int FROM, int TO>
+  __device__ __forceinline__ void read(const unsigned char* sm_k, const TreeQueries& qs) {
+    const unsigned char* at = sm_k + qs.col * kTreeRowBytes;
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const int t = t0 + lrow + u * kRowStep;
-        kx[u] = load16<false>(Kh + (int64_t)(SEL ? sm_rows[t] : row0 + t) * a.k_stride_tok);
-      }
+    for (int t = FROM; t < TO; ++t)
+      k[t] = *reinterpret_cast<const tree_bf16x8*>(at + (((2 * t + qs.half) ^ (qs.col & 15)) << 4));
+  }
+  // logits: S^T = K Q^T
+  template <int FROM, int TO>
+  __device__ __forceinline__ void add(tree_f32x16& z, const TreeQueries& qs) const {
+    if constexpr (FROM == 0) {
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const int t = t0 + lrow + u * kRowStep;
-        vx[u] = load16<false>(Vh + (int64_t)(SEL ? sm_rows[t] : row0 + t) * a.v_stride_tok);
-      }
-    } else {
+      for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+    }
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const int t = t0 + lrow + u * kRowStep;
-        kx[u] = vx[u] = make_uint4(0, 0, 0, 0);
-        if (t < t_end) {
-          kx[u] = load16<false>(k_row(t));
-          vx[u] = load16<false>(v_row(t, Vh, lc));
+    for (int t = FROM; t < TO; ++t) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[t], qs.q[t], z, 0, 0, 0);
+  }
+};
+
+__device__ __forceinline__ void tree_hide(tree_f32x16& z, uint32_t allow, int half) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    z[i] = (allow >> (8 * (i >> 2) + 4 * half + (i & 3))) & 1u ? z[i] : -__builtin_inff();
+}
+
+// the larger of a value and the other half's
+__device__ __forceinline__ float tree_half_max(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float tree_max(const tree_f32x16& z) {
+  float m = z[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) m = fmaxf(m, z[i]);
+  return tree_half_max(m);
+}
+
+// the weights of a tile, in TERMS bf16 terms
+template <int TERMS>
+struct TreeWeights {
+  tree_bf16x8 w[TERMS][2];
+  __device__ __forceinline__ void set(float (&p)[16]) {
+#pragma unroll
+    for (int term = 0; term < TERMS; ++term) {
+      uint32_t x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = tree_pack(p[2 * i], p[2 * i + 1]);
+        if (term + 1 < TERMS) {                          // what the terms so far leave
+          p[2 * i] -= bf16_lo(x[i]);
+          p[2 * i + 1] -= bf16_hi(x[i]);
         }
       }
+      w[term][0] = __builtin_bit_cast(tree_bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+      w[term][1] = __builtin_bit_cast(tree_bf16x8, make_uint4(x[4], x[5], x[6], x[7]));
     }
-  };
+  }
+};
 
-  float m = -__builtin_inff(), l = 0.0f;                 // running maximum (of q.K, not scaled) and this half's sum of a query
-  tree_f32x16 O[4];
+struct TreeVFrag {
+  tree_bf16x8 v[4][2];
+  template <int T>                                       // 16 of the keys
+  __device__ __forceinline__ void read(const unsigned char* sm_v) {
+    const int lane = threadIdx.x & (DSK_WAVE - 1), half = lane >> 5;
+    const int quad = (lane & 15) >> 2;                   // of the four keys of a transposing read
+    const unsigned char* vt = sm_v + (4 * half + quad) * kTreeRowBytes + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) +
+                              ((lane & 1) << 3);
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) {
+      const unsigned char* at = vt + ((ct ^ quad) << 6) + T * 16 * kTreeRowBytes;
+      const tree_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) tree_s16x4*)(at));
+      const tree_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) tree_s16x4*)(at + 8 * kTreeRowBytes));
+      v[ct][T] = __builtin_bit_cast(tree_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+  // O^T += V^T P^T
+  template <int TERMS>
+  __device__ __forceinline__ void add(tree_f32x16 (&O)[4], const TreeWeights<TERMS>& p, int t) const {   // 16 of the keys
+#pragma unroll
+    for (int term = TERMS - 1; term >= 0; --term)
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct)
+        O[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[ct][t], p.w[term][t], O[ct], 0, 0, 0);
+  }
+};
+
+// The values that put() left out of a tile, for the nodes that see them.
+template <class KEYS>
+__device__ __forceinline__ void tree_values_left_out(tree_f32x16 (&O)[4], const KEYS& keys, const uint32_t* sm_bad,
+                                                     uint32_t allow, int t0, int half) {
+  for (uint32_t bad = __builtin_amdgcn_readfirstlane(sm_bad[(t0 - keys.t_mixed) / kTreeTile]); bad != 0; bad &= bad - 1) {
+    const int j = __builtin_ctz(bad);
+    if (!((allow >> j) & 1u)) continue;
+    const uint16_t* v = keys.v_at(t0 + j) - keys.lc * 8 + 4 * half;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint16_t x = v[ct * 32 + 8 * (i >> 2) + (i & 3)];
+        if ((x & 0x7F80u) == 0x7F80u) O[ct][i] += bf16_to_f32(x);
+      }
+  }
+}
+
+__device__ __forceinline__ void tree_scale(tree_f32x16 (&O)[4], float f) {
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) O[ct][i] = 0.0f;
-  const float scale_log2 = scale * kLog2e;
+    for (int i = 0; i < 16; ++i) O[ct][i] *= f;
+}
 
-  if (tid < KW * NT) sm_bad[0][tid] = 0;
-  if (t_begin < t_end) fetch(t_begin);
-  __syncthreads();
-  int flip = 0;
-  for (int t0 = t_begin; t0 < t_end; t0 += kKeys, flip ^= 1) {
-    const bool plain = t0 + kKeys <= P;                  // prefix only: nothing is masked
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const int row = lrow + u * kRowStep;
-      if (!plain) {
-        // a masked row may hold anything, and 0 * NaN is NaN: such values stay out of the product, and their row is noted
-        uint32_t* w = reinterpret_cast<uint32_t*>(&vx[u]);
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if ((w[i] & 0x7F80u) == 0x7F80u) { w[i] &= 0xFFFF0000u; bad = true; }
-          if ((w[i] & 0x7F800000u) == 0x7F800000u) { w[i] &= 0xFFFFu; bad = true; }
-        }
-        if (bad) atomicOr(&sm_bad[flip][row / kTreeTile], 1u << (row % kTreeTile));
-      }
-      *reinterpret_cast<uint4*>(sm_k + row * kTreeRowBytes + ((lc ^ (row & 15)) << 4)) = kx[u];
-      *reinterpret_cast<uint4*>(sm_v + row * kTreeRowBytes + ((lc ^ ((row & 3) << 2)) << 4)) = vx[u];
-    }
-    __syncthreads();
-    if (tid < KW * NT) sm_bad[flip ^ 1][tid] = 0;
-    if (t0 + kKeys < t_end) fetch(t0 + kKeys);
-    if (busy) {
-#pragma unroll 1
-      for (int sub = 0; sub < NT; ++sub) {
-        const int tile = kw * NT + sub, tt = t0 + tile * kTreeTile;
-        if (tt >= t_end) break;
-        // S^T: keys x queries
-        tree_f32x16 z;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) z[i] = 0.0f;
-        const unsigned char* kt = sm_k + (tile * kTreeTile + col) * kTreeRowBytes;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const tree_bf16x8 kf = *reinterpret_cast<const tree_bf16x8*>(kt + (((2 * t + half) ^ (col & 15)) << 4));
-          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[t], z, 0, 0, 0);
-        }
-        uint32_t allow = 0xFFFFFFFFu;
-        if (!plain) {
-          allow = real ? mask.window(tt - P) : 0u;
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            z[i] = (allow >> (8 * (i >> 2) + 4 * half + (i & 3))) & 1u ? z[i] : -__builtin_inff();
-        }
-        float mx = z[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, z[i]);
-        mx = fmaxf(mx, shfl_xor_f(mx, 32));
-        // The reference of the exponents only has to be near the maximum: it moves when a query's grows by more than 8 in
-        // log2 units, so most tiles rescale nothing, and the weights stay below 2^8.
-        if (__any((mx - m) * scale_log2 > 8.0f)) {       // m = -inf: true unless nothing has been seen
-          const float m_new = fmaxf(m, mx);
-          const float f = m == -__builtin_inff() ? 0.0f : exp2_small((m - m_new) * scale_log2);
-          l *= f;
-#pragma unroll
-          for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) O[ct][i] *= f;
-          m = m_new;
-        }
-        const float ref = m == -__builtin_inff() ? 0.0f : m;
-        float p[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          // the difference before the scale: exact for the largest, however large it is
-          p[i] = exp2_small((z[i] - ref) * scale_log2);
-          l += p[i];
-        }
-        tree_bf16x8 pf[TERMS][2];
-#pragma unroll
-        for (int term = 0; term < TERMS; ++term) {
-          uint32_t w[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            w[i] = tree_pack(p[2 * i], p[2 * i + 1]);
-            if (term + 1 < TERMS) {                      // what the terms so far leave
-              p[2 * i] -= bf16_lo(w[i]);
-              p[2 * i + 1] -= bf16_hi(w[i]);
-            }
-          }
-          pf[term][0] = __builtin_bit_cast(tree_bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-          pf[term][1] = __builtin_bit_cast(tree_bf16x8, make_uint4(w[4], w[5], w[6], w[7]));
-        }
-        // O^T: channels x queries
-        const int quad = (lane & 15) >> 2;               // of the four keys of a transposing read
-        const unsigned char* vt = sm_v + (tile * kTreeTile + 4 * half + quad) * kTreeRowBytes +
-                                  ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + ((lane & 1) << 3);
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct) {
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const unsigned char* at = vt + ((ct ^ quad) << 6) + t * 16 * kTreeRowBytes;
-            const tree_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) tree_s16x4*)(at));
-            const tree_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) tree_s16x4*)(at + 8 * kTreeRowBytes));
-            const tree_bf16x8 vf = __builtin_bit_cast(tree_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int term = TERMS - 1; term >= 0; --term)
-              O[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[term][t], O[ct], 0, 0, 0);
-          }
-        }
-        if (!plain) {                                    // the values left out above, for the nodes that see them
-          for (uint32_t bad = __builtin_amdgcn_readfirstlane(sm_bad[flip][tile]); bad != 0; bad &= bad - 1) {
-            const int j = __builtin_ctz(bad);
-            if (!((allow >> j) & 1u)) continue;
-            const uint16_t* v = v_row(tt + j, Vh - lc * 8, 0) + 4 * half;
-#pragma unroll
-            for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const uint16_t x = v[ct * 32 + 8 * (i >> 2) + (i & 3)];
-                if ((x & 0x7F80u) == 0x7F80u) O[ct][i] += bf16_to_f32(x);
-              }
-          }
-        }
-      }
-    }
-    __syncthreads();
-  }
-  l += shfl_xor_f(l, 32);
-
-  // ---- wavefronts that took other keys for the same queries, in order ---------------------------------------
-  if constexpr (KW > 1) {
-    float* const sm_o = reinterpret_cast<float*>(sm_kv);   // (KW - 1) * QW blocks of 64 values of 64 lanes
-    if (kw > 0 && busy) {
-      const int at = (kw - 1) * QW + qw;
-      sm_ml[at * DSK_WAVE + lane] = make_float2(m, l);
-#pragma unroll
-      for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sm_o[(at * 64 + ct * 16 + i) * DSK_WAVE + lane] = O[ct][i];
-    }
-    __syncthreads();
-    if (kw > 0) return;
-    if (busy) {
-      float M = m;
-#pragma unroll
-      for (int o = 0; o < KW - 1; ++o) M = fmaxf(M, sm_ml[(o * QW + qw) * DSK_WAVE + lane].x);
-      const float f = m == -__builtin_inff() ? 0.0f : exp2_small((m - M) * scale_log2);
+// A query's running softmax: the reference of its exponents in log2 units (-inf: nothing seen) and this half's sum.
+struct TreeSoftmax {
+  float m, l, scale_log2;
+  FmaExponent exponent;
+  __device__ __forceinline__ explicit TreeSoftmax(float scale) : m(-__builtin_inff()), l(0.0f), scale_log2(scale), exponent(scale, 0.0f) {}
+  // weights of a tile from its logits
+  template <int TERMS>
+  __device__ __forceinline__ void take(const tree_f32x16& z, tree_f32x16 (&O)[4], TreeWeights<TERMS>& w) {
+    const float mx = tree_max(z) * scale_log2;
+    // The reference only has to be near the maximum: it moves when a query's maximum grows by more than 8, so most tiles
+    // rescale nothing, and the weights stay below 2^8.
+    if (__any(mx - m > 8.0f)) {                          // m = -inf: true unless nothing has been seen
+      const float m_new = fmaxf(m, mx);
+      const float f = m == -__builtin_inff() ? 0.0f : exp2_small(m - m_new);
       l *= f;
-#pragma unroll
-      for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) O[ct][i] *= f;
-#pragma unroll
-      for (int o = 0; o < KW - 1; ++o) {
-        const int at = o * QW + qw;
-        const float2 ml = sm_ml[at * DSK_WAVE + lane];
-        const float fo = ml.x == -__builtin_inff() ? 0.0f : exp2_small((ml.x - M) * scale_log2);
-        l = fmaf(ml.y, fo, l);
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) O[ct][i] = fmaf(sm_o[(at * 64 + ct * 16 + i) * DSK_WAVE + lane], fo, O[ct][i]);
-      }
-      m = M;
+      tree_scale(O, f);
+      m = m_new;
+      exponent = FmaExponent(scale_log2, m == -__builtin_inff() ? 0.0f : m);
     }
+    float p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p[i] = exp2_small(exponent.of(z[i]));
+      l += p[i];
+    }
+    w.set(p);
   }
-  if (!real) return;
-  // a lane's channels: four in a row, at 32 ct + 8 i + 4 half
+};
+
+// The states of KW wavefronts that took other keys for the same queries, in order, into that of the first (kw = 0).
+// sm_o: (KW - 1) * QW blocks of 64 values of 64 lanes.
+template <int QW, int KW>
+__device__ __forceinline__ void tree_join(TreeSoftmax& sm, tree_f32x16 (&O)[4], bool busy, int qw, int kw, float* sm_o, float2* sm_ml) {
+  const int lane = threadIdx.x & (DSK_WAVE - 1);
+  if (kw > 0 && busy) {
+    const int blk = (kw - 1) * QW + qw;
+    sm_ml[blk * DSK_WAVE + lane] = make_float2(sm.m, sm.l);
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sm_o[(blk * 64 + ct * 16 + i) * DSK_WAVE + lane] = O[ct][i];
+  }
+  __syncthreads();
+  if (kw > 0 || !busy) return;
+  float M = sm.m;
+#pragma unroll
+  for (int o = 0; o < KW - 1; ++o) M = fmaxf(M, sm_ml[(o * QW + qw) * DSK_WAVE + lane].x);
+  const float f = sm.m == -__builtin_inff() ? 0.0f : exp2_small(sm.m - M);
+  sm.l *= f;
+  tree_scale(O, f);
+#pragma unroll
+  for (int o = 0; o < KW - 1; ++o) {
+    const int blk = o * QW + qw;
+    const float2 ml = sm_ml[blk * DSK_WAVE + lane];
+    const float fo = ml.x == -__builtin_inff() ? 0.0f : exp2_small(ml.x - M);
+    sm.l = fmaf(ml.y, fo, sm.l);
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) O[ct][i] = fmaf(sm_o[(blk * 64 + ct * 16 + i) * DSK_WAVE + lane], fo, O[ct][i]);
+  }
+  sm.m = M;
+}
+
+// A lane's row: final, or this part's share.  Its channels lie four in a row, at 32 ct + 8 i + 4 half.
+__device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const TreeQueries& qs, const tree_f32x16 (&O)[4], float m,
+                                           float l, int used, int nsplit, int split, float2* part_ml, float* part_acc) {
+  if (!qs.real) return;
   if (used == 1) {
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
@@ -394,22 +493,303 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float4 x = make_float4(O[ct][4 * i] * inv, O[ct][4 * i + 1] * inv, O[ct][4 * i + 2] * inv, O[ct][4 * i + 3] * inv);
-        const int64_t at = out_row * DSK_HEAD_DIM + ct * 32 + 8 * i + 4 * half;
+        const int64_t at = qs.out_row * DSK_HEAD_DIM + ct * 32 + 8 * i + 4 * qs.half;
         if (a.out != nullptr) *reinterpret_cast<float4*>(a.out + at) = x;
         if (a.out_bf16 != nullptr)
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out_bf16) + at) = make_uint2(tree_pack(x.x, x.y), tree_pack(x.z, x.w));
       }
-    if (half == 0 && a.lse != nullptr) a.lse[out_row] = l > 0.0f ? (m * scale_log2 + log2f(l)) * kLn2 : -__builtin_inff();
+    if (qs.half == 0 && a.lse != nullptr) a.lse[qs.out_row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
   } else {
-    const int64_t part = out_row * sp.nsplit + split;
+    const int64_t part = qs.out_row * nsplit + split;
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(part_acc + part * DSK_HEAD_DIM + ct * 32 + 8 * i + 4 * half) =
+        *reinterpret_cast<float4*>(part_acc + part * DSK_HEAD_DIM + ct * 32 + 8 * i + 4 * qs.half) =
             make_float4(O[ct][4 * i], O[ct][4 * i + 1], O[ct][4 * i + 2], O[ct][4 * i + 3]);
-    if (half == 0) part_ml[part] = make_float2(m, l);
+    if (qs.half == 0) part_ml[part] = make_float2(m, l);
   }
+}
+
+// TERMS: bf16 terms that a weight is split into for the second product, 1 (bf16 result) or 3 (all 24 bits of it: fp32 result).
+// KW wavefronts take other tiles of a stage for the same queries.
+template <int QW, int KW, int NT, int TERMS, bool SEL, bool STREAM>
+__global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree_attn_kernel(
+    dsk_tree_attn_args a, int G, int q_tiles, TreeSplit sp, float scale_log2, float2* __restrict__ part_ml,
+    float* __restrict__ part_acc) {
+  constexpr int kThreads = QW * KW * DSK_WAVE;
+  constexpr int kTiles = KW * NT, kKeys = kTreeTile * kTiles;   // of a stage
+  __shared__ __align__(16) unsigned char sm_kv[2 * kTiles * kTreeTileBytes];
+  __shared__ float2 sm_ml[KW > 1 ? (KW - 1) * QW * DSK_WAVE : 1];
+  __shared__ uint32_t sm_bad[kTreeMixedTiles];
+  static_assert(kTiles + DSK_TREE_MAX_NODES / kTreeTile + 1 <= kTreeMixedTiles, "words of sm_bad");
+  __shared__ int32_t sm_rows[SEL ? kTreeMaxListed : 1];
+
+  unsigned char* const sm_k = sm_kv;
+  unsigned char* const sm_v = sm_kv + kTiles * kTreeTileBytes;
+  const int split = blockIdx.x, s = blockIdx.z;
+  const int hk = blockIdx.y / q_tiles, q_tile = blockIdx.y - hk * q_tiles;
+  const int tid = threadIdx.x, wave = tid / DSK_WAVE;
+  const int qw = wave % QW, kw = wave / QW;
+
+  const TreePlace at(a, s);
+  if (q_tile * QW * kTreeTile >= at.n * G) return;       // uniform: no row of this pass
+  const int used = at.used(a, sp, SEL, (int64_t)s * a.Hkv + hk);
+  if (split >= used) return;
+  TreeKeys<kThreads, kKeys * 16 / kThreads, SEL, STREAM> keys(a, sp, at, s, hk, split, used, sm_rows);
+  const TreeQueries qs(a, at, G, hk, (q_tile * QW + qw) * kTreeTile, keys.nodes());
+
+  TreeSoftmax sm(scale_log2);
+  tree_f32x16 O[4];
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) O[ct][i] = 0.0f;
+
+  if (tid < kTreeMixedTiles) sm_bad[tid] = 0;
+  auto tiles = [&](int t0, auto mixed) {                 // this wavefront's tiles of the stage in LDS
+    constexpr bool kMixed = decltype(mixed)::value;
+#pragma unroll
+    for (int sub = 0; sub < NT; ++sub) {
+      const int tile = kw * NT + sub, tt = t0 + tile * kTreeTile;
+      if (kMixed && tt >= keys.t_end) break;
+      TreeKFrag kf;
+      kf.read<0, 8>(sm_k + tile * kTreeTileBytes, qs);
+      tree_f32x16 z;
+      kf.add<0, 8>(z, qs);
+      uint32_t allow = 0;
+      if constexpr (kMixed) {
+        allow = qs.allowed(tt, keys.P);
+        tree_hide(z, allow, qs.half);
+      }
+      TreeWeights<TERMS> w;
+      sm.take(z, O, w);
+      TreeVFrag vf;
+      vf.read<0>(sm_v + tile * kTreeTileBytes);
+      vf.read<1>(sm_v + tile * kTreeTileBytes);
+      vf.add<TERMS>(O, w, 0);
+      vf.add<TERMS>(O, w, 1);
+      if constexpr (kMixed) tree_values_left_out(O, keys, sm_bad, allow, tt, qs.half);
+    }
+  };
+  using Plain = std::integral_constant<bool, false>;
+  using Mixed = std::integral_constant<bool, true>;
+  int t0 = keys.t_begin;
+  typename decltype(keys)::Regs x;
+  keys.fetch(x, t0);
+  for (; keys.plain(t0) && t0 < keys.t_end; t0 += kKeys) {   // the prefix: nothing is masked
+    keys.template put<false>(x, t0, sm_k, sm_v, nullptr);
+    __syncthreads();
+    keys.fetch(x, t0 + kKeys);
+    if (qs.busy) tiles(t0, Plain());
+    __syncthreads();
+  }
+  if (t0 == keys.t_begin) __syncthreads();               // sm_bad
+  for (; t0 < keys.t_end; t0 += kKeys) {                 // its end and the nodes
+    keys.template put<true>(x, t0, sm_k, sm_v, sm_bad);
+    __syncthreads();
+    keys.fetch(x, t0 + kKeys);
+    if (qs.busy) tiles(t0, Mixed());
+    __syncthreads();
+  }
+  sm.l += shfl_xor_f(sm.l, 32);
+  if constexpr (KW > 1) {
+    static_assert((KW - 1) * QW <= kTiles, "a block is as large as a tile of K and V");
+    tree_join<QW, KW>(sm, O, qs.busy, qw, kw, reinterpret_cast<float*>(sm_kv), sm_ml);
+    if (kw > 0) return;
+  }
+  tree_store(a, qs, O, sm.m, sm.l, used, sp.nsplit, split, part_ml, part_acc);
+}
+
+// The same for many rows, where the matrix cores bound it (bf16 results): eight wavefronts, two on a SIMD, of which one has the
+// matrix cores while the other makes exponentials.  Time goes in slots with a barrier after each.  The first four wavefronts
+// multiply step i in slot 2 i (V of step i - 1, then K of step i) and take its softmax in slot 2 i + 1; the other four do
+// either a slot later.  A step is a tile of 32 keys for each of KW wavefronts: with KW = 1 all eight have rows of their own,
+// with KW = 2 the two groups have the same rows and every other tile.
+// Steps go round four LDS buffers.  In the softmax slot of step i the first group puts its half of step i + 1 (slot 2 i + 1),
+// the second its half of step i + 2 (slot 2 i + 2), so a step is whole one slot before its first use, and the step that it
+// replaces was last read long before.  Loads are issued 64 KB before they are put.
+template <int QW, int KW, bool SEL, bool STREAM>
+__global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_wide_kernel(
+    dsk_tree_attn_args a, int G, int q_tiles, TreeSplit sp, float scale_log2, float2* __restrict__ part_ml,
+    float* __restrict__ part_acc) {
+  static_assert(QW * KW == 8 && KW <= 2, "two groups of four wavefronts");
+  constexpr int kThreads = QW * KW * DSK_WAVE;
+  constexpr int kKeys = kTreeTile * KW;                  // of a step
+  constexpr int kBufs = 4, kBufBytes = 2 * KW * kTreeTileBytes;
+  constexpr int kSets = 4 / KW;                          // steps on their way in registers: 64 KB
+  __shared__ __align__(16) unsigned char sm_kv[kBufs * kBufBytes];
+  __shared__ float2 sm_ml[KW > 1 ? QW * DSK_WAVE : 1];
+  __shared__ uint32_t sm_bad[kTreeMixedTiles];
+  static_assert(KW + DSK_TREE_MAX_NODES / kTreeTile + 1 <= kTreeMixedTiles, "words of sm_bad");
+  __shared__ int32_t sm_rows[SEL ? kTreeMaxListed : 1];
+
+  const int split = blockIdx.x, s = blockIdx.z;
+  const int hk = blockIdx.y / q_tiles, q_tile = blockIdx.y - hk * q_tiles;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / DSK_WAVE);
+  const int qw = wave % QW, kw = wave / QW;
+  const bool late = wave >= 4;
+
+  const TreePlace at(a, s);
+  if (q_tile * QW * kTreeTile >= at.n * G) return;       // uniform: no row of this pass
+  const int used = at.used(a, sp, SEL, (int64_t)s * a.Hkv + hk);
+  if (split >= used) return;
+  using Keys = TreeKeys<kThreads, kKeys * 16 / kThreads, SEL, STREAM>;
+  const Keys keys(a, sp, at, s, hk, split, used, sm_rows);
+  const TreeQueries qs(a, at, G, hk, (q_tile * QW + qw) * kTreeTile, keys.nodes());
+  TreeSoftmax sm(scale_log2);
+  tree_f32x16 O[4];
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) O[ct][i] = 0.0f;
+
+  const int steps = keys.t_end > keys.t_begin ? (keys.t_end - keys.t_begin + kKeys - 1) / kKeys : 0;
+  auto t_of = [&](int i) { return keys.t_begin + i * kKeys; };
+  auto barrier = [] {
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // steps below `plain_steps` are of the prefix alone
+  const int plain_steps = keys.P > keys.t_begin ? ((keys.P < keys.t_end ? keys.P : keys.t_end) - keys.t_begin) / kKeys : 0;
+  // kPlain: what is put and fetched is known to be plain; beyond the last step it is put and fetched again, and not read.
+  using Plain = std::integral_constant<bool, true>;
+  using Any = std::integral_constant<bool, false>;
+  auto put = [&](auto plain, typename Keys::Regs& x, int i, int buf) {
+    unsigned char* to = sm_kv + buf * kBufBytes;
+    if (decltype(plain)::value || i < plain_steps) keys.template put<false>(x, t_of(i), to, to + KW * kTreeTileBytes, nullptr);
+    else if (i < steps) keys.template put<true>(x, t_of(i), to, to + KW * kTreeTileBytes, sm_bad);
+  };
+  auto fetch = [&](typename Keys::Regs& x, int i) {
+    if (i < plain_steps) keys.fetch_plain(x, t_of(i));
+    else if (i < steps) keys.fetch_mixed(x, t_of(i));
+  };
+  // Step i goes through set i % kSets of the first group, (i - 1) % kSets of the second, so that both put set (i + 1) % kSets
+  // in their softmax slot of step i.
+  typename Keys::Regs x[kSets];
+  if (tid < kTreeMixedTiles) sm_bad[tid] = 0;
+  // the first step multiplies weights of 0 by the values of "the step before" it: those have to be numbers
+  for (int i = tid; i < KW * kTreeTileBytes / 16; i += kThreads)
+    *reinterpret_cast<uint4*>(sm_kv + (kBufs - 1) * kBufBytes + KW * kTreeTileBytes + i * 16) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int j = 0; j < kSets; ++j) fetch(x[j], late ? (j + 1) % kSets : j);
+  __syncthreads();
+  if (!late) {
+    put(Any(), x[0], 0, 0);
+    fetch(x[0], kSets);
+  } else {
+    put(Any(), x[kSets - 1], 0, 0);
+    fetch(x[kSets - 1], kSets);
+  }
+  barrier();
+  if (late) {
+    put(Any(), x[0], 1, 1);
+    fetch(x[0], kSets + 1);
+    barrier();
+  }
+  const int ahead = late ? 2 : 1;
+  // what the loop of plain steps fetches next, from the first step that is not fetched yet; the last one again when it is through
+  int fetched = ahead + kSets < plain_steps ? ahead + kSets : (plain_steps > 0 ? plain_steps - 1 : 0);
+  tree_global k_next = keys.Ku + t_of(fetched) * keys.kst * 2, v_next = keys.Vu + t_of(fetched) * keys.vst * 2;
+  int64_t k_inc = kKeys * keys.kst * 2, v_inc = kKeys * keys.vst * 2;
+  int64_t k_half = Keys::kRowStep * keys.kst * 2, v_half = Keys::kRowStep * keys.vst * 2;
+  asm("" : "+s"(k_inc), "+s"(v_inc), "+s"(k_half), "+s"(v_half));   // no more of the arguments is kept for them
+  auto fetch_next = [&](typename Keys::Regs& x) {
+    if constexpr (SEL) {
+      keys.fetch_plain(x, t_of(fetched));
+      fetched += fetched + 1 < plain_steps;
+    } else {
+#pragma unroll
+      for (int u = 0; u < KW; ++u) x.k[u] = load16_at<STREAM>(k_next + u * k_half, keys.k_off);
+#pragma unroll
+      for (int u = 0; u < KW; ++u) x.v[u] = load16_at<STREAM>(v_next + u * v_half, keys.v_off);
+      const bool more = fetched + 1 < plain_steps;
+      fetched += more;
+      k_next += more ? k_inc : 0;
+      v_next += more ? v_inc : 0;
+    }
+  };
+  TreeVFrag vf;                                          // values and weights of the step before, for its product
+  TreeWeights<1> w;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) w.w[0][t] = __builtin_bit_cast(tree_bf16x8, make_uint4(0, 0, 0, 0));
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct) vf.v[ct][0] = w.w[0][0];
+  unsigned char* const sm_mine = sm_kv + kw * kTreeTileBytes;
+  // A wavefront without rows, or without a tile in the last step, multiplies what is there: nothing reads its result, or
+  // nothing of the tile is allowed.
+  auto step = [&](auto plain, auto buffer, int i, typename Keys::Regs& regs) {
+    constexpr bool kPlain = decltype(plain)::value;
+    constexpr int kBuf = decltype(buffer)::value, kBefore = (kBuf + kBufs - 1) % kBufs;
+    const unsigned char* from = sm_mine + kBuf * kBufBytes;
+    // Fragments are read well ahead of their products; left to itself the compiler reads each one right before, and waits.
+    TreeKFrag kf;
+    tree_f32x16 z;
+    vf.template read<1>(sm_mine + kBefore * kBufBytes + KW * kTreeTileBytes);
+    __builtin_amdgcn_sched_barrier(0);
+    vf.template add<1>(O, w, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    kf.template read<0, 4>(from, qs);
+    __builtin_amdgcn_sched_barrier(0);
+    vf.template add<1>(O, w, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    kf.template read<4, 8>(from, qs);
+    __builtin_amdgcn_sched_barrier(0);
+    kf.template add<0, 4>(z, qs);
+    kf.template add<4, 8>(z, qs);
+    if (!kPlain && i > plain_steps) {
+      const int before = t_of(i - 1) + kw * kTreeTile;
+      tree_values_left_out(O, keys, sm_bad, qs.allowed(before, keys.P), before, qs.half);
+    }
+    barrier();
+    put(plain, regs, i + ahead, late ? (kBuf + 2) % kBufs : (kBuf + 1) % kBufs);
+    if constexpr (kPlain) fetch_next(regs);
+    else fetch(regs, i + ahead + kSets);
+    if (!kPlain && i >= plain_steps) tree_hide(z, qs.allowed(t_of(i) + kw * kTreeTile, keys.P), qs.half);
+    vf.template read<0>(from + KW * kTreeTileBytes);
+    __builtin_amdgcn_sched_barrier(0);
+    sm.take(z, O, w);
+    barrier();
+  };
+  // Steps of which all that they put and fetch is plain: the others only meet the end of the prefix.
+  const int easy = steps == plain_steps ? steps : plain_steps - kSets - 2;
+  int i = 0;
+  using B0 = std::integral_constant<int, 0>;
+  using B1 = std::integral_constant<int, 1>;
+  using B2 = std::integral_constant<int, 2>;
+  using B3 = std::integral_constant<int, 3>;
+  for (; i + kBufs <= easy; i += kBufs) {
+    step(Plain(), B0(), i, x[1 % kSets]);
+    step(Plain(), B1(), i + 1, x[2 % kSets]);
+    step(Plain(), B2(), i + 2, x[3 % kSets]);
+    step(Plain(), B3(), i + 3, x[0]);
+  }
+  for (; i < steps; i += kBufs) {
+    step(Any(), B0(), i, x[1 % kSets]);
+    if (i + 1 < steps) step(Any(), B1(), i + 1, x[2 % kSets]);
+    if (i + 2 < steps) step(Any(), B2(), i + 2, x[3 % kSets]);
+    if (i + 3 < steps) step(Any(), B3(), i + 3, x[0]);
+  }
+  const int buf_before = (steps + kBufs - 1) % kBufs;
+  vf.add<1>(O, w, 0);
+  if (steps > 0) {
+    vf.read<1>(sm_kv + buf_before * kBufBytes + kw * kTreeTileBytes + KW * kTreeTileBytes);
+    vf.add<1>(O, w, 1);
+  }
+  if (steps > plain_steps) {
+    const int before = t_of(steps - 1) + kw * kTreeTile;
+    tree_values_left_out(O, keys, sm_bad, qs.allowed(before, keys.P), before, qs.half);
+  }
+  if (!late) barrier();                                  // as many as the others
+  sm.l += shfl_xor_f(sm.l, 32);
+  if constexpr (KW > 1) {
+    static_assert((KW - 1) * QW <= kBufs * KW, "a block is as large as a tile of K and V");
+    __syncthreads();
+    tree_join<QW, KW>(sm, O, qs.busy, qw, kw, reinterpret_cast<float*>(sm_kv), sm_ml);
+    if (kw > 0) return;
+  }
+  tree_store(a, qs, O, sm.m, sm.l, used, sp.nsplit, split, part_ml, part_acc);
 }
 
 // The parts of a row put together in order: a wavefront a row, two channels a lane.  `used` as in the kernel above.
@@ -418,32 +798,16 @@ constexpr int kTreeMergeBatch = 8;             // partials on their way at once
 
 template <bool SEL>
 __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
-    dsk_tree_attn_args a, int G, TreeSplit sp, float scale_log2, const float2* __restrict__ part_ml,
+    dsk_tree_attn_args a, int G, TreeSplit sp, const float2* __restrict__ part_ml,
     const float* __restrict__ part_acc) {
   const int s = blockIdx.y, lane = threadIdx.x & (DSK_WAVE - 1);
   const int item = blockIdx.x * kTreeMergeWaves + threadIdx.x / DSK_WAVE;
   const int node = item / a.Hq, h = item - node * a.Hq;
-  int tok0 = a.cu_new[s], n = a.cu_new[s + 1] - tok0;
-  if (tok0 < 0 || n <= 0 || tok0 > a.n_tokens) return;
-  n = n < a.max_nodes ? n : a.max_nodes;
-  n = n < a.n_tokens - tok0 ? n : a.n_tokens - tok0;
-  if (node >= n) return;
-  int used;
-  if constexpr (SEL) {
-    int count = a.sel_count[(int64_t)s * a.Hkv + h / G];
-    count = count < 0 ? 0 : (count < a.k ? count : a.k);
-    used = (count + sp.slots_per_split - 1) / sp.slots_per_split;
-  } else {
-    int64_t row0 = a.seq_row0[s], len = a.seq_len[s];
-    if (row0 < 0 || row0 > a.total_rows || len < 0) row0 = len = 0;
-    len = len < a.max_seqlen ? len : a.max_seqlen;
-    len = len < a.total_rows - row0 ? len : a.total_rows - row0;
-    const int n_keys = a.Kd != nullptr || n < a.total_rows - row0 - len ? n : (int)(a.total_rows - row0 - len);
-    used = (int)((len + n_keys + sp.keys_per_split - 1) / sp.keys_per_split);
-    used = used < sp.nsplit ? used : sp.nsplit;
-  }
+  const TreePlace at(a, s);
+  if (node >= at.n) return;
+  const int used = at.used(a, sp, SEL, (int64_t)s * a.Hkv + h / G);
   if (used <= 1) return;                                 // finished by the kernel above
-  const int64_t row = (int64_t)(tok0 + node) * a.Hq + h;
+  const int64_t row = (int64_t)(at.tok0 + node) * a.Hq + h;
   const float2* ml = part_ml + row * sp.nsplit;
   const float2* acc = reinterpret_cast<const float2*>(part_acc + row * sp.nsplit * DSK_HEAD_DIM) + lane;
   float M = -__builtin_inff(), l = 0.0f;
@@ -461,7 +825,7 @@ __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
 #pragma unroll
     for (int u = 0; u < kTreeMergeBatch; ++u) {
       if (c0 + u >= used || v[u].x == -__builtin_inff()) continue;
-      const float f = exp2_small((v[u].x - M) * scale_log2);
+      const float f = exp2_small(v[u].x - M);
       l = fmaf(v[u].y, f, l);
       o.x = fmaf(x[u].x, f, o.x);
       o.y = fmaf(x[u].y, f, o.y);
@@ -473,41 +837,54 @@ __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
   if (a.out != nullptr) *reinterpret_cast<float2*>(a.out + row * DSK_HEAD_DIM + 2 * lane) = o;
   if (a.out_bf16 != nullptr)
     *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out_bf16) + row * DSK_HEAD_DIM + 2 * lane) = tree_pack(o.x, o.y);
-  if (lane == 0 && a.lse != nullptr) a.lse[row] = l > 0.0f ? (M * scale_log2 + log2f(l)) * kLn2 : -__builtin_inff();
+  if (lane == 0 && a.lse != nullptr) a.lse[row] = l > 0.0f ? (M + log2f(l)) * kLn2 : -__builtin_inff();
 }
+
+// K and V larger than the memory-side cache are hardly found there again by the next step, so they are read past it (one pass
+// over them; several share its lines).  32 / 8 heads, 16 nodes: 128K tokens (512 MB) 116 us through it, 103 past it; 8 / 8 heads,
+// 32 nodes, 32K tokens (128 MB) 40.3 and 42.8.
+constexpr int64_t kTreeStreamBytes = 288ll << 20;
 
 // ---- geometry: follows the host's bounds alone ---------------------------------------------------------------
 struct TreeLaunch {
   TreeSplit sp;
   int q_waves;        // QW
+  bool wide;          // tree_wide_kernel
+  bool stream;        // K and V are read past the memory-side cache
   int q_tiles;        // passes over a (sequence, KV head)'s keys
   size_t part_acc, total;
 };
 
-static int tree_stage_keys(int q_waves) { return q_waves == 1 ? 128 : 64; }
 
-static TreeLaunch tree_layout(const dsk_tree_attn_args& a) {
+
+static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   TreeLaunch t;
   const int rows = a.max_nodes * (a.Hq / a.Hkv);
   t.q_waves = rows <= 32 ? 1 : (rows <= 64 ? 2 : (rows <= 128 ? 4 : 8));
   t.q_tiles = (rows + t.q_waves * kTreeTile - 1) / (t.q_waves * kTreeTile);
-  constexpr int64_t kWant = 512;                         // workgroups: two per CU
+  t.wide = !f32 && t.q_waves >= 4;
+  const int64_t want = t.wide ? 256 : 512;               // workgroups: one of eight wavefronts a CU, or two of four
   const int64_t heads = (int64_t)a.Hkv * t.q_tiles;
   t.sp.keys_per_split = t.sp.slots_per_split = 0;
+  t.stream = false;
   if (a.sel_start != nullptr) {
     const int64_t slots = (int64_t)a.k * a.B * heads;
-    int64_t per = (slots + kWant - 1) / kWant;
+    int64_t per = (slots + want - 1) / want;
     const int64_t least = (128 + a.b - 1) / a.b, most = kTreeMaxListed / a.b < kTreeMaxSlots ? kTreeMaxListed / a.b : kTreeMaxSlots;
     per = per > least ? per : least;
     per = per < most ? per : most;
     t.sp.slots_per_split = (int)per;
     t.sp.nsplit = (int)((a.k + per - 1) / per);
   } else {
-    const int stage = tree_stage_keys(t.q_waves);
+    const int stage = t.wide || t.q_waves == 1 ? 128 : 64;   // a multiple of the keys that the kernels take at once
     int64_t keys = (int64_t)a.B * a.max_seqlen;
     keys = (keys < a.total_rows ? keys : a.total_rows) + (int64_t)a.B * a.max_nodes;
+    t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
     const int64_t longest = (int64_t)a.max_seqlen + a.max_nodes;
-    int64_t per = (keys * heads + kWant - 1) / kWant;
+    // a sequence's last part is a shorter one: leave room for one of each
+    int64_t parts = want / heads - (a.B - 1);
+    parts = parts > 1 ? parts : 1;
+    int64_t per = (keys + parts - 1) / parts;
     const int64_t least = 256, fewest = (longest + kTreeMaxSplit - 1) / kTreeMaxSplit;
     per = per > least ? per : least;
     per = per > fewest ? per : fewest;
@@ -522,38 +899,62 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a) {
   return t;
 }
 
-size_t tree_ws_bytes(const dsk_tree_attn_args& a) { return tree_layout(a).total; }
+// whichever outputs the call will ask for
+size_t tree_ws_bytes(const dsk_tree_attn_args& a) {
+  const size_t f32 = tree_layout(a, true).total, bf16 = tree_layout(a, false).total;
+  return f32 > bf16 ? f32 : bf16;
+}
 
-template <int QW, int KW, int NT>
-static void launch_tree(const dsk_tree_attn_args& a, const TreeLaunch& t, float scale, float2* ml, float* acc, hipStream_t st) {
+template <int QW, int KW, int NT, bool BF16>
+static void launch_tree(const dsk_tree_attn_args& a, const TreeLaunch& t, float scale_log2, float2* ml, float* acc, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
   const dim3 grid((unsigned)t.sp.nsplit, (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(QW * KW * DSK_WAVE);
-  if (a.sel_start != nullptr) {
-    if (a.out != nullptr) tree_attn_kernel<QW, KW, NT, 3, true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale, ml, acc);
-    else tree_attn_kernel<QW, KW, NT, 1, true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale, ml, acc);
-  } else {
-    if (a.out != nullptr) tree_attn_kernel<QW, KW, NT, 3, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale, ml, acc);
-    else tree_attn_kernel<QW, KW, NT, 1, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale, ml, acc);
+#define DSK_TREE(terms)                                                                                                        \
+  do {                                                                                                                         \
+    if (a.sel_start != nullptr)                                                                                                \
+      tree_attn_kernel<QW, KW, NT, terms, true, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);    \
+    else if (t.stream)                                                                                                         \
+      tree_attn_kernel<QW, KW, NT, terms, false, true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);    \
+    else                                                                                                                       \
+      tree_attn_kernel<QW, KW, NT, terms, false, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);   \
+  } while (0)
+  if (a.out != nullptr) {
+    DSK_TREE(3);
+  } else if constexpr (BF16) {
+    DSK_TREE(1);
   }
+#undef DSK_TREE
+}
+
+template <int QW, int KW>
+static void launch_tree_wide(const dsk_tree_attn_args& a, const TreeLaunch& t, float scale_log2, float2* ml, float* acc, hipStream_t st) {
+  const int G = a.Hq / a.Hkv;
+  const dim3 grid((unsigned)t.sp.nsplit, (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(QW * KW * DSK_WAVE);
+  if (a.sel_start != nullptr) tree_wide_kernel<QW, KW, true, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
+  else if (t.stream) tree_wide_kernel<QW, KW, false, true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
+  else tree_wide_kernel<QW, KW, false, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
 }
 
 hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st) {
-  const TreeLaunch t = tree_layout(a);
+  const TreeLaunch t = tree_layout(a, a.out != nullptr);
   if ((int64_t)a.Hkv * t.q_tiles > 65535) return hipErrorInvalidValue;
   const float scale = a.scale != 0.0f ? a.scale : 0.08838834764831845f;   // 128^-1/2
   float2* ml = static_cast<float2*>(a.workspace);
   float* acc = reinterpret_cast<float*>(static_cast<unsigned char*>(a.workspace) + t.part_acc);
-  if (t.q_waves == 1) launch_tree<1, 4, 1>(a, t, scale, ml, acc, st);
-  else if (t.q_waves == 2) launch_tree<2, 2, 1>(a, t, scale, ml, acc, st);
-  else if (t.q_waves == 4) launch_tree<4, 1, 2>(a, t, scale, ml, acc, st);
-  else launch_tree<8, 1, 2>(a, t, scale, ml, acc, st);
+  const float scale_log2 = scale * kLog2e;
+  if (t.wide && t.q_waves == 4) launch_tree_wide<4, 2>(a, t, scale_log2, ml, acc, st);
+  else if (t.wide) launch_tree_wide<8, 1>(a, t, scale_log2, ml, acc, st);
+  else if (t.q_waves == 1) launch_tree<1, 4, 1, true>(a, t, scale_log2, ml, acc, st);
+  else if (t.q_waves == 2) launch_tree<2, 2, 1, true>(a, t, scale_log2, ml, acc, st);
+  else if (t.q_waves == 4) launch_tree<4, 1, 2, false>(a, t, scale_log2, ml, acc, st);
+  else launch_tree<8, 1, 2, false>(a, t, scale_log2, ml, acc, st);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || t.sp.nsplit <= 1) return err;
   const dim3 grid((unsigned)((a.max_nodes * a.Hq + kTreeMergeWaves - 1) / kTreeMergeWaves), (unsigned)a.B);
   const dim3 block(kTreeMergeWaves * DSK_WAVE);
   const int G = a.Hq / a.Hkv;
-  if (a.sel_start != nullptr) tree_merge_kernel<true><<<grid, block, 0, st>>>(a, G, t.sp, scale * kLog2e, ml, acc);
-  else tree_merge_kernel<false><<<grid, block, 0, st>>>(a, G, t.sp, scale * kLog2e, ml, acc);
+  if (a.sel_start != nullptr) tree_merge_kernel<true><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
+  else tree_merge_kernel<false><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
   return hipGetLastError();
 }
 

@@ -215,14 +215,17 @@ def test_scale_and_sharp_logits():
 
 
 def test_logits_near_the_end_of_the_range():
-    """Logits of 1e30: all the weight is on the largest, and nothing overflows."""
+    """Logits of 1e30: all the weight is on the largest, and nothing overflows.  That weight is no power of two (it is relative
+    to a rounded maximum), so a bf16 result has its rounding, 2^-8 of the size, beside its own."""
     c = Case([400], [6], 4, 2, seed=12)
     c.q = (c.q.float() * 1e30).bfloat16()
     out, size, lse = c.reference()
     for kw in ({}, dict(want_f32=False, want_bf16=True)):
         r = c.run(**kw)
-        got = (r.out if r.out is not None else r.out_bf16).double()
-        assert bool(((got - out).abs() <= BF16 * out.abs() + 1e-5 * size).all())
+        if kw:
+            assert bool(((r.out_bf16.double() - out).abs() <= BF16 * (out.abs() * (1 + BF16) + size) + F32 * size).all())
+        else:
+            assert bool(((r.out.double() - out).abs() <= F32 * size).all())
         assert bool(((r.lse.double() - lse).abs() <= 1e-5 * lse.abs()).all())
 
 
