@@ -53,6 +53,15 @@ __device__ __forceinline__ uint4 load16_at(tree_global base, uint32_t off) {
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 
+// 16 bytes of each lane from its address to LDS, lane after lane from a uniform address on
+template <bool STREAM>
+__device__ __forceinline__ void lds_copy16(const void* from, unsigned char* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0,
+                                   STREAM ? 2 : 0);
+}
+// every copy of this wavefront has arrived
+__device__ __forceinline__ void lds_copies_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
 // a bf16 pair with 0 for what is not finite
 __device__ __forceinline__ uint32_t finite_bf16(uint32_t w) {
   if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
@@ -246,10 +255,18 @@ struct TreeKeys {
       }
     }
   }
-  __device__ __forceinline__ void fetch(Regs& x, int t0) const {
-    if (t0 >= t_end) return;
-    if (plain(t0)) fetch_plain(x, t0);
-    else fetch_mixed(x, t0);
+  // The same straight to LDS, with no register between.  A wavefront's 1 KB lies in LDS in the order of its lanes, so the
+  // swizzle is in what a lane reads: chunk lc of a row is that chunk's place, K's or V's chunk lc ^ f(row) belongs there.
+  __device__ __forceinline__ void copy_plain(int t0, unsigned char* sm_k, unsigned char* sm_v) const {
+    const int w_row = (int)(threadIdx.x / DSK_WAVE) * 4;
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      const int row = lrow + u * kRowStep, t = t0 + row;
+      const int kc = (lc ^ (row & 15)) - lc, vc = (lc ^ ((row & 3) << 2)) - lc;
+      const int64_t r = SEL ? rows[t] : t;
+      lds_copy16<STREAM>(K + r * kst + kc * 8, sm_k + (u * kRowStep + w_row) * kTreeRowBytes);
+      lds_copy16<STREAM>(V + r * vst + vc * 8, sm_v + (u * kRowStep + w_row) * kTreeRowBytes);
+    }
   }
   // sm_bad: a word per tile from t_mixed on, zero before; rows of V that hold values that are not finite
   template <bool MIXED>
@@ -575,20 +592,19 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree
   using Plain = std::integral_constant<bool, false>;
   using Mixed = std::integral_constant<bool, true>;
   int t0 = keys.t_begin;
-  typename decltype(keys)::Regs x;
-  keys.fetch(x, t0);
   for (; keys.plain(t0) && t0 < keys.t_end; t0 += kKeys) {   // the prefix: nothing is masked
-    keys.template put<false>(x, t0, sm_k, sm_v, nullptr);
+    keys.copy_plain(t0, sm_k, sm_v);
+    lds_copies_done();
     __syncthreads();
-    keys.fetch(x, t0 + kKeys);
     if (qs.busy) tiles(t0, Plain());
     __syncthreads();
   }
   if (t0 == keys.t_begin) __syncthreads();               // sm_bad
   for (; t0 < keys.t_end; t0 += kKeys) {                 // its end and the nodes
+    typename decltype(keys)::Regs x;
+    keys.fetch_mixed(x, t0);
     keys.template put<true>(x, t0, sm_k, sm_v, sm_bad);
     __syncthreads();
-    keys.fetch(x, t0 + kKeys);
     if (qs.busy) tiles(t0, Mixed());
     __syncthreads();
   }
@@ -860,7 +876,7 @@ struct TreeLaunch {
 static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   TreeLaunch t;
   const int rows = a.max_nodes * (a.Hq / a.Hkv);
-  t.q_waves = rows <= 32 ? 1 : (rows <= 64 ? 2 : (rows <= 128 ? 4 : 8));
+  t.q_waves = rows <= 32 ? 1 : (rows <= 64 ? 2 : (rows <= 128 || f32 ? 4 : 8));
   t.q_tiles = (rows + t.q_waves * kTreeTile - 1) / (t.q_waves * kTreeTile);
   t.wide = !f32 && t.q_waves >= 4;
   const int64_t want = t.wide ? 256 : 512;               // workgroups: one of eight wavefronts a CU, or two of four
@@ -876,7 +892,7 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     t.sp.slots_per_split = (int)per;
     t.sp.nsplit = (int)((a.k + per - 1) / per);
   } else {
-    const int stage = t.wide || t.q_waves == 1 ? 128 : 64;   // a multiple of the keys that the kernels take at once
+    constexpr int stage = 128;                           // a multiple of the keys that the kernels take at once
     int64_t keys = (int64_t)a.B * a.max_seqlen;
     keys = (keys < a.total_rows ? keys : a.total_rows) + (int64_t)a.B * a.max_nodes;
     t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
@@ -945,9 +961,8 @@ hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st) {
   if (t.wide && t.q_waves == 4) launch_tree_wide<4, 2>(a, t, scale_log2, ml, acc, st);
   else if (t.wide) launch_tree_wide<8, 1>(a, t, scale_log2, ml, acc, st);
   else if (t.q_waves == 1) launch_tree<1, 4, 1, true>(a, t, scale_log2, ml, acc, st);
-  else if (t.q_waves == 2) launch_tree<2, 2, 1, true>(a, t, scale_log2, ml, acc, st);
-  else if (t.q_waves == 4) launch_tree<4, 1, 2, false>(a, t, scale_log2, ml, acc, st);
-  else launch_tree<8, 1, 2, false>(a, t, scale_log2, ml, acc, st);
+  else if (t.q_waves == 2) launch_tree<2, 2, 2, true>(a, t, scale_log2, ml, acc, st);
+  else launch_tree<4, 1, 4, false>(a, t, scale_log2, ml, acc, st);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || t.sp.nsplit <= 1) return err;
   const dim3 grid((unsigned)((a.max_nodes * a.Hq + kTreeMergeWaves - 1) / kTreeMergeWaves), (unsigned)a.B);
