@@ -620,39 +620,36 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree
 // The same for many rows, where the matrix cores bound it (bf16 results): eight wavefronts, two on a SIMD, of which one has the
 // matrix cores while the other makes exponentials.  Time goes in slots with a barrier after each.  The first four wavefronts
 // multiply step i in slot 2 i (V of step i - 1, then K of step i) and take its softmax in slot 2 i + 1; the other four do
-// either a slot later.  A step is a tile of 32 keys for each of KW wavefronts: with KW = 1 all eight have rows of their own,
-// with KW = 2 the two groups have the same rows and every other tile.
+// either a slot later.  A step is a tile of 32 keys, and every wavefront has 32 rows of its own.
 // Steps go round four LDS buffers.  In the softmax slot of step i the first group puts its half of step i + 1 (slot 2 i + 1),
 // the second its half of step i + 2 (slot 2 i + 2), so a step is whole one slot before its first use, and the step that it
 // replaces was last read long before.  Loads are issued 64 KB before they are put.
-template <int QW, int KW, bool SEL, bool STREAM>
-__global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_wide_kernel(
+constexpr int kWideWaves = 8;
+
+template <bool STREAM>
+__global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
     dsk_tree_attn_args a, int G, int q_tiles, TreeSplit sp, float scale_log2, float2* __restrict__ part_ml,
     float* __restrict__ part_acc) {
-  static_assert(QW * KW == 8 && KW <= 2, "two groups of four wavefronts");
-  constexpr int kThreads = QW * KW * DSK_WAVE;
-  constexpr int kKeys = kTreeTile * KW;                  // of a step
-  constexpr int kBufs = 4, kBufBytes = 2 * KW * kTreeTileBytes;
-  constexpr int kSets = 4 / KW;                          // steps on their way in registers: 64 KB
+  constexpr int kThreads = kWideWaves * DSK_WAVE;
+  constexpr int kKeys = kTreeTile;                       // of a step
+  constexpr int kBufs = 4, kBufBytes = 2 * kTreeTileBytes;
+  constexpr int kSets = 4;                               // steps on their way in registers: 64 KB
   __shared__ __align__(16) unsigned char sm_kv[kBufs * kBufBytes];
-  __shared__ float2 sm_ml[KW > 1 ? QW * DSK_WAVE : 1];
   __shared__ uint32_t sm_bad[kTreeMixedTiles];
-  static_assert(KW + DSK_TREE_MAX_NODES / kTreeTile + 1 <= kTreeMixedTiles, "words of sm_bad");
-  __shared__ int32_t sm_rows[SEL ? kTreeMaxListed : 1];
+  static_assert(1 + DSK_TREE_MAX_NODES / kTreeTile + 1 <= kTreeMixedTiles, "words of sm_bad");
 
   const int split = blockIdx.x, s = blockIdx.z;
   const int hk = blockIdx.y / q_tiles, q_tile = blockIdx.y - hk * q_tiles;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / DSK_WAVE);
-  const int qw = wave % QW, kw = wave / QW;
   const bool late = wave >= 4;
 
   const TreePlace at(a, s);
-  if (q_tile * QW * kTreeTile >= at.n * G) return;       // uniform: no row of this pass
-  const int used = at.used(a, sp, SEL, (int64_t)s * a.Hkv + hk);
+  if (q_tile * kWideWaves * kTreeTile >= at.n * G) return;       // uniform: no row of this pass
+  const int used = at.used(a, sp, false, 0);
   if (split >= used) return;
-  using Keys = TreeKeys<kThreads, kKeys * 16 / kThreads, SEL, STREAM>;
-  const Keys keys(a, sp, at, s, hk, split, used, sm_rows);
-  const TreeQueries qs(a, at, G, hk, (q_tile * QW + qw) * kTreeTile, keys.nodes());
+  using Keys = TreeKeys<kThreads, kKeys * 16 / kThreads, false, STREAM>;
+  const Keys keys(a, sp, at, s, hk, split, used, nullptr);
+  const TreeQueries qs(a, at, G, hk, (q_tile * kWideWaves + wave) * kTreeTile, keys.nodes());
   TreeSoftmax sm(scale_log2);
   tree_f32x16 O[4];
 #pragma unroll
@@ -674,8 +671,8 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_wide_kernel(
   using Any = std::integral_constant<bool, false>;
   auto put = [&](auto plain, typename Keys::Regs& x, int i, int buf) {
     unsigned char* to = sm_kv + buf * kBufBytes;
-    if (decltype(plain)::value || i < plain_steps) keys.template put<false>(x, t_of(i), to, to + KW * kTreeTileBytes, nullptr);
-    else if (i < steps) keys.template put<true>(x, t_of(i), to, to + KW * kTreeTileBytes, sm_bad);
+    if (decltype(plain)::value || i < plain_steps) keys.template put<false>(x, t_of(i), to, to + kTreeTileBytes, nullptr);
+    else if (i < steps) keys.template put<true>(x, t_of(i), to, to + kTreeTileBytes, sm_bad);
   };
   auto fetch = [&](typename Keys::Regs& x, int i) {
     if (i < plain_steps) keys.fetch_plain(x, t_of(i));
@@ -686,8 +683,8 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_wide_kernel(
   typename Keys::Regs x[kSets];
   if (tid < kTreeMixedTiles) sm_bad[tid] = 0;
   // the first step multiplies weights of 0 by the values of "the step before" it: those have to be numbers
-  for (int i = tid; i < KW * kTreeTileBytes / 16; i += kThreads)
-    *reinterpret_cast<uint4*>(sm_kv + (kBufs - 1) * kBufBytes + KW * kTreeTileBytes + i * 16) = make_uint4(0, 0, 0, 0);
+  for (int i = tid; i < kTreeTileBytes / 16; i += kThreads)
+    *reinterpret_cast<uint4*>(sm_kv + (kBufs - 1) * kBufBytes + kTreeTileBytes + i * 16) = make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int j = 0; j < kSets; ++j) fetch(x[j], late ? (j + 1) % kSets : j);
   __syncthreads();
@@ -709,22 +706,14 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_wide_kernel(
   int fetched = ahead + kSets < plain_steps ? ahead + kSets : (plain_steps > 0 ? plain_steps - 1 : 0);
   tree_global k_next = keys.Ku + t_of(fetched) * keys.kst * 2, v_next = keys.Vu + t_of(fetched) * keys.vst * 2;
   int64_t k_inc = kKeys * keys.kst * 2, v_inc = kKeys * keys.vst * 2;
-  int64_t k_half = Keys::kRowStep * keys.kst * 2, v_half = Keys::kRowStep * keys.vst * 2;
-  asm("" : "+s"(k_inc), "+s"(v_inc), "+s"(k_half), "+s"(v_half));   // no more of the arguments is kept for them
+  asm("" : "+s"(k_inc), "+s"(v_inc));                    // no more of the arguments is kept for them
   auto fetch_next = [&](typename Keys::Regs& x) {
-    if constexpr (SEL) {
-      keys.fetch_plain(x, t_of(fetched));
-      fetched += fetched + 1 < plain_steps;
-    } else {
-#pragma unroll
-      for (int u = 0; u < KW; ++u) x.k[u] = load16_at<STREAM>(k_next + u * k_half, keys.k_off);
-#pragma unroll
-      for (int u = 0; u < KW; ++u) x.v[u] = load16_at<STREAM>(v_next + u * v_half, keys.v_off);
-      const bool more = fetched + 1 < plain_steps;
-      fetched += more;
-      k_next += more ? k_inc : 0;
-      v_next += more ? v_inc : 0;
-    }
+    x.k[0] = load16_at<STREAM>(k_next, keys.k_off);
+    x.v[0] = load16_at<STREAM>(v_next, keys.v_off);
+    const bool more = fetched + 1 < plain_steps;
+    fetched += more;
+    k_next += more ? k_inc : 0;
+    v_next += more ? v_inc : 0;
   };
   TreeVFrag vf;                                          // values and weights of the step before, for its product
   TreeWeights<1> w;
@@ -732,17 +721,15 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_wide_kernel(
   for (int t = 0; t < 2; ++t) w.w[0][t] = __builtin_bit_cast(tree_bf16x8, make_uint4(0, 0, 0, 0));
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct) vf.v[ct][0] = w.w[0][0];
-  unsigned char* const sm_mine = sm_kv + kw * kTreeTileBytes;
-  // A wavefront without rows, or without a tile in the last step, multiplies what is there: nothing reads its result, or
-  // nothing of the tile is allowed.
+  // A wavefront without rows multiplies what is there: nothing reads its result.
   auto step = [&](auto plain, auto buffer, int i, typename Keys::Regs& regs) {
     constexpr bool kPlain = decltype(plain)::value;
     constexpr int kBuf = decltype(buffer)::value, kBefore = (kBuf + kBufs - 1) % kBufs;
-    const unsigned char* from = sm_mine + kBuf * kBufBytes;
+    const unsigned char* from = sm_kv + kBuf * kBufBytes;
     // Fragments are read well ahead of their products; left to itself the compiler reads each one right before, and waits.
     TreeKFrag kf;
     tree_f32x16 z;
-    vf.template read<1>(sm_mine + kBefore * kBufBytes + KW * kTreeTileBytes);
+    vf.template read<1>(sm_kv + kBefore * kBufBytes + kTreeTileBytes);
     __builtin_amdgcn_sched_barrier(0);
     vf.template add<1>(O, w, 0);
     __builtin_amdgcn_sched_barrier(0);
@@ -755,15 +742,14 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_wide_kernel(
     kf.template add<0, 4>(z, qs);
     kf.template add<4, 8>(z, qs);
     if (!kPlain && i > plain_steps) {
-      const int before = t_of(i - 1) + kw * kTreeTile;
-      tree_values_left_out(O, keys, sm_bad, qs.allowed(before, keys.P), before, qs.half);
+      tree_values_left_out(O, keys, sm_bad, qs.allowed(t_of(i - 1), keys.P), t_of(i - 1), qs.half);
     }
     barrier();
     put(plain, regs, i + ahead, late ? (kBuf + 2) % kBufs : (kBuf + 1) % kBufs);
     if constexpr (kPlain) fetch_next(regs);
     else fetch(regs, i + ahead + kSets);
-    if (!kPlain && i >= plain_steps) tree_hide(z, qs.allowed(t_of(i) + kw * kTreeTile, keys.P), qs.half);
-    vf.template read<0>(from + KW * kTreeTileBytes);
+    if (!kPlain && i >= plain_steps) tree_hide(z, qs.allowed(t_of(i), keys.P), qs.half);
+    vf.template read<0>(from + kTreeTileBytes);
     __builtin_amdgcn_sched_barrier(0);
     sm.take(z, O, w);
     barrier();
@@ -776,35 +762,28 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_wide_kernel(
   using B2 = std::integral_constant<int, 2>;
   using B3 = std::integral_constant<int, 3>;
   for (; i + kBufs <= easy; i += kBufs) {
-    step(Plain(), B0(), i, x[1 % kSets]);
-    step(Plain(), B1(), i + 1, x[2 % kSets]);
-    step(Plain(), B2(), i + 2, x[3 % kSets]);
+    step(Plain(), B0(), i, x[1]);
+    step(Plain(), B1(), i + 1, x[2]);
+    step(Plain(), B2(), i + 2, x[3]);
     step(Plain(), B3(), i + 3, x[0]);
   }
   for (; i < steps; i += kBufs) {
-    step(Any(), B0(), i, x[1 % kSets]);
-    if (i + 1 < steps) step(Any(), B1(), i + 1, x[2 % kSets]);
-    if (i + 2 < steps) step(Any(), B2(), i + 2, x[3 % kSets]);
+    step(Any(), B0(), i, x[1]);
+    if (i + 1 < steps) step(Any(), B1(), i + 1, x[2]);
+    if (i + 2 < steps) step(Any(), B2(), i + 2, x[3]);
     if (i + 3 < steps) step(Any(), B3(), i + 3, x[0]);
   }
   const int buf_before = (steps + kBufs - 1) % kBufs;
   vf.add<1>(O, w, 0);
   if (steps > 0) {
-    vf.read<1>(sm_kv + buf_before * kBufBytes + kw * kTreeTileBytes + KW * kTreeTileBytes);
+    vf.read<1>(sm_kv + buf_before * kBufBytes + kTreeTileBytes);
     vf.add<1>(O, w, 1);
   }
   if (steps > plain_steps) {
-    const int before = t_of(steps - 1) + kw * kTreeTile;
-    tree_values_left_out(O, keys, sm_bad, qs.allowed(before, keys.P), before, qs.half);
+    tree_values_left_out(O, keys, sm_bad, qs.allowed(t_of(steps - 1), keys.P), t_of(steps - 1), qs.half);
   }
   if (!late) barrier();                                  // as many as the others
   sm.l += shfl_xor_f(sm.l, 32);
-  if constexpr (KW > 1) {
-    static_assert((KW - 1) * QW <= kBufs * KW, "a block is as large as a tile of K and V");
-    __syncthreads();
-    tree_join<QW, KW>(sm, O, qs.busy, qw, kw, reinterpret_cast<float*>(sm_kv), sm_ml);
-    if (kw > 0) return;
-  }
   tree_store(a, qs, O, sm.m, sm.l, used, sp.nsplit, split, part_ml, part_acc);
 }
 
@@ -873,40 +852,58 @@ struct TreeLaunch {
 
 
 
+// Keys of a workgroup from which on the kernel for many rows gains (its first and last steps are slower): 256 rows, 2K tokens
+// (256 keys) 25.9 us with it and 21.4 without, 8 x 2K (768) 50 and 59, 32K (1056) 62.6 and 70.8, 128K (4224) 192 and 207.
+constexpr int kTreeWideKeys = 512;
+
 static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
-  TreeLaunch t;
+  constexpr int stage = 128;                             // a multiple of the keys that the kernels take at once
   const int rows = a.max_nodes * (a.Hq / a.Hkv);
-  t.q_waves = rows <= 32 ? 1 : (rows <= 64 ? 2 : (rows <= 128 || f32 ? 4 : 8));
-  t.q_tiles = (rows + t.q_waves * kTreeTile - 1) / (t.q_waves * kTreeTile);
-  t.wide = !f32 && t.q_waves >= 4;
-  const int64_t want = t.wide ? 256 : 512;               // workgroups: one of eight wavefronts a CU, or two of four
-  const int64_t heads = (int64_t)a.Hkv * t.q_tiles;
-  t.sp.keys_per_split = t.sp.slots_per_split = 0;
-  t.stream = false;
-  if (a.sel_start != nullptr) {
-    const int64_t slots = (int64_t)a.k * a.B * heads;
-    int64_t per = (slots + want - 1) / want;
-    const int64_t least = (128 + a.b - 1) / a.b, most = kTreeMaxListed / a.b < kTreeMaxSlots ? kTreeMaxListed / a.b : kTreeMaxSlots;
-    per = per > least ? per : least;
-    per = per < most ? per : most;
-    t.sp.slots_per_split = (int)per;
-    t.sp.nsplit = (int)((a.k + per - 1) / per);
-  } else {
-    constexpr int stage = 128;                           // a multiple of the keys that the kernels take at once
-    int64_t keys = (int64_t)a.B * a.max_seqlen;
-    keys = (keys < a.total_rows ? keys : a.total_rows) + (int64_t)a.B * a.max_nodes;
-    t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
-    const int64_t longest = (int64_t)a.max_seqlen + a.max_nodes;
-    // a sequence's last part is a shorter one: leave room for one of each
-    int64_t parts = want / heads - (a.B - 1);
+  const bool sel = a.sel_start != nullptr;
+  int64_t keys = (int64_t)a.B * a.max_seqlen;
+  keys = (keys < a.total_rows ? keys : a.total_rows) + (int64_t)a.B * a.max_nodes;
+  TreeLaunch t;
+  auto rows_of = [&](int q_waves) {
+    t.q_waves = q_waves;
+    t.q_tiles = (rows + q_waves * kTreeTile - 1) / (q_waves * kTreeTile);
+  };
+  // parts of `want` workgroups in all: keys of one
+  auto keys_of = [&](int64_t want) {
+    const int64_t heads = (int64_t)a.Hkv * t.q_tiles, longest = (int64_t)a.max_seqlen + a.max_nodes;
+    int64_t parts = want / heads - (a.B - 1);            // a sequence's last part is a shorter one: room for one of each
     parts = parts > 1 ? parts : 1;
     int64_t per = (keys + parts - 1) / parts;
     const int64_t least = 256, fewest = (longest + kTreeMaxSplit - 1) / kTreeMaxSplit;
     per = per > least ? per : least;
     per = per > fewest ? per : fewest;
-    per = (per + stage - 1) / stage * stage;
-    t.sp.keys_per_split = (int)per;
-    t.sp.nsplit = (int)((longest + per - 1) / per);
+    return (per + stage - 1) / stage * stage;
+  };
+  t.sp.keys_per_split = t.sp.slots_per_split = 0;
+  t.wide = t.stream = false;
+  if (!sel) {
+    if (rows > 128 && !f32) {
+      rows_of(kWideWaves);
+      t.sp.keys_per_split = (int)keys_of(256);           // one a CU
+      t.wide = t.sp.keys_per_split >= kTreeWideKeys;
+    }
+    if (!t.wide) {
+      rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
+      // Two a CU, and three for every two that fit where sequences differ in length (8 sequences of 16K to 64K tokens 305 us with
+      // 512, 288 with 768; one of 128K, 40 heads 421 and 427).
+      t.sp.keys_per_split = (int)keys_of(a.B > 1 ? 768 : 512);
+    }
+    t.sp.nsplit = (int)(((int64_t)a.max_seqlen + a.max_nodes + t.sp.keys_per_split - 1) / t.sp.keys_per_split);
+    t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
+  } else {
+    rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
+    const int64_t slots = (int64_t)a.k * a.B * a.Hkv * t.q_tiles;
+    // at least 256 tokens (32 nodes, 4 heads a group, 4096 tokens: 26.2 us with 128, 23.6 with 256, 27.6 with 512)
+    const int64_t least = (256 + a.b - 1) / a.b, most = kTreeMaxListed / a.b < kTreeMaxSlots ? kTreeMaxListed / a.b : kTreeMaxSlots;
+    int64_t per = (slots + 511) / 512;
+    per = per > least ? per : least;
+    per = per < most ? per : most;
+    t.sp.slots_per_split = (int)per;
+    t.sp.nsplit = (int)((a.k + per - 1) / per);
   }
   const size_t parts = t.sp.nsplit > 1 ? (size_t)a.n_tokens * a.Hq * t.sp.nsplit : 0;
   t.part_acc = align_up(parts * sizeof(float2));
@@ -921,7 +918,7 @@ size_t tree_ws_bytes(const dsk_tree_attn_args& a) {
   return f32 > bf16 ? f32 : bf16;
 }
 
-template <int QW, int KW, int NT, bool BF16>
+template <int QW, int KW, int NT>
 static void launch_tree(const dsk_tree_attn_args& a, const TreeLaunch& t, float scale_log2, float2* ml, float* acc, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
   const dim3 grid((unsigned)t.sp.nsplit, (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(QW * KW * DSK_WAVE);
@@ -934,21 +931,9 @@ static void launch_tree(const dsk_tree_attn_args& a, const TreeLaunch& t, float 
     else                                                                                                                       \
       tree_attn_kernel<QW, KW, NT, terms, false, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);   \
   } while (0)
-  if (a.out != nullptr) {
-    DSK_TREE(3);
-  } else if constexpr (BF16) {
-    DSK_TREE(1);
-  }
+  if (a.out != nullptr) DSK_TREE(3);
+  else DSK_TREE(1);
 #undef DSK_TREE
-}
-
-template <int QW, int KW>
-static void launch_tree_wide(const dsk_tree_attn_args& a, const TreeLaunch& t, float scale_log2, float2* ml, float* acc, hipStream_t st) {
-  const int G = a.Hq / a.Hkv;
-  const dim3 grid((unsigned)t.sp.nsplit, (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(QW * KW * DSK_WAVE);
-  if (a.sel_start != nullptr) tree_wide_kernel<QW, KW, true, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
-  else if (t.stream) tree_wide_kernel<QW, KW, false, true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
-  else tree_wide_kernel<QW, KW, false, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
 }
 
 hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st) {
@@ -958,16 +943,19 @@ hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st) {
   float2* ml = static_cast<float2*>(a.workspace);
   float* acc = reinterpret_cast<float*>(static_cast<unsigned char*>(a.workspace) + t.part_acc);
   const float scale_log2 = scale * kLog2e;
-  if (t.wide && t.q_waves == 4) launch_tree_wide<4, 2>(a, t, scale_log2, ml, acc, st);
-  else if (t.wide) launch_tree_wide<8, 1>(a, t, scale_log2, ml, acc, st);
-  else if (t.q_waves == 1) launch_tree<1, 4, 1, true>(a, t, scale_log2, ml, acc, st);
-  else if (t.q_waves == 2) launch_tree<2, 2, 2, true>(a, t, scale_log2, ml, acc, st);
-  else launch_tree<4, 1, 4, false>(a, t, scale_log2, ml, acc, st);
+  const int G = a.Hq / a.Hkv;
+  if (t.wide) {
+    const dim3 grid((unsigned)t.sp.nsplit, (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(kWideWaves * DSK_WAVE);
+    if (t.stream) tree_wide_kernel<true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
+    else tree_wide_kernel<false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
+  }
+  else if (t.q_waves == 1) launch_tree<1, 4, 1>(a, t, scale_log2, ml, acc, st);
+  else if (t.q_waves == 2) launch_tree<2, 2, 2>(a, t, scale_log2, ml, acc, st);
+  else launch_tree<4, 1, 4>(a, t, scale_log2, ml, acc, st);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || t.sp.nsplit <= 1) return err;
   const dim3 grid((unsigned)((a.max_nodes * a.Hq + kTreeMergeWaves - 1) / kTreeMergeWaves), (unsigned)a.B);
   const dim3 block(kTreeMergeWaves * DSK_WAVE);
-  const int G = a.Hq / a.Hkv;
   if (a.sel_start != nullptr) tree_merge_kernel<true><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
   else tree_merge_kernel<false><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
   return hipGetLastError();
