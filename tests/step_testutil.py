@@ -73,18 +73,13 @@ def tree_reference(q, Kp, Vp, Kn, Vn, seen, scale):
     """One sequence and KV head: q [n, G, D], prefix [L, D], nodes [n, D], seen bool [n, n].  64 bits; returns out
     [n, G, D], the same of |V| (how large the weighted sums are), lse [n, G]."""
     n, G, _ = q.shape
-    q, Kp, Vp, Kn, Vn = (x.double() for x in (q, Kp, Vp, Kn, Vn))
-    out, size = torch.zeros(n, G, D, dtype=torch.float64, device=q.device), torch.zeros(n, G, D, dtype=torch.float64, device=q.device)
-    lse = torch.full((n, G), -math.inf, dtype=torch.float64, device=q.device)
-    for i in range(n):
-        own = torch.from_numpy(np.flatnonzero(seen[i])).to(q.device)
-        K, V = torch.cat([Kp, Kn[own]]), torch.cat([Vp, Vn[own]])
-        if not len(K):
-            continue
-        z = q[i] @ K.t().contiguous() * scale
-        p = torch.softmax(z, 1)
-        out[i], size[i], lse[i] = p @ V, p @ V.abs(), torch.logsumexp(z, 1)
-    return out, size, lse
+    q, Kp, Vp, Kn, Vn = (x.double() for x in (q.reshape(n * G, D), Kp, Vp, Kn, Vn))
+    hidden = torch.from_numpy(~seen).to(q.device).repeat_interleave(G, 0)
+    z = torch.cat([q @ Kp.t().contiguous(), (q @ Kn.t().contiguous()).masked_fill(hidden, -math.inf)], 1) * scale
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse.masked_fill(lse == -math.inf, 0.0)[:, None])     # rows that see nothing: 0
+    V = torch.cat([Vp, Vn])
+    return (p @ V).view(n, G, D), (p @ V.abs()).view(n, G, D), lse.view(n, G)
 
 
 def accept_reference(parent, draft, target, most):

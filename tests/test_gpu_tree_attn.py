@@ -294,3 +294,71 @@ def test_one_node_equals_the_decode_attention():
     r = c.run()
     torch.cuda.synchronize()
     assert float((r.out - den.out).abs().max()) <= 1e-5 and float((r.lse - den.lse).abs().max()) <= 1e-5
+
+
+# ---- the kernel for many rows (bf16 results, more than 128 rows, at least 512 keys a workgroup) ------------------
+@pytest.mark.parametrize("lens, n_new, Hq, Hkv", [
+    ([20000], [64], 32, 8),                                      # every wavefront has rows
+    ([20033], [33], 40, 8),                                      # 165 rows: two wavefronts have none, one has five
+    ([30000, 0, 21, 29999], [64, 64, 3, 40], 32, 8),             # an empty prefix, a short one, fewer nodes than announced
+    ([70001, 4096], [256, 1], 8, 4),                             # 512 rows: two passes
+    ([34100], [100], 32, 16),
+])
+@pytest.mark.parametrize("packed", [False, True])
+def test_many_rows_over_long_contexts(lens, n_new, Hq, Hkv, packed):
+    Case(lens, n_new, Hq, Hkv, seed=len(lens) + n_new[0], packed=packed, nhd=packed, pad_tokens=2).check()
+
+
+@pytest.mark.parametrize("end", list(range(20480 - 3, 20480 + 3)) + [20480 + 31, 20480 + 33, 20480 + 64, 20480 + 127])
+def test_many_rows_where_the_prefix_ends_in_any_place_of_a_step(end):
+    Case([end], [40], 32, 8, seed=end).check()
+
+
+def test_many_rows_any_mask():
+    c = Case([20000, 100], [64, 64], 32, 8, masks="any", seed=21)
+    assert any((~m.any(1)).any() for m in c.seen)
+    c.check()
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_many_rows_masked_rows_may_hold_anything(packed):
+    c = Case([20017], [64], 32, 8, seed=22, packed=packed)
+    bf16 = dict(want_f32=False, want_bf16=True)
+    clean = c.run(**bf16)
+    for j in (1, 14, 15, 30, 47, 63):                            # by 32 keys: the first, middle and last of a tile and its neighbour
+        blind = torch.from_numpy(~c.seen[0][:, j]).cuda()
+        X, at = ((c.Kd, c.Vd), j) if packed else ((c.K, c.V), c.lens[0] + j)
+        old = [x[:, at].clone() for x in X]
+        for x in X:
+            x[:, at, ::3] = float("nan")
+            x[:, at, 1::3] = float("inf")
+        r = c.run(**bf16)
+        assert torch.equal(r.out_bf16[blind], clean.out_bf16[blind]) and torch.equal(r.lse[blind], clean.lse[blind])
+        assert bool(r.out_bf16[~blind].isnan().any(-1).all())
+        for x, o in zip(X, old):
+            x[:, at] = o
+    for x in (c.K, c.V):                                         # the room behind
+        x[:, c.lens[0] + (0 if packed else 64):] = float("nan")
+    r = c.run(**bf16)
+    assert torch.equal(r.out_bf16, clean.out_bf16) and torch.equal(r.lse, clean.lse)
+
+
+@pytest.mark.parametrize("Hq, Hkv, nodes", [(8, 8, 5), (32, 8, 13), (32, 8, 30), (32, 8, 40)])
+def test_caches_larger_than_the_memory_side_cache(Hq, Hkv, nodes):
+    """288 MB of K and V and more are read past that cache, by kernels of their own for every number of rows."""
+    c = Case([75001], [nodes], Hq, Hkv, seed=nodes)
+    assert c.rows * Hkv * 512 >= 288 << 20
+    c.check()
+
+
+def test_a_nan_that_is_seen_reaches_those_who_see_it():
+    c = Case([70, 20017], [21, 64], 32, 8, seed=23)
+    for s, j in ((0, 4), (1, 9)):
+        c.V[:, c.row0[s] + c.lens[s] + j, 5] = float("nan")
+    for kw in ({}, dict(want_f32=False, want_bf16=True)):
+        r = c.run(**kw)
+        got = (r.out if r.out is not None else r.out_bf16).isnan()
+        for s, j in ((0, 4), (1, 9)):
+            sees = torch.from_numpy(c.seen[s][:, j]).cuda()
+            own = got[c.cu[s]: c.cu[s + 1]]
+            assert bool(own[sees][..., 5].all()) and not bool(own[~sees].any()) and not bool(own[..., :5].any())
