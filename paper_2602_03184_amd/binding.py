@@ -379,8 +379,14 @@ def dsk_attn_partials_layout(args: dsk_attn_args) -> dsk_attn_partials:
     return lay
 
 
+# torch.cuda.current_stream() takes as long as a kernel launch (2.8 us): its handle alone takes 0.1
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
+        if _current_raw_stream is not None:
+            return _current_raw_stream(torch.cuda.current_device()) or None
         stream = torch.cuda.current_stream()
     if isinstance(stream, int):
         return stream or None
@@ -1022,6 +1028,14 @@ def make_reuser(sel: Selection, K: Optional[torch.Tensor], V: Optional[torch.Ten
 
 
 # ---- a step of several new tokens per sequence -------------------------------------------------
+def _call(fn, args, device: torch.device, stream, check: bool) -> int:
+    """fn on the device of its tensors, which need not be the current one (its current stream if none is given)."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        return fn(args, stream, check=check)
+    with torch.cuda.device(device):
+        return fn(args, stream, check=check)
+
+
 def _i32_on(t: Optional[torch.Tensor], n: int) -> None:
     """An int32 device array of at least n entries (or none)."""
     assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= n)
@@ -1040,7 +1054,7 @@ class StepPlan:
     keep: tuple
 
     def step(self, stream=None, check: bool = True) -> int:
-        return dsk_step_plan(self.args, stream, check=check)
+        return _call(dsk_step_plan, self.args, self.cu_new.device, stream, check)
 
 
 def make_step_plan(*, seq_row0: torch.Tensor, seq_len: torch.Tensor, n_new: torch.Tensor, max_tokens: int,
@@ -1085,9 +1099,10 @@ class NormRope:
     q_out: Optional[torch.Tensor]     # bf16 [tokens, Hq, D]
     args: dsk_norm_rope_args
     keep: tuple
+    device: torch.device
 
     def step(self, stream=None, check: bool = True) -> int:
-        return dsk_qk_norm_rope(self.args, stream, check=check)
+        return _call(dsk_qk_norm_rope, self.args, self.device, stream, check)
 
 
 def make_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optional[torch.Tensor],
@@ -1138,7 +1153,7 @@ def make_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Opti
     _i32_on(row, n)
     a.tok_pos, a.tok_row, a.inv_freq = _ptr(pos), _ptr(row), _ptr(inv_freq)
     a.flags = DSK_ROPE_INTERLEAVED if interleaved else 0
-    return NormRope(q_out=q_out, args=a, keep=(q, k, v, K, V, pos, row, q_weight, k_weight, inv_freq))
+    return NormRope(q_out=q_out, args=a, keep=(q, k, v, K, V, pos, row, q_weight, k_weight, inv_freq), device=dev)
 
 
 @dataclass
@@ -1204,7 +1219,7 @@ def make_tree_attn_args(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *, se
 def tree_decode_attn(q, K, V, *, stream=None, check: bool = True, **kw) -> TreeAttnOut:
     """dsk_tree_decode_attn with outputs and workspace made here; keywords as in make_tree_attn_args."""
     r = make_tree_attn_args(q, K, V, **kw)
-    dsk_tree_decode_attn(r.args, stream, check=check)
+    _call(dsk_tree_decode_attn, r.args, q.device, stream, check)
     return r
 
 
@@ -1221,7 +1236,7 @@ class Acceptor:
     keep: tuple
 
     def step(self, stream=None, check: bool = True) -> int:
-        return dsk_accept_draft(self.args, stream, check=check)
+        return _call(dsk_accept_draft, self.args, self.path.device, stream, check)
 
 
 def make_acceptor(K: Optional[torch.Tensor], V: Optional[torch.Tensor], *, seq_row0: torch.Tensor,

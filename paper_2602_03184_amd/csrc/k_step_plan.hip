@@ -19,6 +19,7 @@ template <int WORDS>
 __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_args a, int per_thread) {
   __shared__ uint32_t sm_base[kPlanThreads + 1];
   __shared__ uint32_t sm_wave[kPlanWaves];
+  __shared__ int32_t sm_len[kPlanThreads], sm_row0[kPlanThreads];
   __shared__ int32_t sm_parent[DSK_TREE_MAX_NODES + kPlanThreads];
   const int tid = threadIdx.x, lane = tid & (DSK_WAVE - 1), wave = tid / DSK_WAVE;
   const bool tree = a.parent != nullptr, limited = tree || WORDS > 0;
@@ -39,17 +40,27 @@ __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_a
       sm_parent[i] = t >= 0 && t < a.max_tokens ? a.parent[t] : -1;
     }
   }
-  uint32_t mine = 0;
-  for (int i = 0; i < per; ++i) {
-    const int s = tid * per + i;
-    if (s < a.B) mine = add_sat(mine, count_of(s), cap);
+  uint32_t mine = 0, own = 0;
+  if (per == 1) {                                              // a sequence a thread: all that it has is on its way at once
+    if (tid < a.B) {
+      sm_len[tid] = a.seq_len[tid];
+      sm_row0[tid] = a.seq_row0[tid];
+      mine = own = count_of(tid);
+    }
+  } else {
+    for (int i = 0; i < per; ++i) {
+      const int s = tid * per + i;
+      if (s < a.B) mine = add_sat(mine, count_of(s), cap);
+    }
   }
+  // inclusive scan over the wavefront, as wave_incl_scan_i
   uint32_t incl = mine;
-#pragma unroll
-  for (int d = 1; d < DSK_WAVE; d *= 2) {
-    const uint32_t o = (uint32_t)__shfl_up((int)incl, d, DSK_WAVE);
-    if (lane >= d) incl = add_sat(incl, o, cap);
-  }
+  incl = add_sat(incl, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, kDppRowShr + 1, 0xF, 0xF, false), cap);
+  incl = add_sat(incl, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, kDppRowShr + 2, 0xF, 0xF, false), cap);
+  incl = add_sat(incl, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, kDppRowShr + 4, 0xF, 0xF, false), cap);
+  incl = add_sat(incl, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, kDppRowShr + 8, 0xF, 0xF, false), cap);
+  incl = add_sat(incl, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, kDppBcast15, 0xA, 0xF, false), cap);
+  incl = add_sat(incl, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)incl, kDppBcast31, 0xC, 0xF, false), cap);
   if (lane == DSK_WAVE - 1) sm_wave[wave] = incl;
   uint32_t before = (uint32_t)__shfl_up((int)incl, 1, DSK_WAVE);
   if (lane == 0) before = 0;
@@ -69,7 +80,7 @@ __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_a
       const int s = tid * per + i;
       if (s < a.B) {
         a.cu_new[s] = (int32_t)(c < fit ? c : fit);
-        c = add_sat(c, count_of(s), cap);
+        c = add_sat(c, per == 1 ? own : count_of(s), cap);
         if (s == a.B - 1) a.cu_new[a.B] = (int32_t)(c < fit ? c : fit);
       }
     }
@@ -126,7 +137,8 @@ __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_a
           bits[w] = n >= 32 ? 0xFFFFFFFFu : (n > 0 ? (1u << n) - 1u : 0u);
         }
       }
-      const int64_t len = a.seq_len[s], row0 = a.seq_row0[s], row = row0 + len + i, pos = len + depth;
+      const int64_t len = per == 1 ? sm_len[s] : a.seq_len[s], row0 = per == 1 ? sm_row0[s] : a.seq_row0[s];
+      const int64_t row = row0 + len + i, pos = len + depth;
       const bool ok = row0 >= 0 && len >= 0 && row < a.total_rows;
       if (!ok) set_status(a.dev_status, DSK_ERR_CAPACITY);
       a.tok_seq[t] = s;
