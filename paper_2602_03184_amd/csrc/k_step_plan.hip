@@ -1,7 +1,9 @@
 // Tables of a step with several new tokens per sequence: packed starts, slot map, positions and ancestor masks from the
 // sequences' lengths.  A few bytes a token and no arithmetic to speak of: latency for a decoding step, writes for prompts.
 // One launch: every workgroup scans the B counts for itself (they are a cache line or two) instead of waiting for one that
-// has, and then looks its own tokens up.
+// has, and then looks its own tokens up.  Ancestors are found by doubling: a node takes over what its parent has and then its
+// parent's parent, so the rounds go with the logarithm of the depth (a walk from node to node, an LDS read each, took 5.8 us
+// for eight trees of 64 nodes some 20 deep; this takes 5.3, most of it launch and the latency of three reads).
 #include "dsk_common.hpp"
 #include "dsk_internal.hpp"
 
@@ -20,7 +22,12 @@ __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_a
   __shared__ uint32_t sm_base[kPlanThreads + 1];
   __shared__ uint32_t sm_wave[kPlanWaves];
   __shared__ int32_t sm_len[kPlanThreads], sm_row0[kPlanThreads];
-  __shared__ int32_t sm_parent[DSK_TREE_MAX_NODES + kPlanThreads];
+  // The tile's nodes, and those of a sequence that begins before it.
+  constexpr int kNodes = DSK_TREE_MAX_NODES + kPlanThreads, kPer = 2;
+  static_assert(kNodes == kPer * kPlanThreads, "two nodes a thread");
+  __shared__ int32_t sm_up[kNodes];                            // an ancestor that is not taken over yet, -1: none
+  __shared__ int32_t sm_depth[kNodes];
+  __shared__ uint32_t sm_bits[WORDS > 0 ? WORDS : 1][kNodes];
   const int tid = threadIdx.x, lane = tid & (DSK_WAVE - 1), wave = tid / DSK_WAVE;
   const bool tree = a.parent != nullptr, limited = tree || WORDS > 0;
   const uint32_t cap = (uint32_t)a.max_tokens + 1u;            // one more than fit: an overflow stays visible
@@ -34,10 +41,12 @@ __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_a
     return (uint32_t)n < cap ? (uint32_t)n : cap;
   };
   const int64_t tile0 = (int64_t)blockIdx.x * per_thread * kPlanThreads;
-  if (tree) {                                                  // the tile's parents, and those of a sequence that begins before it
-    for (int i = tid; i < DSK_TREE_MAX_NODES + kPlanThreads; i += kPlanThreads) {
-      const int64_t t = tile0 - DSK_TREE_MAX_NODES + i;
-      sm_parent[i] = t >= 0 && t < a.max_tokens ? a.parent[t] : -1;
+  int parent[kPer];
+  if (tree) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int64_t t = tile0 - DSK_TREE_MAX_NODES + k * kPlanThreads + tid;
+      parent[k] = t >= 0 && t < a.max_tokens ? a.parent[t] : -1;
     }
   }
   uint32_t mine = 0, own = 0;
@@ -73,6 +82,7 @@ __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_a
   }
   before = add_sat(before, waves_before, cap);
   sm_base[tid] = before;
+  if (tid == 0) sm_base[kPlanThreads] = total;
   const uint32_t fit = (uint32_t)a.max_tokens;
   if (first_wg) {
     uint32_t c = before;
@@ -89,9 +99,74 @@ __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_a
   }
   __syncthreads();
   const uint32_t used = total < fit ? total : fit;
+  // (threads without a sequence: sm_base is the total, above every t)
+  int top = 1;                                                 // of the search: the largest power of two below the threads in use
+  while (2 * top * per < a.B) top *= 2;
+  // the sequence of a token below `used` and its first token
+  auto find = [&](uint32_t t, int& s, uint32_t& base) {
+    int lo = 0;                                                // the last thread whose sequences begin at or before t
+    for (int step = top; step > 0; step /= 2)
+      if (sm_base[lo + step] <= t) lo += step;
+    s = lo * per;
+    base = sm_base[lo];
+    if (per > 1)
+      for (uint32_t n; t >= base + (n = count_of(s)); ++s) base += n;
+  };
+  int seq = 0;
+  uint32_t first = 0;                                          // of this thread's token
+  if (tree) {
+    const int64_t own_t = tile0 + tid;
+    const bool real = own_t < used;
+    if (real) find((uint32_t)own_t, seq, first);
+    // the place in LDS of the first node of the sequence that the tile begins in; the same for every thread
+    int s0 = 0;
+    uint32_t first0 = 0;
+    if (tile0 < used) find((uint32_t)tile0, s0, first0);
+    const int start0 = (int)((int64_t)first0 - tile0) + DSK_TREE_MAX_NODES;
+    int up[kPer], depth[kPer];
+    uint32_t bits[kPer][WORDS > 0 ? WORDS : 1];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int at = k * kPlanThreads + tid;
+      const bool mine = k == kPer - 1;                         // of the tile; the others belong to its first sequence, or to none
+      const int start = mine ? (int)((int64_t)first - tile0) + DSK_TREE_MAX_NODES : start0;
+      const bool there = mine ? real : tile0 < used && at >= start0;
+      const int node = there ? at - start : 0;
+      bool ok = there && parent[k] >= -1 && parent[k] < node;
+      if (there && !ok && mine) set_status(a.dev_status, DSK_ERR_ORDER);
+      up[k] = ok && parent[k] >= 0 ? start + parent[k] : -1;
+      depth[k] = up[k] >= 0 ? 1 : 0;                           // ancestors taken over, and the next one
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) bits[k][w] = there && (node >> 5) == w ? 1u << (node & 31) : 0u;
+      sm_up[at] = up[k];
+      sm_depth[at] = depth[k];
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) sm_bits[w][at] = bits[k][w];
+    }
+    // ends: a node's ancestors are below it, and a round leaves half of them at most
+    while (__syncthreads_or(up[0] >= 0 || up[kPer - 1] >= 0)) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        if (up[k] < 0) continue;
+        depth[k] += sm_depth[up[k]];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) bits[k][w] |= sm_bits[w][up[k]];
+        up[k] = sm_up[up[k]];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        const int at = k * kPlanThreads + tid;
+        sm_up[at] = up[k];
+        sm_depth[at] = depth[k];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) sm_bits[w][at] = bits[k][w];
+      }
+    }
+  }
 
   for (int k = 0; k < per_thread; ++k) {
-    const int64_t t64 = tile0 + (int64_t)k * kPlanThreads + tid;
+    const int64_t t64 = tile0 + (int64_t)tid * per_thread + k;  // neighbours: the search is made once
     if (t64 >= a.max_tokens) break;
     const uint32_t t = (uint32_t)t64;
     uint32_t bits[WORDS > 0 ? WORDS : 1];
@@ -102,35 +177,24 @@ __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_a
       a.tok_pos[t] = 0;
       a.tok_row[t] = -1;
     } else {
-      int lo = 0;                                              // the last thread whose sequences begin at or before t
-#pragma unroll
-      for (int step = kPlanThreads / 2; step > 0; step /= 2)
-        if (sm_base[lo + step] <= t) lo += step;
-      int s = lo * per;
-      uint32_t base = sm_base[lo];
-      if (per > 1)
-        for (uint32_t n; t >= base + (n = count_of(s)); ++s) base += n;
-      const int i = (int)(t - base);
-      int depth = i;
-      if (tree) {
-        const int32_t* par = sm_parent + (int)(t64 - tile0) + DSK_TREE_MAX_NODES - i;   // the sequence's first node
-        depth = 0;
-        int node = i;
-#pragma unroll
-        for (int w = 0; w < WORDS; ++w) bits[w] |= (node >> 5) == w ? 1u << (node & 31) : 0u;
-        for (;;) {                                             // ends: every parent taken is below its node
-          const int up = par[node];
-          if (up < -1 || up >= node) {
-            set_status(a.dev_status, DSK_ERR_ORDER);
-            break;
-          }
-          if (up < 0) break;
-          node = up;
-          ++depth;
-#pragma unroll
-          for (int w = 0; w < WORDS; ++w) bits[w] |= (node >> 5) == w ? 1u << (node & 31) : 0u;
+      if (!tree) {
+        if (k == 0 || per > 1) {
+          find(t, seq, first);
+        } else {
+          while (t >= sm_base[seq + 1]) first = sm_base[++seq];
         }
+      }
+      const int s = seq;
+      const uint32_t base = first;
+      int depth;
+      const int i = (int)(t - base);
+      if (tree) {
+        const int at = DSK_TREE_MAX_NODES + tid;
+        depth = sm_depth[at];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) bits[w] = sm_bits[w][at];
       } else {
+        depth = i;
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) {
           const int n = i + 1 - 32 * w;                        // nodes 0..i
