@@ -11,10 +11,10 @@ namespace dsk {
 
 constexpr int kPlanThreads = 256;
 constexpr int kPlanWaves = kPlanThreads / DSK_WAVE;
-constexpr int kPlanPerThread = 4;              // tokens of a thread where there is no tree to walk
+constexpr int kPlanPerThread = 4;              // tokens of a thread where there is no tree
 
-// a + b, at most cap: associative on 0..cap, so any order of a scan gives the same, and it fits 32 bits
-__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b, uint32_t cap) { return a + b < cap ? a + b : cap; }
+// a + b of 0..cap, at most cap: associative, so any order of a scan gives the same; a sum of two may pass 32 bits
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b, uint32_t cap) { return b < cap - a ? a + b : cap; }
 
 // WORDS: mask words kept in registers (0: no masks), >= mask_words
 template <int WORDS>
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kPlanThreads) void step_plan_kernel(dsk_step_plan_a
 }
 
 hipError_t launch_step_plan(const dsk_step_plan_args& a, hipStream_t st) {
-  // walks take as long as a tree is deep, so a thread takes one node; without a tree it takes several tokens
+  // a tile of a tree is a node a thread, as its LDS; without a tree a thread makes one search for several tokens
   const int per_thread = a.parent != nullptr ? 1 : kPlanPerThread;
   const int tile = per_thread * kPlanThreads;
   const dim3 grid((unsigned)(((int64_t)a.max_tokens + tile - 1) / tile)), block(kPlanThreads);

@@ -112,3 +112,35 @@ def test_many_sequences():
     most = sum(n_new) + 100
     p = _run(n_new, lens, row0[:-1], row0[-1], most)
     _expect(p, n_new, lens, row0, most, [range(n) for n in n_new])
+
+
+def test_masks_beyond_32_bits():
+    """2^28 tokens and more with mask rows of eight words."""
+    dsk = _dsk()
+    n = (1 << 28) + 5
+    p = dsk.make_step_plan(seq_row0=i32([0, 1000]), seq_len=i32([10, 20]), n_new=i32([256, 200]), max_tokens=n, total_rows=2000,
+                           max_nodes=256, want_mask=True)
+    p.step()
+    torch.cuda.synchronize()
+    assert p.cu_new.tolist() == [0, 256, 456] and int(p.dev_status) == 0
+    for t in (p.tok_seq[456:], p.tok_row[456:]):
+        assert int(t.min()) == int(t.max()) == -1
+    assert int(p.mask[456:].abs().max()) == 0
+    assert p.mask[255].tolist() == [-1] * 8 and p.mask[455].tolist() == [-1] * 6 + [(1 << 8) - 1, 0]
+    del p, t
+    torch.cuda.empty_cache()
+
+
+def test_counts_that_pass_32_bits_when_added():
+    dsk = _dsk()
+    most = 2 ** 31 - 1
+    for B in (5, 300):                                           # a sequence a thread, and several
+        p = dsk.make_step_plan(seq_row0=i32([0] * B), seq_len=i32([3] * B), n_new=i32([2] + [most] * (B - 1)), max_tokens=most,
+                               total_rows=100)
+        p.step()
+        torch.cuda.synchronize()
+        assert p.cu_new.tolist() == [0, 2] + [most] * (B - 1) and int(p.dev_status) == dsk.DSK_ERR_CAPACITY
+        assert p.tok_seq[:4].tolist() == [0, 0, 1, 1] and p.tok_row[:4].tolist() == [3, 4, 3, 4]
+        assert p.tok_seq[-2:].tolist() == [1, 1] and p.tok_row[-1:].tolist() == [-1] and p.tok_pos[-1:].tolist() == [most - 1 - 2 + 3]
+        del p
+        torch.cuda.empty_cache()
