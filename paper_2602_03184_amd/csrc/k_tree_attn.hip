@@ -10,8 +10,10 @@
 // second product wants there: key 16 t + 8 (e / 4) + 4 (lane / 32) + e % 4 in place e of step t, if V^T is read with the same
 // order of keys (two transposing LDS reads of four keys each).  No weight passes through LDS.
 //
-// K and V tiles go through registers to LDS (the loads of the next tile are under way during the products of this one), 16-byte
-// chunks swizzled by row so that the reads of both products and the writes are free of bank conflicts.
+// K and V tiles lie in LDS with their 16-byte chunks swizzled by row, so that the reads of both products and the writes are free
+// of bank conflicts.  The kernel for up to 128 rows copies a stage of the prefix straight to LDS and leaves the overlap of loads
+// and products to the second workgroup of its CU; the one for more rows has a schedule of its own and takes them through
+// registers.  Stages that hold nodes go through registers in both, where what a mask may hide is looked at.
 #include "dsk_attn_fold.hpp"
 #include "dsk_common.hpp"
 #include "dsk_internal.hpp"
@@ -133,8 +135,8 @@ struct TreePlace {
 };
 
 // The keys of a workgroup: t in [t_begin, t_end), of which those below P are the prefix's and t - P is a node's number.  A
-// stage of LOADS * THREADS / 16 keys is fetched to registers and put to LDS, a thread taking a 16-byte chunk of every
-// THREADS / 16-th row.
+// stage of LOADS * THREADS / 16 keys is copied to LDS, or fetched to registers and put there, a thread taking a 16-byte chunk of
+// every THREADS / 16-th row.
 template <int THREADS, int LOADS, bool SEL, bool STREAM>
 struct TreeKeys {
   static constexpr int kRowStep = THREADS / 16;
@@ -232,17 +234,11 @@ struct TreeKeys {
   }
   // a stage of the prefix alone
   __device__ __forceinline__ void fetch_plain(Regs& x, int t0) const {
-    if constexpr (SEL) {
+    static_assert(!SEL, "rows in order");
 #pragma unroll
-      for (int u = 0; u < LOADS; ++u) x.k[u] = load16<false>(K + rows[t0 + lrow + u * kRowStep] * kst);
+    for (int u = 0; u < LOADS; ++u) x.k[u] = load16_at<STREAM>(Ku + (t0 + u * kRowStep) * kst * 2, k_off);
 #pragma unroll
-      for (int u = 0; u < LOADS; ++u) x.v[u] = load16<false>(V + rows[t0 + lrow + u * kRowStep] * vst);
-    } else {
-#pragma unroll
-      for (int u = 0; u < LOADS; ++u) x.k[u] = load16_at<STREAM>(Ku + (t0 + u * kRowStep) * kst * 2, k_off);
-#pragma unroll
-      for (int u = 0; u < LOADS; ++u) x.v[u] = load16_at<STREAM>(Vu + (t0 + u * kRowStep) * vst * 2, v_off);
-    }
+    for (int u = 0; u < LOADS; ++u) x.v[u] = load16_at<STREAM>(Vu + (t0 + u * kRowStep) * vst * 2, v_off);
   }
   __device__ __forceinline__ void fetch_mixed(Regs& x, int t0) const {
 #pragma unroll
@@ -850,8 +846,6 @@ struct TreeLaunch {
   size_t part_acc, total;
 };
 
-
-
 // Keys of a workgroup from which on the kernel for many rows gains (its first and last steps are slower): 256 rows, 2K tokens
 // (256 keys) 25.9 us with it and 21.4 without, 8 x 2K (768) 50 and 59, 32K (1056) 62.6 and 70.8, 128K (4224) 192 and 207.
 constexpr int kTreeWideKeys = 512;
@@ -948,10 +942,13 @@ hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st) {
     const dim3 grid((unsigned)t.sp.nsplit, (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(kWideWaves * DSK_WAVE);
     if (t.stream) tree_wide_kernel<true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
     else tree_wide_kernel<false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
+  } else if (t.q_waves == 1) {
+    launch_tree<1, 4, 1>(a, t, scale_log2, ml, acc, st);
+  } else if (t.q_waves == 2) {
+    launch_tree<2, 2, 2>(a, t, scale_log2, ml, acc, st);
+  } else {
+    launch_tree<4, 1, 4>(a, t, scale_log2, ml, acc, st);
   }
-  else if (t.q_waves == 1) launch_tree<1, 4, 1>(a, t, scale_log2, ml, acc, st);
-  else if (t.q_waves == 2) launch_tree<2, 2, 2>(a, t, scale_log2, ml, acc, st);
-  else launch_tree<4, 1, 4>(a, t, scale_log2, ml, acc, st);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || t.sp.nsplit <= 1) return err;
   const dim3 grid((unsigned)((a.max_nodes * a.Hq + kTreeMergeWaves - 1) / kTreeMergeWaves), (unsigned)a.B);
