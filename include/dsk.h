@@ -550,8 +550,8 @@ typedef struct dsk_step_plan_args {
  *   (2i, 2i + 1) with DSK_ROPE_INTERLEAVED
  * in fp32, angles reduced in fp64, rounded to bf16 once.  Queries go to q_out, keys to row tok_row[t] of K, values as they
  * are to the same row of V.  A token whose tok_row is outside [0, total_rows) is skipped: nothing of it
- * is written, q_out included.  The rows of tokens that are not skipped must be distinct.  q_out may be q itself
- * if q is packed.  Inputs are strided views, e.g. of one fused projection's output.
+ * is written, q_out included.  The rows of tokens that are not skipped must be distinct.  Outputs overlap no input, but
+ * q_out may be q itself if q is packed.  Inputs are strided views, e.g. of one fused projection's output.
  * ---------------------------------------------------------------------------------------- */
 #define DSK_ROPE_INTERLEAVED 1u
 
@@ -591,8 +591,8 @@ typedef struct dsk_norm_rope_args {
  * lets a node see may hold anything, NaN included.  Mask bits of nodes that do not exist are ignored.
  * `out` asks for fp32 accuracy; where only out_bf16 is asked for, the softmax weights are rounded to bf16
  * for the products with V (lse is fp32 in both).  Sums are in fp32, split over the keys with a merge in a fixed
- * order; how they are split, and with it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen (k and b with
- * a selection) and which outputs are asked for.
+ * order; how they are split, and with it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen, total_rows (k and b
+ * with a selection) and which outputs are asked for.  A token that several selected slots hold counts as often.
  * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths or spans outside the
  * arrays are cut, never followed: a prefix to max_seqlen and total_rows, nodes to max_nodes.
  * ---------------------------------------------------------------------------------------- */
@@ -636,7 +636,8 @@ typedef struct dsk_tree_attn_args {
  * at most) are the sequence's next tokens: the K/V rows of all layers go to rows seq_row0[s] + seq_len[s]
  * + 0, 1, .. of the cache, from where dsk_tree_decode_attn reads them (behind the sequence, in place, or Kd / Vd), their ids to
  * the same rows of token_ids.  len_new = seq_len + n_accepted is what dsk_append_tokens_batch takes next, next_id
- * the target's choice after the last accepted node (-1 without nodes).  seq_len is not changed.
+ * the target's choice after the last accepted node (-1 without nodes).  seq_len is not changed; outputs overlap no input
+ * (refused for len_new and token_ids).
  * One launch; no workspace.  Data-dependent errors through *dev_status: DSK_ERR_CAPACITY if a path ends at
  * max_path or total_rows although a further node fits, DSK_ERR_SHAPE if cu_new does not fit n_tokens or max_nodes (cut).
  * ---------------------------------------------------------------------------------------- */
@@ -662,9 +663,9 @@ typedef struct dsk_accept_args {
   int64_t kd_stride_tok, kd_stride_head, kd_stride_layer, vd_stride_tok, vd_stride_head, vd_stride_layer;
   int32_t* path;               /* [dev] out [B, max_path] accepted nodes, -1 padding */
   int32_t* n_accepted;         /* [dev] out [B] */
-  int32_t* len_new;            /* [dev] out [B]; not seq_len itself */
+  int32_t* len_new;            /* [dev] out [B]; not in seq_len */
   int32_t* next_id;            /* [dev] out [B] */
-  int32_t* token_ids;          /* [dev] optional in/out [total_rows] */
+  int32_t* token_ids;          /* [dev] optional in/out [total_rows]; draft_ids and target_ids are not in it */
   int32_t* dev_status;         /* [dev] optional */
 } dsk_accept_args;
 

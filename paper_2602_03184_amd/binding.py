@@ -1030,10 +1030,15 @@ def make_reuser(sel: Selection, K: Optional[torch.Tensor], V: Optional[torch.Ten
 # ---- a step of several new tokens per sequence -------------------------------------------------
 def _call(fn, args, device: torch.device, stream, check: bool) -> int:
     """fn on the device of its tensors, which need not be the current one (its current stream if none is given)."""
+    assert device.type == "cuda", "tensors of a call are on the GPU"
     if device.index is None or device.index == torch.cuda.current_device():
         return fn(args, stream, check=check)
     with torch.cuda.device(device):
         return fn(args, stream, check=check)
+
+
+def _on(dev: torch.device, *tensors: Optional[torch.Tensor]) -> None:
+    assert all(t is None or t.device == dev for t in tensors), "tensors of a call are on one device"
 
 
 def _i32_on(t: Optional[torch.Tensor], n: int) -> None:
@@ -1080,6 +1085,7 @@ def make_step_plan(*, seq_row0: torch.Tensor, seq_len: torch.Tensor, n_new: torc
     dev_status = torch.zeros(1, **i32)
     a.cu_new, a.tok_seq, a.tok_pos, a.tok_row = _ptr(cu_new), _ptr(tok_seq), _ptr(tok_pos), _ptr(tok_row)
     a.mask, a.dev_status = _ptr(mask), _ptr(dev_status)
+    _on(dev, seq_row0, seq_len, n_new, parent)
     return StepPlan(cu_new=cu_new, tok_seq=tok_seq, tok_pos=tok_pos, tok_row=tok_row, mask=mask, dev_status=dev_status,
                     args=a, keep=(seq_row0, seq_len, n_new, parent))
 
@@ -1153,6 +1159,7 @@ def make_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Opti
     _i32_on(row, n)
     a.tok_pos, a.tok_row, a.inv_freq = _ptr(pos), _ptr(row), _ptr(inv_freq)
     a.flags = DSK_ROPE_INTERLEAVED if interleaved else 0
+    _on(dev, q, k, v, K, V, pos, row, q_weight, k_weight, inv_freq, q_out)
     return NormRope(q_out=q_out, args=a, keep=(q, k, v, K, V, pos, row, q_weight, k_weight, inv_freq), device=dev)
 
 
@@ -1212,6 +1219,7 @@ def make_tree_attn_args(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *, se
     a.out, a.out_bf16, a.lse = _ptr(out), _ptr(ob), _ptr(lse)
     ws = _ws(dsk_tree_attn_workspace_bytes(a), dev)
     a.workspace, a.workspace_bytes = _ptr(ws), ws.numel()
+    _on(dev, q, K, V, Kd, Vd, seq_row0, seq_len, cu_new, mask, sel_start, sel_len, sel_count)
     return TreeAttnOut(out=out, lse=lse, args=a, out_bf16=ob,
                        keep=(q, K, V, Kd, Vd, seq_row0, seq_len, cu_new, mask, sel_start, sel_len, sel_count, ws))
 
@@ -1285,5 +1293,6 @@ def make_acceptor(K: Optional[torch.Tensor], V: Optional[torch.Tensor], *, seq_r
     dev_status = torch.zeros(1, **i32)
     a.path, a.n_accepted, a.len_new, a.next_id = _ptr(path), _ptr(n_accepted), _ptr(len_new), _ptr(next_id)
     a.token_ids, a.dev_status = _ptr(token_ids), _ptr(dev_status)
+    _on(dev, K, V, Kd, Vd, seq_row0, seq_len, cu_new, parent, draft_ids, target_ids, token_ids, len_new)
     return Acceptor(path=path, n_accepted=n_accepted, len_new=len_new, next_id=next_id, dev_status=dev_status, args=a,
                     keep=(K, V, Kd, Vd, seq_row0, seq_len, cu_new, parent, draft_ids, target_ids, token_ids))

@@ -303,13 +303,13 @@ static dsk_status validate_norm_rope(const dsk_norm_rope_args* a) {
   if (a == nullptr) return DSK_ERR_NULL;
   if (a->struct_size != sizeof(dsk_norm_rope_args)) return DSK_ERR_VERSION;
   if (a->D != DSK_HEAD_DIM || a->n_tokens < 0 || a->total_rows < 0) return DSK_ERR_SHAPE;
-  if (!a->q && !a->k) return DSK_ERR_NULL;
+  if (!a->q && !a->k && a->n_tokens > 0) return DSK_ERR_NULL;
   if ((a->q && (a->Hq < 1 || a->Hq > 65535)) || ((a->k || a->v) && (a->Hkv < 1 || a->Hkv > 65535))) return DSK_ERR_SHAPE;
   if (a->flags & ~DSK_ROPE_INTERLEAVED) return DSK_ERR_PARAM;
   if (a->rot_dim < 0 || a->rot_dim > DSK_HEAD_DIM || a->rot_dim % 16) return DSK_ERR_PARAM;
   if ((a->q_weight || a->k_weight) && !(a->eps > 0.0f)) return DSK_ERR_PARAM;
-  if (a->rot_dim > 0 && (!a->tok_pos || !a->inv_freq)) return DSK_ERR_NULL;
-  if ((a->q && !a->q_out) || (a->k && !a->K) || (a->v && !a->V)) return DSK_ERR_NULL;
+  if (a->rot_dim > 0 && (!a->inv_freq || (!a->tok_pos && a->n_tokens > 0))) return DSK_ERR_NULL;
+  if ((a->q && !a->q_out && a->n_tokens > 0) || (a->k && !a->K) || (a->v && !a->V)) return DSK_ERR_NULL;
   if ((a->q && (a->q_stride_tok < 0 || a->q_stride_head < 0)) || (a->k && (a->k_stride_tok < 0 || a->k_stride_head < 0)) ||
       (a->v && (a->v_stride_tok < 0 || a->v_stride_head < 0)))
     return DSK_ERR_SHAPE;
@@ -332,8 +332,8 @@ static dsk_status validate_tree(const dsk_tree_attn_args* a) {
   if (a->max_nodes < 1 || a->max_nodes > DSK_TREE_MAX_NODES) return DSK_ERR_PARAM;
   if (!(a->scale >= 0.0f) || a->flags != 0) return DSK_ERR_PARAM;
   if (a->mask != nullptr && a->mask_words < (a->max_nodes + 31) / 32) return DSK_ERR_PARAM;
-  if (!a->seq_row0 || !a->seq_len || !a->cu_new || (!a->out && !a->out_bf16)) return DSK_ERR_NULL;
-  if (!a->q && a->n_tokens > 0) return DSK_ERR_NULL;
+  if (!a->seq_row0 || !a->seq_len || !a->cu_new) return DSK_ERR_NULL;
+  if ((!a->q || (!a->out && !a->out_bf16)) && a->n_tokens > 0) return DSK_ERR_NULL;
   if ((!a->K || !a->V) && a->total_rows > 0) return DSK_ERR_NULL;
   if ((a->Kd == nullptr) != (a->Vd == nullptr)) return DSK_ERR_NULL;
   if (a->sel_start || a->sel_len || a->sel_count) {
@@ -358,6 +358,13 @@ static dsk_status validate_tree(const dsk_tree_attn_args* a) {
   return DSK_OK;
 }
 
+// n and m 32-bit entries at p and q share memory
+static bool overlap32(const void* p, int64_t n, const void* q, int64_t m) {
+  if (p == nullptr || q == nullptr) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+  return x < y + 4 * (uintptr_t)m && y < x + 4 * (uintptr_t)n;
+}
+
 static dsk_status validate_accept(const dsk_accept_args* a) {
   if (a == nullptr) return DSK_ERR_NULL;
   if (a->struct_size != sizeof(dsk_accept_args)) return DSK_ERR_VERSION;
@@ -370,7 +377,10 @@ static dsk_status validate_accept(const dsk_accept_args* a) {
     return DSK_ERR_NULL;
   if ((!a->parent || !a->draft_ids || !a->target_ids) && a->n_tokens > 0) return DSK_ERR_NULL;
   if ((a->K == nullptr) != (a->V == nullptr) || (a->Kd == nullptr) != (a->Vd == nullptr)) return DSK_ERR_NULL;
-  if (a->len_new == a->seq_len) return DSK_ERR_PARAM;          // read by every workgroup while one of them writes
+  // read by every workgroup while one of them writes
+  if (overlap32(a->len_new, a->B, a->seq_len, a->B) || overlap32(a->token_ids, a->total_rows, a->draft_ids, a->n_tokens) ||
+      overlap32(a->token_ids, a->total_rows, a->target_ids, a->n_tokens))
+    return DSK_ERR_PARAM;
   if (a->K == nullptr) return a->Kd == nullptr ? DSK_OK : DSK_ERR_NULL;
   const struct { const void* X; int64_t tok, head, layer; } x[4] = {
       {a->K, a->k_stride_tok, a->k_stride_head, a->k_stride_layer}, {a->V, a->v_stride_tok, a->v_stride_head, a->v_stride_layer},

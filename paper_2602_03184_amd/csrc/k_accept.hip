@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(dsk_accept_args 
 hipError_t launch_accept(const dsk_accept_args& a, hipStream_t st) {
   const int64_t items = a.K != nullptr ? (int64_t)a.n_layers * a.Hkv * 2 : 1;
   const int64_t wgs = (items + kAcceptGroups - 1) / kAcceptGroups;
-  if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (wgs > 0xFFFFFFFFll / kAcceptThreads) return hipErrorInvalidValue;
   accept_kernel<<<dim3((unsigned)wgs, (unsigned)a.B), dim3(kAcceptThreads), 0, st>>>(a);
   return hipGetLastError();
 }

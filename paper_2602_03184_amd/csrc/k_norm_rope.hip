@@ -134,7 +134,7 @@ hipError_t launch_norm_rope(const dsk_norm_rope_args& a, hipStream_t st) {
   while (per_wave > 1 && (int64_t)a.n_tokens * ((quads + per_wave - 1) / per_wave) < 4096) per_wave = (per_wave + 1) / 2;
   const int waves = (quads + per_wave - 1) / per_wave;
   const int64_t wgs = ((int64_t)a.n_tokens * waves + kRopeWaves - 1) / kRopeWaves;
-  if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (wgs > 0xFFFFFFFFll / kRopeThreads) return hipErrorInvalidValue;
   const dim3 grid((unsigned)wgs), block(kRopeThreads);
   if (a.rot_dim == 0) norm_rope_kernel<RopePairs::kNone><<<grid, block, 0, st>>>(a, waves, per_wave);
   else if (a.flags & DSK_ROPE_INTERLEAVED) norm_rope_kernel<RopePairs::kInterleaved><<<grid, block, 0, st>>>(a, waves, per_wave);

@@ -91,6 +91,10 @@ def test_norm_rope_refuses(dsk):
     a = _rope(dsk)
     a.n_tokens = 0                                               # nothing to do, nothing launched
     assert dsk.dsk_qk_norm_rope(a, 0, check=False) == dsk.DSK_OK
+    a.q_out = None
+    assert dsk.dsk_qk_norm_rope(a, 0, check=False) == dsk.DSK_OK
+    a.q = a.k = a.v = a.tok_pos = a.tok_row = None
+    assert dsk.dsk_qk_norm_rope(a, 0, check=False) == dsk.DSK_OK
 
 
 def _tree(dsk):
@@ -119,6 +123,8 @@ def test_tree_attention_refuses(dsk):
              ("v_stride_head", -8, dsk.DSK_ERR_SHAPE), ("kd_stride_head", 12, dsk.DSK_ERR_ALIGN),
              ("k_stride_tok", 132, dsk.DSK_ERR_ALIGN), ("K", FAKE + 8, dsk.DSK_ERR_ALIGN), ("Vd", FAKE + 8, dsk.DSK_ERR_ALIGN),
              ("q", FAKE + 8, dsk.DSK_ERR_ALIGN), ("out", FAKE + 8, dsk.DSK_ERR_ALIGN), ("out_bf16", FAKE + 8, dsk.DSK_ERR_ALIGN),
+             ("k_stride_tok", (1 << 24) + 8, dsk.DSK_ERR_SHAPE), ("v_stride_tok", (1 << 24) + 8, dsk.DSK_ERR_SHAPE),
+             ("max_seqlen", 0x7FFF0001, dsk.DSK_ERR_SHAPE),
              ("workspace_bytes", 0, dsk.DSK_ERR_WORKSPACE), ("workspace", None, dsk.DSK_ERR_WORKSPACE)]
     cases += [(f, None, dsk.DSK_ERR_NULL) for f in ("q", "K", "V", "Kd", "Vd", "seq_row0", "seq_len", "cu_new", "sel_start",
                                                     "sel_len", "sel_count")]
@@ -131,6 +137,7 @@ def test_tree_attention_refuses(dsk):
     assert dsk.dsk_tree_decode_attn(a, 0, check=False) == dsk.DSK_ERR_ALIGN
     a = _tree(dsk)
     a.n_tokens, a.workspace_bytes = 0, 1 << 40                   # no node: nothing launched
+    a.q = a.out = a.out_bf16 = None
     assert dsk.dsk_tree_decode_attn(a, 0, check=False) == dsk.DSK_OK
 
 
@@ -142,7 +149,7 @@ def _accept(dsk):
     for f in ("seq_row0", "seq_len", "cu_new", "parent", "draft_ids", "target_ids", "K", "V", "Kd", "Vd", "path",
               "n_accepted", "next_id", "token_ids"):
         setattr(a, f, FAKE)
-    a.len_new = 2 * FAKE
+    a.len_new, a.token_ids = 2 * FAKE, 4 * FAKE
     for x in ("k", "v", "kd", "vd"):
         setattr(a, x + "_stride_tok", 128)
         setattr(a, x + "_stride_head", 128 * 1000)
@@ -154,7 +161,9 @@ def test_accept_refuses(dsk):
     cases = [("struct_size", 8, dsk.DSK_ERR_VERSION), ("D", 64, dsk.DSK_ERR_SHAPE), ("B", 0, dsk.DSK_ERR_SHAPE),
              ("Hkv", 0, dsk.DSK_ERR_SHAPE), ("n_layers", 0, dsk.DSK_ERR_SHAPE), ("n_tokens", -1, dsk.DSK_ERR_SHAPE),
              ("max_nodes", 257, dsk.DSK_ERR_PARAM), ("max_path", 0, dsk.DSK_ERR_PARAM), ("max_path", 21, dsk.DSK_ERR_PARAM),
-             ("len_new", FAKE, dsk.DSK_ERR_PARAM), ("k_stride_layer", 0, dsk.DSK_ERR_SHAPE),
+             ("len_new", FAKE, dsk.DSK_ERR_PARAM), ("len_new", FAKE + 4, dsk.DSK_ERR_PARAM),
+             ("token_ids", FAKE - 4 * 999, dsk.DSK_ERR_PARAM), ("target_ids", 4 * FAKE + 4 * 999, dsk.DSK_ERR_PARAM),
+             ("k_stride_layer", 0, dsk.DSK_ERR_SHAPE),
              ("vd_stride_layer", 4, dsk.DSK_ERR_ALIGN), ("k_stride_tok", 64, dsk.DSK_ERR_SHAPE),
              ("v_stride_head", 0, dsk.DSK_ERR_SHAPE), ("Kd", FAKE + 8, dsk.DSK_ERR_ALIGN), ("V", FAKE + 8, dsk.DSK_ERR_ALIGN)]
     cases += [(f, None, dsk.DSK_ERR_NULL) for f in ("seq_row0", "seq_len", "cu_new", "parent", "draft_ids", "target_ids", "K",
@@ -163,3 +172,19 @@ def test_accept_refuses(dsk):
     a = _accept(dsk)
     a.K = a.V = None                                             # the nodes' own buffers without a cache to move them to
     assert dsk.dsk_accept_draft(a, 0, check=False) == dsk.DSK_ERR_NULL
+
+
+def test_helpers_refuse_tensors_that_are_not_on_the_gpu(dsk):
+    import torch
+    i = torch.zeros(4, dtype=torch.int32)
+    X = torch.zeros(2, 8, 128, dtype=torch.bfloat16)
+    for made in (dsk.make_step_plan(seq_row0=i, seq_len=i, n_new=i, max_tokens=3, total_rows=8),
+                 dsk.make_norm_rope(X, X, X, X.transpose(0, 1), X.transpose(0, 1)),
+                 dsk.make_acceptor(X, X, seq_row0=i, seq_len=i, cu_new=torch.zeros(5, dtype=torch.int32), parent=i,
+                                   draft_ids=i, target_ids=i, max_nodes=2)):
+        with pytest.raises(AssertionError):
+            made.step()
+    with pytest.raises(AssertionError):
+        dsk.tree_decode_attn(X, X, X, seq_row0=i[:1], seq_len=i[:1], cu_new=i, mask=None, max_nodes=2, max_seqlen=4)
+    with pytest.raises(AssertionError):                          # one of them elsewhere
+        dsk.make_step_plan(seq_row0=i, seq_len=i.to("meta"), n_new=i, max_tokens=3, total_rows=8)

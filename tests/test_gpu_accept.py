@@ -131,3 +131,48 @@ def test_the_walk_alone_and_a_table_that_does_not_fit():
         acc.step()
         torch.cuda.synchronize()
         assert acc.path.tolist() == path and int(acc.dev_status.item()) == dsk.DSK_ERR_SHAPE
+
+
+def test_rows_and_layers_beyond_32_bits():
+    """Layers 2^30 channels apart, and rows of 10240 channels of which the last lie beyond 2^31."""
+    dsk = _dsk()
+    step, chain = 1 << 30, [list(range(-1, 11))]
+    draft, target = [list(range(100, 112))], [list(range(101, 113))]
+    common = dict(cu_new=i32([0, 12]), parent=_flat(chain), draft_ids=_flat(draft), target_ids=_flat(target), max_nodes=12)
+    own = torch.randn(4, 3, 2, 12, D, device="cuda").bfloat16()  # of K and V; layers, heads, nodes
+    base = torch.empty(2 * step + 400 * D, dtype=torch.bfloat16, device="cuda")
+    K, V = (base.as_strided((3, 2, 50, D), (step, 100 * D, D, 1), o) for o in (0, 200 * D))
+    acc = dsk.make_acceptor(K, V, seq_row0=i32([5]), seq_len=i32([30]), Kd=own[0], Vd=own[1], **common)
+    acc.step()
+    torch.cuda.synchronize()
+    assert acc.path.tolist() == [list(range(12))]
+    assert torch.equal(K[:, :, 35:47], own[0]) and torch.equal(V[:, :, 35:47], own[1])
+    del base, K, V
+    cache = torch.empty(225_000, 80, D, dtype=torch.bfloat16, device="cuda")
+    K, V = cache[:, 2:4].transpose(0, 1), cache[:, 78:80].transpose(0, 1)
+    skip = [[-1, 0, 0, 2, 2, 4, 4, 6, 6, 8, 8, 10]]              # 0 and its even descendants
+    draft = [[1, 90, 2, 90, 3, 90, 4, 90, 5, 90, 6, 90]]
+    target = [[2, 0, 3, 0, 4, 0, 5, 0, 6, 0, 7, 0]]
+    at = 100_000 + 120_000
+    K[:, at:at + 12], V[:, at:at + 12] = own[2, 0], own[3, 0]
+    common.update(parent=_flat(skip), draft_ids=_flat(draft), target_ids=_flat(target))
+    acc = dsk.make_acceptor(K, V, seq_row0=i32([100_000]), seq_len=i32([120_000]), **common)
+    acc.step()
+    torch.cuda.synchronize()
+    assert acc.path[0, :6].tolist() == [0, 2, 4, 6, 8, 10] and int(acc.next_id) == 7
+    for X, old in ((K, own[2, 0]), (V, own[3, 0])):
+        assert torch.equal(X[:, at:at + 6], old[:, ::2]) and torch.equal(X[:, at + 6:at + 12], old[:, 6:])
+    del cache, K, V
+    torch.cuda.empty_cache()
+
+
+def test_no_token_at_all():
+    dsk = _dsk()
+    K, V = (torch.full((1, 2, 9, D), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    none = i32([])
+    acc = dsk.make_acceptor(K, V, seq_row0=i32([0, 5]), seq_len=i32([3, 2]), cu_new=i32([0, 0, 0]), parent=none, draft_ids=none,
+                            target_ids=none, max_nodes=4)
+    acc.step()
+    torch.cuda.synchronize()
+    assert acc.n_accepted.tolist() == [0, 0] and acc.len_new.tolist() == [3, 2] and acc.next_id.tolist() == [-1, -1]
+    assert bool((acc.path == -1).all()) and bool((K == 5.0).all()) and bool((V == 5.0).all())

@@ -147,3 +147,42 @@ def test_values_that_are_not_finite_stay_in_their_row():
     hit[1, 2] = hit[2, 0] = True
     assert bool(r.q_out.cpu()[hit].isnan().any(-1).all())
     _close(r.q_out.cpu()[~hit], want[~hit], size[~hit])
+
+
+def test_rows_and_tokens_beyond_32_bits():
+    """Tokens, results and cache rows of which the last lie more than 2^31 channels behind the first."""
+    dsk = _dsk()
+    n, step = 3, 1 << 30
+    x = torch.empty(2 * step + 8 * D, dtype=torch.bfloat16, device="cuda").as_strided((n, 8, D), (step, D, 1))
+    x.copy_(torch.randn(n, 8, D, device="cuda") * 3)
+    cache = torch.empty(225_000, 80, D, dtype=torch.bfloat16, device="cuda")
+    K, V = cache[:, 40:42].transpose(0, 1), cache[:, 78:80].transpose(0, 1)
+    pos, row, f = i32([5, 6, 7]), i32([224_999, 17, 224_000]), _freq(128)
+    q, k, v = x[:, :4], x[:, 4:6], x[:, 6:8]
+    r = dsk.make_norm_rope(q, k, v, K, V, pos=pos, row=row, inv_freq=f)
+    r.step()
+    torch.cuda.synchronize()
+    _close(r.q_out, *rope_reference(q, None, 0, pos, f, False))
+    _close(K[:, row.long()].transpose(0, 1), *rope_reference(k, None, 0, pos, f, False))
+    assert torch.equal(V[:, row.long()].transpose(0, 1), v)
+    del x, cache, K, V, q, k, v
+    one = torch.randn(1, 128, D, device="cuda").bfloat16()
+    many = one.expand(132_000, 128, D)                           # 2^31 channels and more of results
+    assert many.numel() > 2 ** 31
+    pos = torch.full((132_000,), 9, dtype=torch.int32, device="cuda")
+    r = dsk.make_norm_rope(many, None, None, None, None, pos=pos, inv_freq=f, total_rows=132_000)
+    r.step()
+    torch.cuda.synchronize()
+    _close(r.q_out[:1], *rope_reference(one, None, 0, pos[:1], f, False))
+    assert all(torch.equal(r.q_out[t], r.q_out[0]) for t in (1, 65_535, 131_072, 131_999))
+    torch.cuda.empty_cache()
+
+
+def test_no_token_at_all():
+    dsk = _dsk()
+    q, k, v, wq, wk, _ = _inputs(1, 4, 2)
+    K, V = (torch.full((2, 5, D), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    r = dsk.make_norm_rope(q[:0], k[:0], v[:0], K, V, pos=i32([]), q_weight=wq, k_weight=wk, inv_freq=_freq(128))
+    r.step()
+    torch.cuda.synchronize()
+    assert r.q_out.shape == (0, 4, D) and bool((K == 5.0).all()) and bool((V == 5.0).all())

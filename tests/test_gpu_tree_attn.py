@@ -362,3 +362,51 @@ def test_a_nan_that_is_seen_reaches_those_who_see_it():
             sees = torch.from_numpy(c.seen[s][:, j]).cuda()
             own = got[c.cu[s]: c.cu[s + 1]]
             assert bool(own[sees][..., 5].all()) and not bool(own[~sees].any()) and not bool(own[..., :5].any())
+
+
+# ---- offsets that pass 32 bits ----------------------------------------------------------------------------------
+@pytest.fixture(scope="module")
+def far():
+    """K and V of three heads as views of rows of 10240 channels: 225,000 rows are 2^31 channels and more."""
+    rows, g = 225_000, torch.Generator(device="cuda")
+    g.manual_seed(31)
+    X = torch.empty(rows, 80, D, dtype=torch.bfloat16, device="cuda")
+    assert (rows - 5_000) * 80 * D > 2 ** 31
+    X[:, :6] = torch.randn(rows, 6, D, generator=g, device="cuda").bfloat16()
+    yield X[:, :3].transpose(0, 1), X[:, 3:6].transpose(0, 1)
+    del X
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("Hq, nodes, packed", [(3, 9, False), (6, 40, False), (6, 40, True), (24, 30, False), (24, 30, True)])
+def test_rows_beyond_32_bits(far, Hq, nodes, packed):
+    for lens in ([224_900], [2_000, 222_800]):                   # the second sequence begins far away
+        c = Case(lens, [nodes] * len(lens), Hq, 3, packed=packed, seed=nodes, spare=0)
+        assert c.rows <= 225_000
+        c.K, c.V = far
+        c.check()
+
+
+def test_selected_rows_beyond_32_bits(far):
+    c = Case([224_950], [25], 12, 3, seed=33, spare=0)
+    c.K, c.V = far
+    c.select(40, 32)
+    for h in range(3):
+        c.sel[0][0, h, -30:] = np.sort(c.rng.choice(np.arange(219_000, 224_900, 32), 30, replace=False))
+        c.sel[1][0, h, -30:] = 32
+    c.check()
+
+
+def test_no_token_at_all():
+    c = Case([40, 3], [0, 0], 8, 2, seed=34)
+    c.q = torch.empty(0, 8, D, dtype=torch.bfloat16, device="cuda")
+    r = _dsk().tree_decode_attn(c.q, c.K, c.V, **{**c.kwargs(), "mask": None}, want_bf16=True)
+    torch.cuda.synchronize()
+    assert r.out.shape == r.out_bf16.shape == (0, 8, D)
+
+
+def test_a_token_of_several_slots_counts_as_often():
+    c = Case([300], [7], 8, 2, seed=35).select(6, 16)
+    for x in c.sel[:2]:
+        x[0, :, 1], x[0, :, 4] = x[0, :, 0], x[0, :, 3]
+    c.check()
