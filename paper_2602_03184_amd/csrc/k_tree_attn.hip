@@ -119,18 +119,39 @@ struct TreePlace {
     len = len < a.total_rows - row0 ? len : a.total_rows - row0;
     n_keys = a.Kd != nullptr || n < a.total_rows - row0 - len ? n : (int)(a.total_rows - row0 - len);
   }
-  // parts of its keys that have any
-  __device__ __forceinline__ int used(const dsk_tree_attn_args& a, const TreeSplit& sp, bool selected, int64_t s_hk) const {
+  // parts of its keys that have any; count: of the selection
+  __device__ __forceinline__ int used(const TreeSplit& sp, bool selected, int count) const {
     int64_t u;
     if (selected) {
-      int count = a.sel_count[s_hk];
-      count = count < 0 ? 0 : (count < a.k ? count : a.k);
       u = (count + sp.slots_per_split - 1) / sp.slots_per_split;
     } else {
       u = (len + n_keys + sp.keys_per_split - 1) / sp.keys_per_split;
     }
     u = u > 0 ? u : 1;                                   // the nodes go with the last slots
     return (int)(u < sp.nsplit ? u : sp.nsplit);         // (never more: the host counts max_seqlen + max_nodes keys)
+  }
+};
+
+__device__ __forceinline__ int tree_sel_count(const dsk_tree_attn_args& a, int s, int hk) {
+  const int count = a.sel_count[(int64_t)s * a.Hkv + hk];
+  return count < 0 ? 0 : (count < a.k ? count : a.k);
+}
+
+// A part of a selection: how many slots there are in all, and a thread's slot of the part (as the caller wrote it).  Read before
+// anything is known about the sequence, so that it costs no round trip of its own.
+template <bool SEL>
+struct TreeSlots {
+  int count = 0, start = 0, len = 0;
+  __device__ __forceinline__ TreeSlots(const dsk_tree_attn_args& a, const TreeSplit& sp, int s, int hk, int split) {
+    if constexpr (SEL) {
+      const int tid = threadIdx.x, first = split * sp.slots_per_split;
+      count = tree_sel_count(a, s, hk);
+      if (tid < sp.slots_per_split && tid < a.k - first) {
+        const int64_t at = ((int64_t)s * a.Hkv + hk) * a.k + first + tid;
+        start = a.sel_start[at];
+        len = a.sel_len[at];
+      }
+    }
   }
 };
 
@@ -154,8 +175,8 @@ struct TreeKeys {
     uint4 k[LOADS], v[LOADS];
   };
 
-  __device__ __forceinline__ TreeKeys(const dsk_tree_attn_args& a, const TreeSplit& sp, const TreePlace& at, int s, int hk,
-                                      int split, int used, int32_t* sm_rows) {
+  __device__ __forceinline__ TreeKeys(const dsk_tree_attn_args& a, const TreeSplit& sp, const TreePlace& at, const TreeSlots<SEL>& slots,
+                                      int hk, int split, int used, int32_t* sm_rows) {
     const int tid = threadIdx.x, lane = tid & (DSK_WAVE - 1), wave = tid / DSK_WAVE;
     lrow = tid >> 4;
     lc = tid & 15;
@@ -185,18 +206,11 @@ struct TreeKeys {
     if constexpr (SEL) {
       __shared__ int32_t sm_slot[3][kTreeMaxSlots];
       __shared__ int32_t sm_wave[kTreeMaxSlots / DSK_WAVE];
-      const int64_t sk = (int64_t)s * a.Hkv + hk;
-      int count = a.sel_count[sk];
-      count = count < 0 ? 0 : (count < a.k ? count : a.k);
       const int first = split * sp.slots_per_split;
-      const int here = count - first < sp.slots_per_split ? count - first : sp.slots_per_split;
-      int start = 0, ln = 0;
-      if (tid < here) {
-        start = a.sel_start[sk * a.k + first + tid];
-        ln = a.sel_len[sk * a.k + first + tid];
-        ln = ln < a.b ? ln : a.b;
-        if (start < 0 || ln <= 0 || start > a.total_rows - ln) ln = 0;
-      }
+      const int here = slots.count - first < sp.slots_per_split ? slots.count - first : sp.slots_per_split;
+      const int start = slots.start;
+      int ln = slots.len < a.b ? slots.len : a.b;
+      if (tid >= here || start < 0 || ln <= 0 || start > a.total_rows - ln) ln = 0;
       if (tid < kTreeMaxSlots) {
         const int incl = wave_incl_scan_i(ln, lane);
         if (lane == DSK_WAVE - 1) sm_wave[wave] = incl;
@@ -291,7 +305,7 @@ struct TreeQueries {
   TreeMask mask;
   tree_bf16x8 q[8];     // channels 16 t + 8 half .. + 7
 
-  __device__ __forceinline__ TreeQueries(const dsk_tree_attn_args& a, const TreePlace& at, int G, int hk, int r0, int n_keys) {
+  __device__ __forceinline__ TreeQueries(const dsk_tree_attn_args& a, const TreePlace& at, int G, int hk, int r0) {
     const int lane = threadIdx.x & (DSK_WAVE - 1);
     col = lane & 31;
     half = lane >> 5;
@@ -309,7 +323,7 @@ struct TreeQueries {
     }
     mask.row = a.mask != nullptr ? a.mask + (int64_t)(at.tok0 + node) * a.mask_words : nullptr;
     mask.node = node;
-    mask.n = n_keys;
+    mask.n = 0;                                          // until the keys are known
   }
   __device__ __forceinline__ uint32_t allowed(int t0, int P) const { return real ? mask.window(t0 - P) : 0u; }
 };
@@ -545,12 +559,14 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree
   const int tid = threadIdx.x, wave = tid / DSK_WAVE;
   const int qw = wave % QW, kw = wave / QW;
 
+  const TreeSlots<SEL> slots(a, sp, s, hk, split);
   const TreePlace at(a, s);
   if (q_tile * QW * kTreeTile >= at.n * G) return;       // uniform: no row of this pass
-  const int used = at.used(a, sp, SEL, (int64_t)s * a.Hkv + hk);
+  const int used = at.used(sp, SEL, slots.count);
   if (split >= used) return;
-  TreeKeys<kThreads, kKeys * 16 / kThreads, SEL, STREAM> keys(a, sp, at, s, hk, split, used, sm_rows);
-  const TreeQueries qs(a, at, G, hk, (q_tile * QW + qw) * kTreeTile, keys.nodes());
+  TreeQueries qs(a, at, G, hk, (q_tile * QW + qw) * kTreeTile);
+  const TreeKeys<kThreads, kKeys * 16 / kThreads, SEL, STREAM> keys(a, sp, at, slots, hk, split, used, sm_rows);
+  qs.mask.n = keys.nodes();
 
   TreeSoftmax sm(scale_log2);
   tree_f32x16 O[4];
@@ -641,11 +657,12 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
 
   const TreePlace at(a, s);
   if (q_tile * kWideWaves * kTreeTile >= at.n * G) return;       // uniform: no row of this pass
-  const int used = at.used(a, sp, false, 0);
+  const int used = at.used(sp, false, 0);
   if (split >= used) return;
   using Keys = TreeKeys<kThreads, kKeys * 16 / kThreads, false, STREAM>;
-  const Keys keys(a, sp, at, s, hk, split, used, nullptr);
-  const TreeQueries qs(a, at, G, hk, (q_tile * kWideWaves + wave) * kTreeTile, keys.nodes());
+  const Keys keys(a, sp, at, TreeSlots<false>(a, sp, s, hk, split), hk, split, used, nullptr);
+  TreeQueries qs(a, at, G, hk, (q_tile * kWideWaves + wave) * kTreeTile);
+  qs.mask.n = keys.nodes();
   TreeSoftmax sm(scale_log2);
   tree_f32x16 O[4];
 #pragma unroll
@@ -796,7 +813,7 @@ __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
   const int node = item / a.Hq, h = item - node * a.Hq;
   const TreePlace at(a, s);
   if (node >= at.n) return;
-  const int used = at.used(a, sp, SEL, (int64_t)s * a.Hkv + h / G);
+  const int used = at.used(sp, SEL, SEL ? tree_sel_count(a, s, h / G) : 0);
   if (used <= 1) return;                                 // finished by the kernel above
   const int64_t row = (int64_t)(at.tok0 + node) * a.Hq + h;
   const float2* ml = part_ml + row * sp.nsplit;
@@ -850,6 +867,8 @@ struct TreeLaunch {
 // (256 keys) 25.9 us with it and 21.4 without, 8 x 2K (768) 50 and 59, 32K (1056) 62.6 and 70.8, 128K (4224) 192 and 207.
 constexpr int kTreeWideKeys = 512;
 
+constexpr int kTreeFewWorkgroups = 128;        // of 256 CUs
+
 static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   constexpr int stage = 128;                             // a multiple of the keys that the kernels take at once
   const int rows = a.max_nodes * (a.Hq / a.Hkv);
@@ -899,6 +918,12 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     t.sp.slots_per_split = (int)per;
     t.sp.nsplit = (int)((a.k + per - 1) / per);
   }
+  // Where workgroups of four wavefronts' rows leave half the CUs idle or more, twice as many take two wavefronts' rows each and
+  // split a stage's keys as well: K and V come from L2 once more, but every wavefront has half as much to do.  128 rows a
+  // selection of 4K tokens (128 workgroups) 23.6 -> 20.9 us, of 2K 20.9 -> 18.0, a prefix of 600 tokens 16.0 -> 14.4; 4K tokens
+  // (136 workgroups) would take 21.8 instead of 20.6.  (Halving two wavefronts' rows again gains nothing: 600 tokens 13.9 and
+  // 14.1.)
+  if (!t.wide && t.q_waves == 4 && (int64_t)a.B * a.Hkv * t.q_tiles * t.sp.nsplit <= kTreeFewWorkgroups) rows_of(2);
   const size_t parts = t.sp.nsplit > 1 ? (size_t)a.n_tokens * a.Hq * t.sp.nsplit : 0;
   t.part_acc = align_up(parts * sizeof(float2));
   t.total = t.part_acc + align_up(parts * DSK_HEAD_DIM * sizeof(float));
