@@ -11,9 +11,9 @@
 // order of keys (two transposing LDS reads of four keys each).  No weight passes through LDS.
 //
 // K and V tiles lie in LDS with their 16-byte chunks swizzled by row, so that the reads of both products and the writes are free
-// of bank conflicts.  The kernel for up to 128 rows copies a stage of the prefix straight to LDS and leaves the overlap of loads
-// and products to the second workgroup of its CU; the one for more rows has a schedule of its own and takes them through
-// registers.  Stages that hold nodes go through registers in both, where what a mask may hide is looked at.
+// of bank conflicts.  The kernel for up to 128 rows copies stages of the prefix straight to LDS; the one for more rows has a
+// schedule of its own and takes them through registers.  Stages that hold nodes go through registers in both, where what a mask
+// may hide is looked at.
 #include "dsk_attn_fold.hpp"
 #include "dsk_common.hpp"
 #include "dsk_internal.hpp"
@@ -32,7 +32,9 @@ constexpr int kTreeTile = 32;                   // keys and queries of a matrix 
 constexpr int kTreeRowBytes = 2 * DSK_HEAD_DIM;
 constexpr int kTreeMaxSlots = 256;              // selected slots of a workgroup
 constexpr int kTreeMaxListed = 2048;            // and their tokens
-constexpr int kTreeMaxSplit = 64;               // parts of a sequence
+// Parts of a sequence at most.  One KV head (4 query heads, 16 nodes, 128K tokens): 36.1 us with 64, 29.5 with 128, 29.6 with 256;
+// four sequences of 32K: 23.1, 25.9 and 33.6.
+constexpr int kTreeMaxSplit = 128;
 constexpr int kTreeMixedTiles = 16;             // tiles from the first one with a node on: 256 nodes, and a stage's other tiles
 constexpr int kTreeTileBytes = kTreeTile * kTreeRowBytes;
 
@@ -394,20 +396,50 @@ struct TreeWeights {
 
 struct TreeVFrag {
   tree_bf16x8 v[4][2];
-  template <int T>                                       // 16 of the keys
-  __device__ __forceinline__ void read(const unsigned char* sm_v) {
+  // a lane's place in a tile for channels 32 ct .. 32 ct + 31
+  static __device__ __forceinline__ int place(int ct) {
     const int lane = threadIdx.x & (DSK_WAVE - 1), half = lane >> 5;
     const int quad = (lane & 15) >> 2;                   // of the four keys of a transposing read
-    const unsigned char* vt = sm_v + (4 * half + quad) * kTreeRowBytes + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) +
-                              ((lane & 1) << 3);
+    return (4 * half + quad) * kTreeRowBytes + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + ((lane & 1) << 3) + ((ct ^ quad) << 6);
+  }
+  template <int T>                                       // 16 of the keys
+  __device__ __forceinline__ void read(const unsigned char* sm_v) {
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) {
-      const unsigned char* at = vt + ((ct ^ quad) << 6) + T * 16 * kTreeRowBytes;
+      const unsigned char* at = sm_v + place(ct) + T * 16 * kTreeRowBytes;
       const tree_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) tree_s16x4*)(at));
       const tree_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (__attribute__((address_space(3))) tree_s16x4*)(at + 8 * kTreeRowBytes));
       v[ct][T] = __builtin_bit_cast(tree_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
+  }
+  // All 32 keys while copies to other parts of LDS are under way: for the builtin the compiler would wait for those first, as it
+  // does not see that they are other parts.
+  __device__ __forceinline__ void read_beside_copies(const unsigned char* sm_v) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)sm_v;
+    u32x2 x[4][4];
+    static_assert(kTreeRowBytes == 256, "offsets: 8 rows");
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:2048\n\t"
+        "ds_read_b64_tr_b16 %4, %17\n\tds_read_b64_tr_b16 %5, %17 offset:2048\n\t"
+        "ds_read_b64_tr_b16 %8, %18\n\tds_read_b64_tr_b16 %9, %18 offset:2048\n\t"
+        "ds_read_b64_tr_b16 %12, %19\n\tds_read_b64_tr_b16 %13, %19 offset:2048\n\t"
+        "ds_read_b64_tr_b16 %2, %16 offset:4096\n\tds_read_b64_tr_b16 %3, %16 offset:6144\n\t"
+        "ds_read_b64_tr_b16 %6, %17 offset:4096\n\tds_read_b64_tr_b16 %7, %17 offset:6144\n\t"
+        "ds_read_b64_tr_b16 %10, %18 offset:4096\n\tds_read_b64_tr_b16 %11, %18 offset:6144\n\t"
+        "ds_read_b64_tr_b16 %14, %19 offset:4096\n\tds_read_b64_tr_b16 %15, %19 offset:6144\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[0][2]), "=&v"(x[0][3]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[1][2]),
+          "=&v"(x[1][3]), "=&v"(x[2][0]), "=&v"(x[2][1]), "=&v"(x[2][2]), "=&v"(x[2][3]), "=&v"(x[3][0]), "=&v"(x[3][1]),
+          "=&v"(x[3][2]), "=&v"(x[3][3])
+        : "v"(at + place(0)), "v"(at + place(1)), "v"(at + place(2)), "v"(at + place(3))
+        : "memory");
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        v[ct][t] = __builtin_bit_cast(tree_bf16x8, make_uint4(x[ct][2 * t].x, x[ct][2 * t].y, x[ct][2 * t + 1].x, x[ct][2 * t + 1].y));
   }
   // O^T += V^T P^T
   template <int TERMS>
@@ -539,21 +571,21 @@ __device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const Tr
 }
 
 // TERMS: bf16 terms that a weight is split into for the second product, 1 (bf16 result) or 3 (all 24 bits of it: fp32 result).
-// KW wavefronts take other tiles of a stage for the same queries.
-template <int QW, int KW, int NT, int TERMS, bool SEL, bool STREAM>
-__global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree_attn_kernel(
+// KW wavefronts take other tiles of a stage for the same queries, NT of them each.  With two BUFS a stage is copied while the one
+// before it is multiplied; with one that is left to the second workgroup of the CU.
+template <int QW, int KW, int NT, int BUFS, int TERMS, bool SEL, bool STREAM>
+__global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
     dsk_tree_attn_args a, int G, int q_tiles, TreeSplit sp, float scale_log2, float2* __restrict__ part_ml,
     float* __restrict__ part_acc) {
   constexpr int kThreads = QW * KW * DSK_WAVE;
   constexpr int kTiles = KW * NT, kKeys = kTreeTile * kTiles;   // of a stage
-  __shared__ __align__(16) unsigned char sm_kv[2 * kTiles * kTreeTileBytes];
+  constexpr int kBufBytes = 2 * kTiles * kTreeTileBytes;
+  __shared__ __align__(16) unsigned char sm_kv[BUFS * kBufBytes];
   __shared__ float2 sm_ml[KW > 1 ? (KW - 1) * QW * DSK_WAVE : 1];
   __shared__ uint32_t sm_bad[kTreeMixedTiles];
   static_assert(kTiles + DSK_TREE_MAX_NODES / kTreeTile + 1 <= kTreeMixedTiles, "words of sm_bad");
   __shared__ int32_t sm_rows[SEL ? kTreeMaxListed : 1];
 
-  unsigned char* const sm_k = sm_kv;
-  unsigned char* const sm_v = sm_kv + kTiles * kTreeTileBytes;
   const int split = blockIdx.x, s = blockIdx.z;
   const int hk = blockIdx.y / q_tiles, q_tile = blockIdx.y - hk * q_tiles;
   const int tid = threadIdx.x, wave = tid / DSK_WAVE;
@@ -576,8 +608,9 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree
     for (int i = 0; i < 16; ++i) O[ct][i] = 0.0f;
 
   if (tid < kTreeMixedTiles) sm_bad[tid] = 0;
-  auto tiles = [&](int t0, auto mixed) {                 // this wavefront's tiles of the stage in LDS
+  auto tiles = [&](int t0, const unsigned char* sm_k, auto mixed) {   // this wavefront's tiles of the stage in LDS
     constexpr bool kMixed = decltype(mixed)::value;
+    const unsigned char* const sm_v = sm_k + kTiles * kTreeTileBytes;
 #pragma unroll
     for (int sub = 0; sub < NT; ++sub) {
       const int tile = kw * NT + sub, tt = t0 + tile * kTreeTile;
@@ -591,11 +624,18 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree
         allow = qs.allowed(tt, keys.P);
         tree_hide(z, allow, qs.half);
       }
+      TreeVFrag vf;
+      if constexpr (BUFS > 1) {                          // during the products of K, whose results the weights wait for anyway
+        __builtin_amdgcn_sched_barrier(0);
+        vf.read_beside_copies(sm_v + tile * kTreeTileBytes);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       TreeWeights<TERMS> w;
       sm.take(z, O, w);
-      TreeVFrag vf;
-      vf.read<0>(sm_v + tile * kTreeTileBytes);
-      vf.read<1>(sm_v + tile * kTreeTileBytes);
+      if constexpr (BUFS == 1) {
+        vf.template read<0>(sm_v + tile * kTreeTileBytes);
+        vf.template read<1>(sm_v + tile * kTreeTileBytes);
+      }
       vf.add<TERMS>(O, w, 0);
       vf.add<TERMS>(O, w, 1);
       if constexpr (kMixed) tree_values_left_out(O, keys, sm_bad, allow, tt, qs.half);
@@ -604,25 +644,34 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, QW * KW <= 4 ? 2 : 1) void tree
   using Plain = std::integral_constant<bool, false>;
   using Mixed = std::integral_constant<bool, true>;
   int t0 = keys.t_begin;
-  for (; keys.plain(t0) && t0 < keys.t_end; t0 += kKeys) {   // the prefix: nothing is masked
-    keys.copy_plain(t0, sm_k, sm_v);
+  // stages of the prefix alone: nothing is masked
+  auto some = [&](int t) { return keys.plain(t) && t < keys.t_end; };
+  auto copy = [&](int t, unsigned char* to) { keys.copy_plain(t, to, to + kTiles * kTreeTileBytes); };
+  unsigned char *here = sm_kv, *other = sm_kv + (BUFS - 1) * kBufBytes;
+  if (BUFS > 1 && some(t0)) copy(t0, here);
+  for (; some(t0); t0 += kKeys) {
+    if (BUFS == 1) copy(t0, here);
     lds_copies_done();
-    __syncthreads();
-    if (qs.busy) tiles(t0, Plain());
-    __syncthreads();
+    __syncthreads();                                     // the stage is here, and nobody reads the other one any more
+    if (BUFS > 1 && some(t0 + kKeys)) copy(t0 + kKeys, other);
+    if (qs.busy) tiles(t0, here, Plain());
+    if (BUFS == 1) __syncthreads();
+    unsigned char* const read = here;
+    here = other;
+    other = read;
   }
-  if (t0 == keys.t_begin) __syncthreads();               // sm_bad
+  if (BUFS > 1 || t0 == keys.t_begin) __syncthreads();   // (the latter: sm_bad)
   for (; t0 < keys.t_end; t0 += kKeys) {                 // its end and the nodes
     typename decltype(keys)::Regs x;
     keys.fetch_mixed(x, t0);
-    keys.template put<true>(x, t0, sm_k, sm_v, sm_bad);
+    keys.template put<true>(x, t0, sm_kv, sm_kv + kTiles * kTreeTileBytes, sm_bad);
     __syncthreads();
-    if (qs.busy) tiles(t0, Mixed());
+    if (qs.busy) tiles(t0, sm_kv, Mixed());
     __syncthreads();
   }
   sm.l += shfl_xor_f(sm.l, 32);
   if constexpr (KW > 1) {
-    static_assert((KW - 1) * QW <= kTiles, "a block is as large as a tile of K and V");
+    static_assert((KW - 1) * QW <= BUFS * kTiles, "a block is as large as a tile of K and V");
     tree_join<QW, KW>(sm, O, qs.busy, qw, kw, reinterpret_cast<float*>(sm_kv), sm_ml);
     if (kw > 0) return;
   }
@@ -800,16 +849,19 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
   tree_store(a, qs, O, sm.m, sm.l, used, sp.nsplit, split, part_ml, part_acc);
 }
 
-// The parts of a row put together in order: a wavefront a row, two channels a lane.  `used` as in the kernel above.
+// The parts of a row put together in order: WAVES wavefronts a row, two channels a lane.  `used` as in the kernel above.
 constexpr int kTreeMergeWaves = 4;
-constexpr int kTreeMergeBatch = 8;             // partials on their way at once
+constexpr int kTreeMergeBatch = 8;             // partials of a wavefront on their way at once
+// Parts from which on a row has all four: 64 parts of 16 rows 5.5 us less, 33 of 512 rows 1.9, 32 of 2048 none
+constexpr int kTreeMergeMany = 16;
 
-template <bool SEL>
+template <bool SEL, int WAVES>
 __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
     dsk_tree_attn_args a, int G, TreeSplit sp, const float2* __restrict__ part_ml,
     const float* __restrict__ part_acc) {
-  const int s = blockIdx.y, lane = threadIdx.x & (DSK_WAVE - 1);
-  const int item = blockIdx.x * kTreeMergeWaves + threadIdx.x / DSK_WAVE;
+  constexpr int kRows = kTreeMergeWaves / WAVES;
+  const int s = blockIdx.y, lane = threadIdx.x & (DSK_WAVE - 1), wave = threadIdx.x / DSK_WAVE;
+  const int item = blockIdx.x * kRows + wave / WAVES;
   const int node = item / a.Hq, h = item - node * a.Hq;
   const TreePlace at(a, s);
   if (node >= at.n) return;
@@ -822,7 +874,7 @@ __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
   for (int c = lane; c < used; c += DSK_WAVE) M = fmaxf(M, ml[c].x);
   M = wave_max(M);
   float2 o = make_float2(0.0f, 0.0f);
-  for (int c0 = 0; c0 < used; c0 += kTreeMergeBatch) {
+  for (int c0 = wave % WAVES * kTreeMergeBatch; c0 < used; c0 += WAVES * kTreeMergeBatch) {
     float2 x[kTreeMergeBatch], v[kTreeMergeBatch];
 #pragma unroll
     for (int u = 0; u < kTreeMergeBatch; ++u) {
@@ -837,6 +889,23 @@ __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
       l = fmaf(v[u].y, f, l);
       o.x = fmaf(x[u].x, f, o.x);
       o.y = fmaf(x[u].y, f, o.y);
+    }
+  }
+  if constexpr (WAVES > 1) {
+    static_assert(kRows == 1, "all wavefronts of a workgroup have the same row, or none");
+    __shared__ float sm_part[WAVES - 1][3][DSK_WAVE];
+    if (wave > 0) {
+      sm_part[wave - 1][0][lane] = o.x;
+      sm_part[wave - 1][1][lane] = o.y;
+      sm_part[wave - 1][2][lane] = l;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; ++w) {
+      o.x += sm_part[w][0][lane];
+      o.y += sm_part[w][1][lane];
+      l += sm_part[w][2][lane];
     }
   }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
@@ -857,6 +926,7 @@ constexpr int64_t kTreeStreamBytes = 288ll << 20;
 struct TreeLaunch {
   TreeSplit sp;
   int q_waves;        // QW
+  bool deep;          // tree_attn_kernel with eight wavefronts
   bool wide;          // tree_wide_kernel
   bool stream;        // K and V are read past the memory-side cache
   int q_tiles;        // passes over a (sequence, KV head)'s keys
@@ -866,8 +936,9 @@ struct TreeLaunch {
 // Keys of a workgroup from which on the kernel for many rows gains (its first and last steps are slower): 256 rows, 2K tokens
 // (256 keys) 25.9 us with it and 21.4 without, 8 x 2K (768) 50 and 59, 32K (1056) 62.6 and 70.8, 128K (4224) 192 and 207.
 constexpr int kTreeWideKeys = 512;
+constexpr int kTreeLeastKeys = 256;            // of any: a shorter part costs more in partial results than it saves
 
-constexpr int kTreeFewWorkgroups = 128;        // of 256 CUs
+constexpr int kTreeCus = 256;
 
 static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   constexpr int stage = 128;                             // a multiple of the keys that the kernels take at once
@@ -886,32 +957,38 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     int64_t parts = want / heads - (a.B - 1);            // a sequence's last part is a shorter one: room for one of each
     parts = parts > 1 ? parts : 1;
     int64_t per = (keys + parts - 1) / parts;
-    const int64_t least = 256, fewest = (longest + kTreeMaxSplit - 1) / kTreeMaxSplit;
-    per = per > least ? per : least;
+    const int64_t fewest = (longest + kTreeMaxSplit - 1) / kTreeMaxSplit;
+    per = per > kTreeLeastKeys ? per : kTreeLeastKeys;
     per = per > fewest ? per : fewest;
     return (per + stage - 1) / stage * stage;
   };
   t.sp.keys_per_split = t.sp.slots_per_split = 0;
-  t.wide = t.stream = false;
+  t.deep = t.wide = t.stream = false;
   if (!sel) {
     if (rows > 128 && !f32) {
       rows_of(kWideWaves);
-      t.sp.keys_per_split = (int)keys_of(256);           // one a CU
+      t.sp.keys_per_split = (int)keys_of(kTreeCus);
       t.wide = t.sp.keys_per_split >= kTreeWideKeys;
     }
     if (!t.wide) {
       rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
       // Two a CU, and three for every two that fit where sequences differ in length (8 sequences of 16K to 64K tokens 305 us with
       // 512, 288 with 768; one of 128K, 40 heads 421 and 427).
-      t.sp.keys_per_split = (int)keys_of(a.B > 1 ? 768 : 512);
+      t.sp.keys_per_split = (int)keys_of(a.B > 1 ? 3 * kTreeCus : 2 * kTreeCus);
+      // One sequence that gives every CU a workgroup: one of eight wavefronts a CU, which halves the partial results.  32 / 8
+      // heads, 16 nodes: 8K tokens 23.8 -> 21.6 us, 32K 39.5 -> 36.6, 128K 104.7 -> 99.9; fp32 32K 44.3 -> 40.8; 32 nodes: 32K
+      // 50.6 -> 44.6; 4K (136 workgroups) 17.1 and 18.6.  Sequences of several lengths need the finer grain (8 of 16K to 64K
+      // tokens 282 and 312 us).
+      t.deep = a.B == 1 && t.q_waves > 1 && keys * a.Hkv * t.q_tiles >= (int64_t)kTreeCus * kTreeLeastKeys;
+      if (t.deep) t.sp.keys_per_split = (int)keys_of(kTreeCus);
     }
     t.sp.nsplit = (int)(((int64_t)a.max_seqlen + a.max_nodes + t.sp.keys_per_split - 1) / t.sp.keys_per_split);
     t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
   } else {
     rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
     const int64_t slots = (int64_t)a.k * a.B * a.Hkv * t.q_tiles;
-    // at least 256 tokens (32 nodes, 4 heads a group, 4096 tokens: 26.2 us with 128, 23.6 with 256, 27.6 with 512)
-    const int64_t least = (256 + a.b - 1) / a.b, most = kTreeMaxListed / a.b < kTreeMaxSlots ? kTreeMaxListed / a.b : kTreeMaxSlots;
+    // (32 nodes, 4 heads a group, 4096 tokens: 26.2 us with at least 128 tokens, 23.6 with 256, 27.6 with 512)
+    const int64_t least = (kTreeLeastKeys + a.b - 1) / a.b, most = kTreeMaxListed / a.b < kTreeMaxSlots ? kTreeMaxListed / a.b : kTreeMaxSlots;
     int64_t per = (slots + 511) / 512;
     per = per > least ? per : least;
     per = per < most ? per : most;
@@ -923,7 +1000,7 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   // selection of 4K tokens (128 workgroups) 23.6 -> 20.9 us, of 2K 20.9 -> 18.0, a prefix of 600 tokens 16.0 -> 14.4; 4K tokens
   // (136 workgroups) would take 21.8 instead of 20.6.  (Halving two wavefronts' rows again gains nothing: 600 tokens 13.9 and
   // 14.1.)
-  if (!t.wide && t.q_waves == 4 && (int64_t)a.B * a.Hkv * t.q_tiles * t.sp.nsplit <= kTreeFewWorkgroups) rows_of(2);
+  if (!t.wide && t.q_waves == 4 && (int64_t)a.B * a.Hkv * t.q_tiles * t.sp.nsplit <= kTreeCus / 2) rows_of(2);
   const size_t parts = t.sp.nsplit > 1 ? (size_t)a.n_tokens * a.Hq * t.sp.nsplit : 0;
   t.part_acc = align_up(parts * sizeof(float2));
   t.total = t.part_acc + align_up(parts * DSK_HEAD_DIM * sizeof(float));
@@ -937,18 +1014,19 @@ size_t tree_ws_bytes(const dsk_tree_attn_args& a) {
   return f32 > bf16 ? f32 : bf16;
 }
 
-template <int QW, int KW, int NT>
+template <int QW, int KW, int NT, int BUFS, bool MAY_SELECT>
 static void launch_tree(const dsk_tree_attn_args& a, const TreeLaunch& t, float scale_log2, float2* ml, float* acc, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
   const dim3 grid((unsigned)t.sp.nsplit, (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(QW * KW * DSK_WAVE);
 #define DSK_TREE(terms)                                                                                                        \
   do {                                                                                                                         \
-    if (a.sel_start != nullptr)                                                                                                \
-      tree_attn_kernel<QW, KW, NT, terms, true, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);    \
+    if (MAY_SELECT && a.sel_start != nullptr)                                                                                  \
+      tree_attn_kernel<QW, KW, NT, BUFS, terms, MAY_SELECT, false>                                                             \
+          <<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);                                                \
     else if (t.stream)                                                                                                         \
-      tree_attn_kernel<QW, KW, NT, terms, false, true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);    \
+      tree_attn_kernel<QW, KW, NT, BUFS, terms, false, true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc); \
     else                                                                                                                       \
-      tree_attn_kernel<QW, KW, NT, terms, false, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);   \
+      tree_attn_kernel<QW, KW, NT, BUFS, terms, false, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc); \
   } while (0)
   if (a.out != nullptr) DSK_TREE(3);
   else DSK_TREE(1);
@@ -968,18 +1046,26 @@ hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st) {
     if (t.stream) tree_wide_kernel<true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
     else tree_wide_kernel<false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
   } else if (t.q_waves == 1) {
-    launch_tree<1, 4, 1>(a, t, scale_log2, ml, acc, st);
+    launch_tree<1, 4, 1, 1, true>(a, t, scale_log2, ml, acc, st);
   } else if (t.q_waves == 2) {
-    launch_tree<2, 2, 2>(a, t, scale_log2, ml, acc, st);
+    if (t.deep) launch_tree<2, 4, 1, 2, false>(a, t, scale_log2, ml, acc, st);
+    else launch_tree<2, 2, 1, 2, true>(a, t, scale_log2, ml, acc, st);
   } else {
-    launch_tree<4, 1, 4>(a, t, scale_log2, ml, acc, st);
+    if (t.deep) launch_tree<4, 2, 2, 2, false>(a, t, scale_log2, ml, acc, st);
+    else launch_tree<4, 1, 2, 2, true>(a, t, scale_log2, ml, acc, st);
   }
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || t.sp.nsplit <= 1) return err;
-  const dim3 grid((unsigned)((a.max_nodes * a.Hq + kTreeMergeWaves - 1) / kTreeMergeWaves), (unsigned)a.B);
-  const dim3 block(kTreeMergeWaves * DSK_WAVE);
-  if (a.sel_start != nullptr) tree_merge_kernel<true><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
-  else tree_merge_kernel<false><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
+  const bool many = t.sp.nsplit >= kTreeMergeMany;
+  const int rows = a.max_nodes * a.Hq, rows_per_wg = many ? 1 : kTreeMergeWaves;
+  const dim3 grid((unsigned)((rows + rows_per_wg - 1) / rows_per_wg), (unsigned)a.B), block(kTreeMergeWaves * DSK_WAVE);
+  if (a.sel_start != nullptr) {
+    if (many) tree_merge_kernel<true, kTreeMergeWaves><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
+    else tree_merge_kernel<true, 1><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
+  } else {
+    if (many) tree_merge_kernel<false, kTreeMergeWaves><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
+    else tree_merge_kernel<false, 1><<<grid, block, 0, st>>>(a, G, t.sp, ml, acc);
+  }
   return hipGetLastError();
 }
 

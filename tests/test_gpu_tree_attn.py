@@ -410,3 +410,33 @@ def test_a_token_of_several_slots_counts_as_often():
     for x in c.sel[:2]:
         x[0, :, 1], x[0, :, 4] = x[0, :, 0], x[0, :, 3]
     c.check()
+
+
+# ---- one sequence that gives every CU a workgroup of eight wavefronts, and many parts of a row -------------------
+@pytest.mark.parametrize("end", [9000, 9216 - 30, 9216 - 1, 9216, 9216 + 1, 9216 + 63, 9216 + 65, 9216 + 127, 20001])
+@pytest.mark.parametrize("nodes, packed", [(13, False), (30, True)])
+def test_one_long_sequence(end, nodes, packed):
+    Case([end], [nodes], 32, 8, seed=end, packed=packed, nhd=not packed, pad_tokens=1).check()
+
+
+@pytest.mark.parametrize("nodes", [14, 31])
+def test_one_long_sequence_any_mask_and_rows_that_hold_anything(nodes):
+    c = Case([10007], [nodes], 32, 8, masks="any", seed=nodes)
+    c.check()
+    clean = c.run(want_bf16=True)
+    j = nodes - 2
+    blind = torch.from_numpy(~c.seen[0][:, j]).cuda()
+    for x in (c.K, c.V):
+        x[:, c.lens[0] + j, ::3] = float("nan")
+        x[:, c.lens[0] + j, 1::3] = float("inf")
+        x[:, c.lens[0] + nodes:] = float("nan")
+    r = c.run(want_bf16=True)
+    for a, b in ((r.out, clean.out), (r.out_bf16, clean.out_bf16), (r.lse, clean.lse)):
+        assert torch.equal(a[blind], b[blind])
+    assert bool(r.out[~blind].isnan().any(-1).all())
+
+
+@pytest.mark.parametrize("Hq, Hkv, nodes", [(4, 1, 1), (4, 1, 16), (8, 1, 16), (8, 1, 33), (5, 1, 9)])
+@pytest.mark.parametrize("lens", [[65537], [33000, 20, 32999]])
+def test_one_head_in_many_parts(Hq, Hkv, nodes, lens):
+    Case(lens, [nodes] * len(lens), Hq, Hkv, seed=nodes).check()
