@@ -933,9 +933,11 @@ struct TreeLaunch {
   size_t part_acc, total;
 };
 
-// Keys of a workgroup from which on the kernel for many rows gains (its first and last steps are slower): 256 rows, 2K tokens
-// (256 keys) 25.9 us with it and 21.4 without, 8 x 2K (768) 50 and 59, 32K (1056) 62.6 and 70.8, 128K (4224) 192 and 207.
-constexpr int kTreeWideKeys = 512;
+// Keys of a workgroup from which on the kernel for many rows gains (its first and last steps are slower), where the other has eight
+// wavefronts a CU (one sequence) and where it has not.  32 / 8 heads: 64 nodes, 16K tokens (640 keys) 44.4 us with it and 40.6
+// without, 32K (1152) 68.4 and 67.6, 128K (4224) 192 and 214; 40 nodes, 128K 170 and 176; 64 / 8 heads, 64 nodes, 32K (2176) 102.4
+// and 105.9.  8 sequences of 2K, 64 nodes (768) 50.3 and 59.4, of 8K, 40 nodes 110.5 and 126; 64 nodes, 2K (256) 25.7 and 20.3.
+constexpr int kTreeWideKeysOne = 2048, kTreeWideKeys = 512;
 constexpr int kTreeLeastKeys = 256;            // of any: a shorter part costs more in partial results than it saves
 
 constexpr int kTreeCus = 256;
@@ -968,7 +970,7 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     if (rows > 128 && !f32) {
       rows_of(kWideWaves);
       t.sp.keys_per_split = (int)keys_of(kTreeCus);
-      t.wide = t.sp.keys_per_split >= kTreeWideKeys;
+      t.wide = t.sp.keys_per_split >= (a.B > 1 ? kTreeWideKeys : kTreeWideKeysOne);
     }
     if (!t.wide) {
       rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));

@@ -296,13 +296,16 @@ def test_one_node_equals_the_decode_attention():
     assert float((r.out - den.out).abs().max()) <= 1e-5 and float((r.lse - den.lse).abs().max()) <= 1e-5
 
 
-# ---- the kernel for many rows (bf16 results, more than 128 rows, at least 512 keys a workgroup) ------------------
+# ---- more than 128 rows and their kernel (bf16 results, from 512 keys a workgroup on, 2048 for one sequence alone) ---
 @pytest.mark.parametrize("lens, n_new, Hq, Hkv", [
     ([20000], [64], 32, 8),                                      # every wavefront has rows
     ([20033], [33], 40, 8),                                      # 165 rows: two wavefronts have none, one has five
     ([30000, 0, 21, 29999], [64, 64, 3, 40], 32, 8),             # an empty prefix, a short one, fewer nodes than announced
     ([70001, 4096], [256, 1], 8, 4),                             # 512 rows: two passes
     ([34100], [100], 32, 16),
+    ([66000], [64], 32, 8),
+    ([65999], [40], 40, 8),
+    ([131100], [200], 8, 4),
 ])
 @pytest.mark.parametrize("packed", [False, True])
 def test_many_rows_over_long_contexts(lens, n_new, Hq, Hkv, packed):
@@ -440,3 +443,27 @@ def test_one_long_sequence_any_mask_and_rows_that_hold_anything(nodes):
 @pytest.mark.parametrize("lens", [[65537], [33000, 20, 32999]])
 def test_one_head_in_many_parts(Hq, Hkv, nodes, lens):
     Case(lens, [nodes] * len(lens), Hq, Hkv, seed=nodes).check()
+
+
+@pytest.mark.parametrize("end", list(range(20480 - 3, 20480 + 3)) + [20480 + 31, 20480 + 33, 20480 + 64, 20480 + 127])
+def test_many_rows_of_two_sequences_where_the_prefix_ends_in_any_place_of_a_step(end):
+    Case([end, 3], [40, 2], 32, 8, seed=end).check()
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_many_rows_of_two_sequences_masked_rows_may_hold_anything(packed):
+    c = Case([20017, 3], [64, 1], 32, 8, seed=41, packed=packed)
+    bf16 = dict(want_f32=False, want_bf16=True)
+    clean = c.run(**bf16)
+    for j in (1, 14, 15, 30, 47, 63):
+        blind = torch.from_numpy(np.append(~c.seen[0][:, j], True)).cuda()
+        X, at = ((c.Kd, c.Vd), j) if packed else ((c.K, c.V), c.lens[0] + j)
+        old = [x[:, at].clone() for x in X]
+        for x in X:
+            x[:, at, ::3] = float("nan")
+            x[:, at, 1::3] = float("inf")
+        r = c.run(**bf16)
+        assert torch.equal(r.out_bf16[blind], clean.out_bf16[blind]) and torch.equal(r.lse[blind], clean.lse[blind])
+        assert bool(r.out_bf16[~blind].isnan().any(-1).all())
+        for x, o in zip(X, old):
+            x[:, at] = o
