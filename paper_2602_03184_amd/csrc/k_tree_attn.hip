@@ -929,6 +929,7 @@ struct TreeLaunch {
   bool deep;          // tree_attn_kernel with eight wavefronts
   bool wide;          // tree_wide_kernel
   bool stream;        // K and V are read past the memory-side cache
+  bool odd;           // an odd number of parts is launched
   int q_tiles;        // passes over a (sequence, KV head)'s keys
   size_t part_acc, total;
 };
@@ -946,8 +947,10 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   constexpr int stage = 128;                             // a multiple of the keys that the kernels take at once
   const int rows = a.max_nodes * (a.Hq / a.Hkv);
   const bool sel = a.sel_start != nullptr;
-  int64_t keys = (int64_t)a.B * a.max_seqlen;
-  keys = (keys < a.total_rows ? keys : a.total_rows) + (int64_t)a.B * a.max_nodes;
+  const int64_t longest = (int64_t)a.max_seqlen + a.max_nodes;
+  // the cache has no room for all sequences at max_seqlen: they differ in length
+  const bool ragged = a.total_rows < (int64_t)a.B * a.max_seqlen;
+  const int64_t keys = (ragged ? a.total_rows : (int64_t)a.B * a.max_seqlen) + (int64_t)a.B * a.max_nodes;
   TreeLaunch t;
   auto rows_of = [&](int q_waves) {
     t.q_waves = q_waves;
@@ -955,17 +958,18 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   };
   // parts of `want` workgroups in all: keys of one
   auto keys_of = [&](int64_t want) {
-    const int64_t heads = (int64_t)a.Hkv * t.q_tiles, longest = (int64_t)a.max_seqlen + a.max_nodes;
-    int64_t parts = want / heads - (a.B - 1);            // a sequence's last part is a shorter one: room for one of each
+    const int64_t heads = (int64_t)a.Hkv * t.q_tiles;
+    // of all sequences together, the last of each a shorter one, which leaves room for one of each; or of each
+    int64_t parts = ragged ? want / heads - (a.B - 1) : want / (heads * a.B);
     parts = parts > 1 ? parts : 1;
-    int64_t per = (keys + parts - 1) / parts;
+    int64_t per = ((ragged ? keys : longest) + parts - 1) / parts;
     const int64_t fewest = (longest + kTreeMaxSplit - 1) / kTreeMaxSplit;
     per = per > kTreeLeastKeys ? per : kTreeLeastKeys;
     per = per > fewest ? per : fewest;
     return (per + stage - 1) / stage * stage;
   };
   t.sp.keys_per_split = t.sp.slots_per_split = 0;
-  t.deep = t.wide = t.stream = false;
+  t.deep = t.wide = t.stream = t.odd = false;
   if (!sel) {
     if (rows > 128 && !f32) {
       rows_of(kWideWaves);
@@ -974,9 +978,10 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     }
     if (!t.wide) {
       rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
-      // Two a CU, and three for every two that fit where sequences differ in length (8 sequences of 16K to 64K tokens 305 us with
-      // 512, 288 with 768; one of 128K, 40 heads 421 and 427).
-      t.sp.keys_per_split = (int)keys_of(a.B > 1 ? 3 * kTreeCus : 2 * kTreeCus);
+      // Two a CU, all there at once; three for every two that fit where sequences are known to differ in length (8 of 16K to 64K
+      // tokens, 13 nodes: 283 us with 512, 271 with 768, 268 with 1024; 4 of up to 32K, 16 nodes: 92, 84, 93; 16 of up to 16K, 8
+      // nodes: 132, 146, 141).
+      t.sp.keys_per_split = (int)keys_of(ragged ? 3 * kTreeCus : 2 * kTreeCus);
       // One sequence that gives every CU a workgroup: one of eight wavefronts a CU, which halves the partial results.  32 / 8
       // heads, 16 nodes: 8K tokens 23.8 -> 21.6 us, 32K 39.5 -> 36.6, 128K 104.7 -> 99.9; fp32 32K 44.3 -> 40.8; 32 nodes: 32K
       // 50.6 -> 44.6; 4K (136 workgroups) 17.1 and 18.6.  Sequences of several lengths need the finer grain (8 of 16K to 64K
@@ -985,6 +990,11 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
       if (t.deep) t.sp.keys_per_split = (int)keys_of(kTreeCus);
     }
     t.sp.nsplit = (int)(((int64_t)a.max_seqlen + a.max_nodes + t.sp.keys_per_split - 1) / t.sp.keys_per_split);
+    // Workgroups go round the eight XCDs by their number, and those of parts that a shorter sequence lacks end at once: an odd
+    // number of parts begins every sequence and head on another XCD, where a multiple of eight would leave the last ones of all
+    // with less to do (the 8 sequences above 280 -> 267 us).  Not where an XCD's L2 serves several passes over the same keys, nor
+    // with one workgroup a CU (eight wavefronts: 113 -> 122 us).
+    t.odd = a.B > 1 && t.q_tiles == 1 && !t.wide;
     t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
   } else {
     rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
@@ -1019,7 +1029,7 @@ size_t tree_ws_bytes(const dsk_tree_attn_args& a) {
 template <int QW, int KW, int NT, int BUFS, bool MAY_SELECT>
 static void launch_tree(const dsk_tree_attn_args& a, const TreeLaunch& t, float scale_log2, float2* ml, float* acc, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
-  const dim3 grid((unsigned)t.sp.nsplit, (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(QW * KW * DSK_WAVE);
+  const dim3 grid((unsigned)t.sp.nsplit | (t.odd ? 1u : 0u), (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(QW * KW * DSK_WAVE);
 #define DSK_TREE(terms)                                                                                                        \
   do {                                                                                                                         \
     if (MAY_SELECT && a.sel_start != nullptr)                                                                                  \
