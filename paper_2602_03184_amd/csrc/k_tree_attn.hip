@@ -966,6 +966,7 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     const int64_t fewest = (longest + kTreeMaxSplit - 1) / kTreeMaxSplit;
     per = per > kTreeLeastKeys ? per : kTreeLeastKeys;
     per = per > fewest ? per : fewest;
+    per = per < longest ? per : longest;                 // (of more sequences than workgroups)
     return (per + stage - 1) / stage * stage;
   };
   t.sp.keys_per_split = t.sp.slots_per_split = 0;

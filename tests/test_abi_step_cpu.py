@@ -114,6 +114,10 @@ def _tree(dsk):
 
 def test_tree_attention_refuses(dsk):
     assert dsk.dsk_tree_attn_workspace_bytes(_tree(dsk)) >= 256
+    a = _tree(dsk)
+    a.sel_start = a.sel_len = a.sel_count = None
+    a.B, a.total_rows, a.max_seqlen = 65535, 0x7FFFFFFF, 0x7FFF0000      # more sequences than workgroups: a part each
+    assert dsk.dsk_tree_attn_workspace_bytes(a) == 256
     cases = [("struct_size", 8, dsk.DSK_ERR_VERSION), ("D", 64, dsk.DSK_ERR_SHAPE), ("B", 0, dsk.DSK_ERR_SHAPE),
              ("Hkv", 3, dsk.DSK_ERR_SHAPE), ("n_tokens", -1, dsk.DSK_ERR_SHAPE), ("max_seqlen", -1, dsk.DSK_ERR_SHAPE),
              ("total_rows", -1, dsk.DSK_ERR_SHAPE), ("max_nodes", 0, dsk.DSK_ERR_PARAM), ("max_nodes", 257, dsk.DSK_ERR_PARAM),

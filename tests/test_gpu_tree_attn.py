@@ -467,3 +467,15 @@ def test_many_rows_of_two_sequences_masked_rows_may_hold_anything(packed):
         assert bool(r.out_bf16[~blind].isnan().any(-1).all())
         for x, o in zip(X, old):
             x[:, at] = o
+
+
+def test_more_sequences_than_workgroups_and_the_largest_bounds():
+    """Bounds as large as they may be (nothing lies there): 100 sequences of a part each, 2^31 keys and more in all."""
+    c = Case([5 + s % 3 for s in range(100)], [2] * 100, 8, 8, seed=51)
+    r = _dsk().make_tree_attn_args(c.q, c.K, c.V, **c.kwargs(max_seqlen=0x7FFF0000))
+    r.args.total_rows = 0x7FFFFFFF
+    assert _dsk().dsk_tree_attn_workspace_bytes(r.args) <= r.args.workspace_bytes
+    _dsk().dsk_tree_decode_attn(r.args)
+    torch.cuda.synchronize()
+    out, size, _ = c.reference()
+    assert bool(((r.out.double() - out).abs() <= F32 * size).all())
