@@ -557,7 +557,7 @@ __device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const Tr
         if (a.out_bf16 != nullptr)
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out_bf16) + at) = make_uint2(tree_pack(x.x, x.y), tree_pack(x.z, x.w));
       }
-    if (qs.half == 0 && a.lse != nullptr) a.lse[qs.out_row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -__builtin_inff();
+    if (qs.half == 0 && a.lse != nullptr) a.lse[qs.out_row] = l == 0.0f ? -__builtin_inff() : (m + log2f(l)) * kLn2;   // a NaN stays one
   } else {
     const int64_t part = qs.out_row * nsplit + split;
 #pragma unroll
@@ -884,7 +884,7 @@ __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
     }
 #pragma unroll
     for (int u = 0; u < kTreeMergeBatch; ++u) {
-      if (c0 + u >= used || v[u].x == -__builtin_inff()) continue;
+      if (c0 + u >= used || v[u].y == 0.0f) continue;    // (not by the maximum: where every logit is NaN it is -inf)
       const float f = exp2_small(v[u].x - M);
       l = fmaf(v[u].y, f, l);
       o.x = fmaf(x[u].x, f, o.x);
@@ -914,7 +914,7 @@ __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
   if (a.out != nullptr) *reinterpret_cast<float2*>(a.out + row * DSK_HEAD_DIM + 2 * lane) = o;
   if (a.out_bf16 != nullptr)
     *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out_bf16) + row * DSK_HEAD_DIM + 2 * lane) = tree_pack(o.x, o.y);
-  if (lane == 0 && a.lse != nullptr) a.lse[row] = l > 0.0f ? (M + log2f(l)) * kLn2 : -__builtin_inff();
+  if (lane == 0 && a.lse != nullptr) a.lse[row] = l == 0.0f ? -__builtin_inff() : (M + log2f(l)) * kLn2;
 }
 
 // K and V larger than the memory-side cache are hardly found there again by the next step, so they are read past it (one pass

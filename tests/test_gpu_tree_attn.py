@@ -479,3 +479,18 @@ def test_more_sequences_than_workgroups_and_the_largest_bounds():
     torch.cuda.synchronize()
     out, size, _ = c.reference()
     assert bool(((r.out.double() - out).abs() <= F32 * size).all())
+
+
+@pytest.mark.parametrize("lens, Hq, Hkv, nodes", [([40], 8, 2, 5), ([3000], 8, 2, 5), ([20000, 3], 32, 8, 40), ([9000], 32, 8, 30)])
+def test_a_query_that_is_not_a_number_gets_none(lens, Hq, Hkv, nodes):
+    c = Case(lens, [nodes] + [1] * (len(lens) - 1), Hq, Hkv, seed=61)
+    for kw in ({}, dict(want_f32=False, want_bf16=True)):
+        clean = c.run(**kw)
+        c.q[2, 1] = float("nan")
+        r = c.run(**kw)
+        out, want = (x.out if x.out is not None else x.out_bf16 for x in (r, clean))
+        hit = torch.zeros(c.N, Hq, dtype=torch.bool, device="cuda")
+        hit[2, 1] = True
+        assert bool(out[hit].isnan().all()) and bool(r.lse[hit].isnan().all())
+        assert torch.equal(out[~hit], want[~hit]) and torch.equal(r.lse[~hit], clean.lse[~hit])
+        c.q[2, 1] = 1.0
