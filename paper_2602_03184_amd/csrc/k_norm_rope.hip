@@ -3,6 +3,8 @@
 // 16 lanes x 8 channels, as everywhere in the library; a wavefront takes rows of one token, four at a time, so that it makes
 // the token's angles once: a lane each, in 64 bits (an angle of position 131071 has 17 bits before the point), handed round
 // through LDS.
+// 32K tokens of 32 / 8 heads (805 MB) 143 to 156 us, 5.2 to 5.6 TB/s, a large copy's rate; 14K tokens of 40 / 40 heads (875 MB)
+// 184 to 190 us, whatever part is rotated and how; eight tokens 3.6 us.
 #include "dsk_common.hpp"
 #include "dsk_internal.hpp"
 
@@ -130,6 +132,8 @@ __global__ __launch_bounds__(kRopeThreads) void norm_rope_kernel(dsk_norm_rope_a
 hipError_t launch_norm_rope(const dsk_norm_rope_args& a, hipStream_t st) {
   const int rows = (a.q != nullptr ? a.Hq : 0) + (a.k != nullptr ? a.Hkv : 0) + (a.v != nullptr ? a.Hkv : 0);
   const int quads = (rows + 3) / 4;
+  // A wavefront takes all heads of a token and makes its angles once, but where that leaves too few wavefronts (16 a CU) it
+  // takes fewer: what bounds those calls is latency, and the angles are made in all of them at the same time.
   int per_wave = quads;
   while (per_wave > 1 && (int64_t)a.n_tokens * ((quads + per_wave - 1) / per_wave) < 4096) per_wave = (per_wave + 1) / 2;
   const int waves = (quads + per_wave - 1) / per_wave;

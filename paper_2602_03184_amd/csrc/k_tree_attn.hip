@@ -572,7 +572,10 @@ __device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const Tr
 
 // TERMS: bf16 terms that a weight is split into for the second product, 1 (bf16 result) or 3 (all 24 bits of it: fp32 result).
 // KW wavefronts take other tiles of a stage for the same queries, NT of them each.  With two BUFS a stage is copied while the one
-// before it is multiplied; with one that is left to the second workgroup of the CU.
+// before it is multiplied; with one (32 rows, whose products are short) that is left to the second workgroup of the CU.
+// HBM bounds it: 40 / 40 heads, 128K tokens, 16 nodes (2.68 GB) 396 us, 6.8 TB/s; 32 / 8 heads, 16 nodes (0.54 GB) 88, 6.1; eight of
+// 16K to 64K, 13 nodes, token-major (1.48 GB) 260 to 277, 5.4 to 5.7.  Where 4 wavefronts take 128 rows, their matrix instructions
+// and exponentials, about as many cycles each, no longer hide entirely: 32 nodes, 0.54 GB at 5.0 TB/s.
 template <int QW, int KW, int NT, int BUFS, int TERMS, bool SEL, bool STREAM>
 __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
     dsk_tree_attn_args a, int G, int q_tiles, TreeSplit sp, float scale_log2, float2* __restrict__ part_ml,
@@ -685,6 +688,9 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
 // Steps go round four LDS buffers.  In the softmax slot of step i the first group puts its half of step i + 1 (slot 2 i + 1),
 // the second its half of step i + 2 (slot 2 i + 2), so a step is whole one slot before its first use, and the step that it
 // replaces was last read long before.  Loads are issued 64 KB before they are put.
+// 32 / 8 heads, 64 nodes, 128K tokens: 137 GFLOP in 154 us while the chip is cool (0.89 PFLOP/s; a large library product reaches
+// 1.15), 190 without pause: a slot of a SIMD has 512 cycles of products next to 490 to 600 of exponentials, and the clock goes
+// down to what power leaves.  Taking tiles one after the other in every wavefront took 212.
 constexpr int kWideWaves = 8;
 
 template <bool STREAM>
@@ -849,7 +855,9 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
   tree_store(a, qs, O, sm.m, sm.l, used, sp.nsplit, split, part_ml, part_acc);
 }
 
-// The parts of a row put together in order: WAVES wavefronts a row, two channels a lane.  `used` as in the kernel above.
+// The parts of a row put together in order.  2048 rows of 32 parts (34 MB, L2 and memory-side cache) 8.4 to 11.8 us, 1024 of 16
+// 4.2, the least 3.0 to 3.8: launch, lengths, maxima, partials, a round trip each.
+// WAVES wavefronts a row, two channels a lane.  `used` as in the kernel above.
 constexpr int kTreeMergeWaves = 4;
 constexpr int kTreeMergeBatch = 8;             // partials of a wavefront on their way at once
 // Parts from which on a row has all four: 64 parts of 16 rows 5.5 us less, 33 of 512 rows 1.9, 32 of 2048 none
