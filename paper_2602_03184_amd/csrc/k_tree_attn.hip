@@ -101,6 +101,7 @@ struct TreeMask {
 struct TreeSplit {
   int nsplit, keys_per_split;   // parts of a sequence and their keys (a selection: tokens)
   int slots_per_split;          // with a selection
+  bool packed;                  // workgroups are numbered through the parts that there are, not by sequence
 };
 
 // What a sequence has in fact, malformed tables cut to the bounds that the host knows.
@@ -131,6 +132,41 @@ struct TreePlace {
     }
     u = u > 0 ? u : 1;                                   // the nodes go with the last slots
     return (int)(u < sp.nsplit ? u : sp.nsplit);         // (never more: the host counts max_seqlen + max_nodes keys)
+  }
+};
+
+// The p-th part of all sequences', those of a sequence one after the other; false: there are fewer.  Every wavefront for itself.
+__device__ __forceinline__ bool tree_find(const dsk_tree_attn_args& a, const TreeSplit& sp, int p, int& s, int& split) {
+  const int lane = threadIdx.x & (DSK_WAVE - 1);
+  for (int s0 = 0; s0 < a.B; s0 += DSK_WAVE) {
+    int parts = 0;
+    if (s0 + lane < a.B) {
+      const TreePlace at(a, s0 + lane);
+      if (at.n > 0) parts = at.used(sp, false, 0);
+    }
+    const int incl = wave_incl_scan_i(parts, lane), total = __builtin_amdgcn_readlane(incl, DSK_WAVE - 1);
+    if (p < total) {
+      const int before = __builtin_popcountll(__ballot(incl <= p));    // sequences
+      s = s0 + before;
+      split = before > 0 ? p - __builtin_amdgcn_readlane(incl, before - 1) : p;
+      return true;
+    }
+    p -= total;
+  }
+  return false;
+}
+
+// What a workgroup takes: part, sequence, KV head and pass; false: nothing.
+struct TreeWork {
+  int split, s, hk, q_tile;
+  __device__ __forceinline__ bool find(const dsk_tree_attn_args& a, const TreeSplit& sp, int q_tiles) {
+    const int y = sp.packed ? blockIdx.x : blockIdx.y;
+    hk = y / q_tiles;
+    q_tile = y - hk * q_tiles;
+    if (sp.packed) return tree_find(a, sp, blockIdx.y, s, split);
+    split = blockIdx.x;
+    s = blockIdx.z;
+    return true;
   }
 };
 
@@ -589,8 +625,9 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
   static_assert(kTiles + DSK_TREE_MAX_NODES / kTreeTile + 1 <= kTreeMixedTiles, "words of sm_bad");
   __shared__ int32_t sm_rows[SEL ? kTreeMaxListed : 1];
 
-  const int split = blockIdx.x, s = blockIdx.z;
-  const int hk = blockIdx.y / q_tiles, q_tile = blockIdx.y - hk * q_tiles;
+  TreeWork work;
+  if (!work.find(a, sp, q_tiles)) return;                // uniform, as all returns before the end
+  const int split = work.split, s = work.s, hk = work.hk, q_tile = work.q_tile;
   const int tid = threadIdx.x, wave = tid / DSK_WAVE;
   const int qw = wave % QW, kw = wave / QW;
 
@@ -705,8 +742,9 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
   __shared__ uint32_t sm_bad[kTreeMixedTiles];
   static_assert(1 + DSK_TREE_MAX_NODES / kTreeTile + 1 <= kTreeMixedTiles, "words of sm_bad");
 
-  const int split = blockIdx.x, s = blockIdx.z;
-  const int hk = blockIdx.y / q_tiles, q_tile = blockIdx.y - hk * q_tiles;
+  TreeWork work;
+  if (!work.find(a, sp, q_tiles)) return;
+  const int split = work.split, s = work.s, hk = work.hk, q_tile = work.q_tile;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / DSK_WAVE);
   const bool late = wave >= 4;
 
@@ -937,7 +975,6 @@ struct TreeLaunch {
   bool deep;          // tree_attn_kernel with eight wavefronts
   bool wide;          // tree_wide_kernel
   bool stream;        // K and V are read past the memory-side cache
-  bool odd;           // an odd number of parts is launched
   int q_tiles;        // passes over a (sequence, KV head)'s keys
   size_t part_acc, total;
 };
@@ -978,7 +1015,7 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     return (per + stage - 1) / stage * stage;
   };
   t.sp.keys_per_split = t.sp.slots_per_split = 0;
-  t.deep = t.wide = t.stream = t.odd = false;
+  t.deep = t.wide = t.stream = t.sp.packed = false;
   if (!sel) {
     if (rows > 128 && !f32) {
       rows_of(kWideWaves);
@@ -987,23 +1024,22 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     }
     if (!t.wide) {
       rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
-      // Two a CU, all there at once; three for every two that fit where sequences are known to differ in length (8 of 16K to 64K
-      // tokens, 13 nodes: 283 us with 512, 271 with 768, 268 with 1024; 4 of up to 32K, 16 nodes: 92, 84, 93; 16 of up to 16K, 8
-      // nodes: 132, 146, 141).
-      t.sp.keys_per_split = (int)keys_of(ragged ? 3 * kTreeCus : 2 * kTreeCus);
-      // One sequence that gives every CU a workgroup: one of eight wavefronts a CU, which halves the partial results.  32 / 8
-      // heads, 16 nodes: 8K tokens 23.8 -> 21.6 us, 32K 39.5 -> 36.6, 128K 104.7 -> 99.9; fp32 32K 44.3 -> 40.8; 32 nodes: 32K
-      // 50.6 -> 44.6; 4K (136 workgroups) 17.1 and 18.6.  Sequences of several lengths need the finer grain (8 of 16K to 64K
-      // tokens 282 and 312 us).
-      t.deep = a.B == 1 && t.q_waves > 1 && keys * a.Hkv * t.q_tiles >= (int64_t)kTreeCus * kTreeLeastKeys;
+      t.sp.keys_per_split = (int)keys_of(2 * kTreeCus);  // two a CU, all there at once
+      // One of eight wavefronts a CU instead, which halves the partial results, where that gives every CU a workgroup.  32 / 8 heads,
+      // 16 nodes: 8K tokens 23.8 -> 21.6 us, 32K 39.5 -> 36.6, 128K 104.7 -> 99.9; fp32 32K 44.3 -> 40.8; 32 nodes: 32K 50.6 -> 44.6;
+      // 4K (136 workgroups) 17.1 and 18.6; eight sequences of 32K 224 -> 177.  Sequences that are known to differ in length fill the
+      // finer grain better: eight of 16K to 64K tokens, 13 nodes 246 and 269, four of up to 32K 75 and 74.
+      t.deep = (a.B == 1 || !ragged) && t.q_waves > 1 && keys * a.Hkv * t.q_tiles >= (int64_t)kTreeCus * kTreeLeastKeys;
       if (t.deep) t.sp.keys_per_split = (int)keys_of(kTreeCus);
     }
     t.sp.nsplit = (int)(((int64_t)a.max_seqlen + a.max_nodes + t.sp.keys_per_split - 1) / t.sp.keys_per_split);
-    // Workgroups go round the eight XCDs by their number, and those of parts that a shorter sequence lacks end at once: an odd
-    // number of parts begins every sequence and head on another XCD, where a multiple of eight would leave the last ones of all
-    // with less to do (the 8 sequences above 280 -> 267 us).  Not where an XCD's L2 serves several passes over the same keys, nor
-    // with one workgroup a CU (eight wavefronts: 113 -> 122 us).
-    t.odd = a.B > 1 && t.q_tiles == 1 && !t.wide;
+    // Workgroups go round XCDs and their shader engines by their number, whatever those have to do, and the parts that a shorter
+    // sequence lacks end at once: numbered by sequence they leave some engines with two rounds of work and others with none.
+    // Numbered through the parts that there are, each sequence's in turn and the heads fastest, all have the same: eight sequences
+    // of 16K to 64K tokens, 13 nodes 283 -> 246 us, 32 nodes 319 -> 283, two of 32K and 64K 101 -> 85; what it costs is that a
+    // workgroup looks its part up (16 sequences of 700 tokens 21.7 -> 22.3).  Several passes over the same keys stay as they are:
+    // they have an XCD's L2 in common.
+    t.sp.packed = a.B > 1 && t.q_tiles == 1 && (int64_t)a.B * t.sp.nsplit <= 65535;
     t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
   } else {
     rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
@@ -1035,10 +1071,15 @@ size_t tree_ws_bytes(const dsk_tree_attn_args& a) {
   return f32 > bf16 ? f32 : bf16;
 }
 
+static dim3 tree_grid(const dsk_tree_attn_args& a, const TreeLaunch& t) {
+  const unsigned y = (unsigned)(a.Hkv * t.q_tiles);
+  return t.sp.packed ? dim3(y, (unsigned)(a.B * t.sp.nsplit)) : dim3((unsigned)t.sp.nsplit, y, (unsigned)a.B);
+}
+
 template <int QW, int KW, int NT, int BUFS, bool MAY_SELECT>
 static void launch_tree(const dsk_tree_attn_args& a, const TreeLaunch& t, float scale_log2, float2* ml, float* acc, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
-  const dim3 grid((unsigned)t.sp.nsplit | (t.odd ? 1u : 0u), (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(QW * KW * DSK_WAVE);
+  const dim3 grid = tree_grid(a, t), block(QW * KW * DSK_WAVE);
 #define DSK_TREE(terms)                                                                                                        \
   do {                                                                                                                         \
     if (MAY_SELECT && a.sel_start != nullptr)                                                                                  \
@@ -1063,7 +1104,7 @@ hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st) {
   const float scale_log2 = scale * kLog2e;
   const int G = a.Hq / a.Hkv;
   if (t.wide) {
-    const dim3 grid((unsigned)t.sp.nsplit, (unsigned)(a.Hkv * t.q_tiles), (unsigned)a.B), block(kWideWaves * DSK_WAVE);
+    const dim3 grid = tree_grid(a, t), block(kWideWaves * DSK_WAVE);
     if (t.stream) tree_wide_kernel<true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
     else tree_wide_kernel<false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
   } else if (t.q_waves == 1) {

@@ -494,3 +494,37 @@ def test_a_query_that_is_not_a_number_gets_none(lens, Hq, Hkv, nodes):
         assert bool(out[hit].isnan().all()) and bool(r.lse[hit].isnan().all())
         assert torch.equal(out[~hit], want[~hit]) and torch.equal(r.lse[~hit], clean.lse[~hit])
         c.q[2, 1] = 1.0
+
+
+# ---- batches: workgroups are numbered through the parts that there are --------------------------------------------
+@pytest.mark.parametrize("Hq, Hkv, nodes", [(8, 2, 3), (8, 2, 16), (32, 8, 40)])
+def test_many_sequences_with_and_without_nodes(Hq, Hkv, nodes):
+    """More sequences than lanes, some without nodes, some without a prefix, the last ones with none of both."""
+    rng = np.random.default_rng(nodes)
+    lens = [int(rng.integers(0, 900)) if s % 3 else 0 for s in range(150)]
+    n_new = [0 if s % 4 == 1 or s > 146 else int(rng.integers(1, nodes + 1)) for s in range(150)]
+    n_new[10] = nodes
+    Case(lens, n_new, Hq, Hkv, seed=nodes, pad_tokens=1).check()
+
+
+def test_sequences_that_share_their_prefix():
+    """Several drafts over one prompt: the prefixes' keys are more than the cache has rows."""
+    c = Case([30000, 5], [13, 13], 32, 8, seed=71, packed=True)
+    c.row0, c.lens, c.n_new, c.seen = [0] * 5, [30000, 29000, 30000, 7, 30005], [13] * 5, c.seen[:1] * 5
+    c.cu, c.N = starts(c.n_new), 65
+    g = torch.Generator(device="cuda")
+    g.manual_seed(72)
+    c.Kd, c.Vd = (torch.randn(8, 65, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    c.q = torch.randn(65, 32, D, generator=g, device="cuda").bfloat16()
+    c.row0.append(0)
+    c.check()
+
+
+def test_batches_whose_bounds_are_not_reached():
+    """max_seqlen far above every length: parts that no sequence has."""
+    c = Case([3000, 1, 0, 2999], [14, 14, 1, 9], 32, 8, seed=73)
+    out, size, lse = c.reference()
+    for kw in (dict(max_seqlen=200_000), dict(max_seqlen=3000)):
+        r = c.run(**kw)
+        assert bool(((r.out.double() - out).abs() <= F32 * size).all())
+        assert bool(((r.lse.double() - lse).abs() <= 1e-5 * (1 + lse.abs())).all())
