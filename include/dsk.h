@@ -601,7 +601,7 @@ typedef struct dsk_tree_attn_args {
   int32_t B, Hq, Hkv, D;
   int32_t n_tokens;            /* [host] rows of q, out and mask (and of Kd / Vd); bounds cu_new[B] */
   int32_t max_nodes;           /* [host] bound on the nodes of a sequence, 1..DSK_TREE_MAX_NODES */
-  int32_t max_seqlen;          /* [host] bound on seq_len, >= 0 */
+  int32_t max_seqlen;          /* [host] bound on seq_len, >= 0; far above the lengths it leaves CUs idle */
   int32_t total_rows;          /* [host] rows per head of K / V */
   const void* q;               /* [dev] bf16 [n_tokens, Hq, D] */
   const void* K;               /* [dev] bf16, strides as in dsk_compress_args */

@@ -11,8 +11,8 @@
 // order of keys (two transposing LDS reads of four keys each).  No weight passes through LDS.
 //
 // K and V tiles lie in LDS with their 16-byte chunks swizzled by row, so that the reads of both products and the writes are free
-// of bank conflicts.  The kernel for up to 128 rows copies stages of the prefix straight to LDS; the one for more rows has a
-// schedule of its own and takes them through registers.  Stages that hold nodes go through registers in both, where what a mask
+// of bank conflicts.  The general kernel copies stages of the prefix straight to LDS; the one for many rows has a schedule of its
+// own and takes them through registers.  Stages that hold nodes go through registers in both, where what a mask
 // may hide is looked at.
 #include "dsk_attn_fold.hpp"
 #include "dsk_common.hpp"
@@ -610,7 +610,7 @@ __device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const Tr
 // KW wavefronts take other tiles of a stage for the same queries, NT of them each.  With two BUFS a stage is copied while the one
 // before it is multiplied; with one (32 rows, whose products are short) that is left to the second workgroup of the CU.
 // HBM bounds it: 40 / 40 heads, 128K tokens, 16 nodes (2.68 GB) 396 us, 6.8 TB/s; 32 / 8 heads, 16 nodes (0.54 GB) 88, 6.1; eight of
-// 16K to 64K, 13 nodes, token-major (1.48 GB) 260 to 277, 5.4 to 5.7.  Where 4 wavefronts take 128 rows, their matrix instructions
+// 16K to 64K, 13 nodes, token-major (1.48 GB) 238 to 244, 6.1 to 6.2.  Where 4 wavefronts take 128 rows, their matrix instructions
 // and exponentials, about as many cycles each, no longer hide entirely: 32 nodes, 0.54 GB at 5.0 TB/s.
 template <int QW, int KW, int NT, int BUFS, int TERMS, bool SEL, bool STREAM>
 __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
