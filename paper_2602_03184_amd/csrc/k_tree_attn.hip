@@ -1033,14 +1033,6 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
       if (t.deep) t.sp.keys_per_split = (int)keys_of(kTreeCus);
     }
     t.sp.nsplit = (int)(((int64_t)a.max_seqlen + a.max_nodes + t.sp.keys_per_split - 1) / t.sp.keys_per_split);
-    // Workgroups go round XCDs and their shader engines by their number, whatever those have to do, and the parts that a shorter
-    // sequence lacks end at once: numbered by sequence they leave some engines with two rounds of work and others with none.
-    // Numbered through the parts that there are, each sequence's in turn and the heads fastest, all have the same: eight sequences
-    // of 16K to 64K tokens, 13 nodes 283 -> 246 us, 32 nodes 319 -> 283, two of 32K and 64K 101 -> 85; what it costs is that a
-    // workgroup looks its part up (16 sequences of 700 tokens 21.7 -> 22.3).  Several passes over the same keys stay as they are:
-    // they have an XCD's L2 in common.
-    t.sp.packed = a.B > 1 && t.q_tiles == 1 && (int64_t)a.B * t.sp.nsplit <= 65535;
-    t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
   } else {
     rows_of(rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
     const int64_t slots = (int64_t)a.k * a.B * a.Hkv * t.q_tiles;
@@ -1058,6 +1050,16 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   // (136 workgroups) would take 21.8 instead of 20.6.  (Halving two wavefronts' rows again gains nothing: 600 tokens 13.9 and
   // 14.1.)
   if (!t.wide && t.q_waves == 4 && (int64_t)a.B * a.Hkv * t.q_tiles * t.sp.nsplit <= kTreeCus / 2) rows_of(2);
+  if (!sel) {
+    // Workgroups go round XCDs and their shader engines by their number, whatever those have to do, and the parts that a shorter
+    // sequence lacks end at once: numbered by sequence they leave some engines with two rounds of work and others with none.
+    // Numbered through the parts that there are, each sequence's in turn and the heads fastest, all have the same: eight sequences
+    // of 16K to 64K tokens, 13 nodes 283 -> 246 us, 32 nodes 319 -> 283, two of 32K and 64K 101 -> 85; what it costs is that a
+    // workgroup looks its part up (16 sequences of 700 tokens 21.7 -> 22.3).  Several passes over the same keys stay as they are:
+    // they have an XCD's L2 in common.
+    t.sp.packed = a.B > 1 && t.q_tiles == 1 && (int64_t)a.B * t.sp.nsplit <= 65535;
+    t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
+  }
   const size_t parts = t.sp.nsplit > 1 ? (size_t)a.n_tokens * a.Hq * t.sp.nsplit : 0;
   t.part_acc = align_up(parts * sizeof(float2));
   t.total = t.part_acc + align_up(parts * DSK_HEAD_DIM * sizeof(float));
