@@ -588,7 +588,8 @@ typedef struct dsk_norm_rope_args {
  *   out = sum p_t V_t / sum p_t,  p_t = exp(q.K_t * scale);  lse = log sum p_t
  * K and V of node j lie in row seq_row0[s] + seq_len[s] + j of the cache, or, with Kd / Vd, in row
  * cu_new[s] + j of these.  A node that sees nothing gets out = 0 and lse = -inf.  K or V rows that no bit
- * lets a node see may hold anything, NaN included.  Mask bits of nodes that do not exist are ignored.
+ * lets a node see may hold anything, NaN included.  An infinity in a row of V that a node sees gives that infinity, or NaN with its
+ * opposite or where its weight is 2^-80 of the largest or less.  Mask bits of nodes that do not exist are ignored.
  * `out` asks for fp32 accuracy; where only out_bf16 is asked for, the softmax weights are rounded to bf16
  * for the products with V (lse is fp32 in both).  Sums are in fp32, split over the keys with a merge in a fixed
  * order; how they are split, and with it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen, total_rows (k and b

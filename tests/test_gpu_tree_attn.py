@@ -528,3 +528,44 @@ def test_batches_whose_bounds_are_not_reached():
         r = c.run(**kw)
         assert bool(((r.out.double() - out).abs() <= F32 * size).all())
         assert bool(((r.lse.double() - lse).abs() <= 1e-5 * (1 + lse.abs())).all())
+
+
+# ---- infinities in rows that are seen --------------------------------------------------------------------------------
+@pytest.mark.parametrize("lens, n_new, Hq, Hkv, k", [
+    ([300], [5], 4, 2, 0),                                       # up to 32 rows, stages of 128 keys, the last one with the nodes
+    ([300], [21], 8, 4, 0),                                      # up to 64, stages of 64
+    ([300], [40], 4, 2, 0),                                      # more, the same as four wavefronts' rows
+    ([700, 300, 90], [30, 40, 9], 24, 8, 0),
+    ([9003], [12], 32, 8, 0),                                    # eight wavefronts, many parts
+    ([9003], [30], 32, 8, 0),
+    ([20003], [64], 32, 8, 0),
+    ([1500], [9], 8, 2, 40),                                     # a selection
+    ([1500], [40], 8, 2, 40),
+])
+@pytest.mark.parametrize("f32", [True, False])
+def test_an_infinite_value_gives_an_infinity_wherever_its_row_lies(lens, n_new, Hq, Hkv, k, f32):
+    """No weight here is below 2^-90 of the largest (logits of K's scale, up to some 30 apart), so the weighted sum over a row of
+    V with an infinity in a channel is that infinity for every node and head, whatever else it holds, and with both signs NaN."""
+    c = Case(lens, n_new, Hq, Hkv, seed=81)
+    if k:
+        c.select(k, 16)
+    kw = {} if f32 else dict(want_f32=False, want_bf16=True)
+    clean, G, inf, n = c.run(**kw), Hq // Hkv, float("inf"), n_new[0]
+    p = c.prefix(0, 1)
+    L = len(p)
+    for i in sorted({0, 1, 17, 32, 63, 64, 100, L // 3, L // 2, L - 130, L - 65, L - 33, L - 2, L - 1} & set(range(L))):
+        old = c.V[1, p[i]].clone()
+        c.V[1, p[i], 3], c.V[1, p[i], 77] = inf, -inf
+        other = p[(i + L // 2) % L]
+        was = c.V[1, other, 77].clone()
+        r = c.run(**kw)
+        a, b = (x.out if f32 else x.out_bf16 for x in (r, clean))
+        hit = torch.zeros_like(a, dtype=torch.bool)
+        hit[:n, G:2 * G, 3] = hit[:n, G:2 * G, 77] = True
+        assert bool((a[:n, G:2 * G, 3] == inf).all()) and bool((a[:n, G:2 * G, 77] == -inf).all()), i
+        assert torch.equal(a[~hit], b[~hit]) and torch.equal(r.lse, clean.lse), i
+        c.V[1, other, 77] = inf
+        r = c.run(**kw)
+        a = r.out if f32 else r.out_bf16
+        assert bool(a[:n, G:2 * G, 77].isnan().all()) and bool((a[:n, G:2 * G, 3] == inf).all()), i
+        c.V[1, other, 77], c.V[1, p[i]] = was, old
