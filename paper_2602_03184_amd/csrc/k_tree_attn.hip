@@ -525,11 +525,13 @@ __device__ __forceinline__ void tree_scale(tree_f32x16 (&O)[4], float f) {
     for (int i = 0; i < 16; ++i) O[ct][i] *= f;
 }
 
-// A query's running softmax: the reference of its exponents in log2 units (-inf: nothing seen) and this half's sum.
+// A query's running softmax: the reference of its exponents in log2 units (-inf: nothing seen) and this half's sum l - err.  A tile's
+// weights are added up by themselves and join the sum with what rounding took from it carried along: added one after the other, equal
+// weights are rounded alike, 1e-4 of the sum after 8192 of them.
 struct TreeSoftmax {
-  float m, l, scale_log2;
+  float m, l, err, scale_log2;
   FmaExponent exponent;
-  __device__ __forceinline__ explicit TreeSoftmax(float scale) : m(-__builtin_inff()), l(0.0f), scale_log2(scale), exponent(scale, 0.0f) {}
+  __device__ __forceinline__ explicit TreeSoftmax(float scale) : m(-__builtin_inff()), l(0.0f), err(0.0f), scale_log2(scale), exponent(scale, 0.0f) {}
   // weights of a tile from its logits
   template <int TERMS>
   __device__ __forceinline__ void take(const tree_f32x16& z, tree_f32x16 (&O)[4], TreeWeights<TERMS>& w) {
@@ -540,17 +542,25 @@ struct TreeSoftmax {
       const float m_new = fmaxf(m, mx);
       const float f = m == -__builtin_inff() ? 0.0f : exp2_small(m - m_new);
       l *= f;
+      err *= f;
       tree_scale(O, f);
       m = m_new;
       exponent = FmaExponent(scale_log2, m == -__builtin_inff() ? 0.0f : m);
     }
     float p[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      p[i] = exp2_small(exponent.of(z[i]));
-      l += p[i];
-    }
+    for (int i = 0; i < 16; ++i) p[i] = exp2_small(exponent.of(z[i]));
+    const float tile = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])) +
+                       (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
+    const float add = tile - err, sum = l + add;
+    err = (sum - l) - add;
+    l = sum;
     w.set(p);
+  }
+  // both halves' sum
+  __device__ __forceinline__ void close() {
+    l -= err;
+    l += shfl_xor_f(l, 32);
   }
 };
 
@@ -721,7 +731,7 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
     if (qs.busy) tiles(t0, sm_kv, Mixed());
     __syncthreads();
   }
-  sm.l += shfl_xor_f(sm.l, 32);
+  sm.close();
   if constexpr (KW > 1) {
     static_assert((KW - 1) * QW <= BUFS * kTiles, "a block is as large as a tile of K and V");
     tree_join<QW, KW>(sm, O, qs.busy, qw, kw, reinterpret_cast<float*>(sm_kv), sm_ml);
@@ -901,7 +911,7 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
     tree_values_left_out(O, keys, sm_bad, qs.allowed(t_of(steps - 1), keys.P), t_of(steps - 1), qs.half);
   }
   if (!late) barrier();                                  // as many as the others
-  sm.l += shfl_xor_f(sm.l, 32);
+  sm.close();
   tree_store(a, qs, O, sm.m, sm.l, used, sp.nsplit, split, part_ml, part_acc);
 }
 

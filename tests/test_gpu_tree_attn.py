@@ -569,3 +569,35 @@ def test_an_infinite_value_gives_an_infinity_wherever_its_row_lies(lens, n_new, 
         a = r.out if f32 else r.out_bf16
         assert bool(a[:n, G:2 * G, 77].isnan().all()) and bool((a[:n, G:2 * G, 3] == inf).all()), i
         c.V[1, other, 77], c.V[1, p[i]] = was, old
+
+
+# ---- long sums of equal weights ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("a", [2.15625, 4.1875])
+@pytest.mark.parametrize("Hq, nodes, f32, waves", [(8, 4, True, 4), (8, 4, False, 4), (32, 10, True, 2), (32, 32, True, 1), (32, 64, False, 1)])
+def test_long_sums_of_equal_weights(a, Hq, nodes, f32, waves):
+    """64 sequences of 8 KV heads over one prefix, a part each: 128 keys of logit 0, then 65536 alike of logit a, which is not
+    far enough above to become the reference of the exponents, so every weight is e^a.  `waves` wavefronts share the keys.
+    lse: an exponent below 8 is off by 3 * 2^-24 of it (scale, product, rounding), a weight by 2^-22 and less of it; 16 of
+    them and the parts of eight wavefronts are added up with 9 roundings: 2^-20 of the sum in all.  log2 of it (16 to 32) and what
+    is added to it are rounded to 2^-20 each, the result once more: 2^-20 (1 + 2 ln 2 + 0.5) < 4e-6.
+    out (the same in all rows of a channel): a tile is two sums of 16 products, of three terms each in fp32 results; each is added
+    with 2^-24 of the sum so far, half of the final one in the mean."""
+    dsk = _dsk()
+    B, Hkv, L = 64, 8, 65536 + 128
+    K = torch.zeros(Hkv, L, D, dtype=torch.bfloat16, device="cuda")
+    K[:, 128:, 0] = a
+    v = torch.linspace(1.0, 2.0, D, device="cuda").bfloat16()
+    V = v.expand(Hkv, L, D).contiguous()
+    q = torch.zeros(B * nodes, Hq, D, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    Kd = torch.zeros(Hkv, B * nodes, D, dtype=torch.bfloat16, device="cuda")
+    Vd = v.expand(Hkv, B * nodes, D).contiguous()
+    r = dsk.tree_decode_attn(q, K, V, seq_row0=i32([0] * B), seq_len=i32([L] * B), cu_new=i32(range(0, B * nodes + 1, nodes)),
+                             mask=None, max_nodes=nodes, max_seqlen=L, Kd=Kd, Vd=Vd, scale=1.0, want_f32=f32, want_bf16=not f32)
+    torch.cuda.synchronize()
+    want = torch.tensor([math.log(128 + 1 + i + 65536 * math.exp(a)) for i in range(nodes)], dtype=torch.float64, device="cuda")
+    assert float((r.lse.double().view(B, nodes, Hq) - want[None, :, None]).abs().max()) <= 4e-6
+    adds = (L // 32 // waves) * 2 * (3 if f32 else 1)
+    bar = adds / 2 * 2.0 ** -24 + 2.0 ** -20 + (0 if f32 else 2 * BF16)
+    got = (r.out if f32 else r.out_bf16).double()
+    assert bool(((got - v.double()).abs() <= bar * v.double()).all())
