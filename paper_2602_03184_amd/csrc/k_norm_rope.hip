@@ -45,6 +45,7 @@ __global__ __launch_bounds__(kRopeThreads) void norm_rope_kernel(dsk_norm_rope_a
 
   float cs[8], sn[8];                                          // interleaved: four pairs of a lane, in the first half
   int partner = lane;
+  bool inside = false;                                         // the lane's channels are rotated; the others keep what they hold
   if constexpr (PAIRS != RopePairs::kNone) {
     const int half = a.rot_dim / 2;
     if (lane < half) {
@@ -58,13 +59,13 @@ __global__ __launch_bounds__(kRopeThreads) void norm_rope_kernel(dsk_norm_rope_a
     __builtin_amdgcn_wave_barrier();
     constexpr bool kInter = PAIRS == RopePairs::kInterleaved;
     const int chunks = a.rot_dim / 8, half_chunks = chunks / 2;
-    const bool inside = c < chunks;
+    inside = c < chunks;
     const bool upper = !kInter && c >= half_chunks;
     const int first = !inside ? 0 : (kInter ? c * 4 : (upper ? c - half_chunks : c) * 8);
 #pragma unroll
     for (int e = 0; e < (kInter ? 4 : 8); ++e) {
-      cs[e] = inside ? sm_cos[wave][first + e] : 1.0f;
-      sn[e] = inside ? sm_sin[wave][first + e] : 0.0f;
+      cs[e] = sm_cos[wave][first + e];
+      sn[e] = sm_sin[wave][first + e];
       if (!kInter && !upper) sn[e] = -sn[e];                   // mine * cos + partner * (-sin), or + partner * sin
     }
     if (!kInter && inside) partner = upper ? lane - half_chunks : lane + half_chunks;
@@ -108,17 +109,18 @@ __global__ __launch_bounds__(kRopeThreads) void norm_rope_kernel(dsk_norm_rope_a
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float lo = f[2 * e], hi = f[2 * e + 1];
-          f[2 * e] = fmaf(lo, cs[e], -hi * sn[e]);
-          f[2 * e + 1] = fmaf(lo, sn[e], hi * cs[e]);
+          f[2 * e] = inside ? fmaf(lo, cs[e], -hi * sn[e]) : lo;
+          f[2 * e + 1] = inside ? fmaf(lo, sn[e], hi * cs[e]) : hi;
         }
       } else if constexpr (PAIRS != RopePairs::kNone) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float o = PAIRS == RopePairs::kHalfAll ? dpp_f<0x128>(f[e]) : __shfl(f[e], partner, DSK_WAVE);   // 0x128: 8 lanes on in the row of 16
-          f[e] = fmaf(f[e], cs[e], o * sn[e]);
+          f[e] = PAIRS == RopePairs::kHalfAll || inside ? fmaf(f[e], cs[e], o * sn[e]) : f[e];
         }
       }
-      if (!is_v) y = make_uint4(pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3]), pack_bf16_rne(f[4], f[5]), pack_bf16_rne(f[6], f[7]));
+      if (!is_v && (inside || weight != nullptr))
+        y = make_uint4(pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3]), pack_bf16_rne(f[4], f[5]), pack_bf16_rne(f[6], f[7]));
       if (r < rows) {
         uint16_t* to = is_q ? static_cast<uint16_t*>(a.q_out) + ((int64_t)t * a.Hq + r) * DSK_HEAD_DIM
                        : is_v ? static_cast<uint16_t*>(a.V) + row * a.vc_stride_tok + (r - nq - nk) * a.vc_stride_head

@@ -186,3 +186,45 @@ def test_no_token_at_all():
     r.step()
     torch.cuda.synchronize()
     assert r.q_out.shape == (0, 4, D) and bool((K == 5.0).all()) and bool((V == 5.0).all())
+
+
+@pytest.mark.parametrize("rot, inter", [(0, False), (32, False), (32, True), (96, False), (96, True), (112, False), (112, True)])
+def test_channels_that_are_not_rotated_are_copied_bit_for_bit(rot, inter):
+    """Without a norm, whatever they hold: infinities, NaNs of any payload and sign, zeros of both signs, subnormal numbers."""
+    dsk = _dsk()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    x = torch.randint(-2 ** 15, 2 ** 15, (9, 8, D), generator=g, device="cuda", dtype=torch.int16)
+    x[:, :, rot:][torch.rand(9, 8, D - rot, generator=g, device="cuda") < 0.3] = 0x7F80
+    x[:, :, rot:][torch.rand(9, 8, D - rot, generator=g, device="cuda") < 0.1] = -0x8000
+    x[:, :, :rot] = torch.randn(9, 8, rot, generator=g, device="cuda").bfloat16().view(torch.int16)
+    x = x.view(torch.bfloat16)
+    q, k, v = x[:, :4], x[:, 4:6], x[:, 6:]
+    K, V = (torch.zeros(2, 9, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    pos, f = torch.arange(9, dtype=torch.int32, device="cuda") * 77, _freq(rot) if rot else None
+    r = dsk.make_norm_rope(q, k, v, K, V, pos=pos, inv_freq=f, interleaved=inter)
+    r.step()
+    torch.cuda.synchronize()
+    for got, was in ((r.q_out, q), (K.transpose(0, 1), k)):
+        assert torch.equal(got[..., rot:].contiguous().view(torch.int16), was[..., rot:].contiguous().view(torch.int16))
+        if rot:
+            want, size = rope_reference(was[..., :rot].contiguous(), None, 0, pos, f, inter)
+            _close(got[..., :rot], want, size)
+    assert torch.equal(V.transpose(0, 1).contiguous().view(torch.int16), v.contiguous().view(torch.int16))
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_an_infinity_that_is_not_rotated_stays_one_behind_a_norm(inter):
+    """x / sqrt(mean of squares + eps) of a row with an infinity is 0 in its finite channels and NaN in that one; a weight of the
+    other tensor alone leaves the row as it is."""
+    dsk = _dsk()
+    q, k, v, wq, wk, _ = _inputs(3, 4, 2)
+    q, k = q.clone(), k.clone()
+    q[1, 2, 100], k[1, 1, 100] = float("inf"), float("inf")
+    K, V = (torch.zeros(2, 3, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    r = dsk.make_norm_rope(q, k, v, K, V, pos=i32([1, 2, 3]), q_weight=wq, inv_freq=_freq(32), interleaved=inter)
+    r.step()
+    torch.cuda.synchronize()
+    rest = torch.arange(D, device="cuda") != 100
+    assert bool(r.q_out[1, 2, 100].isnan()) and bool((r.q_out[1, 2, rest] == 0).all())
+    assert torch.equal(K.transpose(0, 1)[..., 32:], k[..., 32:])
