@@ -26,13 +26,10 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(dsk_accept_args 
     n = a.max_nodes < a.n_tokens - t0 ? a.max_nodes : a.n_tokens - t0;
     if (first_wg && tid == 0) set_status(a.dev_status, DSK_ERR_SHAPE);
   }
-  // rows that the cache has left for this sequence; in place, a node without a row does not exist
+  // rows that the cache has left for this sequence; in place, the nodes from there on have none and end a path
   int64_t room = row0 >= 0 && len >= 0 ? a.total_rows - row0 - len : 0;
   if (room < 0) room = 0;
-  if (a.K != nullptr && a.Kd == nullptr && n > room) {
-    n = (int)room;
-    if (first_wg && tid == 0) set_status(a.dev_status, DSK_ERR_CAPACITY);
-  }
+  const int placed = a.K != nullptr && a.Kd == nullptr && n > room ? (int)room : n;
   int parent[kAcceptRegs], draft[kAcceptRegs], target[kAcceptRegs];
 #pragma unroll
   for (int r = 0; r < kAcceptRegs; ++r) {
@@ -44,7 +41,7 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(dsk_accept_args 
   const int most = room < a.max_path ? (int)room : a.max_path;
   int cur = n > 0 ? 0 : -1, taken = 0, choice = -1;
   while (cur >= 0) {                                            // ends: the next node is above the current one
-    if (taken >= most) {
+    if (taken >= most || cur >= placed) {
       if (first_wg && tid == 0) set_status(a.dev_status, DSK_ERR_CAPACITY);
       break;
     }

@@ -176,3 +176,16 @@ def test_no_token_at_all():
     torch.cuda.synchronize()
     assert acc.n_accepted.tolist() == [0, 0] and acc.len_new.tolist() == [3, 2] and acc.next_id.tolist() == [-1, -1]
     assert bool((acc.path == -1).all()) and bool((K == 5.0).all()) and bool((V == 5.0).all())
+
+
+@pytest.mark.parametrize("packed", [True, False])
+@pytest.mark.parametrize("room, end", [(6, 3), (4, 4), (4, 5), (1, 1), (1, 2), (0, 0), (0, 1)])
+def test_only_a_path_that_is_cut_reports_its_end(packed, room, end):
+    """A chain of 10 nodes of which `end` are right, in a cache with rows for `room` of them: the status says whether a further
+    node would have been accepted, not whether there are nodes without a row."""
+    dsk = _dsk()
+    chain, draft = [list(range(-1, 9))] if end else [[]], [list(range(10))] if end else [[]]
+    target = [[t + 1 if t + 1 < end else 99 for t in range(10)]] if end else [[]]
+    acc, paths = _check([10 if end else 0], chain, draft, target, packed=packed, max_nodes=10, lens=[20], room=20 + room)
+    assert len(paths[0]) == min(room, end)
+    assert int(acc.dev_status.item()) == (dsk.DSK_ERR_CAPACITY if end > room else 0)
