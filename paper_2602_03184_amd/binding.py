@@ -1119,7 +1119,8 @@ def make_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Opti
                    q_out: Optional[torch.Tensor] = None, total_rows: Optional[int] = None) -> NormRope:
     """q [tokens, Hq, D], k / v [tokens, Hkv, D]: bf16 views, e.g. of one projection's output; K / V: bf16 cache
     [Hkv, rows, D]; pos / row: int32 [tokens] (tok_pos and tok_row of a StepPlan); weights: fp32 [D]; inv_freq: fp32
-    [rot_dim / 2], none = no rotation.  total_rows bounds `row`; it defaults to the rows of K (of V, else the tokens)."""
+    [rot_dim / 2], none = no rotation.  total_rows bounds `row`, beyond it tokens are skipped; it defaults to the rows of K and
+    V, has to be given for queries alone with `row`, and without `row` there are as many rows as tokens."""
     x = q if q is not None else k
     n, dev = x.shape[0], x.device
     a = dsk_norm_rope_args()
@@ -1147,7 +1148,9 @@ def make_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Opti
         a.kc_stride_tok, a.kc_stride_head = _kv_strides(K)
         assert K.shape[0] == a.Hkv
         a.k, a.K = _ptr(k), _ptr(K)
+    assert total_rows is not None or row is None or k is not None or v is not None, "without K / V say how many rows the cache has"
     a.total_rows = rows if total_rows is None else total_rows
+    assert row is not None or n <= a.total_rows, "a row for every token"
     for w in (q_weight, k_weight):
         assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == DSK_HEAD_DIM)
     a.q_weight, a.k_weight, a.eps = _ptr(q_weight), _ptr(k_weight), eps

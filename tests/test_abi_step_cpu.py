@@ -192,3 +192,22 @@ def test_helpers_refuse_tensors_that_are_not_on_the_gpu(dsk):
         dsk.tree_decode_attn(X, X, X, seq_row0=i[:1], seq_len=i[:1], cu_new=i, mask=None, max_nodes=2, max_seqlen=4)
     with pytest.raises(AssertionError):                          # one of them elsewhere
         dsk.make_step_plan(seq_row0=i, seq_len=i.to("meta"), n_new=i, max_tokens=3, total_rows=8)
+
+
+def test_norm_rope_helper_skips_no_token_in_silence(dsk):
+    """Rows of a cache that the call does not see lie above the number of tokens; rows by number need one for every token."""
+    import torch
+    X = torch.zeros(3, 2, 128, dtype=torch.bfloat16)
+    row, pos, f = torch.tensor([900, 901, 902], dtype=torch.int32), torch.zeros(3, dtype=torch.int32), torch.ones(64)
+    with pytest.raises(AssertionError):
+        dsk.make_norm_rope(X, None, None, None, None, row=row, pos=pos, inv_freq=f)
+    assert dsk.make_norm_rope(X, None, None, None, None, row=row, pos=pos, inv_freq=f, total_rows=1000).args.total_rows == 1000
+    assert dsk.make_norm_rope(X, None, None, None, None, pos=pos, inv_freq=f).args.total_rows == 3
+    cache = torch.zeros(2, 2, 128, dtype=torch.bfloat16)
+    with pytest.raises(AssertionError):
+        dsk.make_norm_rope(X, X, X, cache, cache)
+    with pytest.raises(AssertionError):
+        dsk.make_norm_rope(None, X, None, cache, None)
+    with pytest.raises(AssertionError):
+        dsk.make_norm_rope(X, None, None, None, None, total_rows=2)
+    assert dsk.make_norm_rope(X, X, X, cache, cache, row=row).args.total_rows == 2
