@@ -1150,6 +1150,7 @@ def make_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Opti
         a.k, a.K = _ptr(k), _ptr(K)
     assert total_rows is not None or row is None or k is not None or v is not None, "without K / V say how many rows the cache has"
     a.total_rows = rows if total_rows is None else total_rows
+    assert (k is None and v is None) or a.total_rows <= rows, "total_rows is at most the cache's"
     assert row is not None or n <= a.total_rows, "a row for every token"
     for w in (q_weight, k_weight):
         assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == DSK_HEAD_DIM)

@@ -211,3 +211,14 @@ def test_norm_rope_helper_skips_no_token_in_silence(dsk):
     with pytest.raises(AssertionError):
         dsk.make_norm_rope(X, None, None, None, None, total_rows=2)
     assert dsk.make_norm_rope(X, X, X, cache, cache, row=row).args.total_rows == 2
+
+
+def test_norm_rope_helper_writes_no_row_behind_the_cache(dsk):
+    """total_rows bounds the rows that are written, so it is no larger than the shorter of K and V."""
+    import torch
+    X, row = torch.zeros(3, 2, 128, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    K, V = torch.zeros(2, 9, 128, dtype=torch.bfloat16), torch.zeros(2, 7, 128, dtype=torch.bfloat16)
+    for k, v, most in ((X, X, 7), (X, None, 9)):
+        assert dsk.make_norm_rope(X, k, v, K, None if v is None else V, row=row, total_rows=most).args.total_rows == most
+        with pytest.raises(AssertionError):
+            dsk.make_norm_rope(X, k, v, K, None if v is None else V, row=row, total_rows=most + 1)
