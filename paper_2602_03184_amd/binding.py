@@ -1175,6 +1175,9 @@ class TreeAttnOut:
     keep: tuple
     out_bf16: Optional[torch.Tensor] = None
 
+    def step(self, stream=None, check: bool = True) -> int:
+        return _call(dsk_tree_decode_attn, self.args, self.lse.device, stream, check)
+
 
 def make_tree_attn_args(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *, seq_row0: torch.Tensor,
                         seq_len: torch.Tensor, cu_new: torch.Tensor, mask: Optional[torch.Tensor], max_nodes: int,
@@ -1231,7 +1234,7 @@ def make_tree_attn_args(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *, se
 def tree_decode_attn(q, K, V, *, stream=None, check: bool = True, **kw) -> TreeAttnOut:
     """dsk_tree_decode_attn with outputs and workspace made here; keywords as in make_tree_attn_args."""
     r = make_tree_attn_args(q, K, V, **kw)
-    _call(dsk_tree_decode_attn, r.args, q.device, stream, check)
+    r.step(stream, check)
     return r
 
 

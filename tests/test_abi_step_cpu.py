@@ -222,3 +222,30 @@ def test_norm_rope_helper_writes_no_row_behind_the_cache(dsk):
         assert dsk.make_norm_rope(X, k, v, K, None if v is None else V, row=row, total_rows=most).args.total_rows == most
         with pytest.raises(AssertionError):
             dsk.make_norm_rope(X, k, v, K, None if v is None else V, row=row, total_rows=most + 1)
+
+
+def test_a_kept_tree_attention_is_called_on_the_device_of_its_tensors(dsk, monkeypatch):
+    """As the other kept calls: refused where the tensors are not on the GPU, otherwise with that device as the current one."""
+    import contextlib
+
+    import torch
+    i, X = torch.zeros(3, dtype=torch.int32), torch.zeros(2, 8, 128, dtype=torch.bfloat16)
+    kept = dsk.make_tree_attn_args(X, X, X, seq_row0=i[:1], seq_len=i[:1], cu_new=i[:2], mask=None, max_nodes=2, max_seqlen=4)
+    with pytest.raises(AssertionError):
+        kept.step()
+
+    class Elsewhere:
+        device = torch.device("cuda", 1)
+
+    b, order = dsk.binding, []
+
+    @contextlib.contextmanager
+    def on(device):
+        order.append(device.index)
+        yield
+        order.append(0)
+    monkeypatch.setattr(b, "dsk_tree_decode_attn", lambda args, stream, check: order.append((args is kept.args, stream, check)) or 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "device", on)
+    kept.lse = Elsewhere()
+    assert kept.step(5, check=False) == 0 and order == [1, (True, 5, False), 0]

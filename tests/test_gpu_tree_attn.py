@@ -601,3 +601,18 @@ def test_long_sums_of_equal_weights(a, Hq, nodes, f32, waves):
     bar = adds / 2 * 2.0 ** -24 + 2.0 ** -20 + (0 if f32 else 2 * BF16)
     got = (r.out if f32 else r.out_bf16).double()
     assert bool(((got - v.double()).abs() <= bar * v.double()).all())
+
+
+def test_a_kept_call_is_made_again():
+    c = Case([300, 40], [9, 9], 8, 2, seed=91)
+    want = c.run(want_bf16=True)
+    r = _dsk().make_tree_attn_args(c.q, c.K, c.V, **c.kwargs(want_bf16=True))
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (None, st):
+        for t in (r.out, r.out_bf16, r.lse):
+            t.fill_(9.0)
+        torch.cuda.synchronize()
+        assert r.step(stream) == _dsk().DSK_OK
+        torch.cuda.synchronize()
+        assert torch.equal(r.out, want.out) and torch.equal(r.out_bf16, want.out_bf16) and torch.equal(r.lse, want.lse)
