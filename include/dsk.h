@@ -596,7 +596,8 @@ typedef struct dsk_norm_rope_args {
  * order; how they are split, and with it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen, total_rows (k and b
  * with a selection) and which outputs are asked for.  A token that several selected slots hold counts as often.
  * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths or spans outside the
- * arrays are cut, never followed: a prefix to max_seqlen and total_rows, nodes to max_nodes.
+ * arrays are cut, never followed: a prefix to max_seqlen and total_rows (the nodes' rows are those behind it), nodes to max_nodes;
+ * a sequence whose first row or length is no place in the cache has neither prefix nor rows of nodes in it.
  * ---------------------------------------------------------------------------------------- */
 typedef struct dsk_tree_attn_args {
   uint32_t struct_size;

@@ -121,10 +121,12 @@ struct TreePlace {
     n = n < a.n_tokens - tok0 ? n : a.n_tokens - tok0;
     row0 = a.seq_row0[s];
     len = a.seq_len[s];
-    if (row0 < 0 || row0 > a.total_rows || len < 0) row0 = len = 0;
+    const bool nowhere = row0 < 0 || row0 > a.total_rows || len < 0;
+    if (nowhere) row0 = len = 0;
     len = len < a.max_seqlen ? len : a.max_seqlen;
     len = len < a.total_rows - row0 ? len : a.total_rows - row0;
-    n_keys = a.Kd != nullptr || n < a.total_rows - row0 - len ? n : (int)(a.total_rows - row0 - len);
+    const int64_t left = nowhere ? 0 : a.total_rows - row0 - len;
+    n_keys = a.Kd != nullptr || n < left ? n : (int)left;
   }
   // parts of its keys that have any; count: of the selection
   __device__ __forceinline__ int used(const TreeSplit& sp, bool selected, int count) const {

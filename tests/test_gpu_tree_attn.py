@@ -616,3 +616,29 @@ def test_a_kept_call_is_made_again():
         assert r.step(stream) == _dsk().DSK_OK
         torch.cuda.synchronize()
         assert torch.equal(r.out, want.out) and torch.equal(r.out_bf16, want.out_bf16) and torch.equal(r.lse, want.lse)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("row0, length", [(-5, 64), (-5, 0), (0, -1), (70, -2 ** 31), (2 ** 31 - 1, 64)])
+@pytest.mark.parametrize("k", [0, 4])
+def test_a_sequence_that_has_no_place_reads_no_other_one(packed, row0, length, k):
+    """Its nodes lie nowhere in the cache, so in place they see what a selection names at most, and nothing of the rows that begin
+    the cache; in buffers of their own they see each other."""
+    c = Case([64, 64], [8, 8], 4, 2, seed=92, packed=packed)
+    if k:
+        c.select(k, 16)
+    base = c.run()
+    kw = dict(seq_row0=i32([row0, c.row0[1]]), seq_len=i32([length, 64]))
+    r = c.run(**kw)
+    c.K[:, : c.row0[1]], c.V[:, : c.row0[1]] = float("nan"), float("nan")
+    blind = c.run(**kw)
+    assert torch.equal(r.out[8:], base.out[8:]) and torch.equal(r.lse[8:], base.lse[8:])
+    if not k:                                                    # (a selection's slots are taken as they are, of any region)
+        assert torch.equal(blind.out[:8], r.out[:8]) and torch.equal(blind.lse[:8], r.lse[:8])
+    if not k and not packed:
+        assert bool((r.out[:8] == 0).all()) and bool((r.lse[:8] == -math.inf).all())
+    want = Case([0, 64], [8, 8], 4, 2, seed=92, packed=True)
+    if packed and not k:
+        want.Kd, want.Vd, want.q, want.seen = c.Kd, c.Vd, c.q, c.seen
+        alone = want.run(seq_len=i32([0, 0]))
+        assert torch.equal(alone.out[:8], r.out[:8]) and torch.equal(alone.lse[:8], r.lse[:8])
