@@ -604,7 +604,7 @@ typedef struct dsk_tree_attn_args {
   int32_t B, Hq, Hkv, D;
   int32_t n_tokens;            /* [host] rows of q, out and mask (and of Kd / Vd); bounds cu_new[B] */
   int32_t max_nodes;           /* [host] bound on the nodes of a sequence, 1..DSK_TREE_MAX_NODES */
-  int32_t max_seqlen;          /* [host] bound on seq_len, >= 0; far above the lengths it leaves CUs idle */
+  int32_t max_seqlen;          /* [host] bound on seq_len, 0..0x7FFF0000; far above the lengths it leaves CUs idle */
   int32_t total_rows;          /* [host] rows per head of K / V */
   const void* q;               /* [dev] bf16 [n_tokens, Hq, D] */
   const void* K;               /* [dev] bf16, strides as in dsk_compress_args */
@@ -618,7 +618,7 @@ typedef struct dsk_tree_attn_args {
   const int32_t* cu_new;       /* [dev] [B+1] */
   const uint32_t* mask;        /* [dev] optional [n_tokens, mask_words] */
   int32_t mask_words;          /* >= ceil(max_nodes / 32); read with mask only */
-  int32_t k, b;                /* slots per (sequence, KV head) and upper bound of sel_len; read with sel_start only */
+  int32_t k, b;                /* slots per (sequence, KV head), at most 0x7FFF0000, and upper bound of sel_len; read with sel_start only */
   const int32_t* sel_start;    /* [dev] optional [B, Hkv, k]; all three or none */
   const int32_t* sel_len;      /* [dev] [B, Hkv, k] */
   const int32_t* sel_count;    /* [dev] [B, Hkv] */

@@ -338,7 +338,7 @@ static dsk_status validate_tree(const dsk_tree_attn_args* a) {
   if ((a->Kd == nullptr) != (a->Vd == nullptr)) return DSK_ERR_NULL;
   if (a->sel_start || a->sel_len || a->sel_count) {
     if (!a->sel_start || !a->sel_len || !a->sel_count) return DSK_ERR_NULL;
-    if (a->k < 1 || a->b < 1 || a->b > 1024) return DSK_ERR_PARAM;
+    if (a->k < 1 || a->k > kMaxTreePrefix || a->b < 1 || a->b > 1024) return DSK_ERR_PARAM;
   }
   if (a->k_stride_tok < DSK_HEAD_DIM || a->v_stride_tok < DSK_HEAD_DIM || a->k_stride_head < 0 || a->v_stride_head < 0 ||
       a->k_stride_tok > kMaxTokenStride || a->v_stride_tok > kMaxTokenStride)
@@ -532,7 +532,7 @@ dsk_status dsk_qk_norm_rope(const dsk_norm_rope_args* a, void* stream) {
 size_t dsk_tree_attn_workspace_bytes(const dsk_tree_attn_args* a) {
   if (a == nullptr || a->struct_size != sizeof(dsk_tree_attn_args)) return 0;
   if (!geometry_ok(a->B, a->Hq, a->Hkv, a->D) || a->n_tokens < 0 || a->max_seqlen < 0 || a->max_seqlen > kMaxTreePrefix ||
-      a->max_nodes < 1 || a->max_nodes > DSK_TREE_MAX_NODES || (a->sel_start && (a->k < 1 || a->b < 1 || a->b > 1024)))
+      a->max_nodes < 1 || a->max_nodes > DSK_TREE_MAX_NODES || (a->sel_start && (a->k < 1 || a->k > kMaxTreePrefix || a->b < 1 || a->b > 1024)))
     return 0;
   return tree_ws_bytes(*a);
 }

@@ -143,7 +143,7 @@ hipError_t launch_reuse(const dsk_reuse_args& a, hipStream_t st);
 hipError_t launch_step_plan(const dsk_step_plan_args& a, hipStream_t st);
 hipError_t launch_norm_rope(const dsk_norm_rope_args& a, hipStream_t st);
 hipError_t launch_accept(const dsk_accept_args& a, hipStream_t st);
-constexpr int kMaxTreePrefix = 0x7FFF0000;     // keeps a key's number, nodes and a stage's overhang in 32 bits
+constexpr int kMaxTreePrefix = 0x7FFF0000;     // keeps a key's number, nodes and a stage's overhang in 32 bits; slots and a part's too
 size_t tree_ws_bytes(const dsk_tree_attn_args& a);
 hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st);
 

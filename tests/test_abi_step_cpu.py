@@ -249,3 +249,13 @@ def test_a_kept_tree_attention_is_called_on_the_device_of_its_tensors(dsk, monke
     monkeypatch.setattr(torch.cuda, "device", on)
     kept.lse = Elsewhere()
     assert kept.step(5, check=False) == 0 and order == [1, (True, 5, False), 0]
+
+
+def test_tree_attention_refuses_more_slots_than_it_counts(dsk):
+    """Slots and a part's of them are added up in 32 bits."""
+    for k, ok in ((0x7FFF0000, True), (0x7FFF0001, False), (2 ** 31 - 1, False)):
+        a = _tree(dsk)
+        a.k = k
+        assert (dsk.dsk_tree_attn_workspace_bytes(a) > 0) == ok
+        a.workspace_bytes = 0
+        assert dsk.dsk_tree_decode_attn(a, 0, check=False) == (dsk.DSK_ERR_WORKSPACE if ok else dsk.DSK_ERR_PARAM)
