@@ -1261,7 +1261,7 @@ def make_acceptor(K: Optional[torch.Tensor], V: Optional[torch.Tensor], *, seq_r
                   token_ids: Optional[torch.Tensor] = None, len_new: Optional[torch.Tensor] = None,
                   total_rows: Optional[int] = None) -> Acceptor:
     """K / V: bf16 [layers, Hkv, rows, D] (or [Hkv, rows, D]); Kd / Vd: the same with the tokens as rows, none = the
-    nodes' rows lie behind the sequences in K / V; both none: only the walk (total_rows then bounds the rows).
+    nodes' rows lie behind the sequences in K / V; both none: only the walk.  total_rows bounds the rows: K's, if not given.
     len_new: where the new lengths go (a BatchAppender's, say)."""
     dev = seq_len.device
     B, n = seq_len.numel(), parent.numel()
@@ -1278,9 +1278,13 @@ def make_acceptor(K: Optional[torch.Tensor], V: Optional[torch.Tensor], *, seq_r
     a.n_tokens, a.max_nodes, a.max_path = n, max_nodes, max_path
     a.seq_row0, a.seq_len, a.cu_new = _ptr(seq_row0), _ptr(seq_len), _ptr(cu_new)
     a.parent, a.draft_ids, a.target_ids = _ptr(parent), _ptr(draft_ids), _ptr(target_ids)
+    assert (K is None) == (V is None) and (Kd is None) == (Vd is None)
+    assert K is not None or Kd is None, "the nodes' own buffers without a cache to move them to"
     if K is not None:
+        assert total_rows is None or total_rows <= K.shape[-2], "total_rows is at most the cache's"
         four = [None if X is None else (X if X.dim() == 4 else X.unsqueeze(0)) for X in (K, V, Kd, Vd)]
-        a.n_layers, a.Hkv, total_rows = four[0].shape[:3]
+        a.n_layers, a.Hkv, rows = four[0].shape[:3]
+        total_rows = rows if total_rows is None else total_rows
         assert four[1].shape == four[0].shape
         for X, name in zip(four, ("k", "v", "kd", "vd")):
             if X is not None:

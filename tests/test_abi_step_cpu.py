@@ -259,3 +259,18 @@ def test_tree_attention_refuses_more_slots_than_it_counts(dsk):
         assert (dsk.dsk_tree_attn_workspace_bytes(a) > 0) == ok
         a.workspace_bytes = 0
         assert dsk.dsk_tree_decode_attn(a, 0, check=False) == (dsk.DSK_ERR_WORKSPACE if ok else dsk.DSK_ERR_PARAM)
+
+
+def test_acceptor_helper_drops_no_argument(dsk):
+    """K without V, the nodes' own buffers without a cache, and more rows than the cache's are refused; fewer bound the call."""
+    import torch
+    i, X = torch.zeros(3, dtype=torch.int32), torch.zeros(2, 9, 128, dtype=torch.bfloat16)
+    own = torch.zeros(2, 3, 128, dtype=torch.bfloat16)
+    kw = dict(seq_row0=i[:1], seq_len=i[:1], cu_new=i[:2], parent=i, draft_ids=i, target_ids=i, max_nodes=3)
+    assert dsk.make_acceptor(X, X, Kd=own, Vd=own, **kw).args.total_rows == 9
+    assert dsk.make_acceptor(X[None], X[None], total_rows=8, **kw).args.total_rows == 8
+    assert dsk.make_acceptor(None, None, total_rows=7, **kw).args.total_rows == 7
+    for K, V, more in ((None, None, dict(Kd=own, Vd=own, total_rows=9)), (X, None, {}), (None, X, dict(total_rows=9)),
+                       (X, X, dict(Kd=own)), (X, X, dict(total_rows=10)), (None, None, {})):
+        with pytest.raises(AssertionError):
+            dsk.make_acceptor(K, V, **more, **kw)
