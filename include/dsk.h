@@ -627,7 +627,9 @@ typedef struct dsk_tree_attn_args {
   float* out;                  /* [dev] f32 [n_tokens, Hq, D]; one of out and out_bf16 may be NULL */
   void* out_bf16;              /* [dev] bf16 [n_tokens, Hq, D] */
   float* lse;                  /* [dev] f32 [n_tokens, Hq], natural log; may be NULL */
-  void* workspace;             /* [dev] 256-byte aligned, dsk_tree_attn_workspace_bytes() */
+  void* workspace;             /* [dev] 256-byte aligned, dsk_tree_attn_workspace_bytes(), which does not shrink as max_seqlen or
+                                  n_tokens grow: one for the longest serves a growing cache.  It can be more with smaller B,
+                                  max_nodes, total_rows or k: ask for every combination that is used, keep the largest */
   size_t workspace_bytes;
 } dsk_tree_attn_args;
 

@@ -1000,7 +1000,7 @@ struct TreeLaunch {
   bool wide;          // tree_wide_kernel
   bool stream;        // K and V are read past the memory-side cache
   int q_tiles;        // passes over a (sequence, KV head)'s keys
-  size_t part_acc, total;
+  size_t part_acc;    // of the workspace
 };
 
 // Keys of a workgroup from which on the kernel for many rows gains (its first and last steps are slower), where the other has eight
@@ -1086,15 +1086,44 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   }
   const size_t parts = t.sp.nsplit > 1 ? (size_t)a.n_tokens * a.Hq * t.sp.nsplit : 0;
   t.part_acc = align_up(parts * sizeof(float2));
-  t.total = t.part_acc + align_up(parts * DSK_HEAD_DIM * sizeof(float));
-  t.total = t.total > 256 ? t.total : 256;
   return t;
 }
 
-// whichever outputs the call will ask for
+// Parts of a sequence at most, under this max_seqlen and every smaller one: as in keys_of(), without its rounding.
+static int64_t tree_most_parts(const dsk_tree_attn_args& a, int64_t want, int q_tiles) {
+  const int64_t heads = (int64_t)a.Hkv * q_tiles;
+  auto ceil_div = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+  auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
+  auto most = [](int64_t x, int64_t y) { return x > y ? x : y; };
+  const int64_t even_seqlen = least(a.max_seqlen, a.total_rows / a.B);   // the largest that is not `ragged`
+  int64_t n = least(most(want / (heads * a.B), 1), ceil_div(even_seqlen + a.max_nodes, kTreeLeastKeys));
+  if (a.max_seqlen > even_seqlen) {
+    const int64_t keys = a.total_rows + (int64_t)a.B * a.max_nodes, parts = most(want / heads - (a.B - 1), 1);
+    n = most(n, ceil_div((int64_t)a.max_seqlen + a.max_nodes, most(ceil_div(keys, parts), kTreeLeastKeys)));
+  }
+  return least(n, kTreeMaxSplit);
+}
+
+// Whichever outputs the call will ask for, and no less than with a smaller max_seqlen: a workspace that is kept serves every length
+// up to the one that it was made for.
 size_t tree_ws_bytes(const dsk_tree_attn_args& a) {
-  const size_t f32 = tree_layout(a, true).total, bf16 = tree_layout(a, false).total;
-  return f32 > bf16 ? f32 : bf16;
+  int64_t nsplit = 1;
+  for (const bool f32 : {false, true}) {
+    const TreeLaunch t = tree_layout(a, f32);
+    nsplit = t.sp.nsplit > nsplit ? t.sp.nsplit : nsplit;
+  }
+  if (a.sel_start == nullptr) {
+    const int rows = a.max_nodes * (a.Hq / a.Hkv);
+    auto bound = [&](int64_t want, int q_waves) {
+      const int64_t n = tree_most_parts(a, want, (rows + q_waves * kTreeTile - 1) / (q_waves * kTreeTile));
+      nsplit = n > nsplit ? n : nsplit;
+    };
+    bound(2 * kTreeCus, rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
+    if (rows > 128) bound(kTreeCus, kWideWaves);
+  }
+  const size_t parts = nsplit > 1 ? (size_t)a.n_tokens * a.Hq * nsplit : 0;
+  const size_t total = align_up(parts * sizeof(float2)) + align_up(parts * DSK_HEAD_DIM * sizeof(float));
+  return total > 256 ? total : 256;
 }
 
 static dim3 tree_grid(const dsk_tree_attn_args& a, const TreeLaunch& t) {

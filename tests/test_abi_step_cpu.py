@@ -274,3 +274,23 @@ def test_acceptor_helper_drops_no_argument(dsk):
                        (X, X, dict(Kd=own)), (X, X, dict(total_rows=10)), (None, None, {})):
         with pytest.raises(AssertionError):
             dsk.make_acceptor(K, V, **more, **kw)
+
+
+def test_tree_attention_workspace_does_not_shrink_as_the_cache_grows(dsk):
+    """A workspace for the longest cache serves every shorter one: heads, trees and batches of all kernels, bounds around the cache's
+    rows a sequence, where its sequences count as of one length below and as ragged above."""
+    lengths = sorted(set(range(0, 6000, 29)) | set(range(6000, 300_000, 1777)) | {2 ** e + d for e in range(5, 30) for d in (-17, 0, 1)}
+                     | {0x7FFF0000})
+    for B, Hq, Hkv, nodes, rows in ((1, 32, 8, 64, 2 ** 17), (1, 32, 8, 16, 2 ** 17), (8, 32, 8, 13, 400_000), (8, 32, 8, 13, 2 ** 19),
+                                    (3, 5, 1, 9, 100_000), (1, 8, 1, 256, 2 ** 21), (64, 32, 8, 4, 2 ** 18), (4, 40, 40, 16, 2 ** 17),
+                                    (2, 8, 2, 33, 0), (300, 32, 8, 40, 2 ** 20), (5, 32, 8, 75, 70_000), (65535, 8, 8, 256, 2 ** 31 - 1)):
+        a = _tree(dsk)
+        a.sel_start = a.sel_len = a.sel_count = None
+        a.B, a.Hq, a.Hkv, a.max_nodes, a.mask_words, a.total_rows = B, Hq, Hkv, nodes, 8, rows
+        need = 0
+        for L in lengths:
+            a.max_seqlen = L
+            got = dsk.dsk_tree_attn_workspace_bytes(a)
+            assert got >= max(need, 256), (B, Hq, Hkv, nodes, rows, L)
+            need = got
+        assert need <= 256 + a.n_tokens * Hq * 128 * 520 + 512   # 128 parts of a row at most, (m, l) and 128 channels each
