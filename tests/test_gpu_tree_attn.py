@@ -642,3 +642,80 @@ def test_a_sequence_that_has_no_place_reads_no_other_one(packed, row0, length, k
         want.Kd, want.Vd, want.q, want.seen = c.Kd, c.Vd, c.q, c.seen
         alone = want.run(seq_len=i32([0, 0]))
         assert torch.equal(alone.out[:8], r.out[:8]) and torch.equal(alone.lse[:8], r.lse[:8])
+
+
+# ---- batches whose cache has room for all sequences at max_seqlen: parts of equal lengths, whatever the lengths are -------
+ROOMY = dict(spare=4200)
+
+
+def _even(c):
+    """The split takes such a batch for one of sequences of one length."""
+    assert len(c.lens) > 1 and c.rows >= len(c.lens) * max(c.lens)
+    return c
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("lens, n_new, Hq, Hkv, more", [
+    # 33 to 64 rows a KV head, from 256 x 256 keys times heads on: eight wavefronts a CU
+    ([4096] * 4, [13] * 4, 32, 8, {}),
+    ([4096, 1000, 0, 3333], [13, 0, 16, 9], 32, 8, ROOMY),       # different lengths, one without nodes, an empty prefix
+    ([4095, 33, 4000, 1], [0, 9, 1, 13], 32, 8, ROOMY),
+    ([2048] * 32, [9] * 32, 32, 8, {}),
+    ([2048] * 70, [9] * 69 + [0], 16, 4, dict(pad_tokens=3)),    # more sequences than lanes
+    # 65 to 128 rows
+    ([4096] * 4, [30] * 4, 32, 8, {}),
+    ([4096, 1000, 0, 3333], [30, 0, 32, 17], 32, 8, ROOMY),
+    ([4111] * 3, [120, 1, 77], 16, 16, {}),
+    # more: eight wavefronts' rows at once from 512 keys a part on
+    ([20480] * 2, [40, 40], 32, 8, {}),
+    ([8192] * 8, [64] * 8, 32, 8, {}),
+    ([9001] * 4, [100, 3, 100, 99], 32, 8, {}),                  # two passes
+    ([4096, 1000, 0, 4001], [64, 0, 33, 64], 16, 2, ROOMY),
+])
+def test_batches_of_one_length_and_roomy_ones(lens, n_new, Hq, Hkv, more, packed):
+    _even(Case(lens, n_new, Hq, Hkv, seed=sum(n_new), packed=packed, nhd=packed, **more)).check()
+
+
+@pytest.mark.parametrize("nodes", [13, 30, 64])
+def test_batches_of_one_length_any_mask(nodes):
+    c = _even(Case([4200] * 4, [nodes, nodes, 1, nodes - 1], 32, 8, masks="any", seed=nodes))
+    assert any((~m.any(1)).any() for m in c.seen)
+    c.check()
+
+
+@pytest.mark.parametrize("nodes", [13, 30, 40])
+def test_batches_of_one_length_larger_than_the_memory_side_cache(nodes):
+    c = _even(Case([18501] * 4, [nodes] * 4, 32, 8, seed=nodes))
+    assert c.rows * 8 * 512 >= 288 << 20
+    c.check()
+
+
+@pytest.mark.parametrize("nodes", [13, 30, 64])
+def test_batches_of_one_length_rows_that_are_masked_or_free_may_hold_anything(nodes):
+    c = _even(Case([4097, 4090, 20, 0], [nodes] * 4, 32, 8, seed=nodes, **ROOMY))
+    kws = ({}, dict(want_f32=False, want_bf16=True))
+    clean = [c.run(**kw) for kw in kws]
+    for x in (c.K, c.V):
+        for s in range(4):                                       # the room behind every sequence's nodes
+            x[:, c.row0[s] + c.lens[s] + nodes: c.row0[s + 1]] = float("nan")
+    for kw, want in zip(kws, clean):
+        r = c.run(**kw)
+        assert torch.equal(r.lse, want.lse)
+        assert torch.equal(r.out, want.out) if r.out is not None else torch.equal(r.out_bf16, want.out_bf16)
+    j = nodes - 2
+    for x in (c.K, c.V):
+        for s in range(4):
+            x[:, c.row0[s] + c.lens[s] + j, ::3] = float("nan")
+            x[:, c.row0[s] + c.lens[s] + j, 1::3] = float("inf")
+    blind = torch.from_numpy(np.concatenate([~m[:, j] for m in c.seen])).cuda()
+    for kw, want in zip(kws, clean):
+        r = c.run(**kw)
+        a, b = (x.out if x.out is not None else x.out_bf16 for x in (r, want))
+        assert torch.equal(a[blind], b[blind]) and torch.equal(r.lse[blind], want.lse[blind])
+        assert bool(a[~blind].isnan().any(-1).all())
+
+
+@pytest.mark.parametrize("end", [4096 - 33, 4096 - 1, 4096, 4096 + 1, 4096 + 31, 4096 + 65, 4096 + 127])
+@pytest.mark.parametrize("nodes", [13, 30, 64])
+def test_batches_of_one_length_where_the_prefix_ends_in_any_place_of_a_stage(end, nodes):
+    _even(Case([end] * 5, [nodes] * 5, 32, 8, seed=end)).check()
