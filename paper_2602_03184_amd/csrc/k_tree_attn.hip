@@ -1080,8 +1080,9 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     // Numbered through the parts that there are, each sequence's in turn and the heads fastest, all have the same: eight sequences
     // of 16K to 64K tokens, 13 nodes 283 -> 246 us, 32 nodes 319 -> 283, two of 32K and 64K 101 -> 85; what it costs is that a
     // workgroup looks its part up (16 sequences of 700 tokens 21.7 -> 22.3).  Several passes over the same keys stay as they are:
-    // they have an XCD's L2 in common.
-    t.sp.packed = a.B > 1 && t.q_tiles == 1 && (int64_t)a.B * t.sp.nsplit <= 65535;
+    // they have an XCD's L2 in common.  So do sequences of one part each, of which there may be many: each of their workgroups would
+    // look at all before it (150 of 400 tokens 54.5 us by sequence and 56.8, 1024 of 500 363 and 450, 4096 of 60 0.56 and 1.82 ms).
+    t.sp.packed = a.B > 1 && t.q_tiles == 1 && t.sp.nsplit > 1 && (int64_t)a.B * t.sp.nsplit <= 65535;
     t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
   }
   const size_t parts = t.sp.nsplit > 1 ? (size_t)a.n_tokens * a.Hq * t.sp.nsplit : 0;

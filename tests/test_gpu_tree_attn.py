@@ -719,3 +719,41 @@ def test_batches_of_one_length_rows_that_are_masked_or_free_may_hold_anything(no
 @pytest.mark.parametrize("nodes", [13, 30, 64])
 def test_batches_of_one_length_where_the_prefix_ends_in_any_place_of_a_stage(end, nodes):
     _even(Case([end] * 5, [nodes] * 5, 32, 8, seed=end)).check()
+
+
+@pytest.mark.parametrize("B", [257, 4096, 65535])
+@pytest.mark.parametrize("f32", [True, False])
+def test_as_many_sequences_as_there_may_be(B, f32):
+    """A part each, most of them over one of four prefixes with the nodes' rows in buffers of their own."""
+    dsk, g = _dsk(), torch.Generator(device="cuda")
+    g.manual_seed(B)
+    K, V = (torch.randn(2, 400, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    lens, row0 = [130, 0, 33, 64], [0, 7, 300, 140]
+    kinds = torch.arange(B, device="cuda") % 4
+    two = (torch.arange(B, device="cuda") // 4) % 2              # sequences of two nodes and of one
+    cu = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), (1 + two).cumsum(0)]).int()
+    n = int(cu[-1])
+    first = cu[:-1].long()
+    kind = torch.zeros(n, dtype=torch.int64, device="cuda")
+    for t in (first, (first + two)):
+        kind[t] = kinds
+    second = torch.ones(n, dtype=torch.bool, device="cuda")
+    second[first] = False
+    q4, k4, v4 = (torch.randn(8, h, D, generator=g, device="cuda").bfloat16() for h in (6, 2, 2))
+    pick = 2 * kind + second                                     # a node's rows: by its sequence's kind and its place
+    q, Kd, Vd = q4[pick], k4[pick].transpose(0, 1).contiguous(), v4[pick].transpose(0, 1).contiguous()
+    r = dsk.tree_decode_attn(q, K, V, seq_row0=i32(row0)[kinds], seq_len=i32(lens)[kinds], cu_new=cu, mask=None, max_nodes=2,
+                             max_seqlen=130, Kd=Kd, Vd=Vd, want_f32=f32, want_bf16=not f32)
+    torch.cuda.synchronize()
+    got = (r.out if f32 else r.out_bf16).double()
+    for k in range(4):
+        for h in range(2):
+            p, hs = slice(row0[k], row0[k] + lens[k]), slice(3 * h, 3 * h + 3)
+            w = slice(2 * k, 2 * k + 2)
+            out, size, lse = tree_reference(q4[w, hs], K[h, p], V[h, p], k4[w, h], v4[w, h], np.tril(np.ones((2, 2), dtype=bool)),
+                                            1.0 / math.sqrt(D))
+            for i in range(2):
+                t = (kind == k) & (second == bool(i))
+                bar = F32 * size[i] + (0 if f32 else BF16 * (out[i].abs() * (1 + BF16) + size[i]))
+                assert bool(((got[t][:, hs] - out[i]).abs() <= bar).all())
+                assert bool(((r.lse[t][:, hs].double() - lse[i]).abs() <= 1e-5 * (1 + lse[i].abs())).all())
