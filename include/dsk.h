@@ -590,9 +590,9 @@ typedef struct dsk_norm_rope_args {
  * cu_new[s] + j of these.  A node that sees nothing gets out = 0 and lse = -inf.  K or V rows that no bit
  * lets a node see may hold anything, NaN included.  An infinity in a row of V that a node sees gives that infinity, or NaN with its
  * opposite or where its weight is 2^-80 of the largest or less.  Mask bits of nodes that do not exist are ignored.
- * `out` asks for fp32 accuracy; where only out_bf16 is asked for, the softmax weights are rounded to bf16
- * for the products with V (lse is fp32 in both).  Sums are in fp32, that of the weights with its rounding carried along, those
- * over V rounded once for 16 keys (three times with `out`) of at most a part's, and split over the keys with a merge in a fixed
+ * `out` asks for fp32 accuracy.  Where only out_bf16 is asked for, the softmax weights of the products with V are off by 2^-16 of
+ * each at most, and with max_nodes * Hq / Hkv above 64 they are rounded to bf16 (lse is fp32 in all).  Sums are in fp32, that of the
+ * weights with its rounding carried along, those over V rounded up to three times for 16 keys, split over the keys with a merge in a fixed
  * order; how they are split, and with it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen, total_rows (k and b
  * with a selection) and which outputs are asked for.  A token that several selected slots hold counts as often.
  * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths or spans outside the

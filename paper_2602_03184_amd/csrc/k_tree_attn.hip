@@ -414,10 +414,10 @@ __device__ __forceinline__ float tree_max(const tree_f32x16& z) {
   return tree_half_max(m);
 }
 
-// The weights of a tile, in TERMS bf16 terms.  A single term is rounded to nearest.  Three are cut towards zero, 8 bits each, and what
-// is left is made a little more each time, so that no term of a weight above 2^-80 is 0 or negative: an infinite value then stays
-// infinite in the sum over them, where 0 * inf and inf - inf would make it NaN.  The terms add up to 1.1 * 2^-24 .. 3 * 2^-24 more
-// than the weight (2^-23 in the mean; taking what is left exactly and bounding the terms from below made fp32 calls 3 to 5 % slower).
+// The weights of a tile, in TERMS bf16 terms.  A single term, or the last of two, is rounded to nearest.  The others are cut towards
+// zero, 8 bits each, and what is left is made a little more each time, so that no term of a weight above 2^-80 is 0 or negative: an infinite value then stays
+// infinite in the sum over them, where 0 * inf and inf - inf would make it NaN.  Two terms are off by 2^-16 of the
+// weight at most, three add up to 1.1 * 2^-24 .. 3 * 2^-24 more than it (2^-23 in the mean; taking what is left exactly and bounding the terms from below made fp32 calls 3 to 5 % slower).
 template <int TERMS>
 struct TreeWeights {
   tree_bf16x8 w[TERMS][2];
@@ -430,7 +430,7 @@ struct TreeWeights {
         if constexpr (TERMS == 1) {
           x[i] = tree_pack(p[2 * i], p[2 * i + 1]);
         } else {
-          x[i] = tree_pack_cut(p[2 * i], p[2 * i + 1]);
+          x[i] = TERMS == 2 && term == 1 ? tree_pack(p[2 * i], p[2 * i + 1]) : tree_pack_cut(p[2 * i], p[2 * i + 1]);
           if (term + 1 < TERMS) {                        // what the terms so far leave
             const float more = term == 0 ? 1.0f + 0x1p-23f : 1.0f + 0x1p-17f;
             p[2 * i] = fmaf(p[2 * i], more, -bf16_lo(x[i]));
@@ -630,7 +630,8 @@ __device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const Tr
   }
 }
 
-// TERMS: bf16 terms that a weight is split into for the second product, 1 (bf16 result) or 3 (all 24 bits of it: fp32 result).
+// TERMS: bf16 terms that a weight is split into for the second product: 3 for fp32 results, 2 for bf16 ones, or 1 of these where the
+// products bound the call.
 // KW wavefronts take other tiles of a stage for the same queries, NT of them each.  With two BUFS a stage is copied while the one
 // before it is multiplied; with one (32 rows, whose products are short) that is left to the second workgroup of the CU.
 // HBM bounds it: 40 / 40 heads, 128K tokens, 16 nodes (2.68 GB) 396 us, 6.8 TB/s; 32 / 8 heads, 16 nodes (0.54 GB) 88, 6.1; eight of
@@ -1132,23 +1133,40 @@ static dim3 tree_grid(const dsk_tree_attn_args& a, const TreeLaunch& t) {
   return t.sp.packed ? dim3(y, (unsigned)(a.B * t.sp.nsplit)) : dim3((unsigned)t.sp.nsplit, y, (unsigned)a.B);
 }
 
+// Rows of a KV head up to which a bf16 result's weights have two terms.  HBM or latency bounds those calls: 32 / 8 heads, 16 nodes: 128K
+// tokens 91 us with one and 92 with two, 32K 31.6 and 32.2, 8K 18.3 and 19.3; eight of 16K to 64K, 13 nodes 201 and 204; 40 / 40 heads, 128K
+// 402 and 402.  Beyond, the products do: 32 nodes, 128K 113 and 136, eight of 16K to 64K 247 and 303, 64 nodes, 128K 171 and 224.
+constexpr int kTreeTwoTermRows = 64;
+
 template <int QW, int KW, int NT, int BUFS, bool MAY_SELECT>
 static void launch_tree(const dsk_tree_attn_args& a, const TreeLaunch& t, float scale_log2, float2* ml, float* acc, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
   const dim3 grid = tree_grid(a, t), block(QW * KW * DSK_WAVE);
-#define DSK_TREE(terms)                                                                                                        \
-  do {                                                                                                                         \
-    if (MAY_SELECT && a.sel_start != nullptr)                                                                                  \
-      tree_attn_kernel<QW, KW, NT, BUFS, terms, MAY_SELECT, false>                                                             \
-          <<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);                                                \
-    else if (t.stream)                                                                                                         \
-      tree_attn_kernel<QW, KW, NT, BUFS, terms, false, true><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc); \
-    else                                                                                                                       \
-      tree_attn_kernel<QW, KW, NT, BUFS, terms, false, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc); \
-  } while (0)
-  if (a.out != nullptr) DSK_TREE(3);
-  else DSK_TREE(1);
-#undef DSK_TREE
+  auto go = [&](auto terms, auto may_stream) {
+    constexpr int kTerms = decltype(terms)::value;
+    constexpr bool kStream = decltype(may_stream)::value;
+    if (MAY_SELECT && a.sel_start != nullptr)
+      tree_attn_kernel<QW, KW, NT, BUFS, kTerms, MAY_SELECT, false>
+          <<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
+    else if (kStream && t.stream)
+      tree_attn_kernel<QW, KW, NT, BUFS, kTerms, false, kStream><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
+    else
+      tree_attn_kernel<QW, KW, NT, BUFS, kTerms, false, false><<<grid, block, 0, st>>>(a, G, t.q_tiles, t.sp, scale_log2, ml, acc);
+  };
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  using Three = std::integral_constant<int, 3>;
+  static_assert(kTreeTwoTermRows == 2 * kTreeTile, "one wavefront's rows always have two terms, four wavefronts' never");
+  if (a.out != nullptr) {
+    go(Three(), std::true_type());
+  } else if constexpr (QW == 1) {
+    go(Two(), std::true_type());
+  } else if constexpr (QW == 2) {
+    if (a.max_nodes * G <= kTreeTwoTermRows) go(Two(), std::true_type());
+    else go(One(), std::false_type());                   // two passes and more
+  } else {
+    go(One(), std::true_type());
+  }
 }
 
 hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st) {

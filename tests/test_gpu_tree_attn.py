@@ -757,3 +757,25 @@ def test_as_many_sequences_as_there_may_be(B, f32):
                 bar = F32 * size[i] + (0 if f32 else BF16 * (out[i].abs() * (1 + BF16) + size[i]))
                 assert bool(((got[t][:, hs] - out[i]).abs() <= bar).all())
                 assert bool(((r.lse[t][:, hs].double() - lse[i]).abs() <= 1e-5 * (1 + lse[i].abs())).all())
+
+
+@pytest.mark.parametrize("lens, n_new, Hq, Hkv, k", [
+    ([0, 1, 31, 32, 33, 64, 127, 700], [8] * 8, 8, 2, 0),        # 32 rows
+    ([300, 9], [16, 16], 32, 8, 0),                              # 64
+    ([9000], [16], 32, 8, 0),
+    ([20000, 30], [1, 1], 4, 4, 0),
+    ([4096] * 4, [13] * 4, 32, 8, 0),
+    ([75001], [5], 8, 8, 0),                                     # 288 MB and more
+    ([75001], [12], 32, 8, 0),
+    ([1500, 40], [8, 8], 8, 2, 40),                              # a selection
+    ([1500, 40], [16, 3], 16, 4, 40),
+])
+def test_bf16_results_of_up_to_64_rows_are_rounded_once(lens, n_new, Hq, Hkv, k):
+    """Their weights are off by 2^-16 of each, and so is the sum by 2^-16 of its size, beside the rounding of the result."""
+    c = Case(lens, n_new, Hq, Hkv, seed=95)
+    if k:
+        c.select(k, 16)
+    out, size, _ = c.reference()
+    r = c.run(want_f32=False, want_bf16=True)
+    near = (F32 + 2.0 ** -16) * size
+    assert bool(((r.out_bf16.double() - out).abs() <= BF16 * (out.abs() + near) + near).all())
