@@ -548,7 +548,7 @@ typedef struct dsk_step_plan_args {
  *   the first rot_dim channels of y rotated by the angles tok_pos[t] * inv_freq[i], i < rot_dim / 2:
  *   (a, b) -> (a cos - b sin, a sin + b cos) with the pair (a, b) = channels (i, i + rot_dim / 2), or
  *   (2i, 2i + 1) with DSK_ROPE_INTERLEAVED
- * in fp32, angles reduced in fp64, rounded to bf16 once.  Queries go to q_out, keys to row tok_row[t] of K, values as they
+ * in fp32, angles reduced in fp64, rounded to bf16 once; channels from rot_dim on stay y.  Queries go to q_out, keys to row tok_row[t] of K, values as they
  * are to the same row of V.  A token whose tok_row is outside [0, total_rows) is skipped: nothing of it
  * is written, q_out included.  The rows of tokens that are not skipped must be distinct.  Outputs overlap no input, but
  * q_out may be q itself if q is packed.  Inputs are strided views, e.g. of one fused projection's output.
@@ -560,7 +560,7 @@ typedef struct dsk_norm_rope_args {
   int32_t n_tokens;            /* [host] >= 0 */
   int32_t Hq, Hkv, D;
   const void* q;               /* [dev] bf16 [n_tokens, Hq, D], or NULL: no queries in this call */
-  const void* k;               /* [dev] bf16 [n_tokens, Hkv, D], or NULL */
+  const void* k;               /* [dev] bf16 [n_tokens, Hkv, D], or NULL; q or k has to be there */
   const void* v;               /* [dev] bf16 [n_tokens, Hkv, D], or NULL: V is not written */
   int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head; /* multiples of 8 */
   const float* q_weight;       /* [dev] optional [D]: norm of the queries */

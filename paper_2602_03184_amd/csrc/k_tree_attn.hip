@@ -630,12 +630,11 @@ __device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const Tr
   }
 }
 
-// TERMS: bf16 terms that a weight is split into for the second product: 3 for fp32 results, 2 for bf16 ones, or 1 of these where the
-// products bound the call.
+// TERMS: bf16 terms that a weight is split into for the second product: 3 for fp32 results, 2 for bf16 ones, 1 above 64 rows.
 // KW wavefronts take other tiles of a stage for the same queries, NT of them each.  With two BUFS a stage is copied while the one
 // before it is multiplied; with one (32 rows, whose products are short) that is left to the second workgroup of the CU.
-// HBM bounds it: 40 / 40 heads, 128K tokens, 16 nodes (2.68 GB) 396 us, 6.8 TB/s; 32 / 8 heads, 16 nodes (0.54 GB) 88, 6.1; eight of
-// 16K to 64K, 13 nodes, token-major (1.48 GB) 238 to 244, 6.1 to 6.2.  Where 4 wavefronts take 128 rows, their matrix instructions
+// HBM bounds it: 40 / 40 heads, 128K tokens, 16 nodes (2.68 GB) 395 us, 6.8 TB/s; 32 / 8 heads, 16 nodes (0.54 GB) 88, 6.1; eight of
+// 16K to 64K, 13 nodes, token-major (1.48 GB) 240 to 250, 5.9 to 6.2.  Where 4 wavefronts take 128 rows, their matrix instructions
 // and exponentials, about as many cycles each, no longer hide entirely: 32 nodes, 0.54 GB at 5.0 TB/s.
 template <int QW, int KW, int NT, int BUFS, int TERMS, bool SEL, bool STREAM>
 __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
@@ -751,8 +750,9 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
 // the second its half of step i + 2 (slot 2 i + 2), so a step is whole one slot before its first use, and the step that it
 // replaces was last read long before.  Loads are issued 64 KB before they are put.
 // 32 / 8 heads, 64 nodes, 128K tokens: 137 GFLOP in 154 us while the chip is cool (0.89 PFLOP/s; a large library product reaches
-// 1.15), 190 without pause: a slot of a SIMD has 512 cycles of products next to 490 to 600 of exponentials, and the clock goes
-// down to what power leaves.  Taking tiles one after the other in every wavefront took 212.
+// 1.15), 190 without pause, when the clock is lower.  As counted, a slot takes 1020 cycles of a CU, about what its 512 cycles of
+// products and 490 to 600 of exponentials take one after the other (matrix cores 0.49 busy, LDS 0.30): the two groups take turns more
+// than they overlap, and what holds them apart has not been found.  Taking tiles one after the other in every wavefront took 212.
 constexpr int kWideWaves = 8;
 
 template <bool STREAM>
@@ -1135,7 +1135,8 @@ static dim3 tree_grid(const dsk_tree_attn_args& a, const TreeLaunch& t) {
 
 // Rows of a KV head up to which a bf16 result's weights have two terms.  HBM or latency bounds those calls: 32 / 8 heads, 16 nodes: 128K
 // tokens 91 us with one and 92 with two, 32K 31.6 and 32.2, 8K 18.3 and 19.3; eight of 16K to 64K, 13 nodes 201 and 204; 40 / 40 heads, 128K
-// 402 and 402.  Beyond, the products do: 32 nodes, 128K 113 and 136, eight of 16K to 64K 247 and 303, 64 nodes, 128K 171 and 224.
+// 402 and 402.  Beyond, products and their weights count: 32 nodes, 128K 113 and 136, eight of 16K to 64K 247 and 303, a selection of
+// 4096 tokens 18.9 and 20.0, eight of them 45 and 52; 64 nodes, 128K 171 and 224.
 constexpr int kTreeTwoTermRows = 64;
 
 template <int QW, int KW, int NT, int BUFS, bool MAY_SELECT>
