@@ -548,9 +548,9 @@ typedef struct dsk_step_plan_args {
  *   the first rot_dim channels of y rotated by the angles tok_pos[t] * inv_freq[i], i < rot_dim / 2:
  *   (a, b) -> (a cos - b sin, a sin + b cos) with the pair (a, b) = channels (i, i + rot_dim / 2), or
  *   (2i, 2i + 1) with DSK_ROPE_INTERLEAVED
- * in fp32, angles reduced in fp64, rounded to bf16 once; channels from rot_dim on stay y.  Queries go to q_out, keys to row tok_row[t] of K, values as they
- * are to the same row of V.  A token whose tok_row is outside [0, total_rows) is skipped: nothing of it
- * is written, q_out included.  The rows of tokens that are not skipped must be distinct.  Outputs overlap no input, but
+ * in fp32, angles reduced in fp64, rounded to bf16 once; channels from rot_dim on stay y.  Queries go to q_out, keys to row
+ * tok_row[t] of K, values as they are to the same row of V.  A token whose tok_row is outside [0, total_rows) is skipped: nothing
+ * of it is written, q_out included.  The rows of tokens that are not skipped must be distinct.  Outputs overlap no input, but
  * q_out may be q itself if q is packed.  Inputs are strided views, e.g. of one fused projection's output.
  * ---------------------------------------------------------------------------------------- */
 #define DSK_ROPE_INTERLEAVED 1u

@@ -415,9 +415,10 @@ __device__ __forceinline__ float tree_max(const tree_f32x16& z) {
 }
 
 // The weights of a tile, in TERMS bf16 terms.  A single term, or the last of two, is rounded to nearest.  The others are cut towards
-// zero, 8 bits each, and what is left is made a little more each time, so that no term of a weight above 2^-80 is 0 or negative: an infinite value then stays
-// infinite in the sum over them, where 0 * inf and inf - inf would make it NaN.  Two terms are off by 2^-16 of the
-// weight at most, three add up to 1.1 * 2^-24 .. 3 * 2^-24 more than it (2^-23 in the mean; taking what is left exactly and bounding the terms from below made fp32 calls 3 to 5 % slower).
+// zero, 8 bits each, and what is left is made a little more each time, so that no term of a weight above 2^-80 is 0 or negative: an
+// infinite value then stays infinite in the sum over them, where 0 * inf and inf - inf would make it NaN.  Two terms are off by 2^-16
+// of the weight at most; three add up to 1.1 * 2^-24 .. 3 * 2^-24 more than it (2^-23 in the mean; taking what is left exactly and
+// bounding the terms from below made fp32 calls 3 to 5 % slower).
 template <int TERMS>
 struct TreeWeights {
   tree_bf16x8 w[TERMS][2];
