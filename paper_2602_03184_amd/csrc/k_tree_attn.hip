@@ -4,17 +4,13 @@
 // stream, 512 bytes and 512 R flop a key.  Up to some 150 rows HBM bounds that, beyond it the matrix cores do, so both products
 // run on them and K and V are read once per 32 * QW rows.
 //
-// Products are taken transposed: S^T = K Q^T, then O^T = V^T P^T, with 32x32x16 matrix instructions.  A lane then has one query
-// (column lane % 32) and 16 of a tile's 32 keys, so the softmax needs one exchange between the two halves of the wavefront for the
-// maximum, rescaling is a product by a lane's own factor, and the weights that S^T leaves in a lane are already those that the
-// second product wants there: key 16 t + 8 (e / 4) + 4 (lane / 32) + e % 4 in place e of step t, if V^T is read with the same
-// order of keys (two transposing LDS reads of four keys each).  No weight passes through LDS.
+// The products and the softmax are those of dsk_attn_tile.hpp.
 //
 // K and V tiles lie in LDS with their 16-byte chunks swizzled by row, so that the reads of both products and the writes are free
 // of bank conflicts.  The general kernel copies stages of the prefix straight to LDS; the one for many rows has a schedule of its
 // own and takes them through registers.  Stages that hold nodes go through registers in both, where what a mask
 // may hide is looked at.
-#include "dsk_attn_fold.hpp"
+#include "dsk_attn_tile.hpp"
 #include "dsk_common.hpp"
 #include "dsk_internal.hpp"
 
@@ -22,60 +18,12 @@
 
 namespace dsk {
 
-typedef __bf16 tree_bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 tree_bf16x2 __attribute__((ext_vector_type(2)));
-typedef float tree_f32x16 __attribute__((ext_vector_type(16)));
-typedef float tree_f32x2 __attribute__((ext_vector_type(2)));
-typedef short tree_s16x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kTreeTile = 32;                   // keys and queries of a matrix tile
-constexpr int kTreeRowBytes = 2 * DSK_HEAD_DIM;
 constexpr int kTreeMaxSlots = 256;              // selected slots of a workgroup
 constexpr int kTreeMaxListed = 2048;            // and their tokens
 // Parts of a sequence at most.  One KV head (4 query heads, 16 nodes, 128K tokens): 36.1 us with 64, 29.5 with 128, 29.6 with 256;
 // four sequences of 32K: 23.1, 25.9 and 33.6.
 constexpr int kTreeMaxSplit = 128;
 constexpr int kTreeMixedTiles = 16;             // tiles from the first one with a node on: 256 nodes, and a stage's other tiles
-constexpr int kTreeTileBytes = kTreeTile * kTreeRowBytes;
-
-__device__ __forceinline__ uint32_t tree_pack(float lo, float hi) {   // nearest-even bf16 pair
-  const tree_f32x2 f = {lo, hi};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, tree_bf16x2));
-}
-
-__device__ __forceinline__ uint32_t tree_pack_cut(float lo, float hi) {   // a bf16 pair, towards zero
-  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
-}
-
-// 16 bytes at a uniform address and a lane's 32-bit offset, which is one instruction and no arithmetic; left to itself the
-// compiler adds the parts the other way round, with a 64-bit product or sum per lane and load.
-typedef const __attribute__((address_space(1))) char* tree_global;
-template <bool STREAM>
-__device__ __forceinline__ uint4 load16_at(tree_global base, uint32_t off) {
-  asm("" : "+s"(base));
-  typedef const __attribute__((address_space(1))) u32x4_t* at_t;
-  const at_t at = (at_t)(base + off);
-  u32x4_t v;
-  if constexpr (STREAM) v = __builtin_nontemporal_load(at);
-  else v = *at;
-  return make_uint4(v.x, v.y, v.z, v.w);
-}
-
-// 16 bytes of each lane from its address to LDS, lane after lane from a uniform address on
-template <bool STREAM>
-__device__ __forceinline__ void lds_copy16(const void* from, unsigned char* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0,
-                                   STREAM ? 2 : 0);
-}
-// every copy of this wavefront has arrived
-__device__ __forceinline__ void lds_copies_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }
-
-// a bf16 pair with 0 for what is not finite
-__device__ __forceinline__ uint32_t finite_bf16(uint32_t w) {
-  if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
-  if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
-  return w;
-}
 
 // bits x of a node's mask row for nodes 32 w .. 32 w + 31, of those that exist
 struct TreeMask {
@@ -212,7 +160,7 @@ struct TreeKeys {
   int64_t kst, vst, row0;
   const uint16_t *K, *V, *Kn, *Vn;      // this lane's chunk of the prefix (of the whole cache with SEL) and of the nodes
   int64_t knst, vnst;
-  tree_global Ku, Vu;                   // the prefix of the head, without the lane's part
+  tile_global Ku, Vu;                   // the prefix of the head, without the lane's part
   uint32_t k_off, v_off;                // the lane's part in bytes
   const int32_t* rows;                  // cache rows of the selected tokens, in LDS
   struct Regs {
@@ -230,8 +178,8 @@ struct TreeKeys {
     rows = sm_rows;
     K = static_cast<const uint16_t*>(a.K) + hk * a.k_stride_head + row0 * kst;
     V = static_cast<const uint16_t*>(a.V) + hk * a.v_stride_head + row0 * vst;
-    Ku = (tree_global)K;
-    Vu = (tree_global)V;
+    Ku = (tile_global)K;
+    Vu = (tile_global)V;
     k_off = (uint32_t)(lrow * (int)kst + lc * 8) * 2u;   // 32 rows of 2^24 channels at most
     v_off = (uint32_t)(lrow * (int)vst + lc * 8) * 2u;
     K += lc * 8;
@@ -318,8 +266,8 @@ struct TreeKeys {
       const int row = lrow + u * kRowStep, t = t0 + row;
       const int kc = (lc ^ (row & 15)) - lc, vc = (lc ^ ((row & 3) << 2)) - lc;
       const int64_t r = SEL ? rows[t] : t;
-      lds_copy16<STREAM>(K + r * kst + kc * 8, sm_k + (u * kRowStep + w_row) * kTreeRowBytes);
-      lds_copy16<STREAM>(V + r * vst + vc * 8, sm_v + (u * kRowStep + w_row) * kTreeRowBytes);
+      lds_copy16<STREAM>(K + r * kst + kc * 8, sm_k + (u * kRowStep + w_row) * kTileRowBytes);
+      lds_copy16<STREAM>(V + r * vst + vc * 8, sm_v + (u * kRowStep + w_row) * kTileRowBytes);
     }
   }
   // sm_bad: a word per tile from t_mixed on, zero before; rows of V that hold values that are not finite
@@ -333,21 +281,19 @@ struct TreeKeys {
         // a masked row may hold anything, and 0 * NaN is NaN: such values stay out of the product, and their row is noted
         v = make_uint4(finite_bf16(v.x), finite_bf16(v.y), finite_bf16(v.z), finite_bf16(v.w));
         if (v.x != x.v[u].x || v.y != x.v[u].y || v.z != x.v[u].z || v.w != x.v[u].w)
-          atomicOr(&sm_bad[(t0 - t_mixed + row) / kTreeTile], 1u << (row % kTreeTile));
+          atomicOr(&sm_bad[(t0 - t_mixed + row) / kAttnTile], 1u << (row % kAttnTile));
       }
-      *reinterpret_cast<uint4*>(sm_k + row * kTreeRowBytes + ((lc ^ (row & 15)) << 4)) = x.k[u];
-      *reinterpret_cast<uint4*>(sm_v + row * kTreeRowBytes + ((lc ^ ((row & 3) << 2)) << 4)) = v;
+      *reinterpret_cast<uint4*>(sm_k + row * kTileRowBytes + ((lc ^ (row & 15)) << 4)) = x.k[u];
+      *reinterpret_cast<uint4*>(sm_v + row * kTileRowBytes + ((lc ^ ((row & 3) << 2)) << 4)) = v;
     }
   }
 };
 
-// A wavefront's 32 queries: a lane has query lane % 32 and of a tile's 32 keys those at 8 (i / 4) + 4 (lane / 32) + i % 4.
-struct TreeQueries {
+struct TreeQueries : TileQueries {
   bool busy, real;      // the wavefront has rows; the lane's row exists
-  int col, half, node;
+  int node;
   int64_t out_row;
   TreeMask mask;
-  tree_bf16x8 q[8];     // channels 16 t + 8 half .. + 7
 
   __device__ __forceinline__ TreeQueries(const dsk_tree_attn_args& a, const TreePlace& at, int G, int hk, int r0) {
     const int lane = threadIdx.x & (DSK_WAVE - 1);
@@ -363,7 +309,7 @@ struct TreeQueries {
     for (int t = 0; t < 8; ++t) {
       uint4 x = make_uint4(0, 0, 0, 0);
       if (real) x = *reinterpret_cast<const uint4*>(from + t * 16);
-      q[t] = __builtin_bit_cast(tree_bf16x8, x);
+      q[t] = __builtin_bit_cast(tile_bf16x8, x);
     }
     mask.row = a.mask != nullptr ? a.mask + (int64_t)(at.tok0 + node) * a.mask_words : nullptr;
     mask.node = node;
@@ -372,142 +318,11 @@ struct TreeQueries {
   __device__ __forceinline__ uint32_t allowed(int t0, int P) const { return real ? mask.window(t0 - P) : 0u; }
 };
 
-// Fragments of a tile of 32 keys.
-struct TreeKFrag {
-  tree_bf16x8 k[8];
-  template <int FROM, int TO>
-  __device__ __forceinline__ void read(const unsigned char* sm_k, const TreeQueries& qs) {
-    const unsigned char* at = sm_k + qs.col * kTreeRowBytes;
-#pragma unroll
-    for (int t = FROM; t < TO; ++t)
-      k[t] = *reinterpret_cast<const tree_bf16x8*>(at + (((2 * t + qs.half) ^ (qs.col & 15)) << 4));
-  }
-  // logits: S^T = K Q^T
-  template <int FROM, int TO>
-  __device__ __forceinline__ void add(tree_f32x16& z, const TreeQueries& qs) const {
-    if constexpr (FROM == 0) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z[i] = 0.0f;
-    }
-#pragma unroll
-    for (int t = FROM; t < TO; ++t) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[t], qs.q[t], z, 0, 0, 0);
-  }
-};
-
-__device__ __forceinline__ void tree_hide(tree_f32x16& z, uint32_t allow, int half) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    z[i] = (allow >> (8 * (i >> 2) + 4 * half + (i & 3))) & 1u ? z[i] : -__builtin_inff();
-}
-
-// the larger of a value and the other half's
-__device__ __forceinline__ float tree_half_max(float v) {
-  const uint32_t u = __float_as_uint(v);
-  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
-__device__ __forceinline__ float tree_max(const tree_f32x16& z) {
-  float m = z[0];
-#pragma unroll
-  for (int i = 1; i < 16; ++i) m = fmaxf(m, z[i]);
-  return tree_half_max(m);
-}
-
-// The weights of a tile, in TERMS bf16 terms.  A single term, or the last of two, is rounded to nearest.  The others are cut towards
-// zero, 8 bits each, and what is left is made a little more each time, so that no term of a weight above 2^-80 is 0 or negative: an
-// infinite value then stays infinite in the sum over them, where 0 * inf and inf - inf would make it NaN.  Two terms are off by 2^-16
-// of the weight at most; three add up to 1.1 * 2^-24 .. 3 * 2^-24 more than it (2^-23 in the mean; taking what is left exactly and
-// bounding the terms from below made fp32 calls 3 to 5 % slower).
-template <int TERMS>
-struct TreeWeights {
-  tree_bf16x8 w[TERMS][2];
-  __device__ __forceinline__ void set(float (&p)[16]) {
-#pragma unroll
-    for (int term = 0; term < TERMS; ++term) {
-      uint32_t x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (TERMS == 1) {
-          x[i] = tree_pack(p[2 * i], p[2 * i + 1]);
-        } else {
-          x[i] = TERMS == 2 && term == 1 ? tree_pack(p[2 * i], p[2 * i + 1]) : tree_pack_cut(p[2 * i], p[2 * i + 1]);
-          if (term + 1 < TERMS) {                        // what the terms so far leave
-            const float more = term == 0 ? 1.0f + 0x1p-23f : 1.0f + 0x1p-17f;
-            p[2 * i] = fmaf(p[2 * i], more, -bf16_lo(x[i]));
-            p[2 * i + 1] = fmaf(p[2 * i + 1], more, -bf16_hi(x[i]));
-          }
-        }
-      }
-      w[term][0] = __builtin_bit_cast(tree_bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
-      w[term][1] = __builtin_bit_cast(tree_bf16x8, make_uint4(x[4], x[5], x[6], x[7]));
-    }
-  }
-};
-
-struct TreeVFrag {
-  tree_bf16x8 v[4][2];
-  // a lane's place in a tile for channels 32 ct .. 32 ct + 31
-  static __device__ __forceinline__ int place(int ct) {
-    const int lane = threadIdx.x & (DSK_WAVE - 1), half = lane >> 5;
-    const int quad = (lane & 15) >> 2;                   // of the four keys of a transposing read
-    return (4 * half + quad) * kTreeRowBytes + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + ((lane & 1) << 3) + ((ct ^ quad) << 6);
-  }
-  template <int T>                                       // 16 of the keys
-  __device__ __forceinline__ void read(const unsigned char* sm_v) {
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct) {
-      const unsigned char* at = sm_v + place(ct) + T * 16 * kTreeRowBytes;
-      const tree_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) tree_s16x4*)(at));
-      const tree_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) tree_s16x4*)(at + 8 * kTreeRowBytes));
-      v[ct][T] = __builtin_bit_cast(tree_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
-  }
-  // All 32 keys while copies to other parts of LDS are under way: for the builtin the compiler would wait for those first, as it
-  // does not see that they are other parts.
-  __device__ __forceinline__ void read_beside_copies(const unsigned char* sm_v) {
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)sm_v;
-    u32x2 x[4][4];
-    static_assert(kTreeRowBytes == 256, "offsets: 8 rows");
-    asm volatile(
-        "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:2048\n\t"
-        "ds_read_b64_tr_b16 %4, %17\n\tds_read_b64_tr_b16 %5, %17 offset:2048\n\t"
-        "ds_read_b64_tr_b16 %8, %18\n\tds_read_b64_tr_b16 %9, %18 offset:2048\n\t"
-        "ds_read_b64_tr_b16 %12, %19\n\tds_read_b64_tr_b16 %13, %19 offset:2048\n\t"
-        "ds_read_b64_tr_b16 %2, %16 offset:4096\n\tds_read_b64_tr_b16 %3, %16 offset:6144\n\t"
-        "ds_read_b64_tr_b16 %6, %17 offset:4096\n\tds_read_b64_tr_b16 %7, %17 offset:6144\n\t"
-        "ds_read_b64_tr_b16 %10, %18 offset:4096\n\tds_read_b64_tr_b16 %11, %18 offset:6144\n\t"
-        "ds_read_b64_tr_b16 %14, %19 offset:4096\n\tds_read_b64_tr_b16 %15, %19 offset:6144\n\t"
-        "s_waitcnt lgkmcnt(0)"
-        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[0][2]), "=&v"(x[0][3]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[1][2]),
-          "=&v"(x[1][3]), "=&v"(x[2][0]), "=&v"(x[2][1]), "=&v"(x[2][2]), "=&v"(x[2][3]), "=&v"(x[3][0]), "=&v"(x[3][1]),
-          "=&v"(x[3][2]), "=&v"(x[3][3])
-        : "v"(at + place(0)), "v"(at + place(1)), "v"(at + place(2)), "v"(at + place(3))
-        : "memory");
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        v[ct][t] = __builtin_bit_cast(tree_bf16x8, make_uint4(x[ct][2 * t].x, x[ct][2 * t].y, x[ct][2 * t + 1].x, x[ct][2 * t + 1].y));
-  }
-  // O^T += V^T P^T
-  template <int TERMS>
-  __device__ __forceinline__ void add(tree_f32x16 (&O)[4], const TreeWeights<TERMS>& p, int t) const {   // 16 of the keys
-#pragma unroll
-    for (int term = TERMS - 1; term >= 0; --term)
-#pragma unroll
-      for (int ct = 0; ct < 4; ++ct)
-        O[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[ct][t], p.w[term][t], O[ct], 0, 0, 0);
-  }
-};
-
 // The values that put() left out of a tile, for the nodes that see them.
 template <class KEYS>
-__device__ __forceinline__ void tree_values_left_out(tree_f32x16 (&O)[4], const KEYS& keys, const uint32_t* sm_bad,
+__device__ __forceinline__ void tree_values_left_out(tile_f32x16 (&O)[4], const KEYS& keys, const uint32_t* sm_bad,
                                                      uint32_t allow, int t0, int half) {
-  for (uint32_t bad = __builtin_amdgcn_readfirstlane(sm_bad[(t0 - keys.t_mixed) / kTreeTile]); bad != 0; bad &= bad - 1) {
+  for (uint32_t bad = __builtin_amdgcn_readfirstlane(sm_bad[(t0 - keys.t_mixed) / kAttnTile]); bad != 0; bad &= bad - 1) {
     const int j = __builtin_ctz(bad);
     if (!((allow >> j) & 1u)) continue;
     const uint16_t* v = keys.v_at(t0 + j) - keys.lc * 8 + 4 * half;
@@ -521,89 +336,8 @@ __device__ __forceinline__ void tree_values_left_out(tree_f32x16 (&O)[4], const 
   }
 }
 
-__device__ __forceinline__ void tree_scale(tree_f32x16 (&O)[4], float f) {
-#pragma unroll
-  for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) O[ct][i] *= f;
-}
-
-// A query's running softmax: the reference of its exponents in log2 units (-inf: nothing seen) and this half's sum l - err.  A tile's
-// weights are added up by themselves and join the sum with what rounding took from it carried along: added one after the other, equal
-// weights are rounded alike, 1e-4 of the sum after 8192 of them.
-struct TreeSoftmax {
-  float m, l, err, scale_log2;
-  FmaExponent exponent;
-  __device__ __forceinline__ explicit TreeSoftmax(float scale) : m(-__builtin_inff()), l(0.0f), err(0.0f), scale_log2(scale), exponent(scale, 0.0f) {}
-  // weights of a tile from its logits
-  template <int TERMS>
-  __device__ __forceinline__ void take(const tree_f32x16& z, tree_f32x16 (&O)[4], TreeWeights<TERMS>& w) {
-    const float mx = tree_max(z) * scale_log2;
-    // The reference only has to be near the maximum: it moves when a query's maximum grows by more than 8, so most tiles
-    // rescale nothing, and the weights stay below 2^8.
-    if (__any(mx - m > 8.0f)) {                          // m = -inf: true unless nothing has been seen
-      const float m_new = fmaxf(m, mx);
-      const float f = m == -__builtin_inff() ? 0.0f : exp2_small(m - m_new);
-      l *= f;
-      err *= f;
-      tree_scale(O, f);
-      m = m_new;
-      exponent = FmaExponent(scale_log2, m == -__builtin_inff() ? 0.0f : m);
-    }
-    float p[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = exp2_small(exponent.of(z[i]));
-    const float tile = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])) +
-                       (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
-    const float add = tile - err, sum = l + add;
-    err = (sum - l) - add;
-    l = sum;
-    w.set(p);
-  }
-  // both halves' sum
-  __device__ __forceinline__ void close() {
-    l -= err;
-    l += shfl_xor_f(l, 32);
-  }
-};
-
-// The states of KW wavefronts that took other keys for the same queries, in order, into that of the first (kw = 0).
-// sm_o: (KW - 1) * QW blocks of 64 values of 64 lanes.
-template <int QW, int KW>
-__device__ __forceinline__ void tree_join(TreeSoftmax& sm, tree_f32x16 (&O)[4], bool busy, int qw, int kw, float* sm_o, float2* sm_ml) {
-  const int lane = threadIdx.x & (DSK_WAVE - 1);
-  if (kw > 0 && busy) {
-    const int blk = (kw - 1) * QW + qw;
-    sm_ml[blk * DSK_WAVE + lane] = make_float2(sm.m, sm.l);
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sm_o[(blk * 64 + ct * 16 + i) * DSK_WAVE + lane] = O[ct][i];
-  }
-  __syncthreads();
-  if (kw > 0 || !busy) return;
-  float M = sm.m;
-#pragma unroll
-  for (int o = 0; o < KW - 1; ++o) M = fmaxf(M, sm_ml[(o * QW + qw) * DSK_WAVE + lane].x);
-  const float f = sm.m == -__builtin_inff() ? 0.0f : exp2_small(sm.m - M);
-  sm.l *= f;
-  tree_scale(O, f);
-#pragma unroll
-  for (int o = 0; o < KW - 1; ++o) {
-    const int blk = o * QW + qw;
-    const float2 ml = sm_ml[blk * DSK_WAVE + lane];
-    const float fo = ml.x == -__builtin_inff() ? 0.0f : exp2_small(ml.x - M);
-    sm.l = fmaf(ml.y, fo, sm.l);
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) O[ct][i] = fmaf(sm_o[(blk * 64 + ct * 16 + i) * DSK_WAVE + lane], fo, O[ct][i]);
-  }
-  sm.m = M;
-}
-
 // A lane's row: final, or this part's share.  Its channels lie four in a row, at 32 ct + 8 i + 4 half.
-__device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const TreeQueries& qs, const tree_f32x16 (&O)[4], float m,
+__device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const TreeQueries& qs, const tile_f32x16 (&O)[4], float m,
                                            float l, int used, int nsplit, int split, float2* part_ml, float* part_acc) {
   if (!qs.real) return;
   if (used == 1) {
@@ -616,7 +350,7 @@ __device__ __forceinline__ void tree_store(const dsk_tree_attn_args& a, const Tr
         const int64_t at = qs.out_row * DSK_HEAD_DIM + ct * 32 + 8 * i + 4 * qs.half;
         if (a.out != nullptr) *reinterpret_cast<float4*>(a.out + at) = x;
         if (a.out_bf16 != nullptr)
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out_bf16) + at) = make_uint2(tree_pack(x.x, x.y), tree_pack(x.z, x.w));
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out_bf16) + at) = make_uint2(tile_pack(x.x, x.y), tile_pack(x.z, x.w));
       }
     if (qs.half == 0 && a.lse != nullptr) a.lse[qs.out_row] = l == 0.0f ? -__builtin_inff() : (m + log2f(l)) * kLn2;   // a NaN stays one
   } else {
@@ -642,12 +376,12 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
     dsk_tree_attn_args a, int G, int q_tiles, TreeSplit sp, float scale_log2, float2* __restrict__ part_ml,
     float* __restrict__ part_acc) {
   constexpr int kThreads = QW * KW * DSK_WAVE;
-  constexpr int kTiles = KW * NT, kKeys = kTreeTile * kTiles;   // of a stage
-  constexpr int kBufBytes = 2 * kTiles * kTreeTileBytes;
+  constexpr int kTiles = KW * NT, kKeys = kAttnTile * kTiles;   // of a stage
+  constexpr int kBufBytes = 2 * kTiles * kTileBytes;
   __shared__ __align__(16) unsigned char sm_kv[BUFS * kBufBytes];
   __shared__ float2 sm_ml[KW > 1 ? (KW - 1) * QW * DSK_WAVE : 1];
   __shared__ uint32_t sm_bad[kTreeMixedTiles];
-  static_assert(kTiles + DSK_TREE_MAX_NODES / kTreeTile + 1 <= kTreeMixedTiles, "words of sm_bad");
+  static_assert(kTiles + DSK_TREE_MAX_NODES / kAttnTile + 1 <= kTreeMixedTiles, "words of sm_bad");
   __shared__ int32_t sm_rows[SEL ? kTreeMaxListed : 1];
 
   TreeWork work;
@@ -658,15 +392,15 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
 
   const TreeSlots<SEL> slots(a, sp, s, hk, split);
   const TreePlace at(a, s);
-  if (q_tile * QW * kTreeTile >= at.n * G) return;       // uniform: no row of this pass
+  if (q_tile * QW * kAttnTile >= at.n * G) return;       // uniform: no row of this pass
   const int used = at.used(sp, SEL, slots.count);
   if (split >= used) return;
-  TreeQueries qs(a, at, G, hk, (q_tile * QW + qw) * kTreeTile);
+  TreeQueries qs(a, at, G, hk, (q_tile * QW + qw) * kAttnTile);
   const TreeKeys<kThreads, kKeys * 16 / kThreads, SEL, STREAM> keys(a, sp, at, slots, hk, split, used, sm_rows);
   qs.mask.n = keys.nodes();
 
-  TreeSoftmax sm(scale_log2);
-  tree_f32x16 O[4];
+  TileSoftmax sm(scale_log2);
+  tile_f32x16 O[4];
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
@@ -675,31 +409,31 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
   if (tid < kTreeMixedTiles) sm_bad[tid] = 0;
   auto tiles = [&](int t0, const unsigned char* sm_k, auto mixed) {   // this wavefront's tiles of the stage in LDS
     constexpr bool kMixed = decltype(mixed)::value;
-    const unsigned char* const sm_v = sm_k + kTiles * kTreeTileBytes;
+    const unsigned char* const sm_v = sm_k + kTiles * kTileBytes;
 #pragma unroll
     for (int sub = 0; sub < NT; ++sub) {
-      const int tile = kw * NT + sub, tt = t0 + tile * kTreeTile;
+      const int tile = kw * NT + sub, tt = t0 + tile * kAttnTile;
       if (kMixed && tt >= keys.t_end) break;
-      TreeKFrag kf;
-      kf.read<0, 8>(sm_k + tile * kTreeTileBytes, qs);
-      tree_f32x16 z;
+      TileKFrag kf;
+      kf.read<0, 8>(sm_k + tile * kTileBytes, qs);
+      tile_f32x16 z;
       kf.add<0, 8>(z, qs);
       uint32_t allow = 0;
       if constexpr (kMixed) {
         allow = qs.allowed(tt, keys.P);
-        tree_hide(z, allow, qs.half);
+        tile_hide(z, allow, qs.half);
       }
-      TreeVFrag vf;
+      TileVFrag vf;
       if constexpr (BUFS > 1) {                          // during the products of K, whose results the weights wait for anyway
         __builtin_amdgcn_sched_barrier(0);
-        vf.read_beside_copies(sm_v + tile * kTreeTileBytes);
+        vf.read_beside_copies(sm_v + tile * kTileBytes);
         __builtin_amdgcn_sched_barrier(0);
       }
-      TreeWeights<TERMS> w;
+      TileWeights<TERMS> w;
       sm.take(z, O, w);
       if constexpr (BUFS == 1) {
-        vf.template read<0>(sm_v + tile * kTreeTileBytes);
-        vf.template read<1>(sm_v + tile * kTreeTileBytes);
+        vf.template read<0>(sm_v + tile * kTileBytes);
+        vf.template read<1>(sm_v + tile * kTileBytes);
       }
       vf.add<TERMS>(O, w, 0);
       vf.add<TERMS>(O, w, 1);
@@ -711,7 +445,7 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
   int t0 = keys.t_begin;
   // stages of the prefix alone: nothing is masked
   auto some = [&](int t) { return keys.plain(t) && t < keys.t_end; };
-  auto copy = [&](int t, unsigned char* to) { keys.copy_plain(t, to, to + kTiles * kTreeTileBytes); };
+  auto copy = [&](int t, unsigned char* to) { keys.copy_plain(t, to, to + kTiles * kTileBytes); };
   unsigned char *here = sm_kv, *other = sm_kv + (BUFS - 1) * kBufBytes;
   if (BUFS > 1 && some(t0)) copy(t0, here);
   for (; some(t0); t0 += kKeys) {
@@ -729,7 +463,7 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
   for (; t0 < keys.t_end; t0 += kKeys) {                 // its end and the nodes
     typename decltype(keys)::Regs x;
     keys.fetch_mixed(x, t0);
-    keys.template put<true>(x, t0, sm_kv, sm_kv + kTiles * kTreeTileBytes, sm_bad);
+    keys.template put<true>(x, t0, sm_kv, sm_kv + kTiles * kTileBytes, sm_bad);
     __syncthreads();
     if (qs.busy) tiles(t0, sm_kv, Mixed());
     __syncthreads();
@@ -737,7 +471,7 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void tree_attn_kernel(
   sm.close();
   if constexpr (KW > 1) {
     static_assert((KW - 1) * QW <= BUFS * kTiles, "a block is as large as a tile of K and V");
-    tree_join<QW, KW>(sm, O, qs.busy, qw, kw, reinterpret_cast<float*>(sm_kv), sm_ml);
+    tile_join<QW, KW>(sm, O, qs.busy, qw, kw, reinterpret_cast<float*>(sm_kv), sm_ml);
     if (kw > 0) return;
   }
   tree_store(a, qs, O, sm.m, sm.l, used, sp.nsplit, split, part_ml, part_acc);
@@ -761,12 +495,12 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
     dsk_tree_attn_args a, int G, int q_tiles, TreeSplit sp, float scale_log2, float2* __restrict__ part_ml,
     float* __restrict__ part_acc) {
   constexpr int kThreads = kWideWaves * DSK_WAVE;
-  constexpr int kKeys = kTreeTile;                       // of a step
-  constexpr int kBufs = 4, kBufBytes = 2 * kTreeTileBytes;
+  constexpr int kKeys = kAttnTile;                       // of a step
+  constexpr int kBufs = 4, kBufBytes = 2 * kTileBytes;
   constexpr int kSets = 4;                               // steps on their way in registers: 64 KB
   __shared__ __align__(16) unsigned char sm_kv[kBufs * kBufBytes];
   __shared__ uint32_t sm_bad[kTreeMixedTiles];
-  static_assert(1 + DSK_TREE_MAX_NODES / kTreeTile + 1 <= kTreeMixedTiles, "words of sm_bad");
+  static_assert(1 + DSK_TREE_MAX_NODES / kAttnTile + 1 <= kTreeMixedTiles, "words of sm_bad");
 
   TreeWork work;
   if (!work.find(a, sp, q_tiles)) return;
@@ -775,15 +509,15 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
   const bool late = wave >= 4;
 
   const TreePlace at(a, s);
-  if (q_tile * kWideWaves * kTreeTile >= at.n * G) return;       // uniform: no row of this pass
+  if (q_tile * kWideWaves * kAttnTile >= at.n * G) return;       // uniform: no row of this pass
   const int used = at.used(sp, false, 0);
   if (split >= used) return;
   using Keys = TreeKeys<kThreads, kKeys * 16 / kThreads, false, STREAM>;
   const Keys keys(a, sp, at, TreeSlots<false>(a, sp, s, hk, split), hk, split, used, nullptr);
-  TreeQueries qs(a, at, G, hk, (q_tile * kWideWaves + wave) * kTreeTile);
+  TreeQueries qs(a, at, G, hk, (q_tile * kWideWaves + wave) * kAttnTile);
   qs.mask.n = keys.nodes();
-  TreeSoftmax sm(scale_log2);
-  tree_f32x16 O[4];
+  TileSoftmax sm(scale_log2);
+  tile_f32x16 O[4];
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
@@ -803,8 +537,8 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
   using Any = std::integral_constant<bool, false>;
   auto put = [&](auto plain, typename Keys::Regs& x, int i, int buf) {
     unsigned char* to = sm_kv + buf * kBufBytes;
-    if (decltype(plain)::value || i < plain_steps) keys.template put<false>(x, t_of(i), to, to + kTreeTileBytes, nullptr);
-    else if (i < steps) keys.template put<true>(x, t_of(i), to, to + kTreeTileBytes, sm_bad);
+    if (decltype(plain)::value || i < plain_steps) keys.template put<false>(x, t_of(i), to, to + kTileBytes, nullptr);
+    else if (i < steps) keys.template put<true>(x, t_of(i), to, to + kTileBytes, sm_bad);
   };
   auto fetch = [&](typename Keys::Regs& x, int i) {
     if (i < plain_steps) keys.fetch_plain(x, t_of(i));
@@ -815,8 +549,8 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
   typename Keys::Regs x[kSets];
   if (tid < kTreeMixedTiles) sm_bad[tid] = 0;
   // the first step multiplies weights of 0 by the values of "the step before" it: those have to be numbers
-  for (int i = tid; i < kTreeTileBytes / 16; i += kThreads)
-    *reinterpret_cast<uint4*>(sm_kv + (kBufs - 1) * kBufBytes + kTreeTileBytes + i * 16) = make_uint4(0, 0, 0, 0);
+  for (int i = tid; i < kTileBytes / 16; i += kThreads)
+    *reinterpret_cast<uint4*>(sm_kv + (kBufs - 1) * kBufBytes + kTileBytes + i * 16) = make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int j = 0; j < kSets; ++j) fetch(x[j], late ? (j + 1) % kSets : j);
   __syncthreads();
@@ -836,7 +570,7 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
   const int ahead = late ? 2 : 1;
   // what the loop of plain steps fetches next, from the first step that is not fetched yet; the last one again when it is through
   int fetched = ahead + kSets < plain_steps ? ahead + kSets : (plain_steps > 0 ? plain_steps - 1 : 0);
-  tree_global k_next = keys.Ku + t_of(fetched) * keys.kst * 2, v_next = keys.Vu + t_of(fetched) * keys.vst * 2;
+  tile_global k_next = keys.Ku + t_of(fetched) * keys.kst * 2, v_next = keys.Vu + t_of(fetched) * keys.vst * 2;
   int64_t k_inc = kKeys * keys.kst * 2, v_inc = kKeys * keys.vst * 2;
   asm("" : "+s"(k_inc), "+s"(v_inc));                    // no more of the arguments is kept for them
   auto fetch_next = [&](typename Keys::Regs& x) {
@@ -847,10 +581,10 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
     k_next += more ? k_inc : 0;
     v_next += more ? v_inc : 0;
   };
-  TreeVFrag vf;                                          // values and weights of the step before, for its product
-  TreeWeights<1> w;
+  TileVFrag vf;                                          // values and weights of the step before, for its product
+  TileWeights<1> w;
 #pragma unroll
-  for (int t = 0; t < 2; ++t) w.w[0][t] = __builtin_bit_cast(tree_bf16x8, make_uint4(0, 0, 0, 0));
+  for (int t = 0; t < 2; ++t) w.w[0][t] = __builtin_bit_cast(tile_bf16x8, make_uint4(0, 0, 0, 0));
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct) vf.v[ct][0] = w.w[0][0];
   // A wavefront without rows multiplies what is there: nothing reads its result.
@@ -859,9 +593,9 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
     constexpr int kBuf = decltype(buffer)::value, kBefore = (kBuf + kBufs - 1) % kBufs;
     const unsigned char* from = sm_kv + kBuf * kBufBytes;
     // Fragments are read well ahead of their products; left to itself the compiler reads each one right before, and waits.
-    TreeKFrag kf;
-    tree_f32x16 z;
-    vf.template read<1>(sm_kv + kBefore * kBufBytes + kTreeTileBytes);
+    TileKFrag kf;
+    tile_f32x16 z;
+    vf.template read<1>(sm_kv + kBefore * kBufBytes + kTileBytes);
     __builtin_amdgcn_sched_barrier(0);
     vf.template add<1>(O, w, 0);
     __builtin_amdgcn_sched_barrier(0);
@@ -880,8 +614,8 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
     put(plain, regs, i + ahead, late ? (kBuf + 2) % kBufs : (kBuf + 1) % kBufs);
     if constexpr (kPlain) fetch_next(regs);
     else fetch(regs, i + ahead + kSets);
-    if (!kPlain && i >= plain_steps) tree_hide(z, qs.allowed(t_of(i), keys.P), qs.half);
-    vf.template read<0>(from + kTreeTileBytes);
+    if (!kPlain && i >= plain_steps) tile_hide(z, qs.allowed(t_of(i), keys.P), qs.half);
+    vf.template read<0>(from + kTileBytes);
     __builtin_amdgcn_sched_barrier(0);
     sm.take(z, O, w);
     barrier();
@@ -908,7 +642,7 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void tree_wide_kernel(
   const int buf_before = (steps + kBufs - 1) % kBufs;
   vf.add<1>(O, w, 0);
   if (steps > 0) {
-    vf.read<1>(sm_kv + buf_before * kBufBytes + kTreeTileBytes);
+    vf.read<1>(sm_kv + buf_before * kBufBytes + kTileBytes);
     vf.add<1>(O, w, 1);
   }
   if (steps > plain_steps) {
@@ -985,7 +719,7 @@ __global__ __launch_bounds__(kTreeMergeWaves * DSK_WAVE) void tree_merge_kernel(
   o.y *= inv;
   if (a.out != nullptr) *reinterpret_cast<float2*>(a.out + row * DSK_HEAD_DIM + 2 * lane) = o;
   if (a.out_bf16 != nullptr)
-    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out_bf16) + row * DSK_HEAD_DIM + 2 * lane) = tree_pack(o.x, o.y);
+    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out_bf16) + row * DSK_HEAD_DIM + 2 * lane) = tile_pack(o.x, o.y);
   if (lane == 0 && a.lse != nullptr) a.lse[row] = l == 0.0f ? -__builtin_inff() : (M + log2f(l)) * kLn2;
 }
 
@@ -1025,7 +759,7 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
   TreeLaunch t;
   auto rows_of = [&](int q_waves) {
     t.q_waves = q_waves;
-    t.q_tiles = (rows + q_waves * kTreeTile - 1) / (q_waves * kTreeTile);
+    t.q_tiles = (rows + q_waves * kAttnTile - 1) / (q_waves * kAttnTile);
   };
   // parts of `want` workgroups in all: keys of one
   auto keys_of = [&](int64_t want) {
@@ -1085,7 +819,7 @@ static TreeLaunch tree_layout(const dsk_tree_attn_args& a, bool f32) {
     // they have an XCD's L2 in common.  So do sequences of one part each, of which there may be many: each of their workgroups would
     // look at all before it (150 of 400 tokens 54.5 us by sequence and 56.8, 1024 of 500 363 and 450, 4096 of 60 0.56 and 1.82 ms).
     t.sp.packed = a.B > 1 && t.q_tiles == 1 && t.sp.nsplit > 1 && (int64_t)a.B * t.sp.nsplit <= 65535;
-    t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTreeRowBytes >= kTreeStreamBytes;
+    t.stream = t.q_tiles == 1 && keys * a.Hkv * 2 * kTileRowBytes >= kTreeStreamBytes;
   }
   const size_t parts = t.sp.nsplit > 1 ? (size_t)a.n_tokens * a.Hq * t.sp.nsplit : 0;
   t.part_acc = align_up(parts * sizeof(float2));
@@ -1118,7 +852,7 @@ size_t tree_ws_bytes(const dsk_tree_attn_args& a) {
   if (a.sel_start == nullptr) {
     const int rows = a.max_nodes * (a.Hq / a.Hkv);
     auto bound = [&](int64_t want, int q_waves) {
-      const int64_t n = tree_most_parts(a, want, (rows + q_waves * kTreeTile - 1) / (q_waves * kTreeTile));
+      const int64_t n = tree_most_parts(a, want, (rows + q_waves * kAttnTile - 1) / (q_waves * kAttnTile));
       nsplit = n > nsplit ? n : nsplit;
     };
     bound(2 * kTreeCus, rows <= 32 ? 1 : (rows <= 64 ? 2 : 4));
@@ -1158,7 +892,7 @@ static void launch_tree(const dsk_tree_attn_args& a, const TreeLaunch& t, float 
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;
   using Three = std::integral_constant<int, 3>;
-  static_assert(kTreeTwoTermRows == 2 * kTreeTile, "one wavefront's rows always have two terms, four wavefronts' never");
+  static_assert(kTreeTwoTermRows == 2 * kAttnTile, "one wavefront's rows always have two terms, four wavefronts' never");
   if (a.out != nullptr) {
     go(Three(), std::true_type());
   } else if constexpr (QW == 1) {
