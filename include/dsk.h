@@ -27,6 +27,13 @@
  *   dsk_tree_decode_attn    attention of every drafted node over the cached prefix (all of it, or the
  *                           slots of a selection) and its own ancestors.
  *   dsk_accept_draft        the accepted path of every tree, its K/V rows moved behind the sequences.
+ * Three calls serve a cache held in 8 bits, or attention that sees what is near and a few first tokens:
+ *   dsk_kv8_append          norm and rotation of new tokens' queries and keys, keys and values into a cache of
+ *                           8-bit codes with a scale per block of rows and head.
+ *   dsk_window_attn         causal attention of new tokens (a decoding step's one to whole prompts) with a
+ *                           sliding window and visible first tokens, on a cache in bf16 or 8 bits.
+ *   dsk_window_sparse_decode_attn   dsk_sparse_decode_attn with the newest tokens and the first ones beside the
+ *                           selected slots, on a cache in bf16 or 8 bits.
  *
  * Conventions that hold for every call
  *   - Pointers marked [dev] are device (HBM) addresses, [host] are host addresses.
@@ -44,7 +51,7 @@
  *   - Tokens of a ragged batch are flattened: sequence s owns global token positions
  *     cu_seqlens[s] .. cu_seqlens[s+1]-1.  Block boundaries, slot numbers and selected
  *     token spans are all expressed in these global coordinates.
- *   - K, V, q and summaries are bf16 (raw 16-bit patterns), head_dim D must be 128.
+ *   - K, V, q and summaries are bf16 (raw 16-bit patterns) unless a call says otherwise, head_dim D must be 128.
  *   - Same inputs give bit-identical outputs (fixed reduction orders, no float atomics).
  *   - Non-finite K/V/q values give unspecified results but never hang.
  *   - A batch without any token (total_tokens == 0) is valid everywhere: tables come out empty,
@@ -674,6 +681,146 @@ typedef struct dsk_accept_args {
   int32_t* dev_status;         /* [dev] optional */
 } dsk_accept_args;
 
+/* ------------------------------------------------------------------------------------------
+ * A cache in 8 bits.  Codes are e4m3 values (one sign, four exponent, three mantissa bits, no infinities, 0x7F and
+ * 0xFF NaN), a byte each, strides in bytes and multiples of 16.  Rows r of head h with the same r / scale_block share the scale
+ * 2^(byte - 127), byte = scale[h * scale_stride_head + r / scale_block] (e8m0).  A row stands for code * scale, which
+ * is a bf16 number for the scales that dsk_kv8_append makes.  scale_block is 32, 64 or 128.
+ *
+ * dsk_kv8_append -- the counterpart of dsk_qk_norm_rope for such a cache.  Token cu_new[s] + i goes to row
+ * seq_row0[s] + seq_len[s] + i; its position is tok_pos[t], or seq_len[s] + i without tok_pos.  Queries (optional)
+ * and keys are normed and rotated as there, in fp32; queries are rounded to bf16, keys and values to codes, once:
+ *   block     its scale is 2^e, e the least integer with |x| <= 448 * 2^e for all finite x written to it, within [-100, 120]
+ *   new row   code = e4m3(x / scale), to nearest even; what is not finite becomes NaN
+ *   begun     a block that holds rows of the sequence already (rows below seq_len) keeps its scale, or where the new rows need a
+ *             larger one its codes are rounded again to that: exact but for values that fall below 2^-6 of the new scale
+ * so that each row's values are off by 2^-4 of themselves or 2^-10 of the scale, and once more that where the scale grew.
+ * Every sequence begins with a block: seq_row0 is a multiple of scale_block.  Codes of rows below seq_len are changed only where
+ * their block's scale grows; rows behind the new ones and scales of other blocks stay as they are.
+ * One launch; no workspace.  Data-dependent errors through *dev_status:
+ *   DSK_ERR_ALIGN     a seq_row0 that is no multiple of scale_block: nothing of the sequence is written
+ *   DSK_ERR_SHAPE     negative lengths, cu_new that does not ascend or fit n_tokens, more than max_new tokens (cut)
+ *   DSK_ERR_CAPACITY  a row outside [0, total_rows): its token is skipped, query included
+ * ---------------------------------------------------------------------------------------- */
+typedef struct dsk_kv8_append_args {
+  uint32_t struct_size;
+  int32_t B, Hq, Hkv, D;
+  int32_t n_tokens;            /* [host] rows of q, k, v; bounds cu_new[B] */
+  int32_t max_new;             /* [host] bound on the new tokens of a sequence, >= 1; sizes the launch */
+  int32_t total_rows;          /* [host] rows per head of K and V */
+  int32_t scale_block;
+  const int32_t* seq_row0;     /* [dev] [B] */
+  const int32_t* seq_len;      /* [dev] [B] rows in use before the new ones */
+  const int32_t* cu_new;       /* [dev] [B+1] */
+  const int32_t* tok_pos;      /* [dev] optional [n_tokens]; read if rot_dim > 0 */
+  const void* q;               /* [dev] optional bf16 [n_tokens, Hq, D] */
+  const void* k;               /* [dev] bf16 [n_tokens, Hkv, D] */
+  const void* v;               /* [dev] bf16 [n_tokens, Hkv, D] */
+  int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head; /* multiples of 8 */
+  const float* q_weight;       /* [dev] optional [D]: norm of the queries */
+  const float* k_weight;       /* [dev] optional [D] */
+  float eps;                   /* > 0 with a weight */
+  const float* inv_freq;       /* [dev] [rot_dim / 2]; read if rot_dim > 0 */
+  int32_t rot_dim;             /* multiple of 16, 0..D */
+  uint32_t flags;              /* DSK_ROPE_* bits */
+  void* q_out;                 /* [dev] out bf16 [n_tokens, Hq, D]; may be q itself if q is packed */
+  void* K;                     /* [dev] in/out codes: K[h*kc_stride_head + r*kc_stride_tok + d] */
+  void* V;                     /* [dev] in/out */
+  int64_t kc_stride_tok, kc_stride_head, vc_stride_tok, vc_stride_head; /* bytes, multiples of 16 */
+  uint8_t* k_scale;            /* [dev] in/out [Hkv, scale_stride_head] */
+  uint8_t* v_scale;            /* [dev] in/out */
+  int64_t scale_stride_head;   /* >= ceil(total_rows / scale_block), of both */
+  int32_t* dev_status;         /* [dev] optional */
+} dsk_kv8_append_args;
+
+/* ------------------------------------------------------------------------------------------
+ * dsk_window_attn -- causal attention of the new tokens of a step, whose K and V lie in the cache behind the sequence's
+ * already.  Token i of sequence s (row cu_new[s] + i of q) has position p = seq_len[s] + i and sees the positions
+ *   t <= p  with  t > p - window  or  t < n_sink          (position t is row seq_row0[s] + t of K / V)
+ *   out = sum p_t V_t / sum p_t,  p_t = exp(q.K_t * scale);  lse = log sum p_t
+ * K and V are bf16, or with k_scale codes of 8 bits (above).  Rows that a token does not see may hold anything, NaN included; an
+ * infinity in a row of V that it sees gives that infinity, or NaN with its opposite or where its weight is 2^-80 of the
+ * largest or less.  A token that sees nothing (its sequence has no place in the cache) gets out = 0 and lse = -inf.
+ * Accuracy and bits as for dsk_tree_decode_attn, with rows = max_new * Hq / Hkv: `out` asks for fp32 accuracy; where only out_bf16 is
+ * asked for, the weights are off by 2^-16 of each at most, and above 64 rows rounded to bf16.  In 8 bits scales below 2^-100 may
+ * lose small weights.
+ * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths are cut, never followed: tokens to
+ * max_new and n_tokens, seq_len to max_seqlen, rows to total_rows.
+ * ---------------------------------------------------------------------------------------- */
+#define DSK_WINDOW_ALL 0x7FFFFFFF    /* a window that hides nothing */
+
+typedef struct dsk_window_attn_args {
+  uint32_t struct_size;
+  int32_t B, Hq, Hkv, D;
+  int32_t n_tokens;            /* [host] rows of q, out and lse; bounds cu_new[B] */
+  int32_t max_new;             /* [host] bound on the new tokens of a sequence, >= 1; it and n_tokens, times Hq, below 2^31 */
+  int32_t max_seqlen;          /* [host] bound on seq_len, >= 0; max_seqlen + max_new at most 0x7FFF0000 */
+  int32_t total_rows;          /* [host] rows per head of K / V */
+  int32_t window;              /* >= 1 */
+  int32_t n_sink;              /* >= 0 */
+  const void* q;               /* [dev] bf16 [n_tokens, Hq, D] */
+  const void* K;               /* [dev] bf16, strides as in dsk_compress_args, or codes, strides in bytes */
+  const void* V;               /* [dev] */
+  int64_t k_stride_tok, k_stride_head, v_stride_tok, v_stride_head;
+  const uint8_t* k_scale;      /* [dev] optional [Hkv, scale_stride_head]; both or neither */
+  const uint8_t* v_scale;      /* [dev] */
+  int64_t scale_stride_head;   /* >= ceil(total_rows / scale_block); read with k_scale only */
+  int32_t scale_block;         /* 32, 64 or 128; read with k_scale only */
+  const int32_t* seq_row0;     /* [dev] [B]; with k_scale any row, as scales go by rows of the cache */
+  const int32_t* seq_len;      /* [dev] [B] tokens before the new ones */
+  const int32_t* cu_new;       /* [dev] [B+1] */
+  float scale;                 /* 0 -> D^-1/2 */
+  uint32_t flags;              /* must be 0 */
+  float* out;                  /* [dev] f32 [n_tokens, Hq, D]; one of out and out_bf16 may be NULL */
+  void* out_bf16;              /* [dev] bf16 [n_tokens, Hq, D] */
+  float* lse;                  /* [dev] f32 [n_tokens, Hq], natural log; may be NULL */
+  void* workspace;             /* [dev] 256-byte aligned, dsk_window_attn_workspace_bytes(), which does not shrink as max_seqlen
+                                  grows: one for the longest serves a growing cache */
+  size_t workspace_bytes;
+} dsk_window_attn_args;
+
+/* ------------------------------------------------------------------------------------------
+ * dsk_window_sparse_decode_attn -- the attention of dsk_sparse_decode_attn for a sequence whose newest tokens are not in the
+ * tables yet, or whose first and last ones are always wanted.  The query of sequence s sees, of its seq_len[s] tokens
+ * (rows seq_row0[s] + t; the query's own is the last),
+ *   near      the last `window` and the first n_sink
+ *   selected  the tokens of its slots (spans of cache rows as dsk_select_topk writes them) that are not near
+ * so that what is near counts once whatever is selected; a token that several slots hold counts as often.  Spans are cut
+ * to the sequence's rows.  Selections are per query head, or per KV head with DSK_ATTN_SHARED_SELECTION.
+ * K and V are bf16, or with k_scale codes of 8 bits.  Values, accuracy, infinities and rows that are not seen as for
+ * dsk_window_attn with one new token; a query that sees nothing gets out = 0 and lse = -inf.
+ * ---------------------------------------------------------------------------------------- */
+typedef struct dsk_window_sparse_args {
+  uint32_t struct_size;
+  int32_t B, Hq, Hkv, D;
+  int32_t total_rows;          /* [host] rows per head of K / V */
+  int32_t window;              /* >= 0: 0 leaves the selection and the first tokens */
+  int32_t n_sink;              /* >= 0 */
+  int32_t max_seqlen;          /* [host] bound on seq_len, 0..0x7FFF0000 */
+  int32_t k, b;                /* slots per list, 1..0x7FFF0000, and upper bound of sel_len entries, 1..1024 */
+  const void* q;               /* [dev] bf16 [B, Hq, D] */
+  const void* K;               /* [dev] as in dsk_window_attn_args */
+  const void* V;               /* [dev] */
+  int64_t k_stride_tok, k_stride_head, v_stride_tok, v_stride_head;
+  const uint8_t* k_scale;      /* [dev] optional; both or neither */
+  const uint8_t* v_scale;      /* [dev] */
+  int64_t scale_stride_head;
+  int32_t scale_block;
+  const int32_t* seq_row0;     /* [dev] [B] */
+  const int32_t* seq_len;      /* [dev] [B] */
+  const int32_t* sel_start;    /* [dev] [B, Hq, k], or [B, Hkv, k] with DSK_ATTN_SHARED_SELECTION */
+  const int32_t* sel_len;      /* [dev] */
+  const int32_t* sel_count;    /* [dev] [B, Hq] or [B, Hkv] */
+  float scale;                 /* 0 -> D^-1/2 */
+  uint32_t flags;              /* 0 or DSK_ATTN_SHARED_SELECTION */
+  float* out;                  /* [dev] f32 [B, Hq, D]; one of out and out_bf16 may be NULL */
+  void* out_bf16;              /* [dev] bf16 [B, Hq, D] */
+  float* lse;                  /* [dev] f32 [B, Hq], natural log; may be NULL */
+  void* workspace;             /* [dev] 256-byte aligned, dsk_window_sparse_workspace_bytes(), which does not shrink as max_seqlen,
+                                  k or window grow */
+  size_t workspace_bytes;
+} dsk_window_sparse_args;
+
 /* Library / ABI version (DSK_ABI_VERSION of the build). */
 uint32_t dsk_version(void);
 
@@ -696,6 +843,8 @@ size_t dsk_append_workspace_bytes(const dsk_append_args* args);
 size_t dsk_append_batch_workspace_bytes(const dsk_append_batch_args* args);
 size_t dsk_reuse_workspace_bytes(const dsk_reuse_args* args);
 size_t dsk_tree_attn_workspace_bytes(const dsk_tree_attn_args* args);
+size_t dsk_window_attn_workspace_bytes(const dsk_window_attn_args* args);
+size_t dsk_window_sparse_workspace_bytes(const dsk_window_sparse_args* args);
 
 /* Where dsk_sparse_decode_attn leaves its split-K partials in args->workspace (what a caller
  * that sets DSK_ATTN_PARTIALS_ONLY reads).  Chunk c of (sequence s, head h) covers the selected
@@ -751,6 +900,9 @@ dsk_status dsk_step_plan(const dsk_step_plan_args* args, void* stream);
 dsk_status dsk_qk_norm_rope(const dsk_norm_rope_args* args, void* stream);
 dsk_status dsk_tree_decode_attn(const dsk_tree_attn_args* args, void* stream);
 dsk_status dsk_accept_draft(const dsk_accept_args* args, void* stream);
+dsk_status dsk_kv8_append(const dsk_kv8_append_args* args, void* stream);
+dsk_status dsk_window_attn(const dsk_window_attn_args* args, void* stream);
+dsk_status dsk_window_sparse_decode_attn(const dsk_window_sparse_args* args, void* stream);
 
 #ifdef __cplusplus
 }

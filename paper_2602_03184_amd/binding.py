@@ -40,6 +40,7 @@ DSK_REUSE_MAX_K = 2048
 DSK_SUMMARY_MINMAX, DSK_SUMMARY_MEAN = 0, 1
 DSK_TREE_MAX_NODES = 256
 DSK_ROPE_INTERLEAVED = 1
+DSK_WINDOW_ALL = 0x7FFFFFFF
 
 _p = C.c_void_p
 
@@ -247,6 +248,59 @@ class dsk_accept_args(C.Structure):
     ]
 
 
+class dsk_kv8_append_args(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+        ("n_tokens", C.c_int32), ("max_new", C.c_int32), ("total_rows", C.c_int32), ("scale_block", C.c_int32),
+        ("seq_row0", _p), ("seq_len", _p), ("cu_new", _p), ("tok_pos", _p),
+        ("q", _p), ("k", _p), ("v", _p),
+        ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64), ("k_stride_tok", C.c_int64),
+        ("k_stride_head", C.c_int64), ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64),
+        ("q_weight", _p), ("k_weight", _p), ("eps", C.c_float), ("inv_freq", _p),
+        ("rot_dim", C.c_int32), ("flags", C.c_uint32),
+        ("q_out", _p), ("K", _p), ("V", _p),
+        ("kc_stride_tok", C.c_int64), ("kc_stride_head", C.c_int64),
+        ("vc_stride_tok", C.c_int64), ("vc_stride_head", C.c_int64),
+        ("k_scale", _p), ("v_scale", _p), ("scale_stride_head", C.c_int64),
+        ("dev_status", _p),
+    ]
+
+
+_window_cache = [
+    ("q", _p), ("K", _p), ("V", _p),
+    ("k_stride_tok", C.c_int64), ("k_stride_head", C.c_int64),
+    ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64),
+    ("k_scale", _p), ("v_scale", _p), ("scale_stride_head", C.c_int64), ("scale_block", C.c_int32),
+    ("seq_row0", _p), ("seq_len", _p),
+]
+_window_results = [
+    ("scale", C.c_float), ("flags", C.c_uint32),
+    ("out", _p), ("out_bf16", _p), ("lse", _p),
+    ("workspace", _p), ("workspace_bytes", C.c_size_t),
+]
+
+
+class dsk_window_attn_args(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+        ("n_tokens", C.c_int32), ("max_new", C.c_int32), ("max_seqlen", C.c_int32), ("total_rows", C.c_int32),
+        ("window", C.c_int32), ("n_sink", C.c_int32),
+        *_window_cache, ("cu_new", _p), *_window_results,
+    ]
+
+
+class dsk_window_sparse_args(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32),
+        ("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+        ("total_rows", C.c_int32), ("window", C.c_int32), ("n_sink", C.c_int32), ("max_seqlen", C.c_int32),
+        ("k", C.c_int32), ("b", C.c_int32),
+        *_window_cache, ("sel_start", _p), ("sel_len", _p), ("sel_count", _p), *_window_results,
+    ]
+
+
 class dsk_attn_partials(C.Structure):
     _fields_ = [
         ("ml_offset", C.c_size_t), ("acc_offset", C.c_size_t),
@@ -293,6 +347,16 @@ _lib.dsk_tree_decode_attn.restype = C.c_int32
 _lib.dsk_tree_decode_attn.argtypes = [C.POINTER(dsk_tree_attn_args), _p]
 _lib.dsk_accept_draft.restype = C.c_int32
 _lib.dsk_accept_draft.argtypes = [C.POINTER(dsk_accept_args), _p]
+_lib.dsk_kv8_append.restype = C.c_int32
+_lib.dsk_kv8_append.argtypes = [C.POINTER(dsk_kv8_append_args), _p]
+_lib.dsk_window_attn_workspace_bytes.restype = C.c_size_t
+_lib.dsk_window_attn_workspace_bytes.argtypes = [C.POINTER(dsk_window_attn_args)]
+_lib.dsk_window_attn.restype = C.c_int32
+_lib.dsk_window_attn.argtypes = [C.POINTER(dsk_window_attn_args), _p]
+_lib.dsk_window_sparse_workspace_bytes.restype = C.c_size_t
+_lib.dsk_window_sparse_workspace_bytes.argtypes = [C.POINTER(dsk_window_sparse_args)]
+_lib.dsk_window_sparse_decode_attn.restype = C.c_int32
+_lib.dsk_window_sparse_decode_attn.argtypes = [C.POINTER(dsk_window_sparse_args), _p]
 DSK_STATIC_SCRATCH_BYTES = 2112 * 1024
 
 
@@ -451,6 +515,35 @@ def dsk_accept_draft(args: dsk_accept_args, stream=None, check: bool = True) -> 
     st = int(_lib.dsk_accept_draft(C.byref(args), _stream_handle(stream)))
     if check and st != DSK_OK:
         raise DskError(st, "dsk_accept_draft")
+    return st
+
+
+def dsk_kv8_append(args: dsk_kv8_append_args, stream=None, check: bool = True) -> int:
+    st = int(_lib.dsk_kv8_append(C.byref(args), _stream_handle(stream)))
+    if check and st != DSK_OK:
+        raise DskError(st, "dsk_kv8_append")
+    return st
+
+
+def dsk_window_attn_workspace_bytes(args: dsk_window_attn_args) -> int:
+    return int(_lib.dsk_window_attn_workspace_bytes(C.byref(args)))
+
+
+def dsk_window_attn(args: dsk_window_attn_args, stream=None, check: bool = True) -> int:
+    st = int(_lib.dsk_window_attn(C.byref(args), _stream_handle(stream)))
+    if check and st != DSK_OK:
+        raise DskError(st, "dsk_window_attn")
+    return st
+
+
+def dsk_window_sparse_workspace_bytes(args: dsk_window_sparse_args) -> int:
+    return int(_lib.dsk_window_sparse_workspace_bytes(C.byref(args)))
+
+
+def dsk_window_sparse_decode_attn(args: dsk_window_sparse_args, stream=None, check: bool = True) -> int:
+    st = int(_lib.dsk_window_sparse_decode_attn(C.byref(args), _stream_handle(stream)))
+    if check and st != DSK_OK:
+        raise DskError(st, "dsk_window_sparse_decode_attn")
     return st
 
 
@@ -1307,3 +1400,182 @@ def make_acceptor(K: Optional[torch.Tensor], V: Optional[torch.Tensor], *, seq_r
     _on(dev, K, V, Kd, Vd, seq_row0, seq_len, cu_new, parent, draft_ids, target_ids, token_ids, len_new)
     return Acceptor(path=path, n_accepted=n_accepted, len_new=len_new, next_id=next_id, dev_status=dev_status, args=a,
                     keep=(K, V, Kd, Vd, seq_row0, seq_len, cu_new, parent, draft_ids, target_ids, token_ids))
+
+
+# ---- a cache in 8 bits, sliding window and first tokens -----------------------------------------
+def _codes(X: torch.Tensor):
+    """Strides in bytes of a cache of codes: e4m3 [Hkv, rows, D] view with unit channel stride."""
+    assert X.dim() == 3 and X.dtype == torch.float8_e4m3fn and X.shape[2] == DSK_HEAD_DIM
+    if X.numel() == 0:
+        return DSK_HEAD_DIM, DSK_HEAD_DIM
+    assert X.stride(2) == 1
+    return X.stride(1), X.stride(0)
+
+
+def _scales(a, K: torch.Tensor, V: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, scale_block: int) -> None:
+    """Scales (e8m0 [Hkv, blocks], blocks contiguous) of a cache of codes into an argument struct."""
+    for t in (k_scale, v_scale):
+        assert t.dtype == torch.float8_e8m0fnu and t.dim() == 2 and t.shape[0] == K.shape[0] and t.shape[1] * scale_block >= K.shape[1]
+        assert t.shape[1] <= 1 or t.stride(1) == 1
+    stride = [t.stride(0) if t.shape[0] > 1 else t.shape[1] for t in (k_scale, v_scale)]
+    assert V.shape == K.shape and stride[0] == stride[1], "K and V and their scales have one shape"
+    a.k_scale, a.v_scale, a.scale_stride_head, a.scale_block = _ptr(k_scale), _ptr(v_scale), stride[0], scale_block
+
+
+def empty_kv8(Hkv: int, rows: int, *, scale_block: int = 32, device="cuda"):
+    """(codes e4m3 [Hkv, rows, D], scales e8m0 [Hkv, blocks]) of an empty cache of keys or values: codes 0, scales 1."""
+    blocks = (rows + scale_block - 1) // scale_block
+    codes = torch.zeros(Hkv, rows, DSK_HEAD_DIM, dtype=torch.uint8, device=device)
+    scale = torch.full((Hkv, max(blocks, 1)), 127, dtype=torch.uint8, device=device)
+    return codes.view(torch.float8_e4m3fn), scale.view(torch.float8_e8m0fnu)
+
+
+@dataclass
+class Kv8Appender:
+    """Argument struct of dsk_kv8_append bound to its inputs and the cache."""
+    q_out: Optional[torch.Tensor]     # bf16 [tokens, Hq, D]
+    dev_status: torch.Tensor
+    args: dsk_kv8_append_args
+    keep: tuple
+
+    def step(self, stream=None, check: bool = True) -> int:
+        return _call(dsk_kv8_append, self.args, self.dev_status.device, stream, check)
+
+
+def make_kv8_appender(k: torch.Tensor, v: torch.Tensor, K: torch.Tensor, V: torch.Tensor, k_scale: torch.Tensor,
+                      v_scale: torch.Tensor, *, scale_block: int, seq_row0: torch.Tensor, seq_len: torch.Tensor,
+                      cu_new: torch.Tensor, max_new: int, q: Optional[torch.Tensor] = None,
+                      q_out: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                      q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                      inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False) -> Kv8Appender:
+    """k / v [tokens, Hkv, D], q [tokens, Hq, D]: bf16 views, e.g. of one projection's output; K / V: e4m3 [Hkv, rows, D]
+    with scales e8m0 [Hkv, blocks] (empty_kv8); seq_row0 / seq_len / cu_new as in a StepPlan, every sequence beginning with a
+    block; pos: int32 [tokens], none = the places in the sequence; weights: fp32 [D]; inv_freq: fp32 [rot_dim / 2], none =
+    no rotation."""
+    n, dev, B = k.shape[0], k.device, seq_len.numel()
+    a = dsk_kv8_append_args()
+    a.struct_size = C.sizeof(dsk_kv8_append_args)
+    a.B, a.Hkv, a.D, a.n_tokens, a.max_new, a.total_rows = B, k.shape[1], DSK_HEAD_DIM, n, max_new, K.shape[1]
+    assert v.shape == k.shape and K.shape[0] == a.Hkv
+    for t, size in ((seq_row0, B), (seq_len, B), (cu_new, B + 1), (pos, n)):
+        _i32_on(t, size)
+    a.seq_row0, a.seq_len, a.cu_new, a.tok_pos = _ptr(seq_row0), _ptr(seq_len), _ptr(cu_new), _ptr(pos)
+    if q is not None:
+        a.Hq = q.shape[1]
+        a.q_stride_tok, a.q_stride_head = _token_strides(q, n)
+        if q_out is None:
+            q_out = torch.empty(n, a.Hq, DSK_HEAD_DIM, dtype=torch.bfloat16, device=dev)
+        assert q_out.shape == q.shape and q_out.dtype == torch.bfloat16 and q_out.is_contiguous()
+        a.q, a.q_out = _ptr(q), _ptr(q_out)
+    a.k, a.v = _ptr(k), _ptr(v)
+    a.k_stride_tok, a.k_stride_head = _token_strides(k, n)
+    a.v_stride_tok, a.v_stride_head = _token_strides(v, n)
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == DSK_HEAD_DIM)
+    a.q_weight, a.k_weight, a.eps = _ptr(q_weight), _ptr(k_weight), eps
+    if inv_freq is not None:
+        assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
+        a.inv_freq, a.rot_dim = _ptr(inv_freq), 2 * inv_freq.numel()
+    a.flags = DSK_ROPE_INTERLEAVED if interleaved else 0
+    a.K, a.V = _ptr(K), _ptr(V)
+    a.kc_stride_tok, a.kc_stride_head = _codes(K)
+    a.vc_stride_tok, a.vc_stride_head = _codes(V)
+    _scales(a, K, V, k_scale, v_scale, scale_block)
+    dev_status = torch.zeros(1, dtype=torch.int32, device=dev)
+    a.dev_status = _ptr(dev_status)
+    keep = (k, v, K, V, k_scale, v_scale, seq_row0, seq_len, cu_new, q, pos, q_weight, k_weight, inv_freq)
+    _on(dev, q_out, *keep)
+    return Kv8Appender(q_out=q_out if q is not None else None, dev_status=dev_status, args=a, keep=keep)
+
+
+@dataclass
+class WindowAttnOut:
+    """Results and argument struct of dsk_window_attn or dsk_window_sparse_decode_attn."""
+    out: Optional[torch.Tensor]       # f32 [tokens, Hq, D]
+    lse: torch.Tensor                 # f32 [tokens, Hq]
+    args: C.Structure
+    call: object
+    keep: tuple
+    out_bf16: Optional[torch.Tensor] = None
+
+    def step(self, stream=None, check: bool = True) -> int:
+        return _call(self.call, self.args, self.lse.device, stream, check)
+
+
+def _window_call(a, call, workspace_bytes, q, K, V, seq_row0, seq_len, window, n_sink, k_scale, v_scale, scale_block, scale,
+                 want_f32, want_bf16, *more) -> WindowAttnOut:
+    """What the two calls have in common."""
+    n, Hq, D = q.shape
+    dev, B = q.device, seq_len.numel()
+    assert D == DSK_HEAD_DIM and q.dtype == torch.bfloat16 and q.is_contiguous() and V.shape == K.shape
+    _i32_on(seq_row0, B)
+    _i32_on(seq_len, B)
+    a.struct_size = C.sizeof(a)
+    a.B, a.Hq, a.Hkv, a.D, a.total_rows = B, Hq, K.shape[0], D, K.shape[1]
+    a.window, a.n_sink = window, n_sink
+    a.q, a.K, a.V, a.seq_row0, a.seq_len = _ptr(q), _ptr(K), _ptr(V), _ptr(seq_row0), _ptr(seq_len)
+    strides = _kv_strides if k_scale is None else _codes
+    a.k_stride_tok, a.k_stride_head = strides(K)
+    a.v_stride_tok, a.v_stride_head = strides(V)
+    assert (k_scale is None) == (v_scale is None)
+    if k_scale is not None:
+        _scales(a, K, V, k_scale, v_scale, scale_block)
+    a.scale = scale
+    out = torch.empty(n, Hq, D, dtype=torch.float32, device=dev) if want_f32 else None
+    ob = torch.empty(n, Hq, D, dtype=torch.bfloat16, device=dev) if want_bf16 else None
+    lse = torch.empty(n, Hq, dtype=torch.float32, device=dev)
+    a.out, a.out_bf16, a.lse = _ptr(out), _ptr(ob), _ptr(lse)
+    ws = _ws(workspace_bytes(a), dev)
+    a.workspace, a.workspace_bytes = _ptr(ws), ws.numel()
+    keep = (q, K, V, seq_row0, seq_len, k_scale, v_scale, *more, ws)
+    _on(dev, *keep)
+    return WindowAttnOut(out=out, lse=lse, args=a, call=call, out_bf16=ob, keep=keep)
+
+
+def make_window_attn_args(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *, seq_row0: torch.Tensor,
+                          seq_len: torch.Tensor, cu_new: torch.Tensor, max_new: int, max_seqlen: int,
+                          window: int = DSK_WINDOW_ALL, n_sink: int = 0, k_scale: Optional[torch.Tensor] = None,
+                          v_scale: Optional[torch.Tensor] = None, scale_block: int = 32, scale: float = 0.0,
+                          want_f32: bool = True, want_bf16: bool = False) -> WindowAttnOut:
+    """q: bf16 [tokens, Hq, D], the new tokens of all sequences one after the other (cu_new: of a StepPlan), whose rows of K / V lie
+    behind the seq_len earlier ones already.  K / V: bf16 [Hkv, rows, D], or e4m3 with scales e8m0 [Hkv, blocks]."""
+    a = dsk_window_attn_args()
+    _i32_on(cu_new, seq_len.numel() + 1)
+    a.n_tokens, a.max_new, a.max_seqlen, a.cu_new = q.shape[0], max_new, max_seqlen, _ptr(cu_new)
+    return _window_call(a, dsk_window_attn, dsk_window_attn_workspace_bytes, q, K, V, seq_row0, seq_len, window, n_sink, k_scale,
+                        v_scale, scale_block, scale, want_f32, want_bf16, cu_new)
+
+
+def window_attn(q, K, V, *, stream=None, check: bool = True, **kw) -> WindowAttnOut:
+    """dsk_window_attn with outputs and workspace made here; keywords as in make_window_attn_args."""
+    r = make_window_attn_args(q, K, V, **kw)
+    r.step(stream, check)
+    return r
+
+
+def make_window_sparse_args(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *, seq_row0: torch.Tensor,
+                            seq_len: torch.Tensor, sel_start: torch.Tensor, sel_len: torch.Tensor, sel_count: torch.Tensor,
+                            b: int, window: int, n_sink: int = 0, max_seqlen: Optional[int] = None,
+                            k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+                            scale_block: int = 32, scale: float = 0.0, want_f32: bool = True,
+                            want_bf16: bool = False) -> WindowAttnOut:
+    """q: bf16 [B, Hq, D], one token per sequence, whose row is the last of the seq_len in K / V (those as in
+    make_window_attn_args).  sel_*: a selection per query head, or per KV head (select_topk with shared=True)."""
+    a = dsk_window_sparse_args()
+    B, lists, k = sel_start.shape
+    assert q.shape[0] == B == seq_len.numel() and lists in (q.shape[1], K.shape[0])
+    assert sel_len.shape == sel_start.shape and sel_count.shape == (B, lists)
+    for t in (sel_start, sel_len, sel_count):
+        _i32_on(t, 0)
+    a.max_seqlen, a.k, a.b = K.shape[1] if max_seqlen is None else max_seqlen, k, b
+    a.flags = DSK_ATTN_SHARED_SELECTION if lists != q.shape[1] else 0
+    a.sel_start, a.sel_len, a.sel_count = _ptr(sel_start), _ptr(sel_len), _ptr(sel_count)
+    return _window_call(a, dsk_window_sparse_decode_attn, dsk_window_sparse_workspace_bytes, q, K, V, seq_row0, seq_len, window,
+                        n_sink, k_scale, v_scale, scale_block, scale, want_f32, want_bf16, sel_start, sel_len, sel_count)
+
+
+def window_sparse_decode_attn(q, K, V, *, stream=None, check: bool = True, **kw) -> WindowAttnOut:
+    """dsk_window_sparse_decode_attn with outputs and workspace made here; keywords as in make_window_sparse_args."""
+    r = make_window_sparse_args(q, K, V, **kw)
+    r.step(stream, check)
+    return r

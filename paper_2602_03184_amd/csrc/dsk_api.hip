@@ -393,6 +393,91 @@ static dsk_status validate_accept(const dsk_accept_args* a) {
   return DSK_OK;
 }
 
+// codes and scales of a cache in 8 bits; a bf16 cache without k_scale
+static dsk_status scales_ok(const void* k_scale, const void* v_scale, int64_t stride_head, int block, int total_rows) {
+  if (!k_scale || !v_scale) return DSK_ERR_NULL;
+  if (block != 32 && block != 64 && block != 128) return DSK_ERR_PARAM;
+  return stride_head < ((int64_t)total_rows + block - 1) / block ? DSK_ERR_SHAPE : DSK_OK;
+}
+
+static dsk_status validate_kv8_append(const dsk_kv8_append_args* a) {
+  if (a == nullptr) return DSK_ERR_NULL;
+  if (a->struct_size != sizeof(dsk_kv8_append_args)) return DSK_ERR_VERSION;
+  if (a->B < 1 || a->B > 65535 || a->Hkv < 1 || a->Hkv > 65535 || a->D != DSK_HEAD_DIM || a->n_tokens < 0 || a->total_rows < 0)
+    return DSK_ERR_SHAPE;
+  if (a->q && (a->Hq < 1 || (int64_t)a->scale_block * a->Hq > 0x7FFFFFFF)) return DSK_ERR_SHAPE;
+  if (a->max_new < 1 || (a->flags & ~DSK_ROPE_INTERLEAVED)) return DSK_ERR_PARAM;
+  if (a->rot_dim < 0 || a->rot_dim > DSK_HEAD_DIM || a->rot_dim % 16) return DSK_ERR_PARAM;
+  if ((a->q_weight || a->k_weight) && !(a->eps > 0.0f)) return DSK_ERR_PARAM;
+  if (!a->seq_row0 || !a->seq_len || !a->cu_new || !a->K || !a->V) return DSK_ERR_NULL;
+  if (a->rot_dim > 0 && !a->inv_freq) return DSK_ERR_NULL;
+  if (a->n_tokens > 0 && (!a->k || !a->v || (a->q && !a->q_out))) return DSK_ERR_NULL;
+  if (const dsk_status v = scales_ok(a->k_scale, a->v_scale, a->scale_stride_head, a->scale_block, a->total_rows); v != DSK_OK) return v;
+  if (a->k_stride_tok < 0 || a->k_stride_head < 0 || a->v_stride_tok < 0 || a->v_stride_head < 0 ||
+      (a->q && (a->q_stride_tok < 0 || a->q_stride_head < 0)))
+    return DSK_ERR_SHAPE;
+  if (!aligned16(a->k) || !aligned16(a->v) || a->k_stride_tok % 8 || a->k_stride_head % 8 || a->v_stride_tok % 8 || a->v_stride_head % 8)
+    return DSK_ERR_ALIGN;
+  if (a->q && (!aligned16(a->q) || !aligned16(a->q_out) || a->q_stride_tok % 8 || a->q_stride_head % 8)) return DSK_ERR_ALIGN;
+  if (!aligned16(a->q_weight) || !aligned16(a->k_weight) || (reinterpret_cast<uintptr_t>(a->inv_freq) & 3u)) return DSK_ERR_ALIGN;
+  if (const dsk_status v = cache_ok(a->K, a->kc_stride_tok, a->kc_stride_head, a->Hkv); v != DSK_OK) return v;
+  if (const dsk_status v = cache_ok(a->V, a->vc_stride_tok, a->vc_stride_head, a->Hkv); v != DSK_OK) return v;
+  return (a->kc_stride_tok | a->kc_stride_head | a->vc_stride_tok | a->vc_stride_head) % 16 ? DSK_ERR_ALIGN : DSK_OK;
+}
+
+// what the two calls have in common
+template <class ARGS>
+static dsk_status window_cache_ok(const ARGS& a) {
+  if ((!a.K || !a.V) && a.total_rows > 0) return DSK_ERR_NULL;
+  if (a.k_stride_tok < DSK_HEAD_DIM || a.v_stride_tok < DSK_HEAD_DIM || a.k_stride_head < 0 || a.v_stride_head < 0 ||
+      a.k_stride_tok > kMaxTokenStride || a.v_stride_tok > kMaxTokenStride)
+    return DSK_ERR_SHAPE;
+  const int64_t step = a.k_scale || a.v_scale ? 16 : 8;
+  if (a.k_scale || a.v_scale)
+    if (const dsk_status v = scales_ok(a.k_scale, a.v_scale, a.scale_stride_head, a.scale_block, a.total_rows); v != DSK_OK) return v;
+  if (!aligned16(a.q) || !aligned16(a.K) || !aligned16(a.V) || !aligned16(a.out) || !aligned16(a.out_bf16) ||
+      a.k_stride_tok % step || a.k_stride_head % step || a.v_stride_tok % step || a.v_stride_head % step)
+    return DSK_ERR_ALIGN;
+  return DSK_OK;
+}
+
+static bool window_attn_shape_ok(const dsk_window_attn_args& a) {
+  return geometry_ok(a.B, a.Hq, a.Hkv, a.D) && a.n_tokens >= 0 && (int64_t)a.n_tokens * a.Hq <= 0x7FFFFFFF && a.total_rows >= 0 &&
+         a.max_seqlen >= 0 && a.max_new >= 1 && (int64_t)a.max_new * a.Hq <= 0x7FFFFFFF && (int64_t)a.max_seqlen + a.max_new <= kMaxWindowKeys;
+}
+
+static dsk_status validate_window_attn(const dsk_window_attn_args* a) {
+  if (a == nullptr) return DSK_ERR_NULL;
+  if (a->struct_size != sizeof(dsk_window_attn_args)) return DSK_ERR_VERSION;
+  if (!window_attn_shape_ok(*a)) return DSK_ERR_SHAPE;
+  if (a->window < 1 || a->n_sink < 0 || !(a->scale >= 0.0f) || a->flags != 0) return DSK_ERR_PARAM;
+  if (!a->seq_row0 || !a->seq_len || !a->cu_new) return DSK_ERR_NULL;
+  if ((!a->q || (!a->out && !a->out_bf16)) && a->n_tokens > 0) return DSK_ERR_NULL;
+  if (const dsk_status v = window_cache_ok(*a); v != DSK_OK) return v;
+  if (a->workspace == nullptr || a->workspace_bytes < dsk_window_attn_workspace_bytes(a)) return DSK_ERR_WORKSPACE;
+  return aligned256(a->workspace) ? DSK_OK : DSK_ERR_ALIGN;
+}
+
+static bool window_sparse_shape_ok(const dsk_window_sparse_args& a) {
+  return geometry_ok(a.B, a.Hq, a.Hkv, a.D) && a.total_rows >= 0 && a.max_seqlen >= 0 && a.max_seqlen <= kMaxWindowKeys;
+}
+static bool window_sparse_params_ok(const dsk_window_sparse_args& a) {
+  return a.window >= 0 && a.n_sink >= 0 && a.k >= 1 && a.k <= kMaxWindowKeys && a.b >= 1 && a.b <= 1024 &&
+         !(a.flags & ~DSK_ATTN_SHARED_SELECTION);
+}
+
+static dsk_status validate_window_sparse(const dsk_window_sparse_args* a) {
+  if (a == nullptr) return DSK_ERR_NULL;
+  if (a->struct_size != sizeof(dsk_window_sparse_args)) return DSK_ERR_VERSION;
+  if (!window_sparse_shape_ok(*a)) return DSK_ERR_SHAPE;
+  if (!window_sparse_params_ok(*a) || !(a->scale >= 0.0f)) return DSK_ERR_PARAM;
+  if (!a->q || (!a->out && !a->out_bf16) || !a->seq_row0 || !a->seq_len || !a->sel_start || !a->sel_len || !a->sel_count)
+    return DSK_ERR_NULL;
+  if (const dsk_status v = window_cache_ok(*a); v != DSK_OK) return v;
+  if (a->workspace == nullptr || a->workspace_bytes < dsk_window_sparse_workspace_bytes(a)) return DSK_ERR_WORKSPACE;
+  return aligned256(a->workspace) ? DSK_OK : DSK_ERR_ALIGN;
+}
+
 // ---- scratch of dsk_sparse_decode_attn_static ------------------------------------------------
 // One array per GPU the library runs on, held until the process ends.  Host code never uses the
 // array's name as an address: the device address is looked up once per device and kept.
@@ -549,6 +634,41 @@ dsk_status dsk_accept_draft(const dsk_accept_args* a, void* stream) {
   const dsk_status v = validate_accept(a);
   if (v != DSK_OK) return v;
   if (launch_accept(*a, static_cast<hipStream_t>(stream)) != hipSuccess) return DSK_ERR_LAUNCH;
+  return DSK_OK;
+}
+
+dsk_status dsk_kv8_append(const dsk_kv8_append_args* a, void* stream) {
+  const dsk_status v = validate_kv8_append(a);
+  if (v != DSK_OK) return v;
+  if (a->n_tokens == 0) return DSK_OK;
+  if (launch_kv8_append(*a, static_cast<hipStream_t>(stream)) != hipSuccess) return DSK_ERR_LAUNCH;
+  return DSK_OK;
+}
+
+size_t dsk_window_attn_workspace_bytes(const dsk_window_attn_args* a) {
+  if (a == nullptr || a->struct_size != sizeof(dsk_window_attn_args)) return 0;
+  if (!window_attn_shape_ok(*a) || a->window < 1 || a->n_sink < 0) return 0;
+  return window_ws_bytes(*a);
+}
+
+dsk_status dsk_window_attn(const dsk_window_attn_args* a, void* stream) {
+  const dsk_status v = validate_window_attn(a);
+  if (v != DSK_OK) return v;
+  if (a->n_tokens == 0) return DSK_OK;
+  if (launch_window_attn(*a, static_cast<hipStream_t>(stream)) != hipSuccess) return DSK_ERR_LAUNCH;
+  return DSK_OK;
+}
+
+size_t dsk_window_sparse_workspace_bytes(const dsk_window_sparse_args* a) {
+  if (a == nullptr || a->struct_size != sizeof(dsk_window_sparse_args)) return 0;
+  if (!window_sparse_shape_ok(*a) || !window_sparse_params_ok(*a)) return 0;
+  return window_sparse_ws_bytes(*a);
+}
+
+dsk_status dsk_window_sparse_decode_attn(const dsk_window_sparse_args* a, void* stream) {
+  const dsk_status v = validate_window_sparse(a);
+  if (v != DSK_OK) return v;
+  if (launch_window_sparse(*a, static_cast<hipStream_t>(stream)) != hipSuccess) return DSK_ERR_LAUNCH;
   return DSK_OK;
 }
 

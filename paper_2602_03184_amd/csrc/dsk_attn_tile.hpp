@@ -214,14 +214,15 @@ struct TileSoftmax {
   float m, l, err, scale_log2;
   FmaExponent exponent;
   __device__ __forceinline__ explicit TileSoftmax(float scale) : m(-__builtin_inff()), l(0.0f), err(0.0f), scale_log2(scale), exponent(scale, 0.0f) {}
-  // weights of a tile from its logits
-  template <int TERMS>
-  __device__ __forceinline__ void take(const tile_f32x16& z, tile_f32x16 (&O)[4], TileWeights<TERMS>& w) {
+  // Weights of a tile from its logits.  APART: a query's reference moves by its own logits alone, so that no bit of its result depends
+  // on the wavefront's other queries.  by: factors of the keys' values, which go into the weights, at the lane's first key.
+  template <int TERMS, bool APART = false>
+  __device__ __forceinline__ void take(const tile_f32x16& z, tile_f32x16 (&O)[4], TileWeights<TERMS>& w, const float* by = nullptr) {
     const float mx = tile_max(z) * scale_log2;
     // The reference only has to be near the maximum: it moves when a query's maximum grows by more than 8, so most tiles
     // rescale nothing, and the weights stay below 2^8.
     if (__any(mx - m > 8.0f)) {                          // m = -inf: true unless nothing has been seen
-      const float m_new = fmaxf(m, mx);
+      const float m_new = !APART || mx - m > 8.0f ? fmaxf(m, mx) : m;
       const float f = m == -__builtin_inff() ? 0.0f : exp2_small(m - m_new);
       l *= f;
       err *= f;
@@ -237,6 +238,13 @@ struct TileSoftmax {
     const float add = tile - err, sum = l + add;
     err = (sum - l) - add;
     l = sum;
+    if (by != nullptr) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 f = *reinterpret_cast<const float4*>(by + 8 * j);
+        p[4 * j] *= f.x; p[4 * j + 1] *= f.y; p[4 * j + 2] *= f.z; p[4 * j + 3] *= f.w;
+      }
+    }
     w.set(p);
   }
   // both halves' sum

@@ -147,4 +147,12 @@ constexpr int kMaxTreePrefix = 0x7FFF0000;     // keeps a key's number, nodes an
 size_t tree_ws_bytes(const dsk_tree_attn_args& a);
 hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st);
 
+// ---- a cache in 8 bits, sliding window and first tokens ---------------------------------------------
+constexpr int kMaxWindowKeys = 0x7FFF0000;     // positions: a key's number and a tile's overhang in 32 bits
+hipError_t launch_kv8_append(const dsk_kv8_append_args& a, hipStream_t st);
+size_t window_ws_bytes(const dsk_window_attn_args& a);
+hipError_t launch_window_attn(const dsk_window_attn_args& a, hipStream_t st);
+size_t window_sparse_ws_bytes(const dsk_window_sparse_args& a);
+hipError_t launch_window_sparse(const dsk_window_sparse_args& a, hipStream_t st);
+
 }  // namespace dsk

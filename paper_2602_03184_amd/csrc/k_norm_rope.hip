@@ -5,24 +5,14 @@
 // through LDS.
 // 32K tokens of 32 / 8 heads (805 MB) 143 to 156 us, 5.2 to 5.6 TB/s, a large copy's rate; 14K tokens of 40 / 40 heads (875 MB)
 // 184 to 190 us, whatever part is rotated and how; eight tokens 3.6 us.
-#include "dsk_common.hpp"
 #include "dsk_internal.hpp"
+#include "dsk_rope.hpp"
 
 namespace dsk {
 
 constexpr int kRopeWaves = 4;
 constexpr int kRopeThreads = kRopeWaves * DSK_WAVE;
 constexpr int kRopeBatch = 4;                 // quads of rows of a wavefront on their way at once
-constexpr int kRopeHalf = DSK_HEAD_DIM / 2;
-
-enum class RopePairs { kNone, kHalfAll, kHalf, kInterleaved };   // kHalfAll: channels i and i + 64, a fixed lane move
-
-typedef __bf16 rope_bf16x2 __attribute__((ext_vector_type(2)));
-typedef float rope_f32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t pack_bf16_rne(float lo, float hi) {
-  const rope_f32x2 f = {lo, hi};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, rope_bf16x2));
-}
 
 template <RopePairs PAIRS>
 __global__ __launch_bounds__(kRopeThreads) void norm_rope_kernel(dsk_norm_rope_args a, int waves_per_token, int quads_per_wave) {
@@ -93,32 +83,12 @@ __global__ __launch_bounds__(kRopeThreads) void norm_rope_kernel(dsk_norm_rope_a
       unpack8(y, f);
       const float* weight = is_q ? a.q_weight : a.k_weight;
       if (a.q_weight != nullptr || a.k_weight != nullptr) {
-        float ss = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
-        ss = group16_sum(ss);
+        const float ss = rope_square_sum(f);
         if (weight != nullptr && !is_v) {
-          const float inv = 1.0f / sqrtf(ss * (1.0f / DSK_HEAD_DIM) + a.eps);
-          const float4 w0 = *reinterpret_cast<const float4*>(weight + c * 8);
-          const float4 w1 = *reinterpret_cast<const float4*>(weight + c * 8 + 4);
-          f[0] *= inv * w0.x; f[1] *= inv * w0.y; f[2] *= inv * w0.z; f[3] *= inv * w0.w;
-          f[4] *= inv * w1.x; f[5] *= inv * w1.y; f[6] *= inv * w1.z; f[7] *= inv * w1.w;
+          rope_scale(f, ss, weight + c * 8, a.eps);
         }
       }
-      if constexpr (PAIRS == RopePairs::kInterleaved) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float lo = f[2 * e], hi = f[2 * e + 1];
-          f[2 * e] = inside ? fmaf(lo, cs[e], -hi * sn[e]) : lo;
-          f[2 * e + 1] = inside ? fmaf(lo, sn[e], hi * cs[e]) : hi;
-        }
-      } else if constexpr (PAIRS != RopePairs::kNone) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float o = PAIRS == RopePairs::kHalfAll ? dpp_f<0x128>(f[e]) : __shfl(f[e], partner, DSK_WAVE);   // 0x128: 8 lanes on in the row of 16
-          f[e] = PAIRS == RopePairs::kHalfAll || inside ? fmaf(f[e], cs[e], o * sn[e]) : f[e];
-        }
-      }
+      rope_turn<PAIRS>(f, cs, sn, inside, partner);
       if (!is_v && (inside || weight != nullptr))
         y = make_uint4(pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3]), pack_bf16_rne(f[4], f[5]), pack_bf16_rne(f[6], f[7]));
       if (r < rows) {

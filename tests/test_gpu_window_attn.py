@@ -1,0 +1,344 @@
+"""dsk_window_attn against the definition in 64 bits, on the numbers that the cache stands for (codes * scale without rounding).
+Bars: f32_bar() of size = sum p |V| / sum p.  bf16 outputs: weights of two terms are off by 2^-16, single ones by half a step, 2^-8 of
+each and so of the size, the result once more, 2^-8 of it."""
+import math
+
+import pytest
+import torch
+
+from step_testutil import i32, starts
+from window_testutil import D, TINY, as_bytes, attend, f32_bar, quantise, values
+
+pytestmark = pytest.mark.gpu
+
+BF16 = 2.0 ** -8
+ALL = 0x7FFFFFFF
+
+
+def _dsk():
+    import paper_2602_03184_amd as dsk
+    return dsk
+
+
+class Case:
+    """A batch with a region per sequence, K and V with outlier channels, and its reference."""
+
+    def __init__(self, lens, new, Hq, Hkv, *, bits=8, block=32, window=ALL, sinks=0, nhd=False, seed=0, spare=3, pad=0, sharp=1.0,
+                 aligned=True):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        self.lens, self.new, self.Hq, self.Hkv, self.bits, self.block = lens, new, Hq, Hkv, bits, block
+        self.window, self.sinks = window, sinks
+        room = [a + b + spare for a, b in zip(lens, new)]
+        if bits == 8 and aligned:
+            room = [-(-x // block) * block for x in room]
+        self.row0 = starts(room)
+        self.cu, self.rows = starts(new), self.row0[-1]
+        self.N = self.cu[-1] + pad
+
+        def cache():
+            X = torch.randn(Hkv, max(self.rows, 1), D, generator=g, device="cuda")
+            X[..., 7::31] *= 4.0
+            X *= torch.exp(torch.randn(Hkv, max(self.rows, 1), 1, generator=g, device="cuda"))
+            X, scale = (X.bfloat16(), None) if bits == 16 else quantise(X, block)
+            if nhd:
+                wide = torch.zeros(X.shape[1], Hkv, D + 32, dtype=torch.bfloat16 if bits == 16 else torch.uint8, device="cuda")
+                view = wide[..., :D].transpose(0, 1)
+                view.copy_(X if bits == 16 else as_bytes(X))
+                X = view if bits == 16 else view.view(torch.float8_e4m3fn)
+            return X, scale
+        (self.K, self.ks), (self.V, self.vs) = cache(), cache()
+        self.q = (torch.randn(max(self.N, 1), Hq, D, generator=g, device="cuda") * sharp).bfloat16()[: self.N]
+
+    def numbers(self):
+        if self.bits == 16:
+            return self.K.double(), self.V.double()
+        return values(self.K, self.ks, self.block), values(self.V, self.vs, self.block)
+
+    def kwargs(self, **over):
+        kw = dict(seq_row0=i32(self.row0[:-1]), seq_len=i32(self.lens), cu_new=i32(self.cu), max_new=max(max(self.new), 1),
+                  max_seqlen=max(self.lens), window=self.window, n_sink=self.sinks, k_scale=self.ks, v_scale=self.vs,
+                  scale_block=self.block)
+        kw.update(over)
+        return kw
+
+    def run(self, **over):
+        r = _dsk().make_window_attn_args(self.q, self.K, self.V, **self.kwargs(**over))
+        for t in (r.out, r.out_bf16, r.lse):
+            if t is not None:
+                t.fill_(9.0)
+        r.step()
+        torch.cuda.synchronize()
+        return r
+
+    def seen(self, s):
+        L, n = self.lens[s], self.new[s]
+        t = torch.arange(L + n, device="cuda")
+        p = t[L:, None]
+        return (t <= p) & ((p - t < self.window) | (t < self.sinks))
+
+    def reference(self, scale=None):
+        G = self.Hq // self.Hkv
+        K, V = self.numbers()
+        out, size = (torch.zeros(self.cu[-1], self.Hq, D, dtype=torch.float64, device="cuda") for _ in range(2))
+        lse, bar = (torch.zeros(self.cu[-1], self.Hq, dtype=torch.float64, device="cuda") for _ in range(2))
+        for s, n in enumerate(self.new):
+            t, seen = slice(self.cu[s], self.cu[s + 1]), self.seen(s).repeat_interleave(G, 0)
+            for h in range(self.Hkv):
+                hs, rows = slice(h * G, (h + 1) * G), slice(self.row0[s], self.row0[s] + self.lens[s] + n)
+                o, z, l, terms = attend(self.q[t, hs].reshape(n * G, D), K[h, rows], V[h, rows], seen, scale)
+                out[t, hs], size[t, hs], lse[t, hs] = o.view(n, G, D), z.view(n, G, D), l.view(n, G)
+                bar[t, hs] = f32_bar(terms).view(n, G)
+        return out, size, lse, bar
+
+    def check(self, scale=None, want=None):
+        out, size, lse, bar = self.reference(scale) if want is None else want
+        n = self.cu[-1]
+        sc = 0.0 if scale is None else scale
+        a = self.run(scale=sc)
+        b = self.run(scale=sc, want_f32=False, want_bf16=True)
+        c = self.run(scale=sc, want_bf16=True)
+        weights = 2.0 ** -16 if max(self.new) * self.Hq // self.Hkv <= 64 else BF16
+        assert bool(((a.out[:n].double() - out).abs() <= bar[..., None] * size + TINY).all())
+        assert bool(((b.out_bf16[:n].double() - out).abs() <= BF16 * (1 + BF16) * out.abs() + (weights * (1 + BF16) + bar[..., None]) * size + TINY).all())
+        assert torch.equal(c.out[:n], a.out[:n]) and torch.equal(c.out_bf16[:n], a.out[:n].bfloat16())
+        fine = torch.isfinite(lse)
+        for r in (a, b, c):
+            got = r.lse[:n].double()
+            assert torch.equal(got[~fine], lse[~fine])
+            assert bool(((got - lse)[fine].abs() <= bar[fine] + 1e-5 * lse[fine].abs()).all())
+            for t in (r.out, r.out_bf16, r.lse):                 # rows behind the last sequence stay as they were
+                assert t is None or bool((t[n:] == 9.0).all())
+        return a
+
+
+LENS = [0, 1, 31, 32, 33, 64, 127, 129, 700, 1025]
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("Hq, Hkv", [(1, 1), (8, 8), (8, 2), (6, 2), (5, 1), (16, 2), (14, 2), (40, 1)])
+@pytest.mark.parametrize("new", [1, 2, 7, 16, 33])
+def test_group_widths_and_ragged_lengths(Hq, Hkv, new, bits):
+    n = [max(0, new - (s % 3)) for s in range(len(LENS))]
+    Case(LENS, n, Hq, Hkv, bits=bits, seed=new, nhd=new == 7, block=(32, 64, 128)[new % 3], pad=2).check()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("window, sinks", [(1, 0), (1, 1), (5, 0), (31, 4), (32, 32), (33, 33), (64, 1), (100, 64), (100, 500), (640, 4), (5000, 4),
+                                           (ALL, 7), (ALL, ALL), (7, ALL)])
+@pytest.mark.parametrize("new", [1, 12, 150])
+def test_windows_and_first_tokens(window, sinks, new, bits):
+    Case([0, 3, 37, 300, 1000], [new, new, max(new - 1, 1), 0, new], 8, 2, bits=bits, window=window, sinks=sinks, seed=window % 97 + new).check()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("Hq, Hkv, new", [(4, 4, 300), (8, 2, 257), (8, 1, 130), (3, 1, 1000)])
+def test_prompts(Hq, Hkv, new, bits):
+    Case([0, 45, 600], [new, new // 3, new], Hq, Hkv, bits=bits, seed=new, nhd=new == 257).check()
+    Case([0, 45, 600], [new, new // 3, new], Hq, Hkv, bits=bits, seed=new, window=70, sinks=3).check()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_long_contexts_split_over_many_workgroups(bits):
+    Case([20011, 40000, 3], [1, 1, 1], 8, 2, bits=bits, seed=8).check()
+    Case([20011, 40000, 3], [4, 1, 4], 8, 2, bits=bits, seed=8, window=30000, sinks=40).check()
+    Case([33333], [16], 4, 4, bits=bits, seed=9, nhd=True, block=128).check()
+    Case([9000], [128], 8, 1, bits=bits, seed=10).check()
+    Case([70001], [3], 1, 1, bits=bits, seed=11).check()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("end", [4095, 4096, 4097, 4127, 4159, 4223, 4351])
+def test_the_cache_ends_in_any_place_of_a_tile(end, bits):
+    Case([end], [1], 8, 2, bits=bits, seed=end, spare=0).check()
+    Case([end - 40], [40], 8, 2, bits=bits, seed=end, spare=0, window=999).check()
+
+
+def test_sequences_that_begin_within_a_block_of_scales():
+    c = Case([50, 300], [9, 70], 8, 2, seed=5, aligned=False, spare=1)
+    assert c.row0[1] % 32
+    c.check()
+
+
+def test_scale_and_sharp_logits():
+    for bits in (8, 16):
+        c = Case([300, 40], [9, 9], 8, 2, seed=6, bits=bits)
+        c.check(scale=0.03)
+    # one key takes nearly all the weight
+    Case([300, 40], [9, 9], 8, 2, seed=7, sharp=8.0).check()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("new, window, sinks", [(1, 40, 3), (9, 40, 3), (9, ALL, 0), (150, 40, 35), (150, ALL, 0)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_rows_that_are_not_seen_may_hold_anything(what, new, window, sinks, bits):
+    """Rows that have left the window, rows of later tokens, the room behind every sequence and other sequences' rows."""
+    if bits == 8:
+        what = float("nan")                                      # there are no infinities
+    c = Case([70, 0, 333], [new, new, 3], 8, 2, bits=bits, window=window, sinks=sinks, seed=13, spare=20)
+    clean = [c.run(), c.run(want_f32=False, want_bf16=True)]
+
+    def put(X, rows, value):
+        if bits == 16:
+            X[:, rows] = value
+        else:
+            as_bytes(X)[:, rows] = 0x7F if not isinstance(value, torch.Tensor) else value
+    for s in range(3):
+        for X in (c.K, c.V):                                     # the room
+            put(X, slice(c.row0[s] + c.lens[s] + c.new[s], c.row0[s + 1]), what)
+    for s in range(3):
+        seen = c.seen(s)
+        for t in {0, 5, max(c.lens[s] - 41, 0), c.lens[s], c.lens[s] + c.new[s] // 2, c.lens[s] + c.new[s] - 1}:
+            if t >= c.lens[s] + c.new[s]:
+                continue
+            old = [(X if bits == 16 else as_bytes(X))[:, c.row0[s] + t].clone() for X in (c.K, c.V)]
+            for X in (c.K, c.V):
+                put(X, c.row0[s] + t, what)
+            tok = torch.arange(c.cu[s], c.cu[s + 1], device="cuda")
+            for r0, kw in zip(clean, ({}, dict(want_f32=False, want_bf16=True))):
+                r = c.run(**kw)
+                a, b = (x.out if x.out is not None else x.out_bf16 for x in (r, r0))
+                blind, others = tok[~seen[:, t]], torch.cat([torch.arange(0, c.cu[s]), torch.arange(c.cu[s + 1], c.cu[-1])]).cuda()
+                assert torch.equal(a[blind], b[blind]) and torch.equal(r.lse[blind], r0.lse[blind])
+                assert torch.equal(a[others], b[others])
+                assert not bool(torch.isfinite(a[tok[seen[:, t]]]).all(-1).any()) or not bool(seen[:, t].any())
+            for X, o in zip((c.K, c.V), old):
+                put(X, c.row0[s] + t, o)
+
+
+def test_an_infinity_that_is_seen_gives_that_infinity():
+    for new, kw in ((1, {}), (9, {}), (150, dict(window=90, sinks=40))):
+        c = Case([60], [new], 8, 2, bits=16, seed=14, **kw)
+        seen = c.seen(0)
+        c.V[:, 33, 5] = float("inf")
+        c.V[:, 60 + new - 1, 6] = -float("inf")
+        for out in (c.run().out, c.run(want_f32=False, want_bf16=True).out_bf16):
+            assert torch.equal(out[..., 5] == float("inf"), seen[:, 33, None].expand(-1, 8))
+            assert torch.equal(out[..., 6] == -float("inf"), seen[:, 60 + new - 1, None].expand(-1, 8))
+            fine = [i for i in range(D) if i not in (5, 6)]
+            assert bool(torch.isfinite(out[..., fine]).all())
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_a_nan_in_a_query_is_its_rows_alone(bits):
+    for new in (1, 9, 150):
+        c = Case([5000, 20], [new, new], 8, 2, bits=bits, seed=15)
+        a = c.run()
+        c.q[new // 2, 3, 17] = float("nan")
+        b = c.run()
+        assert bool(torch.isnan(b.out[new // 2, 3]).all()) and bool(torch.isnan(b.lse[new // 2, 3]))
+        keep = torch.ones(2 * new, 8, dtype=torch.bool, device="cuda")
+        keep[new // 2, 3] = False
+        assert torch.equal(a.out[keep], b.out[keep]) and torch.equal(a.lse[keep], b.lse[keep])
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_malformed_tables_are_cut(bits):
+    c = Case([64, 64], [8, 8], 4, 2, bits=bits, seed=14, spare=0, aligned=False)
+    base = c.run()
+    r = c.run(cu_new=i32([0, 8, 400]))                           # more tokens than there are rows and max_new
+    assert torch.equal(r.out, base.out)
+    r = c.run(cu_new=i32([0, 8, 3]))
+    assert torch.equal(r.out[:8], base.out[:8]) and bool((r.out[8:] == 9.0).all())
+    r = c.run(cu_new=i32([-1, 8, 16]))
+    assert bool((r.out[:8] == 9.0).all()) and torch.equal(r.out[8:], base.out[8:])
+    r = c.run(seq_len=i32([10 ** 9, 64]))                        # cut to max_seqlen = 64
+    assert torch.equal(r.out, base.out)
+    for kw in (dict(seq_row0=i32([-5, c.row0[1]])), dict(seq_len=i32([-5, 64])), dict(seq_row0=i32([2 ** 31 - 1, c.row0[1]])),
+               dict(seq_row0=i32([c.rows, c.row0[1]]))):
+        for more in ({}, dict(window=3, n_sink=2)):
+            r = c.run(**kw, **more)
+            assert bool((r.out[:8] == 0.0).all()) and bool((r.lse[:8] == -math.inf).all())
+            assert more or torch.equal(r.out[8:], base.out[8:])
+    r = c.run(seq_row0=i32([c.rows - 1, c.row0[1]]))             # one row is left: all tokens see it alone
+    v = c.numbers()[1][:, -1].repeat_interleave(2, 0)
+    assert bool(((r.out[:8].double() - v).abs() <= 1e-5 * v.abs()).all()) and torch.equal(r.out[8:], base.out[8:])
+    r = c.run(seq_row0=i32([c.rows - 1, c.row0[1]]), window=3, n_sink=0)
+    assert bool((r.out[:8] == 0.0).all()) and bool((r.lse[:8] == -math.inf).all())
+
+
+def test_bit_identical_from_call_to_call_on_another_stream_and_in_a_graph():
+    for bits in (8, 16):
+        for new in ([1, 1], [20, 9], [300, 2]):
+            c = Case([5000, 700], new, 8, 2, bits=bits, seed=15)
+            a, b = c.run(), c.run()
+            st = torch.cuda.Stream()
+            r = _dsk().make_window_attn_args(c.q, c.K, c.V, **c.kwargs())
+            torch.cuda.synchronize()
+            r.step(st)
+            st.synchronize()
+            for x in (b, r):
+                assert torch.equal(a.out, x.out) and torch.equal(a.lse, x.lse)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=st):
+                r.step(st)
+            for _ in range(3):
+                r.out.zero_()
+                c.run()
+                graph.replay()
+                torch.cuda.synchronize()
+                assert torch.equal(a.out, r.out) and torch.equal(a.lse, r.lse)
+
+
+def test_one_token_equals_the_decode_attention():
+    dsk = _dsk()
+    c = Case([3000], [1], 32, 8, bits=16, seed=16, spare=0)
+    den = dsk.dense_decode_attn(c.q, c.K, c.V, i32([0, c.rows]), c.rows)
+    r = c.run()
+    torch.cuda.synchronize()
+    _, size, lse, bar = c.reference()                            # either is off by as much from the definition
+    assert bool(((r.out - den.out).double().abs() <= 2 * bar[..., None] * size).all())
+    assert bool(((r.lse - den.lse).double().abs() <= 2 * (bar + 1e-5 * lse.abs())).all())
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_pieces_of_a_prompt_give_what_the_whole_gives(bits):
+    c = Case([0], [700], 8, 2, bits=bits, window=200, sinks=5, seed=17)
+    whole = c.run()
+    _, size, lse, bar = c.reference()
+    at = 0
+    for n in (1, 40, 300, 3, 356):
+        kw = c.kwargs(seq_len=i32([at]), cu_new=i32([0, n]), max_new=n, max_seqlen=at)
+        r = _dsk().window_attn(c.q[at: at + n].contiguous(), c.K, c.V, **kw)
+        torch.cuda.synchronize()
+        t = slice(at, at + n)                                    # either is off by as much from the definition
+        assert bool(((r.out - whole.out[t]).double().abs() <= 2 * bar[t, :, None] * size[t] + TINY).all())
+        assert bool(((r.lse - whole.lse[t]).double().abs() <= 2 * (bar[t] + 1e-5 * lse[t].abs())).all())
+        at += n
+
+
+def test_a_workspace_for_the_longest_cache_serves_shorter_ones():
+    c = Case([9000, 100], [2, 2], 8, 2, seed=18)
+    r = _dsk().make_window_attn_args(c.q, c.K, c.V, **c.kwargs(max_seqlen=120_000))
+    for most in (120_000, 40_000, 9000):
+        r.args.max_seqlen = most
+        r.out.fill_(9.0)
+        r.step()
+        torch.cuda.synchronize()
+        out, size, _, bar = c.reference()
+        assert bool(((r.out.double() - out).abs() <= bar[..., None] * size + TINY).all())
+
+
+def test_large_caches():
+    """A cache whose rows lie beyond 2^32 bytes of a head's first, in both types."""
+    for bits in (8, 16):
+        width = bits // 8
+        rows = (1 << 32) // (2 * D * width) + 128
+        X = torch.zeros(rows, 2, D, dtype=torch.uint8 if bits == 8 else torch.bfloat16, device="cuda")
+        c = Case([40], [9], 4, 1, bits=bits, seed=19, spare=0, aligned=False)
+        row0 = (rows - 100) // 32 * 32
+        K, V = (X[:, h:h + 1].transpose(0, 1) for h in range(2))
+        for big, small in ((K, c.K), (V, c.V)):
+            big[:, row0: row0 + 49] = small if bits == 16 else as_bytes(small)
+        over = dict(seq_row0=i32([row0]))
+        if bits == 8:
+            K, V = K.view(torch.float8_e4m3fn), V.view(torch.float8_e4m3fn)
+            for name, small in (("k_scale", c.ks), ("v_scale", c.vs)):
+                s = torch.full((1, -(-rows // 32)), 127, dtype=torch.uint8, device="cuda")
+                s[:, row0 // 32: row0 // 32 + 2] = as_bytes(small)
+                over[name] = s.view(torch.float8_e8m0fnu)
+        want = c.run()
+        r = _dsk().window_attn(c.q, K, V, **c.kwargs(**over))
+        torch.cuda.synchronize()
+        assert torch.equal(r.out, want.out) and torch.equal(r.lse, want.lse)
+        del X, K, V
