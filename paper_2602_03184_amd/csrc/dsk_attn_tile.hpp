@@ -207,6 +207,10 @@ __device__ __forceinline__ void tile_scale(tile_f32x16 (&O)[4], float f) {
     for (int i = 0; i < 16; ++i) O[ct][i] *= f;
 }
 
+struct TileNoChange {
+  __device__ __forceinline__ void operator()(float (&)[16]) const {}
+};
+
 // A query's running softmax: the reference of its exponents in log2 units (-inf: nothing seen) and this half's sum l - err.  A tile's
 // weights are added up by themselves and join the sum with what rounding took from it carried along: added one after the other, equal
 // weights are rounded alike, 1e-4 of the sum after 8192 of them.
@@ -215,9 +219,9 @@ struct TileSoftmax {
   FmaExponent exponent;
   __device__ __forceinline__ explicit TileSoftmax(float scale) : m(-__builtin_inff()), l(0.0f), err(0.0f), scale_log2(scale), exponent(scale, 0.0f) {}
   // Weights of a tile from its logits.  APART: a query's reference moves by its own logits alone, so that no bit of its result depends
-  // on the wavefront's other queries.  by: factors of the keys' values, which go into the weights, at the lane's first key.
-  template <int TERMS, bool APART = false>
-  __device__ __forceinline__ void take(const tile_f32x16& z, tile_f32x16 (&O)[4], TileWeights<TERMS>& w, const float* by = nullptr) {
+  // on the wavefront's other queries.  change: what else happens to the weights, once their sum is made.
+  template <int TERMS, bool APART = false, class CHANGE = TileNoChange>
+  __device__ __forceinline__ void take(const tile_f32x16& z, tile_f32x16 (&O)[4], TileWeights<TERMS>& w, const CHANGE& change = CHANGE()) {
     const float mx = tile_max(z) * scale_log2;
     // The reference only has to be near the maximum: it moves when a query's maximum grows by more than 8, so most tiles
     // rescale nothing, and the weights stay below 2^8.
@@ -238,13 +242,7 @@ struct TileSoftmax {
     const float add = tile - err, sum = l + add;
     err = (sum - l) - add;
     l = sum;
-    if (by != nullptr) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float4 f = *reinterpret_cast<const float4*>(by + 8 * j);
-        p[4 * j] *= f.x; p[4 * j + 1] *= f.y; p[4 * j + 2] *= f.z; p[4 * j + 3] *= f.w;
-      }
-    }
+    change(p);
     w.set(p);
   }
   // both halves' sum
