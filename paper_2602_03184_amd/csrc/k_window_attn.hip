@@ -9,86 +9,9 @@
 // A cache in 8 bits goes to LDS as it is, half the bytes of bf16 all the way, and is widened when fragments are read: K's codes with
 // their scale, which gives bf16 numbers without rounding; V's as they are, with the scale in the weights instead, since the eight keys
 // of a lane's fragment need not have one scale.
-#include "dsk_window_fold.hpp"
+#include "dsk_window_run.hpp"
 
 namespace dsk {
-
-// ---- which keys ------------------------------------------------------------------------------------------
-// What a sequence has in fact, malformed tables cut to the bounds that the host knows.
-struct WinPlace {
-  int tok0, n;          // its new tokens; 0: nothing to do
-  int64_t row0;
-  int len, there;       // tokens before them; positions that have a row
-  __device__ __forceinline__ WinPlace(const dsk_window_attn_args& a, int s) {
-    tok0 = a.cu_new[s];
-    int64_t m = (int64_t)a.cu_new[s + 1] - tok0;
-    if (tok0 < 0 || tok0 > a.n_tokens || m < 0) m = 0;
-    m = m < a.max_new ? m : a.max_new;
-    m = m < a.n_tokens - tok0 ? m : a.n_tokens - tok0;
-    n = (int)m;
-    row0 = a.seq_row0[s];
-    len = a.seq_len[s];
-    const bool nowhere = row0 < 0 || row0 >= a.total_rows || len < 0;
-    if (nowhere) row0 = len = 0;
-    len = len < a.max_seqlen ? len : a.max_seqlen;
-    const int64_t left = nowhere ? 0 : a.total_rows - row0;
-    there = (int)(len + (int64_t)n < left ? len + (int64_t)n : left);
-  }
-};
-
-// The tiles that rows [r0, r1) of a sequence see: `first` of the first tokens, then those from position lo on.
-struct WinTiles {
-  int p0, p1;           // positions of the first and the last row
-  int first, lo, n;
-  WinTiles() = default;
-  __device__ __forceinline__ WinTiles(const dsk_window_attn_args& a, const WinPlace& at, int G, int r0, int r1) {
-    p0 = at.len + r0 / G;
-    p1 = at.len + (r1 - 1) / G;
-    const int w = p0 - a.window + 1 > 0 ? p0 - a.window + 1 : 0;
-    const int hi = p1 + 1 < at.there ? p1 + 1 : at.there;
-    int sinks = a.n_sink < w ? a.n_sink : w;
-    sinks = sinks < at.there ? sinks : at.there;         // (no row, no tile)
-    first = (int)(((int64_t)sinks + kAttnTile - 1) / kAttnTile);
-    lo = w / kAttnTile * kAttnTile;
-    if (first > 0 && lo <= first * kAttnTile) first = lo = 0;
-    n = first + (hi > lo ? (hi - lo + kAttnTile - 1) / kAttnTile : 0);
-  }
-  __device__ __forceinline__ int t0(int v) const { return v < first ? v * kAttnTile : lo + (v - first) * kAttnTile; }
-  __device__ __forceinline__ int used(int tiles_per_split) const {
-    const int u = (n + tiles_per_split - 1) / tiles_per_split;
-    return u > 0 ? u : 1;
-  }
-};
-
-// Keys of a workgroup that are positions of its sequence: tiles [begin, end).
-struct WinRun {
-  static constexpr bool kRun = true;
-  WinTiles tiles;
-  int begin, end;
-  int64_t row0;
-  int there, window, sinks;
-  // row of the cache of the tile's first position, which there always is, and the last of its positions that there is
-  __device__ __forceinline__ int64_t start(int v) const { return row0 + tiles.t0(v); }
-  __device__ __forceinline__ int last(int v) const {
-    const int left = there - tiles.t0(v);
-    return (left < kAttnTile ? left : kAttnTile) - 1;
-  }
-  __device__ __forceinline__ int row_of(int v, int r) const {   // of the sequence; cut to what there is
-    const int t = tiles.t0(v) + r;
-    return t < there ? t : there - 1;
-  }
-  // every row sees all of the tile
-  __device__ __forceinline__ bool plain(int v) const {
-    const int t = tiles.t0(v);
-    return t + kAttnTile <= (tiles.p0 + 1 < there ? tiles.p0 + 1 : there) && (t > tiles.p1 - window || t + kAttnTile <= sinks);
-  }
-  // keys of the tile that a row at position p sees
-  __device__ __forceinline__ uint32_t allowed(int v, int p) const {
-    const int64_t t = tiles.t0(v);
-    const int64_t gone = (int64_t)p - window + 1;        // positions that have left the window
-    return win_below((p + 1 < there ? p + 1 : there) - t) & (~win_below((gone > 0 ? gone : 0) - t) | win_below(sinks - t));
-  }
-};
 
 // ---- a workgroup's keys folded into its rows -----------------------------------------------------------------
 // QW wavefronts have 32 rows each, KW take other tiles of a stage for the same rows, NT of them each.  With two BUFS a stage is copied
@@ -208,47 +131,6 @@ struct WinFold {
   }
 };
 
-struct WinSplit {
-  int parts, tiles_per_part;
-};
-
-// What a workgroup takes: rows from r0 on of KV head hk, and a part of the tiles that they see; false: nothing.
-struct WinWork {
-  int s, hk, part, used;
-  int64_t r0, all;      // first row; rows of the sequence
-  __device__ __forceinline__ bool find(const dsk_window_attn_args& a, const WinSplit& sp, int G, int q_tiles, int q_rows, WinRun& keys, int& tok0, int& len) {
-    part = blockIdx.y;
-    s = blockIdx.z;
-    hk = blockIdx.x / q_tiles;
-    const WinPlace at(a, s);
-    r0 = (int64_t)(blockIdx.x - hk * q_tiles) * q_rows;
-    all = (int64_t)at.n * G;
-    if (r0 >= all) return false;
-    const WinTiles tiles(a, at, G, (int)r0, (int)(r0 + q_rows < all ? r0 + q_rows : all));
-    used = tiles.used(sp.tiles_per_part);
-    if (part >= used) return false;
-    const int begin = part * sp.tiles_per_part;
-    keys = WinRun{tiles, begin, tiles.n - begin < sp.tiles_per_part ? tiles.n : begin + sp.tiles_per_part, at.row0, at.there, a.window, a.n_sink};
-    tok0 = at.tok0;
-    len = at.len;
-    return true;
-  }
-  // the rows of a wavefront from r0 + first on
-  template <bool E4M3>
-  __device__ __forceinline__ void rows(WinRows& rows, const dsk_window_attn_args& a, int G, int first, int tok0, int len) const {
-    const int lane = threadIdx.x & (DSK_WAVE - 1);
-    rows.col = lane & 31;
-    rows.half = lane >> 5;
-    const int r = (int)r0 + first + rows.col;
-    rows.busy = r0 + first < all;
-    rows.real = r < all;
-    const int i = rows.real ? r / G : 0;
-    rows.pos = len + i;
-    rows.out_row = (int64_t)(tok0 + i) * a.Hq + hk * G + (rows.real ? r - i * G : 0);
-    rows.template load<E4M3>(static_cast<const uint16_t*>(a.q));
-  }
-};
-
 template <int QW, int KW, int NT, int BUFS, int TERMS, bool E4M3>
 __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void window_attn_kernel(dsk_window_attn_args a, WinCache c, WinOut to, int G, int q_tiles,
                                                                             WinSplit sp, float scale_log2) {
@@ -258,7 +140,7 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void window_attn_kernel(dsk_
   WinWork work;
   WinRun keys;
   int tok0 = 0, len = 0;
-  if (!work.find(a, sp, G, q_tiles, QW * kAttnTile, keys, tok0, len)) return;   // uniform, as all returns before the end
+  if (!work.find(a, sp, G, blockIdx.x / q_tiles, blockIdx.x % q_tiles, QW * kAttnTile, keys, tok0, len)) return;   // uniform, as all returns before the end
   WinRows rows;
   work.rows<E4M3>(rows, a, G, qw * kAttnTile, tok0, len);
   TileSoftmax sm(scale_log2);
@@ -281,7 +163,7 @@ __global__ __launch_bounds__(kStreamWaves * DSK_WAVE, E4M3 ? 2 : 1) void window_
   WinWork work;
   WinRun keys;
   int tok0 = 0, len = 0;
-  if (!work.find(a, sp, G, 1, kAttnTile, keys, tok0, len)) return;     // uniform
+  if (!work.find(a, sp, G, blockIdx.x, 0, kAttnTile, keys, tok0, len)) return;     // uniform
   WinRows rows;
   work.rows<E4M3>(rows, a, G, 0, tok0, len);
   TileSoftmax sm(scale_log2);
@@ -309,7 +191,8 @@ __global__ __launch_bounds__(kWinMergeWaves * DSK_WAVE) void window_merge_kernel
 
 // ---- geometry: follows the host's bounds alone ---------------------------------------------------------------
 struct WinLaunch {
-  int q_waves, q_tiles;
+  int q_waves, q_rows, q_tiles;   // wavefronts' rows of a workgroup, its rows, workgroups for all of them
+  bool wide;                      // window_wide_kernel
   WinSplit sp;
 };
 
@@ -321,20 +204,22 @@ static int win_most_parts(const dsk_window_attn_args& a, int q_tiles, int64_t ti
   return (int)(n > 1 ? n : 1);
 }
 
-static WinLaunch win_layout(const dsk_window_attn_args& a) {
+static WinLaunch win_layout(const dsk_window_attn_args& a, bool f32) {
   const int G = a.Hq / a.Hkv;
   const int64_t rows = (int64_t)a.max_new * G;
   WinLaunch t;
   t.q_waves = rows <= kAttnTile ? 1 : (rows <= kWinTwoTermRows ? 2 : 4);
-  t.q_tiles = (int)ceil_div(rows, t.q_waves * kAttnTile);
+  t.wide = rows > 128 && !f32;
+  t.q_rows = t.wide ? kWideRows : t.q_waves * kAttnTile;
+  t.q_tiles = (int)ceil_div(rows, t.q_rows);
   // tiles that a workgroup's rows see at most: the window of all its tokens, the first ones, a tile begun at either end
-  const int64_t tokens = a.max_new < t.q_waves * kAttnTile / G + 2 ? a.max_new : t.q_waves * kAttnTile / G + 2;
+  const int64_t tokens = a.max_new < t.q_rows / G + 2 ? a.max_new : t.q_rows / G + 2;
   const int64_t longest = (int64_t)a.max_seqlen + a.max_new;
   const int64_t near = ceil_div((int64_t)a.window + tokens, kAttnTile) + 1 + ceil_div(a.n_sink, kAttnTile);
   const int64_t tiles = near < ceil_div(longest, kAttnTile) ? near : ceil_div(longest, kAttnTile);
   const int most = win_most_parts(a, t.q_tiles, tiles);
-  // two workgroups a CU; of those that stream bf16 tiles, whose rings are twice as large, one
-  const int64_t want = t.q_waves == 1 && a.k_scale == nullptr ? kWinCus : 2 * kWinCus;
+  // two workgroups a CU; one of those for many rows, and of those that stream bf16 tiles, whose rings are twice as large
+  const int64_t want = t.wide || (t.q_waves == 1 && a.k_scale == nullptr) ? kWinCus : 2 * kWinCus;
   int64_t parts = want / ((int64_t)a.Hkv * t.q_tiles * a.B);
   parts = parts > 1 ? (parts < most ? parts : most) : 1;
   t.sp.tiles_per_part = (int)ceil_div(tiles, parts);
@@ -344,9 +229,13 @@ static WinLaunch win_layout(const dsk_window_attn_args& a) {
   return t;
 }
 
+// Whichever outputs the call will ask for, and no less than with a smaller max_seqlen.
 size_t window_ws_bytes(const dsk_window_attn_args& a) {
-  const WinLaunch t = win_layout(a);
-  const int most = win_most_parts(a, t.q_tiles, ceil_div((int64_t)a.max_seqlen + a.max_new, kAttnTile));
+  int most = 1;
+  for (const bool f32 : {false, true}) {
+    const int n = win_most_parts(a, win_layout(a, f32).q_tiles, ceil_div((int64_t)a.max_seqlen + a.max_new, kAttnTile));
+    most = n > most ? n : most;
+  }
   return win_part_bytes(most > 1 ? (size_t)a.n_tokens * a.Hq * most : 0);
 }
 
@@ -380,12 +269,15 @@ static void launch_stream(const dsk_window_attn_args& a, const WinLaunch& t, con
 }
 
 hipError_t launch_window_attn(const dsk_window_attn_args& a, hipStream_t st) {
-  const WinLaunch t = win_layout(a);
+  const WinLaunch t = win_layout(a, a.out != nullptr);
   const int G = a.Hq / a.Hkv;
   const WinCache c = win_cache(a);
   const WinOut to = win_out(a, t.sp.parts > 1 ? (size_t)a.n_tokens * a.Hq * t.sp.parts : 0);
   const float scale_log2 = (a.scale != 0.0f ? a.scale : kWinScale) * kLog2e;
-  if (t.q_waves == 1) launch_stream(a, t, c, to, scale_log2, st);
+  if (t.wide) {
+    const hipError_t err = launch_window_wide(a, c, to, t.q_tiles, t.sp, scale_log2, st);
+    if (err != hipSuccess) return err;
+  } else if (t.q_waves == 1) launch_stream(a, t, c, to, scale_log2, st);
   else if (t.q_waves == 2) launch_window<2, 2, 2, 1, 2>(a, t, c, to, scale_log2, st);
   else launch_window<4, 1, 4, 2, 2>(a, t, c, to, scale_log2, st);
   const hipError_t err = hipGetLastError();
@@ -393,8 +285,8 @@ hipError_t launch_window_attn(const dsk_window_attn_args& a, hipStream_t st) {
   const bool many = t.sp.parts >= kWinMergeMany;
   const int64_t rows = (int64_t)a.max_new * a.Hq, wgs = ceil_div(rows, many ? 1 : kWinMergeWaves);
   const dim3 grid((unsigned)wgs, (unsigned)a.B), block(kWinMergeWaves * DSK_WAVE);
-  if (many) window_merge_kernel<kWinMergeWaves><<<grid, block, 0, st>>>(a, to, G, t.q_waves * kAttnTile, t.sp);
-  else window_merge_kernel<1><<<grid, block, 0, st>>>(a, to, G, t.q_waves * kAttnTile, t.sp);
+  if (many) window_merge_kernel<kWinMergeWaves><<<grid, block, 0, st>>>(a, to, G, t.q_rows, t.sp);
+  else window_merge_kernel<1><<<grid, block, 0, st>>>(a, to, G, t.q_rows, t.sp);
   return hipGetLastError();
 }
 

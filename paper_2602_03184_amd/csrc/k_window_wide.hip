@@ -1,0 +1,287 @@
+// dsk_window_attn for many rows (prompts): the matrix cores bound it.
+//
+// A wavefront has 64 rows, as two halves of 32 that meet the same fragments of K and V, so that LDS is read half as often a product as
+// with 32; four wavefronts, one a SIMD, make a workgroup.  Each half's products run while the other half's softmax is made: in phase A
+// of tile i the matrix cores have K of tile i and V of tile i - 1 for half 1, in phase B K of tile i + 1 and V of tile i for half 0.  A
+// phase is straight-line code, about 512 cycles of the matrix core and as many of the vector ALU, most of them exponentials; what is
+// rare (masks, a reference that moves) lies between phases.
+//
+// K and V come to LDS through registers, a ring of three tiles in bf16: codes are widened on the way, once for all wavefronts.
+#include "dsk_window_run.hpp"
+
+namespace dsk {
+
+constexpr int kWideHalfRows = kAttnTile;
+
+// What a thread has of a tile on its way: 16-byte chunks of rows.
+template <bool E4M3>
+struct WideStage {
+  static constexpr int kChunks = (E4M3 ? 1 : 2) * DSK_HEAD_DIM / 16;      // of a row
+  static constexpr int kRows = kWideWaves * DSK_WAVE / kChunks;          // at once
+  static constexpr int kLoads = kAttnTile / kRows;
+  uint4 k[kLoads], v[kLoads];
+  uint32_t ks, vs;      // scales of the thread's row
+};
+
+// Tiles on their way, one after the other from the run's first on.  The addresses go along with the tiles, as a lone wavefront of a SIMD
+// has no time for others' arithmetic.
+template <bool E4M3>
+struct WideLoader {
+  using Stage = WideStage<E4M3>;
+  const WinCache& c;
+  const WinRun& keys;
+  int hk, row, chunk;
+  uint32_t k_off, v_off;
+  int v;                // the next tile
+  int64_t at;           // its first row, and its addresses
+  tile_global k, w;
+  __device__ __forceinline__ WideLoader(const WinCache& cache, const WinRun& run, int head) : c(cache), keys(run), hk(head) {
+    row = threadIdx.x / Stage::kChunks;
+    chunk = threadIdx.x % Stage::kChunks;
+    k_off = (uint32_t)(row * (int)c.k_tok + chunk * 16);
+    v_off = (uint32_t)(row * (int)c.v_tok + chunk * 16);
+    go(keys.begin);
+  }
+  __device__ __forceinline__ void go(int tile) {
+    v = tile;
+    at = keys.start(v);
+    k = (tile_global)(c.K + hk * c.k_head + at * c.k_tok);
+    w = (tile_global)(c.V + hk * c.v_head + at * c.v_tok);
+  }
+  // the next tile; beyond the last one that comes again, and is not read
+  __device__ __forceinline__ void fetch(Stage& x) {
+    const bool cut = keys.there - (int)(at - keys.row0) < kAttnTile;
+    if (!cut) {
+#pragma unroll
+      for (int u = 0; u < Stage::kLoads; ++u) {
+        x.k[u] = load16_at<false>(k + u * Stage::kRows * c.k_tok, k_off);
+        x.v[u] = load16_at<false>(w + u * Stage::kRows * c.v_tok, v_off);
+      }
+    } else {
+      const int last = keys.last(v);
+#pragma unroll
+      for (int u = 0; u < Stage::kLoads; ++u) {
+        const int r = row + u * Stage::kRows, n = r < last ? r : last;
+        x.k[u] = load16_at<false>(k, (uint32_t)(n * (int)c.k_tok + chunk * 16));
+        x.v[u] = load16_at<false>(w, (uint32_t)(n * (int)c.v_tok + chunk * 16));
+      }
+    }
+    if constexpr (E4M3) {
+      const int last = cut ? keys.last(v) : kAttnTile - 1;
+      const int64_t block = hk * c.s_head + ((at + (row < last ? row : last)) >> c.s_shift);
+      x.ks = c.ks[block];
+      x.vs = c.vs[block];
+    }
+    if (v + 1 == keys.tiles.first) {
+      if (v + 1 < keys.end) go(v + 1);
+    } else {
+      const bool more = v + 1 < keys.end;
+      v += more;
+      at += more ? kAttnTile : 0;
+      k += more ? kAttnTile * c.k_tok : 0;
+      w += more ? kAttnTile * c.v_tok : 0;
+    }
+  }
+  // Tile v into its buffer.  A masked row may hold anything, and 0 * NaN is NaN: where not every row sees all of the tile, values that are
+  // not finite are left out and the tile is noted.
+  __device__ __forceinline__ void put(Stage& x, int tile, unsigned char* sm_k, int* sm_left_out) const {
+    if (tile < keys.end && !keys.plain(tile)) {
+      uint32_t found = 0;
+#pragma unroll
+      for (int u = 0; u < Stage::kLoads; ++u) {
+        uint32_t* const y = &x.v[u].x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t was = y[i];
+          if constexpr (E4M3) {
+            const uint32_t nan = ((was & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+            y[i] = was & ~((nan << 1) - (nan >> 7));
+          } else {
+            y[i] = finite_bf16(was);
+          }
+          found |= was ^ y[i];
+        }
+      }
+      if (found != 0) *sm_left_out = tile;
+    }
+    unsigned char* const sm_v = sm_k + kTileBytes;
+    auto write = [&](int r, int to, const uint4& a, const uint4& b) {
+      *reinterpret_cast<uint4*>(sm_k + r * kTileRowBytes + ((to ^ (r & 15)) << 4)) = a;
+      *reinterpret_cast<uint4*>(sm_v + r * kTileRowBytes + ((to ^ ((r & 3) << 2)) << 4)) = b;
+    };
+#pragma unroll
+    for (int u = 0; u < Stage::kLoads; ++u) {
+      const int r = row + u * Stage::kRows;
+      if constexpr (!E4M3) {
+        write(r, chunk, x.k[u], x.v[u]);
+      } else {
+        const float s = __uint_as_float(x.ks << 23), t = __uint_as_float(x.vs << 23);
+        write(r, 2 * chunk, __builtin_bit_cast(uint4, win_widen8(x.k[u].x, x.k[u].y, s)), __builtin_bit_cast(uint4, win_widen8(x.v[u].x, x.v[u].y, t)));
+        write(r, 2 * chunk + 1, __builtin_bit_cast(uint4, win_widen8(x.k[u].z, x.k[u].w, s)),
+              __builtin_bit_cast(uint4, win_widen8(x.v[u].z, x.v[u].w, t)));
+      }
+    }
+  }
+};
+
+// Half of a wavefront's rows.  The softmax is that of TileSoftmax, taken apart: exponents are made from the reference as it is when the
+// logits come, and again in the rare case that it has to move.
+struct WideHalf {
+  WinRows rows;
+  TileSoftmax sm;
+  tile_f32x16 O[4];
+  tile_f32x16 z;        // logits of a tile,
+  float x[16];          // their exponents, in log2 units above the reference,
+  float mx;             // and the largest of these
+  TileWeights<1> w;
+  __device__ __forceinline__ explicit WideHalf(float scale_log2) : sm(scale_log2) { win_clear(O); }
+  __device__ __forceinline__ void exponents() {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = sm.exponent.of(z[i]);
+    float a = fmaxf(fmaxf(x[0], x[1]), x[2]), b = fmaxf(fmaxf(x[3], x[4]), x[5]);
+    a = fmaxf(fmaxf(a, x[6]), x[7]);
+    b = fmaxf(fmaxf(b, x[8]), x[9]);
+    a = fmaxf(fmaxf(a, x[10]), x[11]);
+    b = fmaxf(fmaxf(b, x[12]), x[13]);
+    mx = tile_half_max(fmaxf(fmaxf(fmaxf(a, x[14]), x[15]), b));
+  }
+  __device__ __forceinline__ uint32_t allowed(const WinRun& keys, int v) const { return rows.real ? keys.allowed(v, rows.pos) : 0u; }
+  // what comes between the logits of tile v and their weights
+  __device__ __forceinline__ void look(const WinRun& keys, int v, bool plain) {
+    if (!plain) {
+      tile_hide(z, allowed(keys, v) >> (4 * rows.half), 0);
+      exponents();
+    }
+    if (__any(mx > 8.0f || sm.m == -__builtin_inff())) {
+      const float top = tile_max(z) * sm.scale_log2;
+      const bool move = mx > 8.0f || sm.m == -__builtin_inff();
+      const float m_new = move ? fmaxf(sm.m, top) : sm.m;
+      const float f = sm.m == -__builtin_inff() ? 0.0f : exp2_small(sm.m - m_new);
+      sm.l *= f;
+      sm.err *= f;
+      tile_scale(O, f);
+      sm.m = m_new;
+      sm.exponent = FmaExponent(sm.scale_log2, sm.m == -__builtin_inff() ? 0.0f : sm.m);
+      exponents();
+    }
+  }
+};
+
+// A phase: the weights of half s, and meanwhile products of half p, of K for its next logits and of V with its weights.  next: where the
+// fragments of K that come after these are, or nullptr.
+template <bool READ>
+__device__ __forceinline__ void wide_phase(WideHalf& s, WideHalf& p, TileKFrag& kf, const WinVFrag<false>& vf, const unsigned char* next) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(s.x[i]));   // what is made of them is made here
+  kf.template add<0, 8>(p.z, p.rows);
+  vf.template add<1>(p.O, p.w, 0);
+  vf.template add<1>(p.O, p.w, 1);
+  float e[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) e[i] = exp2_small(s.x[i]);
+  const float tile = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])) +
+                     (((e[8] + e[9]) + (e[10] + e[11])) + ((e[12] + e[13]) + (e[14] + e[15])));
+  const float add = tile - s.sm.err, sum = s.sm.l + add;
+  s.sm.err = (sum - s.sm.l) - add;
+  s.sm.l = sum;
+  s.w.set(e);
+  if constexpr (READ) kf.template read<0, 8>(next, p.rows);
+  p.exponents();
+  __builtin_amdgcn_iglp_opt(3);                          // a matrix instruction, an exponential, and what else there is
+  asm volatile("" : "+v"(s.sm.l), "+v"(s.sm.err), "+v"(p.mx));
+}
+
+template <bool E4M3>
+__global__ __launch_bounds__(kWideWaves * DSK_WAVE, 1) void window_wide_kernel(dsk_window_attn_args a, WinCache c, WinOut to, int G, int q_tiles,
+                                                                              WinSplit sp, float scale_log2) {
+  constexpr int kRing = 3, kBuf = 2 * kTileBytes;
+  __shared__ __align__(16) unsigned char sm_kv[kRing * kBuf];
+  __shared__ int sm_left_out[kRing];                     // the tile of which values were left out, -1 none
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / DSK_WAVE);
+  // the last rows of a prompt see the most: they come first, and the workgroups of an XCD have few heads among them
+  const int hk = blockIdx.x % a.Hkv, q_tile = q_tiles - 1 - blockIdx.x / a.Hkv;
+  WinWork work;
+  WinRun keys;
+  int tok0 = 0, len = 0;
+  if (!work.find(a, sp, G, hk, q_tile, kWideRows, keys, tok0, len)) return;     // uniform
+  WideHalf h0(scale_log2), h1(scale_log2);
+  work.rows<false>(h0.rows, a, G, wave * 2 * kWideHalfRows, tok0, len);
+  work.rows<false>(h1.rows, a, G, (wave * 2 + 1) * kWideHalfRows, tok0, len);
+
+  const int begin = keys.begin, count = keys.end - keys.begin;
+  if (threadIdx.x < kRing) sm_left_out[threadIdx.x] = -1;
+  __syncthreads();
+  WideStage<E4M3> x[kRing];
+  TileKFrag kf;
+  WinVFrag<false> vf;
+  auto buffer = [&](int b) { return sm_kv + b * kBuf; };
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    h1.w.w[0][t] = __builtin_bit_cast(tile_bf16x8, make_uint4(0, 0, 0, 0));
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) vf.v[ct][t] = h1.w.w[0][t];
+  }
+  if (count > 0) {
+    WideLoader<E4M3> loader(c, keys, hk);
+    loader.fetch(x[0]);
+    loader.fetch(x[1]);
+    loader.fetch(x[2]);
+    loader.put(x[0], begin, buffer(0), sm_left_out);
+    loader.fetch(x[0]);
+    loader.put(x[1], begin + 1, buffer(1), sm_left_out + 1);
+    loader.fetch(x[1]);
+    __syncthreads();
+    kf.template read<0, 8>(buffer(0), h0.rows);
+    kf.template add<0, 8>(h0.z, h0.rows);
+    h0.exponents();
+    h0.look(keys, begin, keys.plain(begin));
+    // Tile i in buffer B = i % 3: K of tile i in kf, exponents of half 0 in h0.x, weights of half 1 for tile i - 1 in h1.w, its V in vf; set
+    // (i + 2) % 3 of x has tile i + 2.
+    auto step = [&](auto buf, int i) {
+      constexpr int B = decltype(buf)::value, kNext = (B + 1) % kRing, kAfter = (B + 2) % kRing;
+      const int v = begin + i;
+      loader.put(x[kAfter], v + 2, buffer(kAfter), sm_left_out + kAfter);
+      loader.fetch(x[kAfter]);
+      const bool plain = keys.plain(v), plain_next = keys.plain(v + 1);
+      wide_phase<true>(h0, h1, kf, vf, buffer(kNext));   // phase A
+      vf.template read<0>(buffer(B) + kTileBytes);
+      vf.template read<1>(buffer(B) + kTileBytes);
+      h1.look(keys, v, plain);
+      wide_phase<false>(h1, h0, kf, vf, nullptr);        // phase B
+      if (!plain && sm_left_out[B] == v) {
+        win_add_left_out<E4M3>(h0.O, c, keys, hk, v, h0.allowed(keys, v), h0.rows.half);
+        win_add_left_out<E4M3>(h1.O, c, keys, hk, v, h1.allowed(keys, v), h1.rows.half);
+      }
+      if (i + 1 < count) h0.look(keys, v + 1, plain_next);   // (behind the last tile the logits are another one's and nobody's)
+      __syncthreads();
+    };
+    using B0 = std::integral_constant<int, 0>;
+    using B1 = std::integral_constant<int, 1>;
+    using B2 = std::integral_constant<int, 2>;
+    for (int i = 0; i < count; i += kRing) {
+      step(B0(), i);
+      if (i + 1 < count) step(B1(), i + 1);
+      if (i + 2 < count) step(B2(), i + 2);
+    }
+    vf.template add<1>(h1.O, h1.w, 0);
+    vf.template add<1>(h1.O, h1.w, 1);
+  }
+  auto store = [&](WideHalf& h) {
+    h.sm.close();
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) win_store(to, h.rows, h.O[ct], ct, h.sm.m, h.sm.l, work.used == 1, work.part, sp.parts);
+  };
+  store(h0);
+  store(h1);
+}
+
+hipError_t launch_window_wide(const dsk_window_attn_args& a, const WinCache& c, const WinOut& to, int q_tiles, const WinSplit& sp, float scale_log2,
+                              hipStream_t st) {
+  const int G = a.Hq / a.Hkv;
+  const dim3 grid((unsigned)(a.Hkv * q_tiles), (unsigned)sp.parts, (unsigned)a.B), block(kWideWaves * DSK_WAVE);
+  if (a.k_scale != nullptr) window_wide_kernel<true><<<grid, block, 0, st>>>(a, c, to, G, q_tiles, sp, scale_log2);
+  else window_wide_kernel<false><<<grid, block, 0, st>>>(a, c, to, G, q_tiles, sp, scale_log2);
+  return hipGetLastError();
+}
+
+}  // namespace dsk
