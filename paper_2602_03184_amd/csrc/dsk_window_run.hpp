@@ -70,7 +70,24 @@ struct WinRun {
     const int t = tiles.t0(v) + r;
     return t < there ? t : there - 1;
   }
-  // every row sees all of the tile
+  // Every row sees all of the tile: plain(v) as an interval of tiles and those of first tokens before it.
+  struct Plain {
+    int few, from, to;
+    __device__ __forceinline__ bool operator()(int v) const { return v < few || (v >= from && v < to); }
+  };
+  __device__ __forceinline__ Plain plain_tiles() const {
+    const int end = tiles.p0 + 1 < there ? tiles.p0 + 1 : there;       // of what the first row sees
+    const int gone = tiles.p1 - window + 1 - tiles.lo;                 // positions of the run that the last row does not see
+    Plain p;
+    p.few = 0;
+    if (tiles.first > 0 || tiles.lo == 0) {
+      const int most = tiles.first > 0 ? tiles.first : tiles.n, upto = sinks < end ? sinks : end;
+      p.few = upto / kAttnTile < most ? upto / kAttnTile : most;
+    }
+    p.from = tiles.first + (gone > 0 ? (int)(((int64_t)gone + kAttnTile - 1) / kAttnTile) : 0);
+    p.to = end > tiles.lo ? tiles.first + (end - tiles.lo) / kAttnTile : tiles.first;
+    return p;
+  }
   __device__ __forceinline__ bool plain(int v) const {
     const int t = tiles.t0(v);
     return t + kAttnTile <= (tiles.p0 + 1 < there ? tiles.p0 + 1 : there) && (t > tiles.p1 - window || t + kAttnTile <= sinks);

@@ -30,12 +30,13 @@ struct WideLoader {
   using Stage = WideStage<E4M3>;
   const WinCache& c;
   const WinRun& keys;
+  const WinRun::Plain plain;
   int hk, row, chunk;
   uint32_t k_off, v_off;
   int v;                // the next tile
   int64_t at;           // its first row, and its addresses
   tile_global k, w;
-  __device__ __forceinline__ WideLoader(const WinCache& cache, const WinRun& run, int head) : c(cache), keys(run), hk(head) {
+  __device__ __forceinline__ WideLoader(const WinCache& cache, const WinRun& run, int head) : c(cache), keys(run), plain(run.plain_tiles()), hk(head) {
     row = threadIdx.x / Stage::kChunks;
     chunk = threadIdx.x % Stage::kChunks;
     k_off = (uint32_t)(row * (int)c.k_tok + chunk * 16);
@@ -85,7 +86,7 @@ struct WideLoader {
   // Tile v into its buffer.  A masked row may hold anything, and 0 * NaN is NaN: where not every row sees all of the tile, values that are
   // not finite are left out and the tile is noted.
   __device__ __forceinline__ void put(Stage& x, int tile, unsigned char* sm_k, int* sm_left_out) const {
-    if (tile < keys.end && !keys.plain(tile)) {
+    if (!plain(tile)) {                                    // (nor of what lies behind the last one)
       uint32_t found = 0;
 #pragma unroll
       for (int u = 0; u < Stage::kLoads; ++u) {
@@ -167,10 +168,11 @@ struct WideHalf {
   }
 };
 
-// A phase: the weights of half s, and meanwhile products of half p, of K for its next logits and of V with its weights.  next: where the
-// fragments of K that come after these are, or nullptr.
+// A phase: the weights of half s, and meanwhile products of half p, of K for its next logits and of V with its weights.  READ: then the
+// fragments that come after these are read, as each is through.
 template <bool READ>
-__device__ __forceinline__ void wide_phase(WideHalf& s, WideHalf& p, TileKFrag& kf, const WinVFrag<false>& vf, const unsigned char* next) {
+__device__ __forceinline__ void wide_phase(WideHalf& s, WideHalf& p, TileKFrag& kf, WinVFrag<false>& vf, const unsigned char* next,
+                                           const unsigned char* values) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(s.x[i]));   // what is made of them is made here
   kf.template add<0, 8>(p.z, p.rows);
@@ -185,7 +187,11 @@ __device__ __forceinline__ void wide_phase(WideHalf& s, WideHalf& p, TileKFrag& 
   s.sm.err = (sum - s.sm.l) - add;
   s.sm.l = sum;
   s.w.set(e);
-  if constexpr (READ) kf.template read<0, 8>(next, p.rows);
+  if constexpr (READ) {
+    kf.template read<0, 8>(next, p.rows);
+    vf.template read<0>(values);
+    vf.template read<1>(values);
+  }
   p.exponents();
   __builtin_amdgcn_iglp_opt(3);                          // a matrix instruction, an exponential, and what else there is
   asm volatile("" : "+v"(s.sm.l), "+v"(s.sm.err), "+v"(p.mx));
@@ -234,7 +240,7 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 1) void window_wide_kernel(d
     kf.template read<0, 8>(buffer(0), h0.rows);
     kf.template add<0, 8>(h0.z, h0.rows);
     h0.exponents();
-    h0.look(keys, begin, keys.plain(begin));
+    h0.look(keys, begin, loader.plain(begin));
     // Tile i in buffer B = i % 3: K of tile i in kf, exponents of half 0 in h0.x, weights of half 1 for tile i - 1 in h1.w, its V in vf; set
     // (i + 2) % 3 of x has tile i + 2.
     auto step = [&](auto buf, int i) {
@@ -242,12 +248,10 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 1) void window_wide_kernel(d
       const int v = begin + i;
       loader.put(x[kAfter], v + 2, buffer(kAfter), sm_left_out + kAfter);
       loader.fetch(x[kAfter]);
-      const bool plain = keys.plain(v), plain_next = keys.plain(v + 1);
-      wide_phase<true>(h0, h1, kf, vf, buffer(kNext));   // phase A
-      vf.template read<0>(buffer(B) + kTileBytes);
-      vf.template read<1>(buffer(B) + kTileBytes);
+      const bool plain = loader.plain(v), plain_next = loader.plain(v + 1);
+      wide_phase<true>(h0, h1, kf, vf, buffer(kNext), buffer(B) + kTileBytes);   // phase A
       h1.look(keys, v, plain);
-      wide_phase<false>(h1, h0, kf, vf, nullptr);        // phase B
+      wide_phase<false>(h1, h0, kf, vf, nullptr, nullptr);   // phase B
       if (!plain && sm_left_out[B] == v) {
         win_add_left_out<E4M3>(h0.O, c, keys, hk, v, h0.allowed(keys, v), h0.rows.half);
         win_add_left_out<E4M3>(h1.O, c, keys, hk, v, h1.allowed(keys, v), h1.rows.half);
