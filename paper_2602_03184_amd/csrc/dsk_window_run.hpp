@@ -5,7 +5,7 @@
 
 namespace dsk {
 
-constexpr int kWideWaves = 4, kWideRows = kWideWaves * 2 * kAttnTile;   // of a workgroup of the kernel for many rows
+constexpr int kWideWaves = 8, kWideRows = kWideWaves * kAttnTile;   // of a workgroup of the kernel for many rows
 
 // What a sequence has in fact, malformed tables cut to the bounds that the host knows.
 struct WinPlace {

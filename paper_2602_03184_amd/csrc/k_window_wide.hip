@@ -16,15 +16,26 @@ constexpr int kWideHalfRows = kAttnTile;
 // What a thread has of a tile on its way: 16-byte chunks of rows.
 template <bool E4M3>
 struct WideStage {
-  static constexpr int kChunks = (E4M3 ? 1 : 2) * DSK_HEAD_DIM / 16;      // of a row
+  static constexpr int kChunks = DSK_HEAD_DIM / 8;                        // of a row
   static constexpr int kRows = kWideWaves * DSK_WAVE / kChunks;          // at once
-  static constexpr int kLoads = kAttnTile / kRows;
-  uint4 k[kLoads], v[kLoads];
+  static constexpr int kLoads = kAttnTile / kRows, kBytes = E4M3 ? 8 : 16;
+  typename std::conditional<E4M3, uint2, uint4>::type k[kLoads], v[kLoads];
   uint32_t ks, vs;      // scales of the thread's row
 };
 
 // Tiles on their way, one after the other from the run's first on.  The addresses go along with the tiles, as a lone wavefront of a SIMD
 // has no time for others' arithmetic.
+template <int BYTES>
+__device__ __forceinline__ auto wide_load(tile_global base, uint32_t off) {
+  if constexpr (BYTES == 16) {
+    return load16_at<false>(base, off);
+  } else {
+    asm("" : "+s"(base));
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 x = *(const __attribute__((address_space(1))) u32x2*)(base + off);
+    return make_uint2(x.x, x.y);
+  }
+}
 template <bool E4M3>
 struct WideLoader {
   using Stage = WideStage<E4M3>;
@@ -39,8 +50,8 @@ struct WideLoader {
   __device__ __forceinline__ WideLoader(const WinCache& cache, const WinRun& run, int head) : c(cache), keys(run), plain(run.plain_tiles()), hk(head) {
     row = threadIdx.x / Stage::kChunks;
     chunk = threadIdx.x % Stage::kChunks;
-    k_off = (uint32_t)(row * (int)c.k_tok + chunk * 16);
-    v_off = (uint32_t)(row * (int)c.v_tok + chunk * 16);
+    k_off = (uint32_t)(row * (int)c.k_tok + chunk * Stage::kBytes);
+    v_off = (uint32_t)(row * (int)c.v_tok + chunk * Stage::kBytes);
     go(keys.begin);
   }
   __device__ __forceinline__ void go(int tile) {
@@ -55,16 +66,16 @@ struct WideLoader {
     if (!cut) {
 #pragma unroll
       for (int u = 0; u < Stage::kLoads; ++u) {
-        x.k[u] = load16_at<false>(k + u * Stage::kRows * c.k_tok, k_off);
-        x.v[u] = load16_at<false>(w + u * Stage::kRows * c.v_tok, v_off);
+        x.k[u] = wide_load<Stage::kBytes>(k + u * Stage::kRows * c.k_tok, k_off);
+        x.v[u] = wide_load<Stage::kBytes>(w + u * Stage::kRows * c.v_tok, v_off);
       }
     } else {
       const int last = keys.last(v);
 #pragma unroll
       for (int u = 0; u < Stage::kLoads; ++u) {
         const int r = row + u * Stage::kRows, n = r < last ? r : last;
-        x.k[u] = load16_at<false>(k, (uint32_t)(n * (int)c.k_tok + chunk * 16));
-        x.v[u] = load16_at<false>(w, (uint32_t)(n * (int)c.v_tok + chunk * 16));
+        x.k[u] = wide_load<Stage::kBytes>(k, (uint32_t)(n * (int)c.k_tok + chunk * Stage::kBytes));
+        x.v[u] = wide_load<Stage::kBytes>(w, (uint32_t)(n * (int)c.v_tok + chunk * Stage::kBytes));
       }
     }
     if constexpr (E4M3) {
@@ -92,7 +103,7 @@ struct WideLoader {
       for (int u = 0; u < Stage::kLoads; ++u) {
         uint32_t* const y = &x.v[u].x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < Stage::kBytes / 4; ++i) {
           const uint32_t was = y[i];
           if constexpr (E4M3) {
             const uint32_t nan = ((was & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
@@ -117,9 +128,7 @@ struct WideLoader {
         write(r, chunk, x.k[u], x.v[u]);
       } else {
         const float s = __uint_as_float(x.ks << 23), t = __uint_as_float(x.vs << 23);
-        write(r, 2 * chunk, __builtin_bit_cast(uint4, win_widen8(x.k[u].x, x.k[u].y, s)), __builtin_bit_cast(uint4, win_widen8(x.v[u].x, x.v[u].y, t)));
-        write(r, 2 * chunk + 1, __builtin_bit_cast(uint4, win_widen8(x.k[u].z, x.k[u].w, s)),
-              __builtin_bit_cast(uint4, win_widen8(x.v[u].z, x.v[u].w, t)));
+        write(r, chunk, __builtin_bit_cast(uint4, win_widen8(x.k[u].x, x.k[u].y, s)), __builtin_bit_cast(uint4, win_widen8(x.v[u].x, x.v[u].y, t)));
       }
     }
   }
@@ -148,12 +157,15 @@ struct WideHalf {
   }
   __device__ __forceinline__ uint32_t allowed(const WinRun& keys, int v) const { return rows.real ? keys.allowed(v, rows.pos) : 0u; }
   // what comes between the logits of tile v and their weights
-  __device__ __forceinline__ void look(const WinRun& keys, int v, bool plain) {
+  __device__ __forceinline__ void look(const WinRun& keys, int v, bool plain, const WinVFrag<false>& vf) {
     if (!plain) {
       tile_hide(z, allowed(keys, v) >> (4 * rows.half), 0);
       exponents();
     }
     if (__any(mx > 8.0f || sm.m == -__builtin_inff())) {
+      vf.template add<1>(O, w, 0);                       // weights that wait for their product still go by the old reference
+      vf.template add<1>(O, w, 1);
+      w.w[0][0] = w.w[0][1] = __builtin_bit_cast(tile_bf16x8, make_uint4(0, 0, 0, 0));
       const float top = tile_max(z) * sm.scale_log2;
       const bool move = mx > 8.0f || sm.m == -__builtin_inff();
       const float m_new = move ? fmaxf(sm.m, top) : sm.m;
@@ -168,39 +180,35 @@ struct WideHalf {
   }
 };
 
-// A phase: the weights of half s, and meanwhile products of half p, of K for its next logits and of V with its weights.  READ: then the
+// The weights of a tile, and meanwhile products: of K for the logits of the next one, of V with the weights of the one before.  Then the
 // fragments that come after these are read, as each is through.
-template <bool READ>
-__device__ __forceinline__ void wide_phase(WideHalf& s, WideHalf& p, TileKFrag& kf, WinVFrag<false>& vf, const unsigned char* next,
-                                           const unsigned char* values) {
+__device__ __forceinline__ void wide_phase(WideHalf& h, TileKFrag& kf, WinVFrag<false>& vf, const unsigned char* next, const unsigned char* values) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(s.x[i]));   // what is made of them is made here
-  kf.template add<0, 8>(p.z, p.rows);
-  vf.template add<1>(p.O, p.w, 0);
-  vf.template add<1>(p.O, p.w, 1);
-  float e[16];
+  for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(h.x[i]));   // what is made of them is made here
+  kf.template add<0, 8>(h.z, h.rows);
+  vf.template add<1>(h.O, h.w, 0);
+  vf.template add<1>(h.O, h.w, 1);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) e[i] = exp2_small(s.x[i]);
+  for (int i = 0; i < 16; ++i) h.x[i] = exp2_small(h.x[i]);
+  const float (&e)[16] = h.x;
   const float tile = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])) +
                      (((e[8] + e[9]) + (e[10] + e[11])) + ((e[12] + e[13]) + (e[14] + e[15])));
-  const float add = tile - s.sm.err, sum = s.sm.l + add;
-  s.sm.err = (sum - s.sm.l) - add;
-  s.sm.l = sum;
-  s.w.set(e);
-  if constexpr (READ) {
-    kf.template read<0, 8>(next, p.rows);
-    vf.template read<0>(values);
-    vf.template read<1>(values);
-  }
-  p.exponents();
+  const float add = tile - h.sm.err, sum = h.sm.l + add;
+  h.sm.err = (sum - h.sm.l) - add;
+  h.sm.l = sum;
+  h.w.set(h.x);
+  kf.template read<0, 8>(next, h.rows);
+  vf.template read<0>(values);
+  vf.template read<1>(values);
+  h.exponents();
   __builtin_amdgcn_iglp_opt(3);                          // a matrix instruction, an exponential, and what else there is
-  asm volatile("" : "+v"(s.sm.l), "+v"(s.sm.err), "+v"(p.mx));
+  asm volatile("" : "+v"(h.sm.l), "+v"(h.sm.err), "+v"(h.mx));
 }
 
 template <bool E4M3>
-__global__ __launch_bounds__(kWideWaves * DSK_WAVE, 1) void window_wide_kernel(dsk_window_attn_args a, WinCache c, WinOut to, int G, int q_tiles,
+__global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void window_wide_kernel(dsk_window_attn_args a, WinCache c, WinOut to, int G, int q_tiles,
                                                                               WinSplit sp, float scale_log2) {
-  constexpr int kRing = 3, kBuf = 2 * kTileBytes;
+  constexpr int kRing = 4, kBuf = 2 * kTileBytes;
   __shared__ __align__(16) unsigned char sm_kv[kRing * kBuf];
   __shared__ int sm_left_out[kRing];                     // the tile of which values were left out, -1 none
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / DSK_WAVE);
@@ -210,73 +218,67 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 1) void window_wide_kernel(d
   WinRun keys;
   int tok0 = 0, len = 0;
   if (!work.find(a, sp, G, hk, q_tile, kWideRows, keys, tok0, len)) return;     // uniform
-  WideHalf h0(scale_log2), h1(scale_log2);
-  work.rows<false>(h0.rows, a, G, wave * 2 * kWideHalfRows, tok0, len);
-  work.rows<false>(h1.rows, a, G, (wave * 2 + 1) * kWideHalfRows, tok0, len);
+  WideHalf h(scale_log2);
+  work.rows<false>(h.rows, a, G, wave * kWideHalfRows, tok0, len);
 
   const int begin = keys.begin, count = keys.end - keys.begin;
   if (threadIdx.x < kRing) sm_left_out[threadIdx.x] = -1;
   __syncthreads();
-  WideStage<E4M3> x[kRing];
+  WideStage<E4M3> x[2];
   TileKFrag kf;
   WinVFrag<false> vf;
   auto buffer = [&](int b) { return sm_kv + b * kBuf; };
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    h1.w.w[0][t] = __builtin_bit_cast(tile_bf16x8, make_uint4(0, 0, 0, 0));
+    h.w.w[0][t] = __builtin_bit_cast(tile_bf16x8, make_uint4(0, 0, 0, 0));
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct) vf.v[ct][t] = h1.w.w[0][t];
+    for (int ct = 0; ct < 4; ++ct) vf.v[ct][t] = h.w.w[0][t];
   }
   if (count > 0) {
     WideLoader<E4M3> loader(c, keys, hk);
     loader.fetch(x[0]);
     loader.fetch(x[1]);
-    loader.fetch(x[2]);
     loader.put(x[0], begin, buffer(0), sm_left_out);
     loader.fetch(x[0]);
     loader.put(x[1], begin + 1, buffer(1), sm_left_out + 1);
     loader.fetch(x[1]);
+    loader.put(x[0], begin + 2, buffer(2), sm_left_out + 2);
+    loader.fetch(x[0]);
     __syncthreads();
-    kf.template read<0, 8>(buffer(0), h0.rows);
-    kf.template add<0, 8>(h0.z, h0.rows);
-    h0.exponents();
-    h0.look(keys, begin, loader.plain(begin));
-    // Tile i in buffer B = i % 3: K of tile i in kf, exponents of half 0 in h0.x, weights of half 1 for tile i - 1 in h1.w, its V in vf; set
-    // (i + 2) % 3 of x has tile i + 2.
+    kf.template read<0, 8>(buffer(0), h.rows);
+    kf.template add<0, 8>(h.z, h.rows);
+    kf.template read<0, 8>(buffer(1), h.rows);
+    h.exponents();
+    h.look(keys, begin, loader.plain(begin), vf);
+    // Tile i in buffer B = i % 4: its exponents in h.x, K of tile i + 1 in kf, V of tile i - 1 in vf and its weights in h.w; set (i + 1) % 2 of
+    // x has tile i + 3.
     auto step = [&](auto buf, int i) {
-      constexpr int B = decltype(buf)::value, kNext = (B + 1) % kRing, kAfter = (B + 2) % kRing;
+      constexpr int B = decltype(buf)::value, kPut = (B + 3) % kRing, kSet = (B + 1) % 2;
       const int v = begin + i;
-      loader.put(x[kAfter], v + 2, buffer(kAfter), sm_left_out + kAfter);
-      loader.fetch(x[kAfter]);
-      const bool plain = loader.plain(v), plain_next = loader.plain(v + 1);
-      wide_phase<true>(h0, h1, kf, vf, buffer(kNext), buffer(B) + kTileBytes);   // phase A
-      h1.look(keys, v, plain);
-      wide_phase<false>(h1, h0, kf, vf, nullptr, nullptr);   // phase B
-      if (!plain && sm_left_out[B] == v) {
-        win_add_left_out<E4M3>(h0.O, c, keys, hk, v, h0.allowed(keys, v), h0.rows.half);
-        win_add_left_out<E4M3>(h1.O, c, keys, hk, v, h1.allowed(keys, v), h1.rows.half);
-      }
-      if (i + 1 < count) h0.look(keys, v + 1, plain_next);   // (behind the last tile the logits are another one's and nobody's)
+      loader.put(x[kSet], v + 3, buffer(kPut), sm_left_out + kPut);
+      loader.fetch(x[kSet]);
+      wide_phase(h, kf, vf, buffer((B + 2) % kRing), buffer(B) + kTileBytes);
+      if (i + 1 < count) h.look(keys, v + 1, loader.plain(v + 1), vf);   // (behind the last tile the logits are another one's and nobody's)
+      if (!loader.plain(v) && sm_left_out[B] == v)
+        win_add_left_out<E4M3>(h.O, c, keys, hk, v, h.allowed(keys, v), h.rows.half);
       __syncthreads();
     };
     using B0 = std::integral_constant<int, 0>;
     using B1 = std::integral_constant<int, 1>;
     using B2 = std::integral_constant<int, 2>;
+    using B3 = std::integral_constant<int, 3>;
     for (int i = 0; i < count; i += kRing) {
       step(B0(), i);
       if (i + 1 < count) step(B1(), i + 1);
       if (i + 2 < count) step(B2(), i + 2);
+      if (i + 3 < count) step(B3(), i + 3);
     }
-    vf.template add<1>(h1.O, h1.w, 0);
-    vf.template add<1>(h1.O, h1.w, 1);
+    vf.template add<1>(h.O, h.w, 0);
+    vf.template add<1>(h.O, h.w, 1);
   }
-  auto store = [&](WideHalf& h) {
-    h.sm.close();
+  h.sm.close();
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct) win_store(to, h.rows, h.O[ct], ct, h.sm.m, h.sm.l, work.used == 1, work.part, sp.parts);
-  };
-  store(h0);
-  store(h1);
+  for (int ct = 0; ct < 4; ++ct) win_store(to, h.rows, h.O[ct], ct, h.sm.m, h.sm.l, work.used == 1, work.part, sp.parts);
 }
 
 hipError_t launch_window_wide(const dsk_window_attn_args& a, const WinCache& c, const WinOut& to, int q_tiles, const WinSplit& sp, float scale_log2,
