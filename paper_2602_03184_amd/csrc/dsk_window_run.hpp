@@ -101,8 +101,30 @@ struct WinRun {
 };
 
 struct WinSplit {
-  int parts, tiles_per_part;
+  int parts, tiles_per_part;   // of a sequence at most; of a part
+  bool packed;                 // workgroups are numbered through the parts that there are, not by sequence
 };
+
+// The p-th part of all sequences', those of a sequence one after the other; false: there are fewer.  Every wavefront for itself.
+__device__ __forceinline__ bool win_find_part(const dsk_window_attn_args& a, const WinSplit& sp, int G, int p, int& s, int& part) {
+  const int lane = threadIdx.x & (DSK_WAVE - 1);
+  for (int s0 = 0; s0 < a.B; s0 += DSK_WAVE) {
+    int parts = 0;
+    if (s0 + lane < a.B) {
+      const WinPlace at(a, s0 + lane);
+      if (at.n > 0) parts = WinTiles(a, at, G, 0, at.n * G).used(sp.tiles_per_part);
+    }
+    const int incl = wave_incl_scan_i(parts, lane), total = __builtin_amdgcn_readlane(incl, DSK_WAVE - 1);
+    if (p < total) {
+      const int before = __builtin_popcountll(__ballot(incl <= p));    // sequences
+      s = __builtin_amdgcn_readfirstlane(s0 + before);
+      part = before > 0 ? p - __builtin_amdgcn_readlane(incl, before - 1) : p;
+      return true;
+    }
+    p -= total;
+  }
+  return false;
+}
 
 // What a workgroup takes: rows from r0 on of KV head hk, and a part of the tiles that they see; false: nothing.
 struct WinWork {
@@ -111,6 +133,7 @@ struct WinWork {
   __device__ __forceinline__ bool find(const dsk_window_attn_args& a, const WinSplit& sp, int G, int head, int q_tile, int q_rows, WinRun& keys, int& tok0, int& len) {
     part = blockIdx.y;
     s = blockIdx.z;
+    if (sp.packed && !win_find_part(a, sp, G, blockIdx.y, s, part)) return false;
     hk = head;
     const WinPlace at(a, s);
     r0 = (int64_t)q_tile * q_rows;
@@ -141,7 +164,7 @@ struct WinWork {
   }
 };
 
-hipError_t launch_window_wide(const dsk_window_attn_args& a, const WinCache& c, const WinOut& to, int q_tiles, const WinSplit& sp, float scale_log2,
-                              hipStream_t st);
+hipError_t launch_window_wide(const dsk_window_attn_args& a, const WinCache& c, const WinOut& to, dim3 grid, int q_tiles, const WinSplit& sp,
+                              float scale_log2, hipStream_t st);
 
 }  // namespace dsk

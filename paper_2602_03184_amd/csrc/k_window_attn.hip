@@ -190,9 +190,13 @@ __global__ __launch_bounds__(kWinMergeWaves * DSK_WAVE) void window_merge_kernel
 }
 
 // ---- geometry: follows the host's bounds alone ---------------------------------------------------------------
+// K and V larger than the memory-side cache are hardly found there again by the next step, so they are read past it.
+constexpr int64_t kWinStreamBytes = 288ll << 20;
+
 struct WinLaunch {
   int q_waves, q_rows, q_tiles;   // wavefronts' rows of a workgroup, its rows, workgroups for all of them
   bool wide;                      // window_wide_kernel
+  bool stream;                    // K and V are read past the memory-side cache
   WinSplit sp;
 };
 
@@ -217,15 +221,23 @@ static WinLaunch win_layout(const dsk_window_attn_args& a, bool f32) {
   const int64_t longest = (int64_t)a.max_seqlen + a.max_new;
   const int64_t near = ceil_div((int64_t)a.window + tokens, kAttnTile) + 1 + ceil_div(a.n_sink, kAttnTile);
   const int64_t tiles = near < ceil_div(longest, kAttnTile) ? near : ceil_div(longest, kAttnTile);
+  // Tiles of all sequences.  Where the cache has no room for all of them at their longest they differ in length, and the parts are cut to
+  // fill the chip with those that there are: eight sequences of 16K to 64K tokens in 8 bits, four new tokens 174 -> 142 us.
+  const int64_t rows_tiles = (int64_t)a.total_rows / kAttnTile + 2 * (int64_t)a.B, all = a.B * tiles < rows_tiles ? a.B * tiles : rows_tiles;
+  const bool ragged = all < a.B * tiles;
   const int most = win_most_parts(a, t.q_tiles, tiles);
   // two workgroups a CU; one of those for many rows, and of those that stream bf16 tiles, whose rings are twice as large
-  const int64_t want = t.wide || (t.q_waves == 1 && a.k_scale == nullptr) ? kWinCus : 2 * kWinCus;
-  int64_t parts = want / ((int64_t)a.Hkv * t.q_tiles * a.B);
-  parts = parts > 1 ? (parts < most ? parts : most) : 1;
-  t.sp.tiles_per_part = (int)ceil_div(tiles, parts);
-  t.sp.tiles_per_part = t.sp.tiles_per_part > 1 ? t.sp.tiles_per_part : 1;
+  const int64_t want = (t.wide || (t.q_waves == 1 && a.k_scale == nullptr) ? kWinCus : 2 * kWinCus) / ((int64_t)a.Hkv * t.q_tiles);
+  int64_t parts = ragged ? want - (a.B - 1) : want / a.B;  // of all sequences together, the last of each a shorter one; of each
+  parts = parts > 1 ? parts : 1;
+  int64_t per = ceil_div(ragged ? all : tiles, parts);
+  const int64_t least = ceil_div(tiles, most);
+  per = per > least ? per : least;
+  t.sp.tiles_per_part = (int)(per > 1 ? per : 1);
   t.sp.parts = (int)ceil_div(tiles, t.sp.tiles_per_part);
   t.sp.parts = t.sp.parts > 1 ? t.sp.parts : 1;
+  t.sp.packed = ragged && t.q_tiles == 1 && t.sp.parts > 1 && (int64_t)a.B * t.sp.parts <= 65535;
+  t.stream = !t.wide && t.q_tiles == 1 && all * a.Hkv * kAttnTile * DSK_HEAD_DIM * (a.k_scale != nullptr ? 2 : 4) >= kWinStreamBytes;
   return t;
 }
 
@@ -239,10 +251,14 @@ size_t window_ws_bytes(const dsk_window_attn_args& a) {
   return win_part_bytes(most > 1 ? (size_t)a.n_tokens * a.Hq * most : 0);
 }
 
+static dim3 win_grid(const dsk_window_attn_args& a, const WinLaunch& t, int x) {
+  return t.sp.packed ? dim3((unsigned)x, (unsigned)(a.B * t.sp.parts)) : dim3((unsigned)x, (unsigned)t.sp.parts, (unsigned)a.B);
+}
+
 template <int QW, int KW, int NT8, int NT16, int BUFS>
 static void launch_window(const dsk_window_attn_args& a, const WinLaunch& t, const WinCache& c, const WinOut& to, float scale_log2, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
-  const dim3 grid((unsigned)(a.Hkv * t.q_tiles), (unsigned)t.sp.parts, (unsigned)a.B), block(QW * KW * DSK_WAVE);
+  const dim3 grid = win_grid(a, t, a.Hkv * t.q_tiles), block(QW * KW * DSK_WAVE);
   auto go = [&](auto terms) {
     constexpr int kTerms = decltype(terms)::value;
     if (a.k_scale != nullptr)
@@ -257,15 +273,19 @@ static void launch_window(const dsk_window_attn_args& a, const WinLaunch& t, con
 
 static void launch_stream(const dsk_window_attn_args& a, const WinLaunch& t, const WinCache& c, const WinOut& to, float scale_log2, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
-  const dim3 grid((unsigned)a.Hkv, (unsigned)t.sp.parts, (unsigned)a.B), block(kStreamWaves * DSK_WAVE);
+  const dim3 grid = win_grid(a, t, a.Hkv), block(kStreamWaves * DSK_WAVE);
   auto go = [&](auto terms, auto stream) {
     constexpr int kTerms = decltype(terms)::value;
     constexpr bool kStream = decltype(stream)::value;
     if (a.k_scale != nullptr) window_stream_kernel<kTerms, true, kStream><<<grid, block, 0, st>>>(a, c, to, G, t.sp, scale_log2);
     else window_stream_kernel<kTerms, false, kStream><<<grid, block, 0, st>>>(a, c, to, G, t.sp, scale_log2);
   };
-  if (a.out != nullptr) go(std::integral_constant<int, 3>(), std::false_type());
-  else go(std::integral_constant<int, 2>(), std::false_type());
+  auto terms = [&](auto stream) {
+    if (a.out != nullptr) go(std::integral_constant<int, 3>(), stream);
+    else go(std::integral_constant<int, 2>(), stream);
+  };
+  if (t.stream) terms(std::true_type());
+  else terms(std::false_type());
 }
 
 hipError_t launch_window_attn(const dsk_window_attn_args& a, hipStream_t st) {
@@ -275,7 +295,7 @@ hipError_t launch_window_attn(const dsk_window_attn_args& a, hipStream_t st) {
   const WinOut to = win_out(a, t.sp.parts > 1 ? (size_t)a.n_tokens * a.Hq * t.sp.parts : 0);
   const float scale_log2 = (a.scale != 0.0f ? a.scale : kWinScale) * kLog2e;
   if (t.wide) {
-    const hipError_t err = launch_window_wide(a, c, to, t.q_tiles, t.sp, scale_log2, st);
+    const hipError_t err = launch_window_wide(a, c, to, win_grid(a, t, a.Hkv * t.q_tiles), t.q_tiles, t.sp, scale_log2, st);
     if (err != hipSuccess) return err;
   } else if (t.q_waves == 1) launch_stream(a, t, c, to, scale_log2, st);
   else if (t.q_waves == 2) launch_window<2, 2, 2, 1, 2>(a, t, c, to, scale_log2, st);

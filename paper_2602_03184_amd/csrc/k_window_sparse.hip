@@ -132,17 +132,22 @@ static WinSparse win_sparse_layout(const dsk_window_sparse_args& a) {
   const bool shared = a.flags & DSK_ATTN_SHARED_SELECTION;
   sp.G = a.Hq / a.Hkv;
   sp.heads = shared ? a.Hkv : a.Hq;
-  const int64_t least = win_least_slots(a.b), most = win_most_slots(a.b);
-  int64_t per = ceil_div((int64_t)a.k * a.B * sp.heads, 2 * kWinCus);
-  per = per > least ? per : least;
-  per = per < most ? per : most;
-  sp.slots_per_part = (int)per;
-  sp.slot_parts = (int)ceil_div(a.k, per);
   const int64_t near = (int64_t)a.window + a.n_sink < a.max_seqlen ? (int64_t)a.window + a.n_sink : a.max_seqlen;
-  int64_t near_per = ceil_div(near * a.B * a.Hkv, 2 * kWinCus);
-  near_per = near_per > kWinLeastKeys ? near_per : kWinLeastKeys;
-  sp.near_per_part = (int)(near_per < kWinMaxListed ? near_per : kWinMaxListed);
-  sp.near_parts = (int)ceil_div(near, sp.near_per_part);
+  // Tokens of a part: as few as leave all parts in one round of workgroups, two a CU in 8 bits and one in bf16, whose rings are twice as
+  // large.
+  const int64_t want = a.k_scale != nullptr ? 2 * kWinCus : kWinCus, lists = (int64_t)a.B * sp.heads, groups = (int64_t)a.B * a.Hkv;
+  int64_t tokens = (lists * a.k * a.b + groups * near) / want / kAttnTile * kAttnTile;
+  tokens = tokens > kWinLeastKeys ? tokens : kWinLeastKeys;
+  for (;; tokens += kAttnTile) {
+    tokens = tokens < kWinMaxListed ? tokens : kWinMaxListed;
+    int64_t per = tokens / a.b > 1 ? tokens / a.b : 1;
+    per = per < win_most_slots(a.b) ? per : win_most_slots(a.b);
+    sp.slots_per_part = (int)per;
+    sp.slot_parts = (int)ceil_div(a.k, per);
+    sp.near_per_part = (int)tokens;
+    sp.near_parts = (int)ceil_div(near, tokens);
+    if (tokens == kWinMaxListed || lists * sp.slot_parts + groups * sp.near_parts <= want) break;
+  }
   sp.row_tiles = (int)ceil_div(sp.G, kAttnTile);
   return sp;
 }

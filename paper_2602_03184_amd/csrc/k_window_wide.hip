@@ -281,10 +281,10 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void window_wide_kernel(d
   for (int ct = 0; ct < 4; ++ct) win_store(to, h.rows, h.O[ct], ct, h.sm.m, h.sm.l, work.used == 1, work.part, sp.parts);
 }
 
-hipError_t launch_window_wide(const dsk_window_attn_args& a, const WinCache& c, const WinOut& to, int q_tiles, const WinSplit& sp, float scale_log2,
-                              hipStream_t st) {
+hipError_t launch_window_wide(const dsk_window_attn_args& a, const WinCache& c, const WinOut& to, dim3 grid, int q_tiles, const WinSplit& sp,
+                              float scale_log2, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
-  const dim3 grid((unsigned)(a.Hkv * q_tiles), (unsigned)sp.parts, (unsigned)a.B), block(kWideWaves * DSK_WAVE);
+  const dim3 block(kWideWaves * DSK_WAVE);
   if (a.k_scale != nullptr) window_wide_kernel<true><<<grid, block, 0, st>>>(a, c, to, G, q_tiles, sp, scale_log2);
   else window_wide_kernel<false><<<grid, block, 0, st>>>(a, c, to, G, q_tiles, sp, scale_log2);
   return hipGetLastError();

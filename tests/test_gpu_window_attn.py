@@ -342,3 +342,16 @@ def test_large_caches():
         torch.cuda.synchronize()
         assert torch.equal(r.out, want.out) and torch.equal(r.lse, want.lse)
         del X, K, V
+
+
+def test_sequences_that_share_their_rows():
+    """More tokens in all than the cache has rows, of different lengths: every part of every sequence is taken."""
+    for bits in (8, 16):
+        c = Case([30000, 29000, 5], [2, 2, 2], 8, 2, bits=bits, seed=20, spare=0)
+        c.row0 = [0, 0, 0, c.row0[3]]
+        c.lens = [30000, 21000, 29999]
+        c.check()
+        c = Case([9000] + [5] * 9, [2] * 10, 8, 2, bits=bits, seed=21, spare=0)
+        c.row0 = [0] * 10 + [c.row0[10]]
+        c.lens = [9000 - 31 * s for s in range(10)]
+        c.check()
