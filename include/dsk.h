@@ -713,7 +713,7 @@ typedef struct dsk_kv8_append_args {
   const int32_t* seq_len;      /* [dev] [B] rows in use before the new ones */
   const int32_t* cu_new;       /* [dev] [B+1] */
   const int32_t* tok_pos;      /* [dev] optional [n_tokens]; read if rot_dim > 0 */
-  const void* q;               /* [dev] optional bf16 [n_tokens, Hq, D] */
+  const void* q;               /* [dev] optional bf16 [n_tokens, Hq, D], Hq at most 4096 */
   const void* k;               /* [dev] bf16 [n_tokens, Hkv, D] */
   const void* v;               /* [dev] bf16 [n_tokens, Hkv, D] */
   int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head; /* multiples of 8 */

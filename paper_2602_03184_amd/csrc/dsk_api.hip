@@ -405,7 +405,7 @@ static dsk_status validate_kv8_append(const dsk_kv8_append_args* a) {
   if (a->struct_size != sizeof(dsk_kv8_append_args)) return DSK_ERR_VERSION;
   if (a->B < 1 || a->B > 65535 || a->Hkv < 1 || a->Hkv > 65535 || a->D != DSK_HEAD_DIM || a->n_tokens < 0 || a->total_rows < 0)
     return DSK_ERR_SHAPE;
-  if (a->q && (a->Hq < 1 || (int64_t)a->scale_block * a->Hq > 0x7FFFFFFF)) return DSK_ERR_SHAPE;
+  if (a->q && (a->Hq < 1 || a->Hq > kMaxAppendHeads)) return DSK_ERR_SHAPE;
   if (a->max_new < 1 || (a->flags & ~DSK_ROPE_INTERLEAVED)) return DSK_ERR_PARAM;
   if (a->rot_dim < 0 || a->rot_dim > DSK_HEAD_DIM || a->rot_dim % 16) return DSK_ERR_PARAM;
   if ((a->q_weight || a->k_weight) && !(a->eps > 0.0f)) return DSK_ERR_PARAM;

@@ -149,6 +149,7 @@ hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st);
 
 // ---- a cache in 8 bits, sliding window and first tokens ---------------------------------------------
 constexpr int kMaxWindowKeys = 0x7FFF0000;     // positions: a key's number and a tile's overhang in 32 bits
+constexpr int kMaxAppendHeads = 4096;          // query heads: 128 rows of a block times heads squared fits 32 bits
 hipError_t launch_kv8_append(const dsk_kv8_append_args& a, hipStream_t st);
 size_t window_ws_bytes(const dsk_window_attn_args& a);
 hipError_t launch_window_attn(const dsk_window_attn_args& a, hipStream_t st);

@@ -25,7 +25,7 @@ __device__ __forceinline__ float rope_square_sum(const float (&f)[8]) {
   return group16_sum(ss);
 }
 
-// the norm of a row of that sum of squares; weight: of the lane's channels
+// the norm of a row of that sum of squares; weight: of the lane's channels, 16-byte aligned if it is in memory
 __device__ __forceinline__ void rope_scale(float (&f)[8], float ss, const float* weight, float eps) {
   const float inv = 1.0f / sqrtf(ss * (1.0f / DSK_HEAD_DIM) + eps);
   const float4 w0 = *reinterpret_cast<const float4*>(weight);

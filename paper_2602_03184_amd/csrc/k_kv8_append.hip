@@ -8,8 +8,7 @@
 //
 // A workgroup takes a block of rows of a sequence, all heads of it or some.  So that no scale has two writers, sequences begin with a
 // block.  The angles of the block's tokens are made once, in LDS, for all heads; a wavefront takes 32 rows of a head of K or V at a time
-// (blocks of 64 and 128 rows: two and four wavefronts, which exchange their largest values), or 32 rows of queries.  Its rows stay in
-// registers between the largest value and the codes.
+// (blocks of 64 and 128 rows: two and four wavefronts, which exchange their largest values), or 32 rows of queries.
 #include "dsk_internal.hpp"
 #include "dsk_rope.hpp"
 
@@ -47,9 +46,10 @@ __device__ __forceinline__ void kv8_decode(const uint2& c, float (&f)[8]) {
   f[4] = d[0]; f[5] = d[1]; f[6] = e[0]; f[7] = e[1];
 }
 
-// WPI wavefronts an item of K or V: blocks of 32 WPI rows
-template <RopePairs PAIRS, int WPI>
-__global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_args a, int groups) {
+// WPI wavefronts an item of K or V: blocks of 32 WPI rows.  Workgroups 0 .. kv_groups - 1 of a block take K and V, those from there on the
+// queries, QUADS * 4 rows a wavefront at a time.
+template <RopePairs PAIRS, int WPI, int QUADS>
+__global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_args a, int kv_groups, uint32_t by_heads) {
   constexpr int kBlock = WPI * kKv8Rows;
   constexpr bool kRotate = PAIRS != RopePairs::kNone, kInter = PAIRS == RopePairs::kInterleaved;
   __shared__ __align__(16) float sm_cos[kRotate ? kBlock : 1][kRopeHalf];
@@ -87,6 +87,40 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_
   const int off = (int)(lo - block_row), count = (int)(hi - lo);
   const int64_t tok = tok0 + (lo - begin);               // of the block's first new row
 
+  // ---- what is taken first is on its way while the angles are made ----
+  const bool queries = (int)blockIdx.y >= kv_groups;
+  const int group = queries ? (int)blockIdx.y - kv_groups : (int)blockIdx.y, groups = queries ? (int)gridDim.y - kv_groups : kv_groups;
+  constexpr int kTogether = kKv8Waves / WPI;             // items of the workgroup at once
+  const int part = wave % WPI;                           // of an item's rows
+  uint4 x[kKv8Quads];
+  // item h is head h of K, item Hkv + h of V: neighbours in the projection's output side by side
+  auto load_kv = [&](int item) {
+    const bool real = item < 2 * a.Hkv, is_v = item >= a.Hkv;
+    const int h = is_v ? item - a.Hkv : item;
+    const uint16_t* from = is_v ? static_cast<const uint16_t*>(a.v) + h * a.v_stride_head : static_cast<const uint16_t*>(a.k) + h * a.k_stride_head;
+    const int64_t from_tok = is_v ? a.v_stride_tok : a.k_stride_tok;
+#pragma unroll
+    for (int u = 0; u < kKv8Quads; ++u) {
+      const int r = part * kKv8Rows + 4 * u + grp - off;  // of the new rows
+      x[u] = make_uint4(0, 0, 0, 0);
+      if (real && r >= 0 && r < count) x[u] = load16<true>(from + (tok + r) * from_tok + c * 8);
+    }
+  };
+  // queries: rows of the block's tokens and heads, one after the other
+  const int rows = queries ? count * a.Hq : 0;
+  constexpr int kQueryRows = 4 * QUADS;
+  auto token_of = [&](int r) { return a.Hq == 1 ? r : (int)__umulhi((uint32_t)r, by_heads); };   // r / Hq: exact as r * Hq is below 2^32
+  auto load_q = [&](int r0) {
+#pragma unroll
+    for (int u = 0; u < QUADS; ++u) {
+      const int r = r0 + 4 * u + grp, t = token_of(r), h = r - t * a.Hq;
+      x[u] = make_uint4(0, 0, 0, 0);
+      if (r < rows) x[u] = load16<true>(static_cast<const uint16_t*>(a.q) + (tok + t) * a.q_stride_tok + h * a.q_stride_head + c * 8);
+    }
+  };
+  if (queries) load_q((group * kKv8Waves + wave) * kQueryRows);
+  else load_kv(group * kTogether + wave / WPI);
+
   int partner = lane, angle0 = 0;
   bool inside = false, upper = false;
   if constexpr (kRotate) {
@@ -111,8 +145,15 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_
     __syncthreads();
   }
   // a row of the block's token t, normed and rotated
-  auto turn = [&](float (&f)[8], const float* weight, int t) {
-    if (weight != nullptr) rope_scale(f, rope_square_sum(f), weight + c * 8, a.eps);
+  const float* const weight = queries ? a.q_weight : a.k_weight;
+  float wt[8];
+  if (weight != nullptr) {
+    const float4 w0 = *reinterpret_cast<const float4*>(weight + c * 8), w1 = *reinterpret_cast<const float4*>(weight + c * 8 + 4);
+    wt[0] = w0.x; wt[1] = w0.y; wt[2] = w0.z; wt[3] = w0.w;
+    wt[4] = w1.x; wt[5] = w1.y; wt[6] = w1.z; wt[7] = w1.w;
+  }
+  auto turn = [&](float (&f)[8], int t) {
+    if (weight != nullptr) rope_scale(f, rope_square_sum(f), wt, a.eps);
     if constexpr (kRotate) {
       float cs[8], sn[8];
 #pragma unroll
@@ -130,34 +171,26 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_
     }
   };
 
-  // ---- keys and values: item 2 h is head h of K, item 2 h + 1 of V ----
-  constexpr int kTogether = kKv8Waves / WPI;             // items of the workgroup at once
-  const int part = wave % WPI;                           // of an item's rows
-  for (int i0 = blockIdx.y * kTogether; i0 < 2 * a.Hkv; i0 += groups * kTogether) {   // uniform: barriers inside
+  // ---- keys and values ----
+  for (int i0 = group * kTogether; !queries && i0 < 2 * a.Hkv; i0 += groups * kTogether) {   // uniform: barriers inside
     const int item = i0 + wave / WPI;
-    const bool real = item < 2 * a.Hkv, is_v = item & 1;
-    const int h = real ? item >> 1 : 0;
+    const bool real = item < 2 * a.Hkv, is_v = item >= a.Hkv;
+    const int h = !real ? 0 : (is_v ? item - a.Hkv : item);
     uint8_t* scale = (is_v ? a.v_scale : a.k_scale) + h * a.scale_stride_head + block;
     const int before = real && off > 0 ? *scale : 0;
-    const uint16_t* from = is_v ? static_cast<const uint16_t*>(a.v) + h * a.v_stride_head : static_cast<const uint16_t*>(a.k) + h * a.k_stride_head;
-    const int64_t from_tok = is_v ? a.v_stride_tok : a.k_stride_tok;
-    uint4 x[kKv8Quads];
+    // The rows stay in registers from their largest value to the codes: made twice they need 124 registers instead of 168, but five prompts
+    // of 40 heads then take 180 us instead of 159.
+    float f[kKv8Quads][8];
+    auto any_new = [&](int u) { return part * kKv8Rows + 4 * u - off + 3 >= 0 && part * kKv8Rows + 4 * u - off < count; };   // of the four
+    float largest = 0.0f;
 #pragma unroll
     for (int u = 0; u < kKv8Quads; ++u) {
-      const int r = part * kKv8Rows + 4 * u + grp - off;  // of the new rows
-      x[u] = make_uint4(0, 0, 0, 0);
-      if (real && r >= 0 && r < count) x[u] = load16<true>(from + (tok + r) * from_tok + c * 8);
-    }
-    float f[kKv8Quads][8], largest = 0.0f;
-#pragma unroll
-    for (int u = 0; u < kKv8Quads; ++u) {
-      const int r0 = part * kKv8Rows + 4 * u - off;
       unpack8(x[u], f[u]);
-      if (r0 + 3 < 0 || r0 >= count) continue;           // uniform: no row of the four is new
+      if (!any_new(u)) continue;                         // uniform
       if (!is_v) {
-        int r = r0 + grp;
+        int r = part * kKv8Rows + 4 * u + grp - off;
         r = r < 0 ? 0 : (r < count ? r : count - 1);     // lanes without a row turn zeros
-        turn(f[u], a.k_weight, r);
+        turn(f[u], r);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -165,6 +198,7 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_
         largest = fmaxf(largest, m < __builtin_inff() ? m : 0.0f);
       }
     }
+    load_kv(item + groups * kTogether);
     largest = wave_max(largest);
     if constexpr (WPI > 1) {
       if (lane == 0) sm_max[wave] = largest;
@@ -173,7 +207,6 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_
       for (int w = 0; w < WPI; ++w) largest = fmaxf(largest, sm_max[wave - part + w]);
       __syncthreads();
     }
-    if (!real) continue;
     int e = kv8_exponent(largest);
     const bool grows = off > 0 && e > before - kKv8Bias;
     if (off > 0 && !grows) e = before - kKv8Bias;
@@ -183,8 +216,9 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_
 #pragma unroll
     for (int u = 0; u < kKv8Quads; ++u) {
       const int r = part * kKv8Rows + 4 * u + grp;
-      if (r >= off && r < off + count) *reinterpret_cast<uint2*>(to + (block_row + r) * to_row) = kv8_encode(f[u], by);
+      if (real && r >= off && r < off + count) *reinterpret_cast<uint2*>(to + (block_row + r) * to_row) = kv8_encode(f[u], by);
     }
+    if (!real) continue;
     if (grows) {                                         // uniform for the item
       const float less = ldexpf(1.0f, before - kKv8Bias - e);
       for (int u = 0; u < kKv8Quads; ++u) {
@@ -199,54 +233,62 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_
     if (part == 0 && lane == 0 && (off == 0 || grows)) *scale = (uint8_t)(e + kKv8Bias);
   }
 
-  // ---- queries: rows of the block's tokens and heads, one after the other ----
-  if (a.q == nullptr) return;
-  const int rows = count * a.Hq;
-  for (int r0 = (blockIdx.y * kKv8Waves + wave) * kKv8Rows; r0 < rows; r0 += groups * kKv8Waves * kKv8Rows) {
-    uint4 x[kKv8Quads];
+  // ---- queries ----
+  if (!queries) return;
+  for (int r0 = (group * kKv8Waves + wave) * kQueryRows; r0 < rows; r0 += groups * kKv8Waves * kQueryRows) {
+    uint4 y[QUADS];
 #pragma unroll
-    for (int u = 0; u < kKv8Quads; ++u) {
-      const int r = r0 + 4 * u + grp, t = r / a.Hq, h = r - t * a.Hq;
-      x[u] = make_uint4(0, 0, 0, 0);
-      if (r < rows) x[u] = load16<true>(static_cast<const uint16_t*>(a.q) + (tok + t) * a.q_stride_tok + h * a.q_stride_head + c * 8);
-    }
+    for (int u = 0; u < QUADS; ++u) y[u] = x[u];
+    load_q(r0 + groups * kKv8Waves * kQueryRows);
 #pragma unroll
-    for (int u = 0; u < kKv8Quads; ++u) {
+    for (int u = 0; u < QUADS; ++u) {
       if (r0 + 4 * u >= rows) break;
       const int r = r0 + 4 * u + grp;
       float f[8];
-      unpack8(x[u], f);
-      turn(f, a.q_weight, r < rows ? r / a.Hq : 0);
-      uint4 y = x[u];
-      if (inside || a.q_weight != nullptr)
-        y = make_uint4(pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3]), pack_bf16_rne(f[4], f[5]), pack_bf16_rne(f[6], f[7]));
-      if (r < rows) store16<false>(static_cast<uint16_t*>(a.q_out) + (tok * a.Hq + r) * DSK_HEAD_DIM + c * 8, y);
+      unpack8(y[u], f);
+      turn(f, r < rows ? token_of(r) : 0);
+      if (inside || weight != nullptr)
+        y[u] = make_uint4(pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3]), pack_bf16_rne(f[4], f[5]), pack_bf16_rne(f[6], f[7]));
+      if (r < rows) store16<false>(static_cast<uint16_t*>(a.q_out) + (tok * a.Hq + r) * DSK_HEAD_DIM + c * 8, y[u]);
     }
   }
 }
 
+template <RopePairs PAIRS, int WPI>
+static void launch_block(const dsk_kv8_append_args& a, int64_t blocks, hipStream_t st) {
+  // Heads and queries are spread over as many workgroups as it takes to have 16 wavefronts a CU, angles are made in each; a wavefront then
+  // takes 8 rows of queries at a time instead of 32 (a token of 8 sequences, 32 + 8 heads: 5.9 us, nearly all of it the wait for the
+  // sequence, the rows and the angles, one after the other; with a workgroup a block 8.2).  With more blocks than that one workgroup takes
+  // a block's K and V, and its queries go to so many that each has about as many rows: 32K tokens of 32 + 8 heads 155 us with two (4.8 TB/s
+  // of 0.74 GB read and written), 161 with one, 160 with four; two for K and V 162.
+  const int64_t most = ((int64_t)2 * a.Hkv * WPI + kKv8Waves - 1) / kKv8Waves;
+  const int64_t wanted = (4096 / kKv8Waves + a.B * blocks - 1) / (a.B * blocks);
+  const int kv_groups = (int)(wanted < most ? wanted : most);
+  const bool few = wanted > 1;
+  const int64_t rows = (int64_t)(a.max_new < a.scale_block ? a.max_new : a.scale_block) * (a.q != nullptr ? a.Hq : 0);
+  const int64_t q_most = (rows + 8 * kKv8Waves - 1) / (8 * kKv8Waves);
+  const int even = (a.Hq + 2 * a.Hkv - 1) / (2 * a.Hkv);
+  const int q_groups = a.q == nullptr ? 0 : (int)(few ? (wanted < q_most ? wanted : q_most) : even);
+  const dim3 grid((unsigned)blocks, (unsigned)(kv_groups + q_groups), (unsigned)a.B), block(kKv8Threads);
+  const uint32_t by_heads = a.q == nullptr || a.Hq == 1 ? 0xFFFFFFFFu : (uint32_t)(((1ull << 32) + a.Hq - 1) / a.Hq);
+  if (few) kv8_append_kernel<PAIRS, WPI, 2><<<grid, block, 0, st>>>(a, kv_groups, by_heads);
+  else kv8_append_kernel<PAIRS, WPI, kKv8Quads><<<grid, block, 0, st>>>(a, kv_groups, by_heads);
+}
+
 template <RopePairs PAIRS>
-static void launch_pairs(const dsk_kv8_append_args& a, dim3 grid, int groups, hipStream_t st) {
-  const dim3 block(kKv8Threads);
-  if (a.scale_block == 32) kv8_append_kernel<PAIRS, 1><<<grid, block, 0, st>>>(a, groups);
-  else if (a.scale_block == 64) kv8_append_kernel<PAIRS, 2><<<grid, block, 0, st>>>(a, groups);
-  else kv8_append_kernel<PAIRS, 4><<<grid, block, 0, st>>>(a, groups);
+static void launch_pairs(const dsk_kv8_append_args& a, hipStream_t st) {
+  // blocks that max_new tokens can meet, however the first of them lies
+  const int64_t blocks = ((int64_t)a.max_new + a.scale_block - 2) / a.scale_block + 1;
+  if (a.scale_block == 32) launch_block<PAIRS, 1>(a, blocks, st);
+  else if (a.scale_block == 64) launch_block<PAIRS, 2>(a, blocks, st);
+  else launch_block<PAIRS, 4>(a, blocks, st);
 }
 
 hipError_t launch_kv8_append(const dsk_kv8_append_args& a, hipStream_t st) {
-  // blocks that max_new tokens can meet, however the first of them lies
-  const int64_t blocks = ((int64_t)a.max_new + a.scale_block - 2) / a.scale_block + 1;
-  // Heads are spread over as many workgroups as it takes to have 16 wavefronts a CU; angles are made in each.
-  const int64_t per_head = (int64_t)a.B * blocks * kKv8Waves;
-  const int items = 2 * a.Hkv * (a.scale_block / kKv8Rows);
-  const int most = (items + kKv8Waves - 1) / kKv8Waves;
-  int64_t groups = (4096 + per_head - 1) / per_head;
-  groups = groups < most ? groups : most;
-  const dim3 grid((unsigned)blocks, (unsigned)groups, (unsigned)a.B);
-  if (a.rot_dim == 0) launch_pairs<RopePairs::kNone>(a, grid, (int)groups, st);
-  else if (a.flags & DSK_ROPE_INTERLEAVED) launch_pairs<RopePairs::kInterleaved>(a, grid, (int)groups, st);
-  else if (a.rot_dim == DSK_HEAD_DIM) launch_pairs<RopePairs::kHalfAll>(a, grid, (int)groups, st);
-  else launch_pairs<RopePairs::kHalf>(a, grid, (int)groups, st);
+  if (a.rot_dim == 0) launch_pairs<RopePairs::kNone>(a, st);
+  else if (a.flags & DSK_ROPE_INTERLEAVED) launch_pairs<RopePairs::kInterleaved>(a, st);
+  else if (a.rot_dim == DSK_HEAD_DIM) launch_pairs<RopePairs::kHalfAll>(a, st);
+  else launch_pairs<RopePairs::kHalf>(a, st);
   return hipGetLastError();
 }
 

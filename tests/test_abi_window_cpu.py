@@ -55,7 +55,7 @@ def _append(dsk):
 
 def test_append_refuses(dsk):
     S, P, A, N = dsk.DSK_ERR_SHAPE, dsk.DSK_ERR_PARAM, dsk.DSK_ERR_ALIGN, dsk.DSK_ERR_NULL
-    cases = [("struct_size", 8, dsk.DSK_ERR_VERSION), ("B", 0, S), ("B", 65536, S), ("Hkv", 0, S), ("Hq", 0, S), ("D", 64, S),
+    cases = [("struct_size", 8, dsk.DSK_ERR_VERSION), ("B", 0, S), ("B", 65536, S), ("Hkv", 0, S), ("Hq", 0, S), ("Hq", 4097, S), ("D", 64, S),
              ("n_tokens", -1, S), ("total_rows", -1, S), ("max_new", 0, P), ("scale_block", 16, P), ("scale_block", 0, P),
              ("scale_block", 256, P), ("scale_stride_head", 31, S), ("rot_dim", 24, P), ("rot_dim", 144, P), ("rot_dim", -16, P),
              ("flags", 2, P), ("eps", 0.0, P), ("eps", float("nan"), P), ("kc_stride_tok", 64, S), ("kc_stride_head", 0, S),
