@@ -11,8 +11,8 @@
 namespace dsk {
 
 constexpr int kWinMaxSplit = 128;              // parts of a sequence at most
-constexpr int kWinLeastTiles = 8;              // of a part: a shorter one costs more in partial results than it saves
-constexpr int kWinLeastKeys = kWinLeastTiles * kAttnTile;
+constexpr int kWinLeastTiles = 4;              // of a part, a tile a wavefront (a head of 4096 tokens: 10.0 us; with 8 tiles 11.2)
+constexpr int kWinLeastKeys = 8 * kAttnTile;   // of a part of selected slots (4096 tokens in each of 32 lists: 12.6 us; with half 13.8)
 constexpr int kWinMaxSlots = 256;              // selected slots of a workgroup
 constexpr int kWinMaxListed = 2048;            // and their tokens
 constexpr int kWinTwoTermRows = 64;            // rows of a KV head up to which a bf16 result's weights have two terms
@@ -445,23 +445,31 @@ constexpr int kWinMergeWaves = 4;
 constexpr int kWinMergeBatch = 8;              // partials of a wavefront on their way at once
 constexpr int kWinMergeMany = 16;              // parts from which on a row has all four
 
-template <int WAVES>
-__device__ __forceinline__ void win_merge(const WinOut& to, int64_t row, int used, int parts, int wave) {
+// The first partials are on their way before it is known which of them there are.
+template <int WAVES, class USED>
+__device__ __forceinline__ void win_merge(const WinOut& to, int64_t row, int parts, int wave, const USED& used_parts) {
   const int lane = threadIdx.x & (DSK_WAVE - 1);
   const float2* ml = to.part_ml + row * parts;
   const float2* acc = reinterpret_cast<const float2*>(to.part_acc + row * parts * DSK_HEAD_DIM) + lane;
-  float M = -__builtin_inff(), l = 0.0f;
-  for (int c = lane; c < used; c += DSK_WAVE) M = fmaxf(M, ml[c].x);
-  M = wave_max(M);
-  float2 o = make_float2(0.0f, 0.0f);
-  for (int c0 = wave % WAVES * kWinMergeBatch; c0 < used; c0 += WAVES * kWinMergeBatch) {
-    float2 x[kWinMergeBatch], v[kWinMergeBatch];
+  float2 x[kWinMergeBatch], v[kWinMergeBatch];
+  auto load = [&](int c0) {
 #pragma unroll
     for (int u = 0; u < kWinMergeBatch; ++u) {
-      const int c = c0 + u < used ? c0 + u : used - 1;
+      const int c = c0 + u < parts ? c0 + u : parts - 1;
       v[u] = ml[c];
       x[u] = acc[(int64_t)c * (DSK_HEAD_DIM / 2)];
     }
+  };
+  int c0 = wave % WAVES * kWinMergeBatch;
+  load(c0);
+  const float2 mine = ml[lane < parts ? lane : parts - 1];
+  const int used = used_parts();
+  if (used <= 1) return;                                 // finished by the kernel before; uniform for a row
+  float M = lane < used ? mine.x : -__builtin_inff(), l = 0.0f;
+  for (int c = lane + DSK_WAVE; c < used; c += DSK_WAVE) M = fmaxf(M, ml[c].x);
+  M = wave_max(M);
+  float2 o = make_float2(0.0f, 0.0f);
+  for (; c0 < used; c0 += WAVES * kWinMergeBatch, load(c0)) {
 #pragma unroll
     for (int u = 0; u < kWinMergeBatch; ++u) {
       if (c0 + u >= used || v[u].y == 0.0f) continue;    // (not by the maximum: where every logit is NaN it is -inf)

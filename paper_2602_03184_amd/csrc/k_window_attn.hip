@@ -182,11 +182,10 @@ __global__ __launch_bounds__(kWinMergeWaves * DSK_WAVE) void window_merge_kernel
   const int i = (int)(item / a.Hq), h = (int)(item - (int64_t)i * a.Hq);
   const WinPlace at(a, s);
   if (i >= at.n) return;
-  const int all = at.n * G, r0 = (i * G + h % G) / q_rows * q_rows;
-  const WinTiles tiles(a, at, G, r0, r0 + q_rows < all ? r0 + q_rows : all);
-  const int used = tiles.used(sp.tiles_per_part);
-  if (used <= 1) return;                                 // finished by the kernel above
-  win_merge<WAVES>(to, (int64_t)(at.tok0 + i) * a.Hq + h, used, sp.parts, wave);
+  win_merge<WAVES>(to, (int64_t)(at.tok0 + i) * a.Hq + h, sp.parts, wave, [&] {
+    const int all = at.n * G, r0 = (i * G + h % G) / q_rows * q_rows;
+    return WinTiles(a, at, G, r0, r0 + q_rows < all ? r0 + q_rows : all).used(sp.tiles_per_part);
+  });
 }
 
 // ---- geometry: follows the host's bounds alone ---------------------------------------------------------------

@@ -120,7 +120,7 @@ template <int WAVES>
 __global__ __launch_bounds__(kWinMergeWaves * DSK_WAVE) void window_sparse_merge_kernel(int64_t rows, WinOut to, int parts) {
   const int wave = threadIdx.x / DSK_WAVE;
   const int64_t row = (int64_t)blockIdx.x * (kWinMergeWaves / WAVES) + wave / WAVES;
-  if (row < rows) win_merge<WAVES>(to, row, parts, parts, wave);
+  if (row < rows) win_merge<WAVES>(to, row, parts, wave, [&] { return parts; });
 }
 
 // ---- geometry: follows the host's bounds alone ---------------------------------------------------------------
