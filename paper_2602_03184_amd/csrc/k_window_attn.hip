@@ -14,9 +14,9 @@
 namespace dsk {
 
 // ---- a workgroup's keys folded into its rows -----------------------------------------------------------------
-// QW wavefronts have 32 rows each, KW take other tiles of a stage for the same rows, NT of them each.  With two BUFS a stage is copied
-// while the one before it is multiplied; with one that is left to the second workgroup of the CU.  TERMS: bf16 terms of a weight.
-template <int QW, int KW, int NT, int BUFS, int TERMS, bool E4M3>
+// QW wavefronts have 32 rows each, KW take other tiles of a stage for the same rows, NT of them each.  A stage is copied while the one
+// before it is multiplied.  TERMS: bf16 terms of a weight.
+template <int QW, int KW, int NT, int TERMS, bool E4M3>
 struct WinFold {
   static constexpr int kThreads = QW * KW * DSK_WAVE;
   static constexpr int kTiles = KW * NT, kKeys = kAttnTile * kTiles;   // of a stage
@@ -26,11 +26,11 @@ struct WinFold {
   static constexpr int kChunks = kRowBytes / 16, kRowsAtOnce = DSK_WAVE / kChunks;   // of a wavefront's copy
   static constexpr int kCopies = kKeys / (kRowsAtOnce * QW * KW);
   static_assert(kKeys <= kThreads && kCopies >= 1, "a thread a scale, every wavefront copies");
-  static_assert(KW == 1 || BUFS * kBuf >= (KW - 1) * QW * 64 * DSK_WAVE * 4, "states are joined in the stages' place");
+  static_assert(KW == 1 || 2 * kBuf >= (KW - 1) * QW * 64 * DSK_WAVE * 4, "states are joined in the stages' place");
   struct Shared {
-    __align__(16) unsigned char kv[BUFS * kBuf];
+    __align__(16) unsigned char kv[2 * kBuf];
     float2 ml[KW > 1 ? (KW - 1) * QW * DSK_WAVE : 1];
-    __align__(16) float scale[E4M3 ? BUFS * 2 * kKeys : 4];
+    __align__(16) float scale[E4M3 ? 4 * kKeys : 4];
   };
 
   template <class KEYS>
@@ -103,38 +103,33 @@ struct WinFold {
     };
     uchar2 b = make_uchar2(0, 0);
     int buf = 0;
-    if (BUFS > 1 && keys.begin < keys.end) {
+    if (keys.begin < keys.end) {
       copy(c, keys, hk, keys.begin, sh.kv);
       b = scales(c, keys, hk, keys.begin);
     }
     for (int v0 = keys.begin; v0 < keys.end; v0 += kTiles) {
-      if (BUFS == 1) {
-        copy(c, keys, hk, v0, sh.kv);
-        b = scales(c, keys, hk, v0);
-      }
       lds_copies_done();
       if (E4M3 && tid < kKeys) {
         sh.scale[buf * 2 * kKeys + tid] = __uint_as_float((uint32_t)b.x << 23);
         sh.scale[buf * 2 * kKeys + kKeys + tid] = __uint_as_float((uint32_t)b.y << 23);
       }
       __syncthreads();                                   // the stage is here, and nobody reads the other one any more
-      if (BUFS > 1 && v0 + kTiles < keys.end) {
+      if (v0 + kTiles < keys.end) {
         copy(c, keys, hk, v0 + kTiles, sh.kv + (buf ^ 1) * kBuf);
         b = scales(c, keys, hk, v0 + kTiles);
       }
       if (rows.busy) tiles(v0, buf);
-      if (BUFS == 1) __syncthreads();
-      else buf ^= 1;
+      buf ^= 1;
     }
-    if (BUFS > 1) __syncthreads();
+    __syncthreads();
     sm.close();
   }
 };
 
-template <int QW, int KW, int NT, int BUFS, int TERMS, bool E4M3>
+template <int QW, int KW, int NT, int TERMS, bool E4M3>
 __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void window_attn_kernel(dsk_window_attn_args a, WinCache c, WinOut to, int G, int q_tiles,
                                                                             WinSplit sp, float scale_log2) {
-  using Fold = WinFold<QW, KW, NT, BUFS, TERMS, E4M3>;
+  using Fold = WinFold<QW, KW, NT, TERMS, E4M3>;
   __shared__ typename Fold::Shared sh;
   const int wave = threadIdx.x / DSK_WAVE, qw = wave % QW, kw = wave / QW;
   WinWork work;
@@ -212,6 +207,9 @@ static WinLaunch win_layout(const dsk_window_attn_args& a, bool f32) {
   const int64_t rows = (int64_t)a.max_new * G;
   WinLaunch t;
   t.q_waves = rows <= kAttnTile ? 1 : (rows <= kWinTwoTermRows ? 2 : 4);
+  // Rows of a KV head, over 131K tokens of 8 heads in 8 bits: 128 rows take four wavefronts 108 us, the eight that fit many rows 167, as
+  // half of them have none; 256 rows 193 and 177 (in bf16 116 and 167, 179 and 167).  A result in 32 bits has weights of three terms,
+  // which those have no registers for.
   t.wide = rows > 128 && !f32;
   t.q_rows = t.wide ? kWideRows : t.q_waves * kAttnTile;
   t.q_tiles = (int)ceil_div(rows, t.q_rows);
@@ -254,16 +252,16 @@ static dim3 win_grid(const dsk_window_attn_args& a, const WinLaunch& t, int x) {
   return t.sp.packed ? dim3((unsigned)x, (unsigned)(a.B * t.sp.parts)) : dim3((unsigned)x, (unsigned)t.sp.parts, (unsigned)a.B);
 }
 
-template <int QW, int KW, int NT8, int NT16, int BUFS>
+template <int QW, int KW, int NT8, int NT16>
 static void launch_window(const dsk_window_attn_args& a, const WinLaunch& t, const WinCache& c, const WinOut& to, float scale_log2, hipStream_t st) {
   const int G = a.Hq / a.Hkv;
   const dim3 grid = win_grid(a, t, a.Hkv * t.q_tiles), block(QW * KW * DSK_WAVE);
   auto go = [&](auto terms) {
     constexpr int kTerms = decltype(terms)::value;
     if (a.k_scale != nullptr)
-      window_attn_kernel<QW, KW, NT8, BUFS, kTerms, true><<<grid, block, 0, st>>>(a, c, to, G, t.q_tiles, t.sp, scale_log2);
+      window_attn_kernel<QW, KW, NT8, kTerms, true><<<grid, block, 0, st>>>(a, c, to, G, t.q_tiles, t.sp, scale_log2);
     else
-      window_attn_kernel<QW, KW, NT16, BUFS, kTerms, false><<<grid, block, 0, st>>>(a, c, to, G, t.q_tiles, t.sp, scale_log2);
+      window_attn_kernel<QW, KW, NT16, kTerms, false><<<grid, block, 0, st>>>(a, c, to, G, t.q_tiles, t.sp, scale_log2);
   };
   static_assert(kWinTwoTermRows == 2 * kAttnTile, "two wavefronts' rows always have two terms, four wavefronts' never");
   if (a.out != nullptr) go(std::integral_constant<int, 3>());
@@ -297,8 +295,8 @@ hipError_t launch_window_attn(const dsk_window_attn_args& a, hipStream_t st) {
     const hipError_t err = launch_window_wide(a, c, to, win_grid(a, t, a.Hkv * t.q_tiles), t.q_tiles, t.sp, scale_log2, st);
     if (err != hipSuccess) return err;
   } else if (t.q_waves == 1) launch_stream(a, t, c, to, scale_log2, st);
-  else if (t.q_waves == 2) launch_window<2, 2, 2, 1, 2>(a, t, c, to, scale_log2, st);
-  else launch_window<4, 1, 4, 2, 2>(a, t, c, to, scale_log2, st);
+  else if (t.q_waves == 2) launch_window<2, 2, 2, 1>(a, t, c, to, scale_log2, st);
+  else launch_window<4, 1, 4, 2>(a, t, c, to, scale_log2, st);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || t.sp.parts <= 1) return err;
   const bool many = t.sp.parts >= kWinMergeMany;

@@ -1,17 +1,16 @@
 // dsk_window_attn for many rows (prompts): the matrix cores bound it.
 //
-// A wavefront has 64 rows, as two halves of 32 that meet the same fragments of K and V, so that LDS is read half as often a product as
-// with 32; four wavefronts, one a SIMD, make a workgroup.  Each half's products run while the other half's softmax is made: in phase A
-// of tile i the matrix cores have K of tile i and V of tile i - 1 for half 1, in phase B K of tile i + 1 and V of tile i for half 0.  A
-// phase is straight-line code, about 512 cycles of the matrix core and as many of the vector ALU, most of them exponentials; what is
-// rare (masks, a reference that moves) lies between phases.
+// Eight wavefronts of 32 rows make a workgroup, two a SIMD, and read each tile of K and V from LDS.  A wavefront's step is straight-line
+// code: products of K for the logits of the next tile and of V with the weights of the one before, and among them the exponentials of
+// this one, so that neither the matrix core nor the vector ALU waits for the other; what is rare (masks, a reference that moves) lies
+// between steps.  The other wavefront of the SIMD fills in where one waits.  Four wavefronts of 64 rows read LDS half as often, but
+// nothing fills in for a lone one: a prompt of 8191 tokens, 32 heads, 702 us instead of 670 (820 TFLOP/s).
 //
-// K and V come to LDS through registers, a ring of three tiles in bf16: codes are widened on the way, once for all wavefronts.
+// K and V come to LDS through registers, a ring of four tiles in bf16: codes are widened on the way, once for all wavefronts.  In step i
+// tile i + 3 is written where tile i - 1 was, while K of tile i + 2 and V of tile i are read: one barrier a step.
 #include "dsk_window_run.hpp"
 
 namespace dsk {
-
-constexpr int kWideHalfRows = kAttnTile;
 
 // What a thread has of a tile on its way: 16-byte chunks of rows.
 template <bool E4M3>
@@ -23,8 +22,8 @@ struct WideStage {
   uint32_t ks, vs;      // scales of the thread's row
 };
 
-// Tiles on their way, one after the other from the run's first on.  The addresses go along with the tiles, as a lone wavefront of a SIMD
-// has no time for others' arithmetic.
+// Tiles on their way, one after the other from the run's first on.  The addresses go along with the tiles: made
+// anew from the tile's number they cost 64-bit products.
 template <int BYTES>
 __device__ __forceinline__ auto wide_load(tile_global base, uint32_t off) {
   if constexpr (BYTES == 16) {
@@ -134,9 +133,9 @@ struct WideLoader {
   }
 };
 
-// Half of a wavefront's rows.  The softmax is that of TileSoftmax, taken apart: exponents are made from the reference as it is when the
+// A wavefront's rows.  The softmax is that of TileSoftmax, taken apart: exponents are made from the reference as it is when the
 // logits come, and again in the rare case that it has to move.
-struct WideHalf {
+struct WideRows {
   WinRows rows;
   TileSoftmax sm;
   tile_f32x16 O[4];
@@ -144,7 +143,7 @@ struct WideHalf {
   float x[16];          // their exponents, in log2 units above the reference,
   float mx;             // and the largest of these
   TileWeights<1> w;
-  __device__ __forceinline__ explicit WideHalf(float scale_log2) : sm(scale_log2) { win_clear(O); }
+  __device__ __forceinline__ explicit WideRows(float scale_log2) : sm(scale_log2) { win_clear(O); }
   __device__ __forceinline__ void exponents() {
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = sm.exponent.of(z[i]);
@@ -182,7 +181,7 @@ struct WideHalf {
 
 // The weights of a tile, and meanwhile products: of K for the logits of the next one, of V with the weights of the one before.  Then the
 // fragments that come after these are read, as each is through.
-__device__ __forceinline__ void wide_phase(WideHalf& h, TileKFrag& kf, WinVFrag<false>& vf, const unsigned char* next, const unsigned char* values) {
+__device__ __forceinline__ void wide_step(WideRows& h, TileKFrag& kf, WinVFrag<false>& vf, const unsigned char* next, const unsigned char* values) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(h.x[i]));   // what is made of them is made here
   kf.template add<0, 8>(h.z, h.rows);
@@ -218,8 +217,8 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void window_wide_kernel(d
   WinRun keys;
   int tok0 = 0, len = 0;
   if (!work.find(a, sp, G, hk, q_tile, kWideRows, keys, tok0, len)) return;     // uniform
-  WideHalf h(scale_log2);
-  work.rows<false>(h.rows, a, G, wave * kWideHalfRows, tok0, len);
+  WideRows h(scale_log2);
+  work.rows<false>(h.rows, a, G, wave * kAttnTile, tok0, len);
 
   const int begin = keys.begin, count = keys.end - keys.begin;
   if (threadIdx.x < kRing) sm_left_out[threadIdx.x] = -1;
@@ -257,7 +256,7 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void window_wide_kernel(d
       const int v = begin + i;
       loader.put(x[kSet], v + 3, buffer(kPut), sm_left_out + kPut);
       loader.fetch(x[kSet]);
-      wide_phase(h, kf, vf, buffer((B + 2) % kRing), buffer(B) + kTileBytes);
+      wide_step(h, kf, vf, buffer((B + 2) % kRing), buffer(B) + kTileBytes);
       if (i + 1 < count) h.look(keys, v + 1, loader.plain(v + 1), vf);   // (behind the last tile the logits are another one's and nobody's)
       if (!loader.plain(v) && sm_left_out[B] == v)
         win_add_left_out<E4M3>(h.O, c, keys, hk, v, h.allowed(keys, v), h.rows.half);
