@@ -197,3 +197,44 @@ def test_helpers_check_their_tensors(dsk):
     for make in bad:
         with pytest.raises(AssertionError):
             make()
+
+
+def test_kept_calls_are_made_on_the_device_of_their_tensors(dsk, monkeypatch):
+    import contextlib
+
+    import torch
+    i, X = torch.zeros(3, dtype=torch.int32), torch.zeros(2, 8, 128, dtype=torch.bfloat16)
+    K, ks = dsk.empty_kv8(2, 32, device="cpu")
+    sel = torch.zeros(1, 2, 4, dtype=torch.int32)
+    x = X[:1].contiguous()
+
+    class Elsewhere:
+        device = torch.device("cuda", 1)
+
+    order = []
+
+    @contextlib.contextmanager
+    def on(device):
+        order.append(device.index)
+        yield
+        order.append(0)
+
+    def noted(args, stream, check):
+        order.append((args, stream, check))
+        return 0
+    for name in ("dsk_kv8_append", "dsk_window_attn", "dsk_window_sparse_decode_attn"):
+        monkeypatch.setattr(dsk.binding, name, noted)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "device", on)
+    new = dict(seq_row0=i[:1], seq_len=i[:1], cu_new=i[:2], max_new=1)
+    app = dsk.make_kv8_appender(x[:, :2], x[:, :2], K, K.clone(), ks, ks.clone(), scale_block=32, **new)
+    app.dev_status = Elsewhere()
+    made = [dsk.make_window_attn_args(x, X, X, max_seqlen=4, **new),
+            dsk.make_window_sparse_args(x, X, X, seq_row0=i[:1], seq_len=i[:1], sel_start=sel, sel_len=sel, sel_count=sel[..., 0].contiguous(),
+                                        b=8, window=0)]
+    for kept in made:
+        kept.lse = Elsewhere()
+    for kept in [app] + made:
+        order.clear()
+        assert kept.step(5, check=False) == 0
+        assert order[0] == 1 and order[2] == 0 and order[1][0] is kept.args and order[1][1:] == (5, False)
