@@ -1,10 +1,13 @@
 // dsk_window_attn for many rows (prompts): the matrix cores bound it.
 //
-// Eight wavefronts of 32 rows make a workgroup, two a SIMD, and read each tile of K and V from LDS.  A wavefront's step is straight-line
-// code: products of K for the logits of the next tile and of V with the weights of the one before, and among them the exponentials of
-// this one, so that neither the matrix core nor the vector ALU waits for the other; what is rare (masks, a reference that moves) lies
-// between steps.  The other wavefront of the SIMD fills in where one waits.  Four wavefronts of 64 rows read LDS half as often, but
-// nothing fills in for a lone one: a prompt of 8191 tokens, 32 heads, 702 us instead of 670 (820 TFLOP/s).
+// Eight wavefronts of 32 rows make a workgroup, two a SIMD, and read each tile of K and V from LDS.  A wavefront's step begins with its
+// products, of K for the logits of the next tile and of V with the weights of the one before, and among them the exponentials of this
+// one; then it reads the fragments that come next, which the other wavefront of the SIMD covers.  What is rare (masks, a reference that
+// moves, the ends of a run) lies on branches that a step in the middle of a run does not take: 624 us for a prompt of 8191 tokens of 32
+// heads in bf16 (880 TFLOP/s; 670 where every step asks for all of it), 184 for 2048 tokens over windows of 4096 in 8 bits.  A step takes
+// about 2300 cycles: 1024 of the matrix core for two wavefronts, 1000 of the vector ALU, the rest waits, mostly for LDS.  Four wavefronts
+// of 64 rows read LDS half as often, but nothing fills in where a lone one waits (702 us); two wavefronts kept half a step apart by a
+// second barrier take 613 us in bf16 and 199 in 8 bits, where widening makes their halves unequal.
 //
 // K and V come to LDS through registers, a ring of four tiles in bf16: codes are widened on the way, once for all wavefronts.  In step i
 // tile i + 3 is written where tile i - 1 was, while K of tile i + 2 and V of tile i are read: one barrier a step.
@@ -12,45 +15,41 @@
 
 namespace dsk {
 
-// What a thread has of a tile on its way: 16-byte chunks of rows.
+// What a thread has of a tile on its way: a 16-byte chunk of a row of K and of V in bf16, or the eight codes that make one.
 template <bool E4M3>
 struct WideStage {
-  static constexpr int kChunks = DSK_HEAD_DIM / 8;                        // of a row
-  static constexpr int kRows = kWideWaves * DSK_WAVE / kChunks;          // at once
-  static constexpr int kLoads = kAttnTile / kRows, kBytes = E4M3 ? 8 : 16;
-  typename std::conditional<E4M3, uint2, uint4>::type k[kLoads], v[kLoads];
-  uint32_t ks, vs;      // scales of the thread's row
+  static constexpr int kBytes = E4M3 ? 8 : 16;
+  typename std::conditional<E4M3, uint2, uint4>::type k, v;
+  uint32_t ks, vs;      // scales of the row
 };
 
-// Tiles on their way, one after the other from the run's first on.  The addresses go along with the tiles: made
-// anew from the tile's number they cost 64-bit products.
+// BYTES of each lane from a uniform address and the lane's 32-bit offset (the asm keeps the compiler from making 64-bit addresses)
 template <int BYTES>
 __device__ __forceinline__ auto wide_load(tile_global base, uint32_t off) {
-  if constexpr (BYTES == 16) {
-    return load16_at<false>(base, off);
-  } else {
-    asm("" : "+s"(base));
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    const u32x2 x = *(const __attribute__((address_space(1))) u32x2*)(base + off);
-    return make_uint2(x.x, x.y);
-  }
+  asm("" : "+s"(base), "+v"(off));
+  typedef uint32_t words __attribute__((ext_vector_type(BYTES / 4)));
+  return __builtin_bit_cast(typename std::conditional<BYTES == 8, uint2, uint4>::type, *(const __attribute__((address_space(1))) words*)(base + off));
 }
+
+// Tiles on their way, one after the other from the run's first on.  Loads lie on no branch: where one does, the compiler waits for more
+// of them than it has to.
 template <bool E4M3>
 struct WideLoader {
   using Stage = WideStage<E4M3>;
+  static constexpr int kChunks = DSK_HEAD_DIM / 8;       // of a row
+  static_assert(kWideWaves * DSK_WAVE == kAttnTile * kChunks, "a thread a chunk of a tile");
   const WinCache& c;
   const WinRun& keys;
   const WinRun::Plain plain;
   int hk, row, chunk;
-  uint32_t k_off, v_off;
   int v;                // the next tile
   int64_t at;           // its first row, and its addresses
   tile_global k, w;
+  uint32_t k_off, v_off;   // of the thread
+  int64_t scale;        // with codes: where the scale of the thread's row is
   __device__ __forceinline__ WideLoader(const WinCache& cache, const WinRun& run, int head) : c(cache), keys(run), plain(run.plain_tiles()), hk(head) {
-    row = threadIdx.x / Stage::kChunks;
-    chunk = threadIdx.x % Stage::kChunks;
-    k_off = (uint32_t)(row * (int)c.k_tok + chunk * Stage::kBytes);
-    v_off = (uint32_t)(row * (int)c.v_tok + chunk * Stage::kBytes);
+    row = threadIdx.x / kChunks;
+    chunk = threadIdx.x % kChunks;
     go(keys.begin);
   }
   __device__ __forceinline__ void go(int tile) {
@@ -58,78 +57,60 @@ struct WideLoader {
     at = keys.start(v);
     k = (tile_global)(c.K + hk * c.k_head + at * c.k_tok);
     w = (tile_global)(c.V + hk * c.v_head + at * c.v_tok);
+    const int last = keys.last(v), n = row < last ? row : last;   // rows behind the last one that there is are that one again
+    k_off = (uint32_t)(n * (int)c.k_tok + chunk * Stage::kBytes);
+    v_off = (uint32_t)(n * (int)c.v_tok + chunk * Stage::kBytes);
+    scale = E4M3 ? at + n : 0;
   }
-  // the next tile; beyond the last one that comes again, and is not read
-  __device__ __forceinline__ void fetch(Stage& x) {
-    const bool cut = keys.there - (int)(at - keys.row0) < kAttnTile;
-    if (!cut) {
-#pragma unroll
-      for (int u = 0; u < Stage::kLoads; ++u) {
-        x.k[u] = wide_load<Stage::kBytes>(k + u * Stage::kRows * c.k_tok, k_off);
-        x.v[u] = wide_load<Stage::kBytes>(w + u * Stage::kRows * c.v_tok, v_off);
-      }
-    } else {
-      const int last = keys.last(v);
-#pragma unroll
-      for (int u = 0; u < Stage::kLoads; ++u) {
-        const int r = row + u * Stage::kRows, n = r < last ? r : last;
-        x.k[u] = wide_load<Stage::kBytes>(k, (uint32_t)(n * (int)c.k_tok + chunk * Stage::kBytes));
-        x.v[u] = wide_load<Stage::kBytes>(w, (uint32_t)(n * (int)c.v_tok + chunk * Stage::kBytes));
-      }
-    }
+  // the next tile; quiet: it is whole, and neither the last one nor the last of the first tokens'
+  __device__ __forceinline__ void fetch(Stage& x, bool quiet) {
+    x.k = wide_load<Stage::kBytes>(k, k_off);
+    x.v = wide_load<Stage::kBytes>(w, v_off);
     if constexpr (E4M3) {
-      const int last = cut ? keys.last(v) : kAttnTile - 1;
-      const int64_t block = hk * c.s_head + ((at + (row < last ? row : last)) >> c.s_shift);
+      const int64_t block = hk * c.s_head + (scale >> c.s_shift);
       x.ks = c.ks[block];
       x.vs = c.vs[block];
     }
-    if (v + 1 == keys.tiles.first) {
-      if (v + 1 < keys.end) go(v + 1);
-    } else {
-      const bool more = v + 1 < keys.end;
-      v += more;
-      at += more ? kAttnTile : 0;
-      k += more ? kAttnTile * c.k_tok : 0;
-      w += more ? kAttnTile * c.v_tok : 0;
+    if (__builtin_expect(quiet, 1)) {
+      v += 1;
+      at += kAttnTile;
+      k += kAttnTile * c.k_tok;
+      w += kAttnTile * c.v_tok;
+      if constexpr (E4M3) scale += kAttnTile;
+    } else if (v + 1 < keys.end) {                       // beyond the last one that comes again, and is not read
+      go(v + 1);
     }
   }
   // Tile v into its buffer.  A masked row may hold anything, and 0 * NaN is NaN: where not every row sees all of the tile, values that are
   // not finite are left out and the tile is noted.
-  __device__ __forceinline__ void put(Stage& x, int tile, unsigned char* sm_k, int* sm_left_out) const {
-    if (!plain(tile)) {                                    // (nor of what lies behind the last one)
+  __device__ __forceinline__ void put(Stage& x, int tile, bool quiet, unsigned char* sm_k, int* sm_left_out) const {
+    if (__builtin_expect(!quiet && !plain(tile), 0)) {                                    // (nor of what lies behind the last one)
       uint32_t found = 0;
+      uint32_t* const y = &x.v.x;
 #pragma unroll
-      for (int u = 0; u < Stage::kLoads; ++u) {
-        uint32_t* const y = &x.v[u].x;
-#pragma unroll
-        for (int i = 0; i < Stage::kBytes / 4; ++i) {
-          const uint32_t was = y[i];
-          if constexpr (E4M3) {
-            const uint32_t nan = ((was & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-            y[i] = was & ~((nan << 1) - (nan >> 7));
-          } else {
-            y[i] = finite_bf16(was);
-          }
-          found |= was ^ y[i];
+      for (int i = 0; i < Stage::kBytes / 4; ++i) {
+        const uint32_t was = y[i];
+        if constexpr (E4M3) {
+          const uint32_t nan = ((was & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+          y[i] = was & ~((nan << 1) - (nan >> 7));
+        } else {
+          y[i] = finite_bf16(was);
         }
+        found |= was ^ y[i];
       }
       if (found != 0) *sm_left_out = tile;
     }
     unsigned char* const sm_v = sm_k + kTileBytes;
-    auto write = [&](int r, int to, const uint4& a, const uint4& b) {
-      *reinterpret_cast<uint4*>(sm_k + r * kTileRowBytes + ((to ^ (r & 15)) << 4)) = a;
-      *reinterpret_cast<uint4*>(sm_v + r * kTileRowBytes + ((to ^ ((r & 3) << 2)) << 4)) = b;
-    };
-#pragma unroll
-    for (int u = 0; u < Stage::kLoads; ++u) {
-      const int r = row + u * Stage::kRows;
-      if constexpr (!E4M3) {
-        write(r, chunk, x.k[u], x.v[u]);
-      } else {
-        const float s = __uint_as_float(x.ks << 23), t = __uint_as_float(x.vs << 23);
-        write(r, chunk, __builtin_bit_cast(uint4, win_widen8(x.k[u].x, x.k[u].y, s)), __builtin_bit_cast(uint4, win_widen8(x.v[u].x, x.v[u].y, t)));
-      }
+    uint4 a, b;
+    if constexpr (!E4M3) {
+      a = x.k;
+      b = x.v;
+    } else {
+      a = __builtin_bit_cast(uint4, win_widen8(x.k.x, x.k.y, __uint_as_float(x.ks << 23)));
+      b = __builtin_bit_cast(uint4, win_widen8(x.v.x, x.v.y, __uint_as_float(x.vs << 23)));
     }
+    *reinterpret_cast<uint4*>(sm_k + row * kTileRowBytes + ((chunk ^ (row & 15)) << 4)) = a;
+    *reinterpret_cast<uint4*>(sm_v + row * kTileRowBytes + ((chunk ^ ((row & 3) << 2)) << 4)) = b;
   }
 };
 
@@ -157,11 +138,11 @@ struct WideRows {
   __device__ __forceinline__ uint32_t allowed(const WinRun& keys, int v) const { return rows.real ? keys.allowed(v, rows.pos) : 0u; }
   // what comes between the logits of tile v and their weights
   __device__ __forceinline__ void look(const WinRun& keys, int v, bool plain, const WinVFrag<false>& vf) {
-    if (!plain) {
+    if (__builtin_expect(!plain, 0)) {
       tile_hide(z, allowed(keys, v) >> (4 * rows.half), 0);
       exponents();
     }
-    if (__any(mx > 8.0f || sm.m == -__builtin_inff())) {
+    if (__builtin_expect(__any(mx > 8.0f || sm.m == -__builtin_inff()), 0)) {
       vf.template add<1>(O, w, 0);                       // weights that wait for their product still go by the old reference
       vf.template add<1>(O, w, 1);
       w.w[0][0] = w.w[0][1] = __builtin_bit_cast(tile_bf16x8, make_uint4(0, 0, 0, 0));
@@ -179,9 +160,9 @@ struct WideRows {
   }
 };
 
-// The weights of a tile, and meanwhile products: of K for the logits of the next one, of V with the weights of the one before.  Then the
-// fragments that come after these are read, as each is through.
-__device__ __forceinline__ void wide_step(WideRows& h, TileKFrag& kf, WinVFrag<false>& vf, const unsigned char* next, const unsigned char* values) {
+// The weights of a tile, and meanwhile products: of K for the logits of the next one, of V with the weights of the one before.
+__device__ __forceinline__ void wide_products(WideRows& h, const TileKFrag& kf, const WinVFrag<false>& vf) {
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(h.x[i]));   // what is made of them is made here
   kf.template add<0, 8>(h.z, h.rows);
@@ -196,12 +177,9 @@ __device__ __forceinline__ void wide_step(WideRows& h, TileKFrag& kf, WinVFrag<f
   h.sm.err = (sum - h.sm.l) - add;
   h.sm.l = sum;
   h.w.set(h.x);
-  kf.template read<0, 8>(next, h.rows);
-  vf.template read<0>(values);
-  vf.template read<1>(values);
-  h.exponents();
   __builtin_amdgcn_iglp_opt(3);                          // a matrix instruction, an exponential, and what else there is
-  asm volatile("" : "+v"(h.sm.l), "+v"(h.sm.err), "+v"(h.mx));
+  asm volatile("" : "+v"(h.sm.l), "+v"(h.sm.err));
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 template <bool E4M3>
@@ -235,14 +213,14 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void window_wide_kernel(d
   }
   if (count > 0) {
     WideLoader<E4M3> loader(c, keys, hk);
-    loader.fetch(x[0]);
-    loader.fetch(x[1]);
-    loader.put(x[0], begin, buffer(0), sm_left_out);
-    loader.fetch(x[0]);
-    loader.put(x[1], begin + 1, buffer(1), sm_left_out + 1);
-    loader.fetch(x[1]);
-    loader.put(x[0], begin + 2, buffer(2), sm_left_out + 2);
-    loader.fetch(x[0]);
+    loader.fetch(x[0], false);
+    loader.fetch(x[1], false);
+    loader.put(x[0], begin, false, buffer(0), sm_left_out);
+    loader.fetch(x[0], false);
+    loader.put(x[1], begin + 1, false, buffer(1), sm_left_out + 1);
+    loader.fetch(x[1], false);
+    loader.put(x[0], begin + 2, false, buffer(2), sm_left_out + 2);
+    loader.fetch(x[0], false);
     __syncthreads();
     kf.template read<0, 8>(buffer(0), h.rows);
     kf.template add<0, 8>(h.z, h.rows);
@@ -251,14 +229,20 @@ __global__ __launch_bounds__(kWideWaves * DSK_WAVE, 2) void window_wide_kernel(d
     h.look(keys, begin, loader.plain(begin), vf);
     // Tile i in buffer B = i % 4: its exponents in h.x, K of tile i + 1 in kf, V of tile i - 1 in vf and its weights in h.w; set (i + 1) % 2 of
     // x has tile i + 3.
+    const int quiet_from = loader.plain.from - begin, quiet_to = (loader.plain.to < keys.end ? loader.plain.to : keys.end) - begin - 7;
     auto step = [&](auto buf, int i) {
+      const bool quiet = i >= quiet_from && i <= quiet_to;   // tiles i to i + 6 are plain
       constexpr int B = decltype(buf)::value, kPut = (B + 3) % kRing, kSet = (B + 1) % 2;
       const int v = begin + i;
-      loader.put(x[kSet], v + 3, buffer(kPut), sm_left_out + kPut);
-      loader.fetch(x[kSet]);
-      wide_step(h, kf, vf, buffer((B + 2) % kRing), buffer(B) + kTileBytes);
-      if (i + 1 < count) h.look(keys, v + 1, loader.plain(v + 1), vf);   // (behind the last tile the logits are another one's and nobody's)
-      if (!loader.plain(v) && sm_left_out[B] == v)
+      wide_products(h, kf, vf);
+      kf.template read<0, 8>(buffer((B + 2) % kRing), h.rows);
+      vf.template read<0>(buffer(B) + kTileBytes);
+      vf.template read<1>(buffer(B) + kTileBytes);
+      loader.put(x[kSet], v + 3, quiet, buffer(kPut), sm_left_out + kPut);
+      loader.fetch(x[kSet], quiet);
+      h.exponents();
+      if (quiet || i + 1 < count) h.look(keys, v + 1, quiet || loader.plain(v + 1), vf);   // (behind the last tile the logits are another one's and nobody's)
+      if (__builtin_expect(!quiet && !loader.plain(v) && sm_left_out[B] == v, 0))
         win_add_left_out<E4M3>(h.O, c, keys, hk, v, h.allowed(keys, v), h.rows.half);
       __syncthreads();
     };
