@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_
   }
   // a row of the block's token t, normed and rotated
   const float* const weight = queries ? a.q_weight : a.k_weight;
-  float wt[8];
+  __align__(16) float wt[8];
   if (weight != nullptr) {
     const float4 w0 = *reinterpret_cast<const float4*>(weight + c * 8), w1 = *reinterpret_cast<const float4*>(weight + c * 8 + 4);
     wt[0] = w0.x; wt[1] = w0.y; wt[2] = w0.z; wt[3] = w0.w;
