@@ -179,12 +179,19 @@ struct WinRows : TileQueries {
   }
 };
 
-// The values that were left out of a tile, for the rows that see them: of key j, four channels at a time.
+// The values that were left out of a tile, for the rows that see them: of key j, four channels at a time.  Of codes: what has no finite
+// value in bf16, and all under a scale that is no number.
 template <bool E4M3, class KEYS>
 __device__ __forceinline__ void win_add_left_out(tile_f32x16 (&O)[4], const WinCache& c, const KEYS& keys, int hk, int v, uint32_t allow, int half) {
   for (int j = 0; j < kAttnTile; ++j) {
     if (!((allow >> j) & 1u)) continue;
-    const unsigned char* at = c.V + hk * c.v_head + (keys.row0 + keys.row_of(v, j)) * c.v_tok + half * (E4M3 ? 4 : 8);
+    const int64_t row = keys.row0 + keys.row_of(v, j);
+    const unsigned char* at = c.V + hk * c.v_head + row * c.v_tok + half * (E4M3 ? 4 : 8);
+    float scale = 1.0f;
+    if constexpr (E4M3) {
+      const uint32_t b = c.vs[hk * c.s_head + (row >> c.s_shift)];
+      scale = b == 255 ? __builtin_nanf("") : __uint_as_float(b << 23);
+    }
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
@@ -192,8 +199,10 @@ __device__ __forceinline__ void win_add_left_out(tile_f32x16 (&O)[4], const WinC
         if constexpr (E4M3) {
           const uint32_t x = *reinterpret_cast<const uint32_t*>(at + ct * 32 + 8 * i);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (((x >> (8 * e)) & 0x7Fu) == 0x7Fu) O[ct][4 * i + e] += __builtin_nanf("");
+          for (int e = 0; e < 4; ++e) {
+            const float y = __builtin_amdgcn_cvt_f32_fp8((int)(x >> (8 * e)), 0) * scale;
+            if (!(fabsf(y) < 0x1.ffp127f)) O[ct][4 * i + e] += y;
+          }
         } else {
           const uint2 x = *reinterpret_cast<const uint2*>(at + 2 * (ct * 32 + 8 * i));
 #pragma unroll
@@ -353,6 +362,10 @@ __device__ __forceinline__ void win_stream(WinStreamLds<E4M3>& sh, const WinCach
       allow = rows.real ? keys.allowed(v, rows.pos) : 0u;
       tile_hide(z, allow >> (4 * rows.half), 0);
       left_out = vf.keep_finite();                       // a masked row may hold anything, and 0 * NaN is NaN
+      if constexpr (E4M3) {                              // and so may its scale
+        left_out |= __any(vs == 255);
+        vs = vs == 255 ? 0 : vs;
+      }
     }
     // values are widened with their scale where the tile has one for all; otherwise it goes into the weights
     float v_scale = 1.0f;

@@ -86,13 +86,24 @@ struct WinFold {
         vf.load(sm_v + tile * kTile);
         __builtin_amdgcn_sched_barrier(0);
         // a masked row may hold anything, and 0 * NaN is NaN: such values stay out of the product
-        const bool left_out = !plain && vf.keep_finite();
+        bool left_out = !plain && vf.keep_finite();
+        bool no_scale = false;                           // nor is every scale a number
+        if constexpr (E4M3) {
+          no_scale = !plain && __any(scale[kKeys + tile * kAttnTile + rows.col] == __builtin_inff());
+          left_out |= no_scale;
+        }
         TileWeights<TERMS> w;
         sm.template take<TERMS, true>(z, O, w, [&](float (&p)[16]) {
           if constexpr (E4M3) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float4 f = *reinterpret_cast<const float4*>(scale + kKeys + tile * kAttnTile + 4 * rows.half + 8 * j);
+              float4 f = *reinterpret_cast<const float4*>(scale + kKeys + tile * kAttnTile + 4 * rows.half + 8 * j);
+              if (no_scale) {
+                f.x = f.x == __builtin_inff() ? 0.0f : f.x;
+                f.y = f.y == __builtin_inff() ? 0.0f : f.y;
+                f.z = f.z == __builtin_inff() ? 0.0f : f.z;
+                f.w = f.w == __builtin_inff() ? 0.0f : f.w;
+              }
               p[4 * j] *= f.x; p[4 * j + 1] *= f.y; p[4 * j + 2] *= f.z; p[4 * j + 3] *= f.w;
             }
           }

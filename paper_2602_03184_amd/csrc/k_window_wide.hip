@@ -82,25 +82,8 @@ struct WideLoader {
     }
   }
   // Tile v into its buffer.  A masked row may hold anything, and 0 * NaN is NaN: where not every row sees all of the tile, values that are
-  // not finite are left out and the tile is noted.
-  __device__ __forceinline__ void put(Stage& x, int tile, bool quiet, unsigned char* sm_k, int* sm_left_out) const {
-    if (__builtin_expect(!quiet && !plain(tile), 0)) {                                    // (nor of what lies behind the last one)
-      uint32_t found = 0;
-      uint32_t* const y = &x.v.x;
-#pragma unroll
-      for (int i = 0; i < Stage::kBytes / 4; ++i) {
-        const uint32_t was = y[i];
-        if constexpr (E4M3) {
-          const uint32_t nan = ((was & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-          y[i] = was & ~((nan << 1) - (nan >> 7));
-        } else {
-          y[i] = finite_bf16(was);
-        }
-        found |= was ^ y[i];
-      }
-      if (found != 0) *sm_left_out = tile;
-    }
-    unsigned char* const sm_v = sm_k + kTileBytes;
+  // not finite (of codes: with their scale) are left out and the tile is noted.
+  __device__ __forceinline__ void put(const Stage& x, int tile, bool quiet, unsigned char* sm_k, int* sm_left_out) const {
     uint4 a, b;
     if constexpr (!E4M3) {
       a = x.k;
@@ -109,6 +92,13 @@ struct WideLoader {
       a = __builtin_bit_cast(uint4, win_widen8(x.k.x, x.k.y, __uint_as_float(x.ks << 23)));
       b = __builtin_bit_cast(uint4, win_widen8(x.v.x, x.v.y, __uint_as_float(x.vs << 23)));
     }
+    if (__builtin_expect(!quiet && !plain(tile), 0)) {   // (nor of what lies behind the last one)
+      uint4 y = make_uint4(finite_bf16(b.x), finite_bf16(b.y), finite_bf16(b.z), finite_bf16(b.w));
+      if (E4M3 && x.vs == 255) y = make_uint4(0, 0, 0, 0);
+      if ((y.x ^ b.x) | (y.y ^ b.y) | (y.z ^ b.z) | (y.w ^ b.w)) *sm_left_out = tile;
+      b = y;
+    }
+    unsigned char* const sm_v = sm_k + kTileBytes;
     *reinterpret_cast<uint4*>(sm_k + row * kTileRowBytes + ((chunk ^ (row & 15)) << 4)) = a;
     *reinterpret_cast<uint4*>(sm_v + row * kTileRowBytes + ((chunk ^ ((row & 3) << 2)) << 4)) = b;
   }

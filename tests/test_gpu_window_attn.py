@@ -206,6 +206,36 @@ def test_rows_that_are_not_seen_may_hold_anything(what, new, window, sinks, bits
                 put(X, c.row0[s] + t, o)
 
 
+@pytest.mark.parametrize("byte", [255, 254])
+@pytest.mark.parametrize("new, window, sinks", [(1, 40, 3), (9, 45, 3), (9, ALL, 0), (150, 70, 35)])
+def test_scales_of_blocks_that_are_not_seen_may_hold_anything(new, window, sinks, byte):
+    """Also 255, which stands for no number; where it is seen, the result is none."""
+    c = Case([170, 0, 333], [new, new, 3], 8, 2, window=window, sinks=sinks, seed=14, spare=7, aligned=False)
+    clean = [c.run(), c.run(want_f32=False, want_bf16=True)]
+    seen = torch.zeros(c.ks.shape[1] * 32, dtype=torch.bool, device="cuda")
+    for s in range(3):
+        seen[c.row0[s]: c.row0[s] + c.lens[s] + c.new[s]] = c.seen(s).any(0)
+    unseen = ~seen.view(-1, 32).any(1)
+    assert bool(unseen.any()) or window == ALL
+    for X in (c.ks, c.vs):
+        as_bytes(X)[:, unseen] = byte
+    for r0, kw in zip(clean, ({}, dict(want_f32=False, want_bf16=True))):
+        r = c.run(**kw)
+        a, b = (x.out if x.out is not None else x.out_bf16 for x in (r, r0))
+        assert torch.equal(a, b) and torch.equal(r.lse, r0.lse)
+        if byte == 254:
+            continue
+        for blk in (0, (c.row0[0] + c.lens[0] + new // 2) // 32, (c.row0[2] + 300) // 32):
+            old = as_bytes(c.vs)[:, blk].clone()
+            as_bytes(c.vs)[:, blk] = 255
+            r = c.run(**kw)
+            a = r.out if r.out is not None else r.out_bf16
+            meets = torch.cat([c.seen(s)[:, [t for t in range(c.lens[s] + c.new[s]) if (c.row0[s] + t) // 32 == blk]].any(1) for s in range(3)])
+            assert torch.equal(a[~meets], b[~meets]) and torch.equal(r.lse[~meets], r0.lse[~meets])
+            assert not bool(torch.isfinite(a[meets]).all(-1).any()) or not bool(meets.any())
+            as_bytes(c.vs)[:, blk] = old
+
+
 def test_an_infinity_that_is_seen_gives_that_infinity():
     for new, kw in ((1, {}), (9, {}), (150, dict(window=90, sinks=40))):
         c = Case([60], [new], 8, 2, bits=16, seed=14, **kw)
