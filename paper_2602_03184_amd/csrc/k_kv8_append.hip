@@ -284,7 +284,9 @@ static void launch_pairs(const dsk_kv8_append_args& a, hipStream_t st) {
   else launch_block<PAIRS, 4>(a, blocks, st);
 }
 
-hipError_t launch_kv8_append(const dsk_kv8_append_args& a, hipStream_t st) {
+hipError_t launch_kv8_append(const dsk_kv8_append_args& args, hipStream_t st) {
+  dsk_kv8_append_args a = args;
+  a.max_new = a.max_new < a.n_tokens ? a.max_new : a.n_tokens;   // more than all of them says nothing more
   if (a.rot_dim == 0) launch_pairs<RopePairs::kNone>(a, st);
   else if (a.flags & DSK_ROPE_INTERLEAVED) launch_pairs<RopePairs::kInterleaved>(a, st);
   else if (a.rot_dim == DSK_HEAD_DIM) launch_pairs<RopePairs::kHalfAll>(a, st);

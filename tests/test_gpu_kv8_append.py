@@ -298,3 +298,13 @@ def test_captured_and_on_another_stream():
         torch.cuda.synchronize()
         start = c.snapshot()
         assert all(torch.equal(a, b) for a, b in zip(start, eager.snapshot()))
+
+
+def test_a_bound_beyond_all_tokens_changes_nothing():
+    a, b = Case([5, 50, 0], [4, 1, 70], seed=21), Case([5, 50, 0], [4, 1, 70], seed=21)
+    ha, hb = a.handle(), b.handle(max_new=0x7FFFFFFF)
+    for h in (ha, hb):
+        h.step()
+    torch.cuda.synchronize()
+    assert int(hb.dev_status) == 0 and torch.equal(ha.q_out, hb.q_out)
+    assert all(torch.equal(x, y) for x, y in zip(a.snapshot(), b.snapshot()))
