@@ -744,7 +744,7 @@ typedef struct dsk_kv8_append_args {
  * largest or less.  A token that sees nothing (its sequence has no place in the cache) gets out = 0 and lse = -inf.
  * Accuracy and bits as for dsk_tree_decode_attn, with rows = max_new * Hq / Hkv: `out` asks for fp32 accuracy; where only out_bf16 is
  * asked for, the weights are off by 2^-16 of each at most, and above 64 rows rounded to bf16.  In 8 bits scales below 2^-100 may
- * lose small weights.
+ * lose small weights.  Values of 2^100 and more may become infinite on the way to a sum that is not.
  * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths are cut, never followed: tokens to
  * max_new and n_tokens, seq_len to max_seqlen, rows to total_rows.
  * ---------------------------------------------------------------------------------------- */
