@@ -219,7 +219,8 @@ __device__ __forceinline__ void win_add_left_out(tile_f32x16 (&O)[4], const WinC
 // ---- a wavefront's stream of tiles -----------------------------------------------------------------------------
 // Where a workgroup's rows fit one wavefront (32), its wavefronts take other tiles each and share nothing until the end: a wavefront
 // copies the tile that it will multiply into LDS of its own, a ring of two tiles, and waits for its own copies alone.  The next tile
-// and, once the fragments of this one are in registers, the one after it are on their way while it is multiplied.
+// and, once the fragments of this one are in registers, the one after it are on their way while it is multiplied: 64 KB a workgroup
+// in 8 bits, of which two fit a CU, 128 KB in bf16.
 constexpr int kStreamWaves = 4;
 constexpr int kStreamRing = 2;
 

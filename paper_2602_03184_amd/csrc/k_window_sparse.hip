@@ -27,7 +27,9 @@ struct WinSparse {
   int row_tiles;              // workgroups for the query heads of a KV head, 32 each
 };
 
-// Parts 0 .. slot_parts - 1 of a list are its slots'; the others, of a KV head, are what is near.  Every part leaves a result.
+// Parts 0 .. slot_parts - 1 of a list are its slots'; the others, of a KV head, are what is near.  Every part leaves a result.  Latency
+// bounds it: lengths and slots, the list of rows in LDS, their scales and codes, two tiles a wavefront.  32 lists of 4096 tokens in 8 bits
+// and 8 windows of 128 take 11.7 us (25 MB), 64 lists of 4096 tokens and 64 windows of 1024 19.3 us (67 MB at 3.5 TB/s).
 template <int TERMS, bool E4M3>
 __global__ __launch_bounds__(kStreamWaves * DSK_WAVE, E4M3 ? 2 : 1) void window_sparse_kernel(dsk_window_sparse_args a, WinCache c, WinOut to, WinSparse sp,
                                                                          float scale_log2) {
