@@ -385,3 +385,35 @@ def test_sequences_that_share_their_rows():
         c.row0 = [0] * 10 + [c.row0[10]]
         c.lens = [9000 - 31 * s for s in range(10)]
         c.check()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("new", [1, 150])
+def test_large_caches_with_few_and_many_tokens(new, bits):
+    """As above for the kernels of few and of many rows, whose result is in bf16."""
+    rows = (1 << 32) // (2 * D * (bits // 8)) + 512
+    X = torch.zeros(rows, 2, D, dtype=torch.uint8 if bits == 8 else torch.bfloat16, device="cuda")
+    c = Case([140], [new], 4, 1, bits=bits, window=100, sinks=5, seed=20, spare=0, aligned=False)
+    row0, n = (rows - 300) // 32 * 32, 140 + new
+    K, V = (X[:, h:h + 1].transpose(0, 1) for h in range(2))
+    for big, small in ((K, c.K), (V, c.V)):
+        big[:, row0: row0 + n] = small if bits == 16 else as_bytes(small)
+    over = dict(seq_row0=i32([row0]))
+    if bits == 8:
+        K, V = K.view(torch.float8_e4m3fn), V.view(torch.float8_e4m3fn)
+        for name, small in (("k_scale", c.ks), ("v_scale", c.vs)):
+            s = torch.full((1, -(-rows // 32)), 127, dtype=torch.uint8, device="cuda")
+            s[:, row0 // 32: row0 // 32 + small.shape[1]] = as_bytes(small)
+            over[name] = s.view(torch.float8_e8m0fnu)
+    kw = dict(want_f32=False, want_bf16=True)
+    want = c.run(**kw)
+    r = _dsk().window_attn(c.q, K, V, **c.kwargs(**over, **kw))
+    torch.cuda.synchronize()
+    assert torch.equal(r.out_bf16, want.out_bf16) and torch.equal(r.lse, want.lse)
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_long_prompts_with_steps_in_the_middle_of_their_runs(bits):
+    """Runs of many tiles of which all but the ends are seen by every row, from the first token, from a window, and split."""
+    for new, lens, kw in ((2100, [0, 700], {}), (700, [3000, 64], dict(window=2500, sinks=40)), (70, [9000], dict(sinks=3))):
+        Case(lens, [new] * len(lens), 8, 1, bits=bits, seed=new, nhd=new == 700, **kw).check()
