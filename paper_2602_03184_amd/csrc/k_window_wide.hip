@@ -127,7 +127,7 @@ struct WideRows {
   }
   __device__ __forceinline__ uint32_t allowed(const WinRun& keys, int v) const { return rows.real ? keys.allowed(v, rows.pos) : 0u; }
   // what comes between the logits of tile v and their weights
-  __device__ __forceinline__ void look(const WinRun& keys, int v, bool plain, const WinVFrag<false>& vf) {
+  __device__ __forceinline__ void look(const WinRun& keys, int v, bool plain, WinVFrag<false>& vf) {
     if (__builtin_expect(!plain, 0)) {
       tile_hide(z, allowed(keys, v) >> (4 * rows.half), 0);
       exponents();
@@ -135,7 +135,13 @@ struct WideRows {
     if (__builtin_expect(__any(mx > 8.0f || sm.m == -__builtin_inff()), 0)) {
       vf.template add<1>(O, w, 0);                       // weights that wait for their product still go by the old reference
       vf.template add<1>(O, w, 1);
-      w.w[0][0] = w.w[0][1] = __builtin_bit_cast(tile_bf16x8, make_uint4(0, 0, 0, 0));
+      // It is taken: what the next step multiplies is 0 in both factors, as 0 times an infinity that all rows see is NaN.
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        w.w[0][t] = __builtin_bit_cast(tile_bf16x8, make_uint4(0, 0, 0, 0));
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) vf.v[ct][t] = w.w[0][t];
+      }
       const float top = tile_max(z) * sm.scale_log2;
       const bool move = mx > 8.0f || sm.m == -__builtin_inff();
       const float m_new = move ? fmaxf(sm.m, top) : sm.m;

@@ -417,3 +417,27 @@ def test_long_prompts_with_steps_in_the_middle_of_their_runs(bits):
     """Runs of many tiles of which all but the ends are seen by every row, from the first token, from a window, and split."""
     for new, lens, kw in ((2100, [0, 700], {}), (700, [3000, 64], dict(window=2500, sinks=40)), (70, [9000], dict(sinks=3))):
         Case(lens, [new] * len(lens), 8, 1, bits=bits, seed=new, nhd=new == 700, **kw).check()
+
+
+@pytest.mark.parametrize("new", [1, 16, 150])
+def test_an_infinity_in_the_middle_of_a_run_stays_when_larger_logits_follow(new):
+    """In a tile that every row sees, and in the next one a key that a row weighs far more than all before, yet not so much that the
+    infinity's weight falls below 2^-80 of the largest."""
+    c = Case([900], [new], 8, 2, bits=16, seed=22, sharp=0.2)    # logits of 12 at most, 34 between two keys
+    for kw in ({}, dict(want_f32=False, want_bf16=True)):
+        clean = c.run(**kw)
+        for row, key in ((100, 140), (300, 333), (511, 512), (896, 897)):
+            oldV, oldK = c.V[:, row].clone(), c.K[:, key].clone()
+            for h in range(2):
+                q = c.q[new // 2, 4 * h + 1].double()            # a logit of 22 for this row
+                c.K[h, key] = (22.0 * math.sqrt(D) / (q @ q) * q).bfloat16()
+            c.V[:, row, 5], c.V[0, row, 6] = float("inf"), -float("inf")
+            r = c.run(**kw)
+            out = r.out if r.out is not None else r.out_bf16
+            assert bool((out[..., 5] == float("inf")).all()) and bool((out[:, :4, 6] == -float("inf")).all())
+            assert bool(torch.isfinite(out[:, 4:, 6]).all()) and bool(torch.isfinite(r.lse).all())
+            fine = [i for i in range(D) if i not in (5, 6)]
+            assert bool(torch.isfinite(out[..., fine]).all())
+            c.V[:, row], c.K[:, key] = oldV, oldK
+        again = c.run(**kw)
+        assert torch.equal(again.lse, clean.lse)
