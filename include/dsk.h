@@ -739,8 +739,8 @@ typedef struct dsk_kv8_append_args {
  *   t <= p  with  t > p - window  or  t < n_sink          (position t is row seq_row0[s] + t of K / V)
  *   out = sum p_t V_t / sum p_t,  p_t = exp(q.K_t * scale);  lse = log sum p_t
  * K and V are bf16, or with k_scale codes of 8 bits (above).  Rows that a token does not see, and scales of blocks of which nobody
- * sees a row, may hold anything, NaN included (a scale of 255 is none: rows under it have no finite result for those who see them); an
- * infinity in a row of V that it sees gives that infinity, or NaN with its opposite or where its weight is 2^-80 of the
+ * sees a row, may hold anything, NaN included (a scale of 255 is none: rows under it have no finite result for those who see them, and
+ * rows under one above 2^119 may have none); an infinity in a row of V that it sees gives that infinity, or NaN with its opposite or where its weight is 2^-80 of the
  * largest or less.  A token that sees nothing (its sequence has no place in the cache) gets out = 0 and lse = -inf.
  * Accuracy and bits as for dsk_tree_decode_attn, with rows = max_new * Hq / Hkv: `out` asks for fp32 accuracy; where only out_bf16 is
  * asked for, the weights are off by 2^-16 of each at most, and above 64 rows rounded to bf16.  In 8 bits scales below 2^-100 may

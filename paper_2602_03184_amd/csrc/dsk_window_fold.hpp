@@ -132,7 +132,9 @@ struct WinVFrag<true> {
         : "v"(at), "v"(at ^ 32u), "v"(at ^ 64u), "v"(at ^ 96u)
         : "memory");
   }
-  __device__ __forceinline__ bool keep_finite() {
+  // 0 for the codes from `least` on, whatever their sign; whether there were any
+  __device__ __forceinline__ bool keep_below(uint32_t least) {
+    const uint32_t add = (0x80u - least) * 0x01010101u;  // sets the top bit of such a code, and passes nothing on to the next one
     uint32_t found = 0;
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct)
@@ -140,12 +142,13 @@ struct WinVFrag<true> {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint32_t nan = ((x[ct][t][i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;   // a code's top bit
-          found |= nan;
-          x[ct][t][i] &= ~((nan << 1) - (nan >> 7));
+          const uint32_t out = ((x[ct][t][i] & 0x7F7F7F7Fu) + add) & 0x80808080u;
+          found |= out;
+          x[ct][t][i] &= ~((out << 1) - (out >> 7));
         }
     return __any(found != 0);
   }
+  __device__ __forceinline__ bool keep_finite() { return keep_below(0x7F); }
   template <int TERMS>
   __device__ __forceinline__ void multiply(tile_f32x16 (&O)[4], const TileWeights<TERMS>& p, float scale) const {
 #pragma unroll
@@ -375,6 +378,8 @@ __device__ __forceinline__ void win_stream(WinStreamLds<E4M3>& sh, const WinCach
       const uint32_t v0 = __builtin_amdgcn_readfirstlane(vs);
       one = __all(vs == v0);
       if (one) v_scale = __uint_as_float(v0 << 23);
+      // a masked row may also hold codes whose value is beyond bf16: from 2^(128 - e) on under the scale 2^e, e >= 120
+      if (!plain && one && v0 >= 247) left_out |= vf.keep_below(0x78u - 8 * (v0 - 247));
     }
     TileWeights<TERMS> w;
     sm.template take<TERMS, true>(z, O, w, [&](float (&p)[16]) {

@@ -441,3 +441,31 @@ def test_an_infinity_in_the_middle_of_a_run_stays_when_larger_logits_follow(new)
             c.V[:, row], c.K[:, key] = oldV, oldK
         again = c.run(**kw)
         assert torch.equal(again.lse, clean.lse)
+
+
+@pytest.mark.parametrize("byte", [246, 247, 250, 254])
+@pytest.mark.parametrize("new, Hq, Hkv", [(1, 4, 4), (3, 8, 2), (8, 8, 2), (16, 8, 2), (30, 8, 2), (70, 8, 2)])
+def test_a_row_that_is_not_seen_may_be_too_large_for_its_scale(new, Hq, Hkv, byte):
+    """A block whose scale puts the largest codes beyond the finite numbers.  Rows of it that are seen hold zeros; the row that is not
+    seen, of a later token or past the window, holds the largest codes."""
+    lens, window = 100, ALL
+    if new == 1:
+        window = 90                                              # positions 0 to 10 are gone, block 0 has 11 to 31 that are seen
+    c = Case([lens], [new], Hq, Hkv, window=window, seed=23)
+    row = 5 if new == 1 else lens + new - 1
+    block = row // 32
+    as_bytes(c.vs)[:, block] = byte
+    as_bytes(c.V)[:, 32 * block: 32 * block + 32] = 0
+    # weights times such scales are out of range themselves where a logit is above the first ones: those of the block are the lowest
+    as_bytes(c.K)[:, 32 * block: 32 * block + 32] = 0
+    blind = ~c.seen(0)[:, row]
+    assert int(blind.sum()) == max(new - 1, 1)
+    for kw in ({}, dict(want_f32=False, want_bf16=True)):
+        clean = c.run(**kw)
+        as_bytes(c.V)[:, row, 5], as_bytes(c.V)[:, row, 6] = 0x7E, 0xFE
+        r = c.run(**kw)
+        as_bytes(c.V)[:, row] = 0
+        a, b = (x.out if x.out is not None else x.out_bf16 for x in (r, clean))
+        assert torch.equal(a[blind], b[blind]) and bool(torch.isfinite(a[blind]).all()) and torch.equal(r.lse, clean.lse)
+        fine = [i for i in range(D) if i not in (5, 6)]
+        assert torch.equal(a[..., fine], b[..., fine])
