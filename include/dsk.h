@@ -691,7 +691,8 @@ typedef struct dsk_accept_args {
  * seq_row0[s] + seq_len[s] + i; its position is tok_pos[t], or seq_len[s] + i without tok_pos.  Queries (optional)
  * and keys are normed and rotated as there, in fp32; queries are rounded to bf16, keys and values to codes, once:
  *   block     its scale is 2^e, e the least integer with |x| <= 448 * 2^e for all finite x written to it, within [-100, 120]
- *   new row   code = e4m3(x / scale), to nearest even; what is not finite becomes NaN
+ *   new row   code = e4m3(x / scale), to nearest even; what is not finite becomes NaN, and a finite |x| above 1.875 * 2^127, whose
+ *             code would stand for 2^128, counts as that
  *   begun     a block that holds rows of the sequence already (rows below seq_len) keeps its scale, or where the new rows need a
  *             larger one its codes are rounded again to that: exact but for values that fall below 2^-6 of the new scale
  * so that each row's values are off by 2^-4 of themselves or 2^-10 of the scale, and once more that where the scale grew.

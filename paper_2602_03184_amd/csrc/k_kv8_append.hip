@@ -39,6 +39,14 @@ __device__ __forceinline__ uint2 kv8_encode(const float (&f)[8], float by) {
   return make_uint2((uint32_t)lo, (uint32_t)hi);
 }
 
+// Under the scales 2^e from 2^120 on the codes from 2^(128 - e) on would stand for 2^128 and more: four codes with those as the one before.
+__device__ __forceinline__ uint32_t kv8_finite(uint32_t codes, int e) {
+  const uint32_t least = 0x78u - 8 * (uint32_t)(e - kKv8MaxExp), size = codes & 0x7F7F7F7Fu;
+  const uint32_t nan = size + 0x01010101u, out = (size + (0x80u - least) * 0x01010101u) & ~nan & 0x80808080u;   // a code's top bit
+  const uint32_t bits = out - (out >> 7);                // the others of it
+  return (codes & ~bits) | (bits & ((least - 1) * 0x01010101u));
+}
+
 __device__ __forceinline__ void kv8_decode(const uint2& c, float (&f)[8]) {
   const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.x, true);
   const auto d = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.y, false), e = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.y, true);
@@ -216,7 +224,11 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_append_kernel(dsk_kv8_append_
 #pragma unroll
     for (int u = 0; u < kKv8Quads; ++u) {
       const int r = part * kKv8Rows + 4 * u + grp;
-      if (real && r >= off && r < off + count) *reinterpret_cast<uint2*>(to + (block_row + r) * to_row) = kv8_encode(f[u], by);
+      if (real && r >= off && r < off + count) {
+        uint2 codes = kv8_encode(f[u], by);
+        if (e >= kKv8MaxExp) codes = make_uint2(kv8_finite(codes.x, e), kv8_finite(codes.y, e));
+        *reinterpret_cast<uint2*>(to + (block_row + r) * to_row) = codes;
+      }
     }
     if (!real) continue;
     if (grows) {                                         // uniform for the item

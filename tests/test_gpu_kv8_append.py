@@ -308,3 +308,28 @@ def test_a_bound_beyond_all_tokens_changes_nothing():
     torch.cuda.synchronize()
     assert int(hb.dev_status) == 0 and torch.equal(ha.q_out, hb.q_out)
     assert all(torch.equal(x, y) for x, y in zip(a.snapshot(), b.snapshot()))
+
+
+def test_the_largest_numbers_stay_finite():
+    """What lies above the largest code that is finite with the scale 2^120, 240 * 2^120, becomes that: within 2^-4 of it."""
+    for block in (32, 128):
+        c = Case([0, 3], [20, 20], Hq=2, Hkv=2, rot=0, norm=False, seed=27, block=block)
+        x = torch.cat([c.q, c.k, c.v], 1)
+        big = torch.finfo(torch.bfloat16).max
+        numbers = torch.tensor([big, -big, 1.9375 * 2.0 ** 127, 1.921875 * 2.0 ** 127, 1.875 * 2.0 ** 127, -1.75 * 2.0 ** 127, 2.0 ** 127,
+                                float("inf"), float("nan")])
+        x[:, 2:, :9] = numbers.bfloat16().cuda()
+        x[:, 2:, 9:] = 0.0
+        c.q, c.k, c.v = x[:, :2], x[:, 2:4], x[:, 4:]
+        as_bytes(c.ks)[:, c.row0[1] // block], as_bytes(c.vs)[:, c.row0[1] // block] = 100, 253   # begun: smaller, or from elsewhere
+        c.handle().step()
+        torch.cuda.synchronize()
+        assert int(as_bytes(c.vs)[0, 0]) == 247 and int(as_bytes(c.vs)[0, c.row0[1] // block]) == 253
+        for X, scale, src in ((c.K, c.ks, c.k), (c.V, c.vs, c.v)):
+            got = values(X, scale, block)
+            for s in range(2):
+                rows = slice(c.row0[s] + c.lens[s], c.row0[s] + c.lens[s] + 20)
+                y, want = got[:, rows, :7], src[20 * s: 20 * s + 20, :, :7].transpose(0, 1).double()
+                assert bool((y.abs() <= 240.0 * 2.0 ** 120).all()) and bool(torch.isfinite(y.float().bfloat16()).all())
+                assert bool(((y - want).abs() <= 2.0 ** -4 * want.abs()).all())
+                assert bool(torch.isnan(got[:, rows, 7:9]).all()) and bool((got[:, rows, 9:] == 0.0).all())
