@@ -743,7 +743,8 @@ typedef struct dsk_kv8_append_args {
  * sees a row, may hold anything, NaN included (a scale of 255 is none: rows under it have no finite result for those who see them, and
  * rows under one above 2^119 may have none); an infinity in a row of V that it sees gives that infinity, or NaN with its opposite or where its weight is 2^-80 of the
  * largest or less.  A token that sees nothing (its sequence has no place in the cache) gets out = 0 and lse = -inf.
- * Accuracy and bits as for dsk_tree_decode_attn, with rows = max_new * Hq / Hkv: `out` asks for fp32 accuracy; where only out_bf16 is
+ * Accuracy and bits as for dsk_tree_decode_attn, with rows = max_new * Hq / Hkv: `out` asks for fp32 accuracy, and sums over V of long
+ * runs are then made in segments, so that equal terms, which are rounded alike, stay below 1e-5 of the sum; where only out_bf16 is
  * asked for, the weights are off by 2^-16 of each at most, and above 64 rows rounded to bf16.  In 8 bits scales below 2^-100 may
  * lose small weights.  Values of 2^100 and more may become infinite on the way to a sum that is not.
  * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths are cut, never followed: tokens to

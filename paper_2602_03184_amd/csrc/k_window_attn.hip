@@ -135,7 +135,6 @@ struct WinFold {
       buf ^= 1;
     }
     __syncthreads();
-    sm.close();
   }
 };
 
@@ -154,13 +153,40 @@ __global__ __launch_bounds__(QW * KW * DSK_WAVE, 2) void window_attn_kernel(dsk_
   TileSoftmax sm(scale_log2);
   tile_f32x16 O[4];
   win_clear(O);
-  Fold::run(sh, c, keys, work.hk, rows, kw, sm, O);
+  WinKept kept;
+  for (;;) {
+    const int end = keys.end;
+    const bool more = TERMS == 3 && end - keys.begin > KW * kWinSegment;   // uniform
+    if (more) keys.end = keys.begin + KW * kWinSegment;
+    Fold::run(sh, c, keys, work.hk, rows, kw, sm, O);
+    if (!more) break;
+    TileSoftmax so_far = sm;                             // (its sum of weights is not used)
+    if constexpr (KW > 1) tile_join<QW, KW>(so_far, O, rows.busy, qw, kw, reinterpret_cast<float*>(sh.kv), sh.ml);
+    if (kw == 0 && rows.real) {
+      float* const at = WinKept::place(to, rows, work.used == 1, work.part, sp.parts);
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct) {
+        if (kept.any) kept.join(at, O[ct], ct, so_far.m);
+        WinKept::put(at, O[ct], ct);
+      }
+    }
+    kept.any = true;
+    kept.m = so_far.m;
+    win_clear(O);
+    if constexpr (KW > 1) __syncthreads();               // the stages' place is free again
+    keys.begin = keys.end;
+    keys.end = end;
+  }
+  sm.close();
   if constexpr (KW > 1) {
     tile_join<QW, KW>(sm, O, rows.busy, qw, kw, reinterpret_cast<float*>(sh.kv), sh.ml);
     if (kw > 0) return;
   }
 #pragma unroll
-  for (int ct = 0; ct < 4; ++ct) win_store(to, rows, O[ct], ct, sm.m, sm.l, work.used == 1, work.part, sp.parts);
+  for (int ct = 0; ct < 4; ++ct) {
+    if (kept.any && rows.real) kept.join(WinKept::place(to, rows, work.used == 1, work.part, sp.parts), O[ct], ct, sm.m);
+    win_store(to, rows, O[ct], ct, sm.m, sm.l, work.used == 1, work.part, sp.parts);
+  }
 }
 
 // The same where the rows fit one wavefront: HBM bounds it.  268 MB of codes take 51 us (5.3 TB/s; with stages that the wavefronts share,
@@ -178,8 +204,19 @@ __global__ __launch_bounds__(kStreamWaves * DSK_WAVE, E4M3 ? 2 : 1) void window_
   TileSoftmax sm(scale_log2);
   tile_f32x16 O[4];
   win_clear(O);
-  win_stream<TERMS, E4M3, STREAM>(sh, c, keys, work.hk, rows, sm, O);
-  win_stream_store<E4M3>(sh, to, rows, sm, O, work.used == 1, work.part, sp.parts);
+  WinKept kept;
+  for (;;) {
+    const int end = keys.end;
+    const bool more = TERMS == 3 && end - keys.begin > kStreamWaves * kWinSegment;   // uniform
+    if (more) keys.end = keys.begin + kStreamWaves * kWinSegment;
+    win_stream<TERMS, E4M3, STREAM>(sh, c, keys, work.hk, rows, sm, O);
+    if (!more) sm.close();
+    win_stream_store<E4M3>(sh, to, rows, sm, O, work.used == 1, work.part, sp.parts, kept, more);
+    if (!more) break;
+    win_clear(O);
+    keys.begin = keys.end;
+    keys.end = end;
+  }
 }
 
 // q_rows: rows of a workgroup of the kernel above

@@ -114,8 +114,11 @@ __global__ __launch_bounds__(kStreamWaves * DSK_WAVE, E4M3 ? 2 : 1) void window_
   tile_f32x16 O[4];
   win_clear(O);
   win_stream<TERMS, E4M3, false>(sh, c, keys, hk, rows, sm, O);
+  sm.close();
   const int parts = sp.slot_parts + sp.near_parts;
-  win_stream_store<E4M3>(sh, to, rows, sm, O, parts == 1, part, parts);
+  static_assert(kWinMaxListed <= kStreamWaves * kWinSegment * kAttnTile, "one segment");
+  WinKept none;
+  win_stream_store<E4M3>(sh, to, rows, sm, O, parts == 1, part, parts, none, false);
 }
 
 template <int WAVES>

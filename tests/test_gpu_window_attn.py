@@ -469,3 +469,38 @@ def test_a_row_that_is_not_seen_may_be_too_large_for_its_scale(new, Hq, Hkv, byt
         assert torch.equal(a[blind], b[blind]) and bool(torch.isfinite(a[blind]).all()) and torch.equal(r.lse, clean.lse)
         fine = [i for i in range(D) if i not in (5, 6)]
         assert torch.equal(a[..., fine], b[..., fine])
+
+
+def _equal_weights(bits, rows, heads):
+    """Keys that all weigh the same but for the first one, and values that are all the same: the result is that value, whatever the
+    weights, which are no powers of two beside the first one's."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(24)
+    K = torch.zeros(1, rows, D, device="cuda")
+    K[0, 0] = 2.0 ** -5                                          # with queries of ones: a logit of 2^-5 * sqrt(128)
+    V = (torch.randint(8, 16, (D,), generator=g, device="cuda") / 16.0).expand(1, rows, D)
+    if bits == 16:
+        return K.bfloat16().expand(heads, rows, D), V.bfloat16().contiguous().expand(heads, rows, D), {}
+    K, V = (x.to(torch.float8_e4m3fn).view(torch.uint8).contiguous().expand(heads, rows, D).view(torch.float8_e4m3fn) for x in (K, V))
+    scale = torch.full((heads, -(-rows // 32)), 127, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+    return K, V, dict(k_scale=scale, v_scale=scale, scale_block=32)
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("B, heads, new, tokens", [(512, 1, 1, 131071), (1, 512, 1, 131071), (1, 256, 1, 131071), (512, 1, 20, 100000),
+                                                   (512, 1, 64, 65472), (512, 1, 128, 32640), (4, 64, 128, 32640), (1, 1, 65536, 0)])
+def test_long_runs_of_equal_weights_keep_32_bits(B, heads, new, tokens, bits):
+    """A wavefront that adds equal terms one after the other rounds them alike.  Runs that one workgroup takes whole, with one wavefront
+    of rows, two and four, and runs in a few long parts.  z0 is the first key's logit, and the sum of its terms' sizes."""
+    K, V, kw = _equal_weights(bits, tokens + new, heads)
+    q = torch.ones(B * new, heads, D, dtype=torch.bfloat16, device="cuda")
+    r = _dsk().window_attn(q, K, V, seq_row0=i32([0] * B), seq_len=i32([tokens] * B), cu_new=i32([new * s for s in range(B + 1)]),
+                           max_new=new, max_seqlen=tokens, **kw)
+    torch.cuda.synchronize()
+    z0 = torch.tensor(2.0 ** -5 * math.sqrt(D), dtype=torch.float64, device="cuda")
+    bar, want = float(f32_bar(z0)), V[0, 0].double()
+    off = float(((r.out.double() - want).abs() / want).max())
+    assert off <= bar, off
+    seen = torch.arange(tokens, tokens + new, dtype=torch.float64, device="cuda").repeat(B)[:, None]
+    lse = torch.log(torch.exp(z0) + seen)
+    assert bool(((r.lse.double() - lse).abs() <= bar + 1e-5 * lse).all())
