@@ -792,6 +792,8 @@ typedef struct dsk_window_attn_args {
  * to the sequence's rows.  Selections are per query head, or per KV head with DSK_ATTN_SHARED_SELECTION.
  * K and V are bf16, or with k_scale codes of 8 bits.  Values, accuracy, infinities and rows that are not seen as for
  * dsk_window_attn with one new token; a query that sees nothing gets out = 0 and lse = -inf.
+ * What a launch does not hold is DSK_ERR_SHAPE: lists of a sequence times ceil(Hq / Hkv / 32) above 65535, 2^24 parts of a list (of
+ * 2048 / b slots, 256 at most) or, from 16 parts on, as many rows B * Hq.
  * ---------------------------------------------------------------------------------------- */
 typedef struct dsk_window_sparse_args {
   uint32_t struct_size;

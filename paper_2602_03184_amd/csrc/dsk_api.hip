@@ -471,6 +471,7 @@ static dsk_status validate_window_sparse(const dsk_window_sparse_args* a) {
   if (a->struct_size != sizeof(dsk_window_sparse_args)) return DSK_ERR_VERSION;
   if (!window_sparse_shape_ok(*a)) return DSK_ERR_SHAPE;
   if (!window_sparse_params_ok(*a) || !(a->scale >= 0.0f)) return DSK_ERR_PARAM;
+  if (!window_sparse_fits(*a)) return DSK_ERR_SHAPE;
   if (!a->q || (!a->out && !a->out_bf16) || !a->seq_row0 || !a->seq_len || !a->sel_start || !a->sel_len || !a->sel_count)
     return DSK_ERR_NULL;
   if (const dsk_status v = window_cache_ok(*a); v != DSK_OK) return v;

@@ -153,6 +153,7 @@ constexpr int kMaxAppendHeads = 4096;          // query heads: 128 rows of a blo
 hipError_t launch_kv8_append(const dsk_kv8_append_args& a, hipStream_t st);
 size_t window_ws_bytes(const dsk_window_attn_args& a);
 hipError_t launch_window_attn(const dsk_window_attn_args& a, hipStream_t st);
+bool window_sparse_fits(const dsk_window_sparse_args& a);   // its launches
 size_t window_sparse_ws_bytes(const dsk_window_sparse_args& a);
 hipError_t launch_window_sparse(const dsk_window_sparse_args& a, hipStream_t st);
 

@@ -157,6 +157,14 @@ static WinSparse win_sparse_layout(const dsk_window_sparse_args& a) {
   return sp;
 }
 
+// A launch has fewer than 2^32 threads in x and at most 65535 workgroups in y.
+bool window_sparse_fits(const dsk_window_sparse_args& a) {
+  const WinSparse sp = win_sparse_layout(a);
+  const int64_t parts = (int64_t)sp.slot_parts + sp.near_parts, rows = (int64_t)a.B * a.Hq;
+  const int64_t merge = parts <= 1 ? 0 : ceil_div(rows, parts >= kWinMergeMany ? 1 : kWinMergeWaves);
+  return (int64_t)sp.heads * sp.row_tiles <= 65535 && parts * kStreamWaves * DSK_WAVE <= 0xFFFFFFFF && merge * kWinMergeWaves * DSK_WAVE <= 0xFFFFFFFF;
+}
+
 // No less than with a smaller k, window or max_seqlen: parts of n things that are at least `least` and at most `most` each and
 // otherwise shared out to 2 * kWinCus / lists parts.
 size_t window_sparse_ws_bytes(const dsk_window_sparse_args& a) {

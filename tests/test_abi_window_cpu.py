@@ -238,3 +238,19 @@ def test_kept_calls_are_made_on_the_device_of_their_tensors(dsk, monkeypatch):
         order.clear()
         assert kept.step(5, check=False) == 0
         assert order[0] == 1 and order[2] == 0 and order[1][0] is kept.args and order[1][1:] == (5, False)
+
+
+def test_selections_beyond_what_a_launch_holds_are_refused(dsk):
+    """Lists times 32 query heads each are one side of the grid, parts of a list another, and a row has a workgroup where its parts
+    are put together."""
+    for B, Hq, Hkv, flags, k, b, fits in (
+            (2, 2048, 1, 0, 8, 16, False), (2, 1440, 1, 0, 8, 16, True), (2, 1472, 1, 0, 8, 16, False), (2, 2048, 1, 2, 8, 16, True),
+            (2, 65535, 65535, 0, 8, 16, True), (2, 65534, 32767, 0, 8, 16, True), (2, 65535, 1, 2, 8, 16, True),
+            (2, 65535, 1, 0, 8, 16, False), (2, 62016, 1938, 0, 8, 16, True), (2, 62130, 1365, 0, 8, 16, False),
+            (1, 1, 1, 0, 2 ** 25, 1000, False), (1, 1, 1, 0, 2 ** 25 - 2048, 1000, True), (1, 1, 1, 0, 2 ** 30, 1, True),
+            (1, 1, 1, 0, 2 ** 30, 64, False), (1, 1, 1, 0, 2 ** 28, 64, True),
+            (65535, 512, 1, 0, 1000, 64, False), (65535, 512, 1, 0, 8, 64, True), (65535, 256, 1, 0, 1000, 64, True)):
+        a = _sparse(dsk)
+        a.B, a.Hq, a.Hkv, a.flags, a.k, a.b, a.workspace_bytes = B, Hq, Hkv, flags, k, b, 0
+        want = dsk.DSK_ERR_WORKSPACE if fits else dsk.DSK_ERR_SHAPE          # (nothing else is wrong with it)
+        assert dsk.dsk_window_sparse_decode_attn(a, 0, check=False) == want, (B, Hq, Hkv, flags, k, b)
