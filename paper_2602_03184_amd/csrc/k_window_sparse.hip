@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kStreamWaves * DSK_WAVE, E4M3 ? 2 : 1) void window_
     }
   } else {
     // what is near is not taken from the slots: a span stays a span
-    slots = slots < a.k ? slots : a.k;
+    slots = slots < 0 ? 0 : (slots < a.k ? slots : a.k);
     if (tid >= slots - first || tid >= sp.slots_per_part || ln <= 0 || start < 0) ln = 0;
     ln = ln < a.b ? ln : a.b;
     int64_t from = start, upto = (int64_t)start + ln;

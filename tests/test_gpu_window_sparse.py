@@ -247,3 +247,12 @@ def test_a_workspace_for_the_longest_cache_serves_shorter_ones():
         r.step()
         torch.cuda.synchronize()
         assert bool(((r.out.double() - out).abs() <= bar[..., None] * size + TINY).all())
+
+
+def test_a_count_far_below_zero_selects_nothing():
+    for bits in (8, 16):
+        c = Case([5000, 700], 8, 2, 60, 32, window=50, sinks=3, bits=bits, seed=12)
+        for count in (-1, -60, -2 ** 31):
+            r = c.run(sel_count=torch.full((2, 8), count, dtype=torch.int32, device="cuda"))
+            none = c.run(sel_count=torch.zeros(2, 8, dtype=torch.int32, device="cuda"))
+            assert torch.equal(r.out, none.out) and torch.equal(r.lse, none.lse)
