@@ -36,11 +36,6 @@ HIPCC_FLAGS = [
 ]
 
 
-# The kernel for many rows has accumulators and fragments for more than 256 registers, of which the vector ALU reads few: told to take
-# vector registers first, the compiler leaves the others with the matrix instructions instead of copying the logits back and forth.
-FILE_FLAGS = {"k_window_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"]}
-
-
 def _hipcc() -> str:
     exe = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
     if not os.path.exists(exe):
@@ -54,7 +49,7 @@ def sources():
 
 def _compile(src: str) -> str:
     obj = os.path.join(BUILD_DIR, os.path.basename(src)[:-4] + ".o")
-    cmd = [_hipcc(), *HIPCC_FLAGS, *FILE_FLAGS.get(os.path.basename(src), []), "-c", src, "-o", obj]
+    cmd = [_hipcc(), *HIPCC_FLAGS, "-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("hipcc failed on %s:\n%s\n%s" % (src, r.stdout, r.stderr))

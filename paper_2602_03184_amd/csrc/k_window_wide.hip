@@ -10,7 +10,8 @@
 // second barrier take 613 us in bf16 and 199 in 8 bits, where widening makes their halves unequal.
 //
 // K and V come to LDS through registers, a ring of four tiles in bf16: codes are widened on the way, once for all wavefronts.  In step i
-// tile i + 3 is written where tile i - 1 was, while K of tile i + 2 and V of tile i are read: one barrier a step.
+// tile i + 3 is written where tile i - 1 was, while K of tile i + 2 and V of tile i are read: one barrier a step.  All 256 registers of a
+// wavefront are taken, and four to six more go through scratch.
 #include "dsk_window_run.hpp"
 
 namespace dsk {
