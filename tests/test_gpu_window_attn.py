@@ -504,3 +504,41 @@ def test_long_runs_of_equal_weights_keep_32_bits(B, heads, new, tokens, bits):
     seen = torch.arange(tokens, tokens + new, dtype=torch.float64, device="cuda").repeat(B)[:, None]
     lse = torch.log(torch.exp(z0) + seen)
     assert bool(((r.lse.double() - lse).abs() <= bar + 1e-5 * lse).all())
+
+
+def test_bf16_results_are_bit_identical_from_call_to_call_on_another_stream_and_in_a_graph():
+    kw = dict(want_f32=False, want_bf16=True)
+    for bits in (8, 16):
+        for new in ([1, 1], [7, 3], [16, 9], [30, 9], [300, 2]):
+            c = Case([5000, 700], new, 8, 2, bits=bits, seed=25)
+            a, b = c.run(**kw), c.run(**kw)
+            st = torch.cuda.Stream()
+            r = _dsk().make_window_attn_args(c.q, c.K, c.V, **c.kwargs(**kw))
+            torch.cuda.synchronize()
+            r.step(st)
+            st.synchronize()
+            for x in (b, r):
+                assert torch.equal(a.out_bf16, x.out_bf16) and torch.equal(a.lse, x.lse)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=st):
+                r.step(st)
+            for _ in range(3):
+                r.out_bf16.zero_()
+                c.run(**kw)
+                graph.replay()
+                torch.cuda.synchronize()
+                assert torch.equal(a.out_bf16, r.out_bf16) and torch.equal(a.lse, r.lse)
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_a_nan_in_a_query_is_its_rows_alone_in_bf16_results(bits):
+    kw = dict(want_f32=False, want_bf16=True)
+    for new in (1, 9, 30, 150):
+        c = Case([5000, 20], [new, new], 8, 2, bits=bits, seed=26)
+        a = c.run(**kw)
+        c.q[new // 2, 3, 17] = float("nan")
+        b = c.run(**kw)
+        assert bool(torch.isnan(b.out_bf16[new // 2, 3]).all()) and bool(torch.isnan(b.lse[new // 2, 3]))
+        keep = torch.ones(2 * new, 8, dtype=torch.bool, device="cuda")
+        keep[new // 2, 3] = False
+        assert torch.equal(a.out_bf16[keep], b.out_bf16[keep]) and torch.equal(a.lse[keep], b.lse[keep])
