@@ -599,8 +599,8 @@ typedef struct dsk_norm_rope_args {
  * opposite or where its weight is 2^-80 of the largest or less.  Mask bits of nodes that do not exist are ignored.
  * `out` asks for fp32 accuracy.  Where only out_bf16 is asked for, the softmax weights of the products with V are off by 2^-16 of
  * each at most, and with max_nodes * Hq / Hkv above 64 they are rounded to bf16 (lse is fp32 in all).  Sums are in fp32, that of the
- * weights with its rounding carried along, those over V rounded up to three times for 16 keys, split over the keys with a merge in a fixed
- * order; how they are split, and with it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen, total_rows (k and b
+ * weights with its rounding carried along, those over V rounded up to three times for 16 keys (equal terms alike: up to 1e-4 of the sum
+ * where one wavefront takes 64K keys), split over the keys with a merge in a fixed order; how they are split, and with it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen, total_rows (k and b
  * with a selection) and which outputs are asked for.  A token that several selected slots hold counts as often.
  * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths or spans outside the
  * arrays are cut, never followed: a prefix to max_seqlen and total_rows (the nodes' rows are those behind it), nodes to max_nodes;
@@ -741,12 +741,15 @@ typedef struct dsk_kv8_append_args {
  *   out = sum p_t V_t / sum p_t,  p_t = exp(q.K_t * scale);  lse = log sum p_t
  * K and V are bf16, or with k_scale codes of 8 bits (above).  Rows that a token does not see, and scales of blocks of which nobody
  * sees a row, may hold anything, NaN included (a scale of 255 is none: rows under it have no finite result for those who see them, and
- * rows under one above 2^119 may have none); an infinity in a row of V that it sees gives that infinity, or NaN with its opposite or where its weight is 2^-80 of the
- * largest or less.  A token that sees nothing (its sequence has no place in the cache) gets out = 0 and lse = -inf.
+ * rows under one above 2^119 may have none).  An infinity in a row of V that it sees gives that infinity, or NaN with its opposite or
+ * where its weight is 2^-80 of the largest or less.  A token that sees nothing (its sequence has no place in the cache) gets out = 0
+ * and lse = -inf.
  * Accuracy and bits as for dsk_tree_decode_attn, with rows = max_new * Hq / Hkv: `out` asks for fp32 accuracy, and sums over V of long
  * runs are then made in segments, so that equal terms, which are rounded alike, stay below 1e-5 of the sum; where only out_bf16 is
  * asked for, the weights are off by 2^-16 of each at most, and above 64 rows rounded to bf16.  In 8 bits scales below 2^-100 may
  * lose small weights.  Values of 2^100 and more may become infinite on the way to a sum that is not.
+ * max_new chooses the kernel and the split of the whole call: sequences with a token each are slow beside one that brings a prompt, as
+ * none of their keys are split then (2048 tokens, and one behind 131K in 8 bits: 4.7 ms; as two calls 0.14).
  * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths are cut, never followed: tokens to
  * max_new and n_tokens, seq_len to max_seqlen, rows to total_rows.
  * ---------------------------------------------------------------------------------------- */
@@ -790,6 +793,8 @@ typedef struct dsk_window_attn_args {
  *   selected  the tokens of its slots (spans of cache rows as dsk_select_topk writes them) that are not near
  * so that what is near counts once whatever is selected; a token that several slots hold counts as often.  Spans are cut
  * to the sequence's rows.  Selections are per query head, or per KV head with DSK_ATTN_SHARED_SELECTION.
+ * The tables behind them come from dsk_compress and dsk_append_tokens, which read keys in bf16: of a cache in 8 bits what its codes
+ * stand for, code * scale, which bf16 holds.
  * K and V are bf16, or with k_scale codes of 8 bits.  Values, accuracy, infinities and rows that are not seen as for
  * dsk_window_attn with one new token; a query that sees nothing gets out = 0 and lse = -inf.
  * What a launch does not hold is DSK_ERR_SHAPE: lists of a sequence times ceil(Hq / Hkv / 32) above 65535, 2^24 parts of a list (of

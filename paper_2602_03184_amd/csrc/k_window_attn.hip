@@ -16,8 +16,9 @@ namespace dsk {
 // ---- a workgroup's keys folded into its rows -----------------------------------------------------------------
 // QW wavefronts have 32 rows each, KW take other tiles of a stage for the same rows, NT of them each.  A stage is copied while the one
 // before it is multiplied.  TERMS: bf16 terms of a weight.  131K tokens of 8 heads in 8 bits: 64 rows a head 78 us (two wavefronts of rows,
-// two of tiles; 3.4 TB/s and 0.44 PFLOP/s), 128 rows 100 us (0.69 PFLOP/s), in bf16 94 and 110.  Here products, exponentials and LDS take
-// turns, and only the second workgroup of a CU fills in.
+// two of tiles; 3.4 TB/s and 0.44 PFLOP/s), 128 rows 100 us (0.69 PFLOP/s), in bf16 94 and 110, without the merge; whole calls 85, 117, 106
+// and 117, with a result in 32 bits 95, 160, 108 and 164.  Here products, exponentials and LDS take turns, and only the second workgroup
+// of a CU fills in.
 template <int QW, int KW, int NT, int TERMS, bool E4M3>
 struct WinFold {
   static constexpr int kThreads = QW * KW * DSK_WAVE;
@@ -259,7 +260,7 @@ static WinLaunch win_layout(const dsk_window_attn_args& a, bool f32) {
   const int64_t rows = (int64_t)a.max_new * G;
   WinLaunch t;
   t.q_waves = rows <= kAttnTile ? 1 : (rows <= kWinTwoTermRows ? 2 : 4);
-  // Rows of a KV head, over 131K tokens of 8 heads in 8 bits: 128 rows take four wavefronts 108 us, the eight that fit many rows 167, as
+  // Rows of a KV head, over 131K tokens of 8 heads in 8 bits, whole calls: 128 rows take four wavefronts 108 us, the eight that fit many rows 167, as
   // half of them have none; 256 rows 193 and 177 (in bf16 116 and 167, 179 and 167).  A result in 32 bits has weights of three terms,
   // which those have no registers for.
   t.wide = rows > 128 && !f32;
@@ -271,7 +272,8 @@ static WinLaunch win_layout(const dsk_window_attn_args& a, bool f32) {
   const int64_t near = ceil_div((int64_t)a.window + tokens, kAttnTile) + 1 + ceil_div(a.n_sink, kAttnTile);
   const int64_t tiles = near < ceil_div(longest, kAttnTile) ? near : ceil_div(longest, kAttnTile);
   // Tiles of all sequences.  Where the cache has no room for all of them at their longest they differ in length, and the parts are cut to
-  // fill the chip with those that there are: eight sequences of 16K to 64K tokens in 8 bits, four new tokens 174 -> 142 us.
+  // fill the chip with those that there are: eight sequences of 16K to 64K tokens in 8 bits, four new tokens 174 -> 142 us.  The lengths
+  // are not known here: the same sequences in regions of 64K rows each are split as if they were as long, 159 us a call instead of 146.
   const int64_t rows_tiles = (int64_t)a.total_rows / kAttnTile + 2 * (int64_t)a.B, all = a.B * tiles < rows_tiles ? a.B * tiles : rows_tiles;
   const bool ragged = all < a.B * tiles;
   const int most = win_most_parts(a, t.q_tiles, tiles);
