@@ -542,3 +542,27 @@ def test_a_nan_in_a_query_is_its_rows_alone_in_bf16_results(bits):
         keep = torch.ones(2 * new, 8, dtype=torch.bool, device="cuda")
         keep[new // 2, 3] = False
         assert torch.equal(a.out_bf16[keep], b.out_bf16[keep]) and torch.equal(a.lse[keep], b.lse[keep])
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("heads, Hkv, new, tokens, kw", [(4, 1, 1, 20000, {}), (8, 2, 8, 36000, dict(window=20011, sinks=40)),
+                                                         (4, 1, 16, 9000, dict(sinks=3000, window=5000)), (1, 1, 100, 7000, {})])
+def test_long_runs_that_one_workgroup_takes_in_segments(heads, Hkv, new, tokens, kw, bits):
+    """So many sequences that none is split, over the same rows.  Results in 32 bits, an infinity of an early segment and a NaN among them."""
+    B = 512 // Hkv
+    c = Case([tokens] + [0] * (B - 1), [new] * B, heads, Hkv, bits=bits, seed=28, spare=0, sharp=0.2, **kw)
+    c.row0 = [0] * B + [c.row0[B]]
+    c.lens = [tokens - 7 * s for s in range(B)]
+    clean = c.check()
+    c.q[3 * new, 0, 17] = float("nan")
+    if bits == 16:
+        c.V[:, 10, 5] = float("inf")                             # of the first tokens, or of the longest windows
+    r = c.run()
+    sees = torch.cat([c.seen(s)[:, 10] for s in range(B)])
+    keep = torch.ones(B * new, heads, dtype=torch.bool, device="cuda")
+    keep[3 * new, 0] = False
+    assert bool(torch.isnan(r.out[3 * new, 0]).all()) and bool(torch.isnan(r.lse[3 * new, 0]))
+    fine = [i for i in range(D) if i != 5]
+    assert torch.equal(r.out[..., fine][keep], clean.out[..., fine][keep]) and torch.equal(r.lse[keep], clean.lse[keep])
+    if bits == 16:
+        assert torch.equal(r.out[..., 5][keep] == float("inf"), sees[:, None].expand(-1, heads)[keep])
