@@ -751,7 +751,8 @@ typedef struct dsk_kv8_append_args {
  * max_new chooses the kernel and the split of the whole call: sequences with a token each are slow beside one that brings a prompt, as
  * none of their keys are split then (2048 tokens, and one behind 131K in 8 bits: 4.7 ms; as two calls 0.14).
  * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths are cut, never followed: tokens to
- * max_new and n_tokens, seq_len to max_seqlen, rows to total_rows.
+ * max_new and n_tokens, seq_len to max_seqlen, rows to total_rows; none of that is reported, so the bounds of a kept argument struct
+ * have to be those of the longest cache that it will meet.
  * ---------------------------------------------------------------------------------------- */
 #define DSK_WINDOW_ALL 0x7FFFFFFF    /* a window that hides nothing */
 
