@@ -600,8 +600,9 @@ typedef struct dsk_norm_rope_args {
  * `out` asks for fp32 accuracy.  Where only out_bf16 is asked for, the softmax weights of the products with V are off by 2^-16 of
  * each at most, and with max_nodes * Hq / Hkv above 64 they are rounded to bf16 (lse is fp32 in all).  Sums are in fp32, that of the
  * weights with its rounding carried along, those over V rounded up to three times for 16 keys (equal terms alike: up to 1e-4 of the sum
- * where one wavefront takes 64K keys), split over the keys with a merge in a fixed order; how they are split, and with it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen, total_rows (k and b
- * with a selection) and which outputs are asked for.  A token that several selected slots hold counts as often.
+ * where one wavefront takes 64K keys), split over the keys with a merge in a fixed order; how they are split, and with
+ * it the last bits, follows B, Hq, Hkv, max_nodes, max_seqlen, total_rows (k and b with a selection) and which outputs
+ * are asked for.  A token that several selected slots hold counts as often.
  * Rows of q, out and lse from cu_new[B] on are neither read nor written.  Malformed lengths or spans outside the
  * arrays are cut, never followed: a prefix to max_seqlen and total_rows (the nodes' rows are those behind it), nodes to max_nodes;
  * a sequence whose first row or length is no place in the cache has neither prefix nor rows of nodes in it.
