@@ -708,7 +708,7 @@ typedef struct dsk_kv8_append_args {
   uint32_t struct_size;
   int32_t B, Hq, Hkv, D;
   int32_t n_tokens;            /* [host] rows of q, k, v; bounds cu_new[B] */
-  int32_t max_new;             /* [host] bound on the new tokens of a sequence, >= 1; sizes the launch */
+  int32_t max_new;             /* [host] bound on the new tokens of a sequence, >= 1; sizes the launch: with n_tokens some 2^24 blocks at most */
   int32_t total_rows;          /* [host] rows per head of K and V */
   int32_t scale_block;
   const int32_t* seq_row0;     /* [dev] [B] */
@@ -761,7 +761,8 @@ typedef struct dsk_window_attn_args {
   uint32_t struct_size;
   int32_t B, Hq, Hkv, D;
   int32_t n_tokens;            /* [host] rows of q, out and lse; bounds cu_new[B] */
-  int32_t max_new;             /* [host] bound on the new tokens of a sequence, >= 1; it and n_tokens, times Hq, below 2^31 */
+  int32_t max_new;             /* [host] bound on the new tokens of a sequence, >= 1; it (in workgroups of 128 rows) and n_tokens, times Hq,
+                                  below 2^31 */
   int32_t max_seqlen;          /* [host] bound on seq_len, >= 0; max_seqlen + max_new at most 0x7FFF0000 */
   int32_t total_rows;          /* [host] rows per head of K / V */
   int32_t window;              /* >= 1 */

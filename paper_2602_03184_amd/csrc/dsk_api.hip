@@ -422,7 +422,8 @@ static dsk_status validate_kv8_append(const dsk_kv8_append_args* a) {
   if (!aligned16(a->q_weight) || !aligned16(a->k_weight) || (reinterpret_cast<uintptr_t>(a->inv_freq) & 3u)) return DSK_ERR_ALIGN;
   if (const dsk_status v = cache_ok(a->K, a->kc_stride_tok, a->kc_stride_head, a->Hkv); v != DSK_OK) return v;
   if (const dsk_status v = cache_ok(a->V, a->vc_stride_tok, a->vc_stride_head, a->Hkv); v != DSK_OK) return v;
-  return (a->kc_stride_tok | a->kc_stride_head | a->vc_stride_tok | a->vc_stride_head) % 16 ? DSK_ERR_ALIGN : DSK_OK;
+  if ((a->kc_stride_tok | a->kc_stride_head | a->vc_stride_tok | a->vc_stride_head) % 16) return DSK_ERR_ALIGN;
+  return kv8_append_fits(*a) ? DSK_OK : DSK_ERR_SHAPE;
 }
 
 // what the two calls have in common
@@ -451,6 +452,7 @@ static dsk_status validate_window_attn(const dsk_window_attn_args* a) {
   if (a->struct_size != sizeof(dsk_window_attn_args)) return DSK_ERR_VERSION;
   if (!window_attn_shape_ok(*a)) return DSK_ERR_SHAPE;
   if (a->window < 1 || a->n_sink < 0 || !(a->scale >= 0.0f) || a->flags != 0) return DSK_ERR_PARAM;
+  if (!window_attn_fits(*a)) return DSK_ERR_SHAPE;
   if (!a->seq_row0 || !a->seq_len || !a->cu_new) return DSK_ERR_NULL;
   if ((!a->q || (!a->out && !a->out_bf16)) && a->n_tokens > 0) return DSK_ERR_NULL;
   if (const dsk_status v = window_cache_ok(*a); v != DSK_OK) return v;

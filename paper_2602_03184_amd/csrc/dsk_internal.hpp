@@ -150,7 +150,9 @@ hipError_t launch_tree_attn(const dsk_tree_attn_args& a, hipStream_t st);
 // ---- a cache in 8 bits, sliding window and first tokens ---------------------------------------------
 constexpr int kMaxWindowKeys = 0x7FFF0000;     // positions: a key's number and a tile's overhang in 32 bits
 constexpr int kMaxAppendHeads = 4096;          // query heads: 128 rows of a block times heads squared fits 32 bits
+bool kv8_append_fits(const dsk_kv8_append_args& a);         // its launch
 hipError_t launch_kv8_append(const dsk_kv8_append_args& a, hipStream_t st);
+bool window_attn_fits(const dsk_window_attn_args& a);
 size_t window_ws_bytes(const dsk_window_attn_args& a);
 hipError_t launch_window_attn(const dsk_window_attn_args& a, hipStream_t st);
 bool window_sparse_fits(const dsk_window_sparse_args& a);   // its launches

@@ -289,10 +289,18 @@ static void launch_block(const dsk_kv8_append_args& a, int64_t blocks, hipStream
   else kv8_append_kernel<PAIRS, WPI, kKv8Quads><<<grid, block, 0, st>>>(a, kv_groups, by_heads);
 }
 
+// blocks that new tokens of a sequence can meet, however the first of them lies; more than all tokens says nothing more
+static int64_t most_blocks(const dsk_kv8_append_args& a) {
+  const int64_t most = a.max_new < a.n_tokens ? a.max_new : a.n_tokens;
+  return (most + a.scale_block - 2) / a.scale_block + 1;
+}
+
+// a launch has fewer than 2^32 threads in x
+bool kv8_append_fits(const dsk_kv8_append_args& a) { return a.n_tokens == 0 || most_blocks(a) * kKv8Threads <= 0xFFFFFFFF; }
+
 template <RopePairs PAIRS>
 static void launch_pairs(const dsk_kv8_append_args& a, hipStream_t st) {
-  // blocks that max_new tokens can meet, however the first of them lies
-  const int64_t blocks = ((int64_t)a.max_new + a.scale_block - 2) / a.scale_block + 1;
+  const int64_t blocks = most_blocks(a);
   if (a.scale_block == 32) launch_block<PAIRS, 1>(a, blocks, st);
   else if (a.scale_block == 64) launch_block<PAIRS, 2>(a, blocks, st);
   else launch_block<PAIRS, 4>(a, blocks, st);
@@ -300,7 +308,7 @@ static void launch_pairs(const dsk_kv8_append_args& a, hipStream_t st) {
 
 hipError_t launch_kv8_append(const dsk_kv8_append_args& args, hipStream_t st) {
   dsk_kv8_append_args a = args;
-  a.max_new = a.max_new < a.n_tokens ? a.max_new : a.n_tokens;   // more than all of them says nothing more
+  a.max_new = a.max_new < a.n_tokens ? a.max_new : a.n_tokens;
   if (a.rot_dim == 0) launch_pairs<RopePairs::kNone>(a, st);
   else if (a.flags & DSK_ROPE_INTERLEAVED) launch_pairs<RopePairs::kInterleaved>(a, st);
   else if (a.rot_dim == DSK_HEAD_DIM) launch_pairs<RopePairs::kHalfAll>(a, st);

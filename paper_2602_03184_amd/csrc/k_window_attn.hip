@@ -292,6 +292,12 @@ static WinLaunch win_layout(const dsk_window_attn_args& a, bool f32) {
   return t;
 }
 
+// A launch has fewer than 2^32 threads in x.  (Rows whose parts are put together are 65536 at most, as more are not split.)
+bool window_attn_fits(const dsk_window_attn_args& a) {
+  const WinLaunch t = win_layout(a, a.out != nullptr);
+  return (int64_t)a.Hkv * t.q_tiles * (t.wide ? kWideWaves : 4) * DSK_WAVE <= 0xFFFFFFFF;
+}
+
 // Whichever outputs the call will ask for, and no less than with a smaller max_seqlen.
 size_t window_ws_bytes(const dsk_window_attn_args& a) {
   int most = 1;

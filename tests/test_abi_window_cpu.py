@@ -254,3 +254,21 @@ def test_selections_beyond_what_a_launch_holds_are_refused(dsk):
         a.B, a.Hq, a.Hkv, a.flags, a.k, a.b, a.workspace_bytes = B, Hq, Hkv, flags, k, b, 0
         want = dsk.DSK_ERR_WORKSPACE if fits else dsk.DSK_ERR_SHAPE          # (nothing else is wrong with it)
         assert dsk.dsk_window_sparse_decode_attn(a, 0, check=False) == want, (B, Hq, Hkv, flags, k, b)
+
+
+def test_new_tokens_beyond_what_a_launch_holds_are_refused(dsk):
+    """256 rows of a KV head, or 128 of a result in 32 bits, are a workgroup of 512 or 256 threads, of which a launch has fewer than 2^32;
+    so are 256 threads for a block of rows to append, and one more block that tokens can meet."""
+    for Hq, Hkv, max_new, f32, fits in ((40000, 40000, 53687, False, False), (40000, 40000, 53687, True, False), (40000, 40000, 53504, False, True),
+                                        (1, 1, 0x7FFE0000, False, True), (1, 1, 0x7FFE0000, True, True), (65535, 65535, 32767, False, True),
+                                        (65535, 65535, 1, True, True)):
+        a = _window(dsk)
+        a.Hq, a.Hkv, a.max_new, a.workspace_bytes = Hq, Hkv, max_new, 0
+        if not f32:
+            a.out = None
+        want = dsk.DSK_ERR_WORKSPACE if fits else dsk.DSK_ERR_SHAPE
+        assert dsk.dsk_window_attn(a, 0, check=False) == want, (Hq, Hkv, max_new, f32)
+    for block, n in ((32, 2 ** 29), (32, 2 ** 29 - 30), (64, 2 ** 30), (128, 2 ** 31 - 1)):
+        a = _append(dsk)
+        a.scale_block, a.n_tokens, a.max_new = block, n, 0x7FFFFFFF
+        assert dsk.dsk_kv8_append(a, 0, check=False) == dsk.DSK_ERR_SHAPE, (block, n)
